@@ -554,6 +554,85 @@ int hmy_k_xent(int32_t prec, const float *logits, const int32_t *targets, double
 int hmy_k_adam(int32_t prec, const float *grad, float *master, float *m, float *v, void *w_out,
                uint64_t n, const hmy_adam *hp, void *stream);
 
+/* ---- operators on rows of logits (all pointers DEVICE, stream as above) ----
+ * logits[T,V], row stride ldl >= V, in fp32 or bf16 (logits_prec: HMY_PREC_*); rows may start at any element.  With a scale
+ * s > 0 (an inverse temperature), m = the row's largest logit and S = sum exp(s (x_j - m)), the log probability of token j is
+ * l_j = s (x_j - m) - log S, p_j = exp l_j.  Sums are held in fp32, a list's terms of hmy_k_distill in fp64; results do not
+ * depend on the order in which workgroups run.
+ *   - A logit of -inf is a token without weight: l = -inf, p = 0, in no list.  A row of nothing else has row_max = log_sum =
+ *     -inf, entropy 0 and l = -inf throughout.  A row that holds a NaN or +inf has NaN results (its list still ranks the
+ *     tokens that are no NaN).
+ *   - An id outside of [0, V) names no token.
+ *   - T >= 1, 1 <= V <= 2^24.  Arrays are aligned to their elements.
+ *   - dlogits[T,V] with row stride ldd: columns V .. V+pad-1 of each row are written as zeros (the padding that
+ *     hmy_k_xent zeroes is pad = ldl - V), columns beyond are left as they are.  dlogits may be the logits themselves (same
+ *     address, type and stride); otherwise the two must not overlap (HMY_E_INVALID where their rows do).
+ *   - workspace: HMY_ROWS_WORKSPACE_BYTES of device memory, aligned to 16 bytes, lets a call of few rows use the whole device;
+ *     without it (NULL, or smaller) each row is one workgroup's.  Nothing in it has to be cleared.  Calls that may overlap
+ *     need one each.  Nothing is allocated, and every call can be captured into a graph. */
+#define HMY_MAX_TOP 128
+#define HMY_ROWS_WORKSPACE_BYTES (1 << 20)
+
+/* Per row: logp = l_target (0 where targets[t] names no token), entropy H = -sum p_j l_j, and the k most likely tokens with
+ * their log probabilities, the most likely first, of equal logits the lower id first; entries beyond the row's tokens are
+ * id -1, log probability -inf.  row_max = m and log_sum = log S are what hmy_k_logprob_bwd takes.  Every output may be NULL:
+ * targets and logp come together, top_ids and top_logp are wanted where k > 0 (and not looked at otherwise). */
+typedef struct hmy_logprob_desc {
+  int32_t logits_prec, T, V, k;  /* 0 <= k <= HMY_MAX_TOP                     */
+  const void *logits; int64_t ldl;
+  const int32_t *targets;        /* [T]                                       */
+  float *logp, *row_max, *log_sum, *entropy;  /* [T] each                     */
+  int32_t *top_ids;              /* [T,k], dense                              */
+  float *top_logp;               /* [T,k], dense                              */
+  void *workspace; uint64_t workspace_bytes;
+  float scale;
+  int32_t reserved_;
+} hmy_logprob_desc;
+int hmy_k_logprob(const hmy_logprob_desc *g, void *stream);
+
+/* dlogits (type prec) of a loss L that depends on logp and entropy:
+ *   dL/dx_j = s (d_logp (1[j = target] - p_j) - d_entropy p_j (l_j + H)).
+ * row_max, log_sum and entropy as hmy_k_logprob left them, for the same logits and scale.  d_logp or d_entropy may be NULL
+ * (zero); d_logp needs targets, d_entropy needs entropy.  Rows whose target names no token get no gradient from d_logp. */
+typedef struct hmy_logprob_grad_desc {
+  int32_t prec, logits_prec, T, V;
+  const void *logits; int64_t ldl;
+  const float *row_max, *log_sum;
+  const int32_t *targets;
+  const float *d_logp, *entropy, *d_entropy;
+  void *dlogits; int64_t ldd;
+  float scale;
+  int32_t pad;
+} hmy_logprob_grad_desc;
+int hmy_k_logprob_bwd(const hmy_logprob_grad_desc *g, void *stream);
+
+/* Distillation: the divergence of a student's rows from a teacher's K listed tokens, and its gradient.  teacher_ids[T,K] and
+ * teacher_logp[T,K] as hmy_k_logprob writes top_ids and top_logp (under the same scale).  An entry whose id names no token or
+ * whose log probability is -inf is not there; one token listed twice has the sum of both probabilities.
+ *   tail = 0: the teacher's probabilities q are exp(teacher_logp), made to add up to 1 over the list;
+ *     row_loss = sum_k q_k (log q_k - l_k),  dL/dx_j = w s (p_j - q_j)
+ *   tail = 1: q = exp(teacher_logp), and the tokens that are not listed form one class more, with the teacher's rest
+ *     q_r = max(0, 1 - sum q_k) and the student's p_r = the sum of their p_j:
+ *     row_loss = sum_k q_k (teacher_logp_k - l_k) + q_r (log q_r - log p_r); with Q = sum q_k + q_r,
+ *     dL/dx_j = w s (Q p_j - q_j) for listed tokens, w s p_j (Q - q_r / p_r) for the others.  Where the student gives the class
+ *     no weight at all (p_r = 0) it is dropped: q_r = 0.
+ * (A token listed twice counts q_k (log q_k - l_k) for each entry.)  w = grad_scale, which also scales what loss_acc (may be
+ * NULL) gets: loss_acc[0] += w sum_t row_loss[t], added up in one order by a launch of its own.  row_loss[T] itself is not
+ * scaled.  A row with no entry at all (padding) has loss 0 and gradient 0.  dlogits NULL: the loss alone. */
+typedef struct hmy_distill_desc {
+  int32_t prec, logits_prec, T, V, K, tail;  /* 1 <= K <= HMY_MAX_TOP         */
+  const void *logits; int64_t ldl;
+  const int32_t *teacher_ids;
+  const float *teacher_logp;
+  float *row_loss;
+  double *loss_acc;
+  void *dlogits; int64_t ldd;
+  void *workspace; uint64_t workspace_bytes;
+  float scale, grad_scale;
+  int32_t pad, reserved_;
+} hmy_distill_desc;
+int hmy_k_distill(const hmy_distill_desc *g, void *stream);
+
 /* ---- the host-side update on its own (all pointers HOST, no GPU needed) ----
  * What HMY_UPDATE_ON_HOST applies to each chunk of a pack (Section 4.4, update task on
  * the CPU): the arithmetic of hmy_k_adam, in place, over n elements, on `threads` CPU

@@ -16,4 +16,6 @@ schedule   the layer-pack-major driver (input-batch grouping, recompute,
            jit-compute, jit-update) and the task list it walks
 swapcount  closed-form swap volumes and an independent ledger walk
 packing    balanced-time packing (Algorithm 2) and the analytic layer profile
+logits     log probabilities, entropy, most likely tokens, divergence from a
+           teacher's listed tokens, and their gradients, row by row
 """

@@ -24,6 +24,8 @@ HMY_GRADIENTS_EXPORTED, HMY_GRADIENTS_ON_DEVICE = 0, 1
 HMY_STATE_SWAPPED, HMY_STATE_RESIDENT_IN_SPARE_BUDGET = 0, 1
 HMY_SWAP_OUT_KERNEL, HMY_SWAP_OUT_MEMCPY = 0, 1
 HMY_MAX_WEIGHT_SLOTS = 4
+HMY_MAX_TOP = 128
+HMY_ROWS_WORKSPACE_BYTES = 1 << 20
 (HMY_OK, HMY_E_INVALID, HMY_E_BUDGET_TOO_SMALL, HMY_E_BAD_SCHEDULE, HMY_E_HIP,
  HMY_E_NOT_BOUND, HMY_E_NO_DEVICE) = (0, -1, -2, -3, -4, -5, -6)
 
@@ -144,13 +146,36 @@ class hmy_gemm_desc(C.Structure):
                 ("res", C.c_void_p), ("ldr", C.c_int64), ("gelu_out", C.c_void_p), ("res_fp32", C.c_int32)]
 
 
+class hmy_logprob_desc(C.Structure):
+    _fields_ = [("logits_prec", C.c_int32), ("T", C.c_int32), ("V", C.c_int32), ("k", C.c_int32),
+                ("logits", C.c_void_p), ("ldl", C.c_int64), ("targets", C.c_void_p), ("logp", C.c_void_p),
+                ("row_max", C.c_void_p), ("log_sum", C.c_void_p), ("entropy", C.c_void_p), ("top_ids", C.c_void_p),
+                ("top_logp", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64),
+                ("scale", C.c_float), ("reserved_", C.c_int32)]
+
+
+class hmy_logprob_grad_desc(C.Structure):
+    _fields_ = [("prec", C.c_int32), ("logits_prec", C.c_int32), ("T", C.c_int32), ("V", C.c_int32),
+                ("logits", C.c_void_p), ("ldl", C.c_int64), ("row_max", C.c_void_p), ("log_sum", C.c_void_p),
+                ("targets", C.c_void_p), ("d_logp", C.c_void_p), ("entropy", C.c_void_p), ("d_entropy", C.c_void_p),
+                ("dlogits", C.c_void_p), ("ldd", C.c_int64), ("scale", C.c_float), ("pad", C.c_int32)]
+
+
+class hmy_distill_desc(C.Structure):
+    _fields_ = [("prec", C.c_int32), ("logits_prec", C.c_int32), ("T", C.c_int32), ("V", C.c_int32), ("K", C.c_int32),
+                ("tail", C.c_int32), ("logits", C.c_void_p), ("ldl", C.c_int64), ("teacher_ids", C.c_void_p),
+                ("teacher_logp", C.c_void_p), ("row_loss", C.c_void_p), ("loss_acc", C.c_void_p), ("dlogits", C.c_void_p),
+                ("ldd", C.c_int64), ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("scale", C.c_float),
+                ("grad_scale", C.c_float), ("pad", C.c_int32), ("reserved_", C.c_int32)]
+
+
 EXPORTS = [
     "hmy_strerror", "hmy_last_error", "hmy_model_size", "hmy_layout", "hmy_profile", "hmy_plan", "hmy_estimate", "hmy_arena",
     "hmy_arena_regions", "hmy_measure_profile",
     "hmy_count_swaps", "hmy_host_alloc", "hmy_host_free", "hmy_create", "hmy_get_schedule", "hmy_bind_state", "hmy_copies_on_engines", "hmy_resident_params", "hmy_sync_state",
     "hmy_iteration", "hmy_destroy", "hmy_set_profiling", "hmy_set_progress", "hmy_set_kernel_path", "hmy_k_embed_fwd", "hmy_k_embed_bwd",
     "hmy_k_layernorm_fwd", "hmy_k_layernorm_bwd", "hmy_k_layernorm_bwd_static", "hmy_k_gelu_fwd", "hmy_k_gelu_bwd", "hmy_k_gelu_bwd_colsum", "hmy_k_colsum",
-    "hmy_k_gemm", "hmy_gemm_tiles", "hmy_k_gemm_on_tiles", "hmy_k_attn_fwd", "hmy_k_attn_bwd", "hmy_k_xent", "hmy_k_adam", "hmy_host_adam",
+    "hmy_k_gemm", "hmy_gemm_tiles", "hmy_k_gemm_on_tiles", "hmy_k_attn_fwd", "hmy_k_attn_bwd", "hmy_k_xent", "hmy_k_logprob", "hmy_k_logprob_bwd", "hmy_k_distill", "hmy_k_adam", "hmy_host_adam",
 ]
 
 lib.hmy_strerror.restype = C.c_char_p
@@ -455,6 +480,34 @@ def hmy_k_attn_bwd(prec, qkv, o, d_o, lse, delta, dqkv, b, s, H, dh, causal, str
 def hmy_k_xent(prec, logits, targets, loss_acc, dlogits, T, V, ldl, inv_ntgt, stream=None):
     _check(lib.hmy_k_xent(prec, _p(logits), _p(targets), _p(loss_acc), _p(dlogits), T, V, C.c_int64(ldl),
                           C.c_float(inv_ntgt), _p(stream)))
+
+
+def _workspace(w):
+    return (_p(w), w.numel() * w.element_size() if w is not None else 0)
+
+
+def hmy_k_logprob(logits_prec, logits, T, V, ldl, targets=None, logp=None, row_max=None, log_sum=None, entropy=None, k=0,
+                  top_ids=None, top_logp=None, scale=1.0, stream=None, workspace=None):
+    """workspace: a tensor of HMY_ROWS_WORKSPACE_BYTES, which lets a call of few rows use the whole device."""
+    g = hmy_logprob_desc(logits_prec, T, V, k, _p(logits), ldl, _p(targets), _p(logp), _p(row_max), _p(log_sum),
+                         _p(entropy), _p(top_ids), _p(top_logp), *_workspace(workspace), scale, 0)
+    _check(lib.hmy_k_logprob(C.byref(g), _p(stream)))
+
+
+def hmy_k_logprob_bwd(prec, logits_prec, logits, row_max, log_sum, dlogits, T, V, ldl, ldd, targets=None, d_logp=None,
+                      entropy=None, d_entropy=None, scale=1.0, pad=0, stream=None):
+    """prec: type of dlogits, whose columns V .. V+pad-1 are zeroed."""
+    g = hmy_logprob_grad_desc(prec, logits_prec, T, V, _p(logits), ldl, _p(row_max), _p(log_sum), _p(targets), _p(d_logp),
+                              _p(entropy), _p(d_entropy), _p(dlogits), ldd, scale, pad)
+    _check(lib.hmy_k_logprob_bwd(C.byref(g), _p(stream)))
+
+
+def hmy_k_distill(prec, logits_prec, logits, teacher_ids, teacher_logp, row_loss, dlogits, T, V, K, ldl, ldd, tail=False,
+                  scale=1.0, grad_scale=1.0, pad=0, loss_acc=None, stream=None, workspace=None):
+    """prec: type of dlogits (None: the loss alone); workspace as for hmy_k_logprob."""
+    g = hmy_distill_desc(prec, logits_prec, T, V, K, int(tail), _p(logits), ldl, _p(teacher_ids), _p(teacher_logp),
+                         _p(row_loss), _p(loss_acc), _p(dlogits), ldd, *_workspace(workspace), scale, grad_scale, pad, 0)
+    _check(lib.hmy_k_distill(C.byref(g), _p(stream)))
 
 
 def hmy_host_adam(prec, grad_ptr, master_ptr, m_ptr, v_ptr, weights_ptr, n, lr, beta1, beta2, eps, step, threads=0):

@@ -265,6 +265,18 @@ int hmy_k_xent(int32_t prec, const float *logits, const int32_t *targets, double
   NOTNULL(logits); NOTNULL(targets); NOTNULL(loss_acc); NOTNULL(dlogits);
   return launch_xent(prec, logits, targets, loss_acc, dlogits, T, V, ldl, inv_ntgt, stream);
 }
+int hmy_k_logprob(const hmy_logprob_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->logits);
+  return launch_logprob(*g, stream);
+}
+int hmy_k_logprob_bwd(const hmy_logprob_grad_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->logits); NOTNULL(g->row_max); NOTNULL(g->log_sum); NOTNULL(g->dlogits);
+  return launch_logprob_bwd(*g, stream);
+}
+int hmy_k_distill(const hmy_distill_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->logits); NOTNULL(g->teacher_ids); NOTNULL(g->teacher_logp); NOTNULL(g->row_loss);
+  return launch_distill(*g, stream);
+}
 int hmy_k_adam(int32_t prec, const float *grad, float *master, float *m, float *v, void *w_out, uint64_t n,
                const hmy_adam *hp, void *stream) {
   NOTNULL(grad); NOTNULL(m); NOTNULL(v); NOTNULL(w_out); NOTNULL(hp);

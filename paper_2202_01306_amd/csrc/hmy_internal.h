@@ -190,6 +190,9 @@ int launch_attn_bwd_f32(const float *qkv, const float *o, const float *d_o, cons
                         int b, int s, int H, int dh, int causal, stream_t st);
 int launch_xent(int prec, const float *logits, const int32_t *targets, double *loss_acc,
                 void *dlogits, int T, int V, int64_t ldl, float inv_ntgt, stream_t st);
+int launch_logprob(const hmy_logprob_desc &g, stream_t st);
+int launch_logprob_bwd(const hmy_logprob_grad_desc &g, stream_t st);
+int launch_distill(const hmy_distill_desc &g, stream_t st);
 int launch_adam(int prec, const float *grad, float *master, float *m, float *v, void *w_out,
                 uint64_t n, const hmy_adam &hp, stream_t st);
 int launch_adam_out(int prec, const float *grad, const float *in_master, const float *in_m, const float *in_v,

@@ -1,0 +1,693 @@
+"""Operators on rows of logits (log probabilities, their gradient, distillation) against the fp64 oracle, element by element.
+
+Bounds, in units of u = 2^-24, half a step of fp32 relative to the value.  An exponent u_j = s (x_j - m) carries three
+roundings, so exp u_j is off by 3 |u_j| u relative, the exponential unit's own 2 u, and the sum of a row by one u per addition
+that a term passes through: at most ceil(V / 256) in a thread and 32 more where threads meet.  Weighted by the probabilities the
+|u_j| add up to at most log V.  So with n = ceil(V / 256) + 34 + 3 log V:
+  log S        n u absolute, and u |log S|
+  log p_j      that, and 4 |u_j| u
+  entropy      log S - A / S, both sums as above: 2 n u (1 + log V)
+  p_j          (n + 4 |l_j| + 4) u relative
+A gradient stored in bf16 is rounded once more, by at most 2^-8 of its value."""
+import ctypes
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import logits as ol
+from paper_2202_01306_amd import binding as B
+from paper_2202_01306_amd import synth
+
+U = 2.0 ** -24
+INF = math.inf
+DT = {"fp32": torch.float32, "bf16": torch.bfloat16}
+PC = {"fp32": B.HMY_PREC_FP32, "bf16": B.HMY_PREC_BF16}
+
+
+def say(msg):
+    print(msg, flush=True)
+
+
+def roundings(V):
+    return math.ceil(V / 256) + 34 + 3 * math.log(V + 1)
+
+
+def rows(rng, T, V, prec, spread=3.0, masked=0.1):
+    """Logits with ties (in bf16 by themselves, in fp32 from values drawn twice), some of them -inf."""
+    x = (rng.standard_normal((T, V)) * spread).astype(np.float32)
+    if V > 4:
+        x[:, V // 2:V // 2 + V // 4] = x[:, :V // 4]
+    if masked:
+        off = rng.random((T, V)) < masked
+        off[np.arange(T), rng.integers(0, V, T)] = False
+        x[off] = -INF
+    return synth.round_bf16(x) if prec == "bf16" else x
+
+
+def on_device(x, ld, prec, fill=float("nan")):
+    """[T, ld] of which the first columns are x and the others must not be looked at."""
+    T, V = x.shape
+    t = torch.full((T, ld), fill, device="cuda", dtype=DT[prec])
+    t[:, :V] = torch.from_numpy(x).to("cuda", DT[prec])
+    return t
+
+
+def f32(*shape):
+    return torch.full(shape, float("nan"), device="cuda", dtype=torch.float32)
+
+
+def i32(a):
+    return torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).cuda()
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def workspace(fill=0xff):
+    return torch.full((B.HMY_ROWS_WORKSPACE_BYTES,), fill, dtype=torch.uint8, device="cuda")
+
+
+class Forward:
+    """One call of hmy_k_logprob with every output."""
+
+    def __init__(self, x, targets, prec, k=0, ld=None, scale=1.0, ws=None, logits=None, stream=None):
+        self.T, self.V = x.shape
+        self.ld = ld or self.V
+        self.logits = on_device(x, self.ld, prec) if logits is None else logits
+        self.targets = i32(targets)
+        self.logp, self.row_max, self.log_sum, self.entropy = (f32(self.T) for _ in range(4))
+        self.top_ids = torch.full((self.T, k), -7, dtype=torch.int32, device="cuda")
+        self.top_logp = f32(self.T, k)
+        self.args = (PC[prec], self.logits, self.T, self.V, self.ld)
+        self.kw = dict(targets=self.targets, logp=self.logp, row_max=self.row_max, log_sum=self.log_sum, entropy=self.entropy,
+                       k=k, top_ids=self.top_ids if k else None, top_logp=self.top_logp if k else None, scale=scale,
+                       workspace=ws)
+        self.call()
+
+    def call(self, **kw):
+        B.hmy_k_logprob(*self.args, **dict(self.kw, **kw))
+
+    def outputs(self):
+        return [self.logp, self.row_max, self.log_sum, self.entropy, self.top_ids, self.top_logp]
+
+
+def near(got, ref, bound):
+    """Equal where the reference is no finite number, within the bound elsewhere."""
+    got, ref = np.asarray(got, np.float64), np.asarray(ref, np.float64)
+    fine = np.isfinite(ref)
+    np.testing.assert_array_equal(got[~fine], ref[~fine])
+    off = np.abs(got[fine] - ref[fine])
+    bound = np.broadcast_to(bound, ref.shape)[fine]
+    assert np.all(off <= bound), (float(off.max()), float((off / np.maximum(bound, 1e-300)).max()))
+
+
+def check_forward(f, x, targets, k, scale):
+    n = roundings(f.V)
+    top_ids, top_logp = f.top_ids.cpu().numpy(), host(f.top_logp)
+    logp, row_max, log_sum, H = host(f.logp), host(f.row_max), host(f.log_sum), host(f.entropy)
+    for r in range(f.T):
+        m, z, l = ol.log_probabilities(x[r], scale)
+        u = np.where(np.isfinite(l), np.abs(l - (0 if not np.isfinite(z) else 0)) + abs(z if np.isfinite(z) else 0), 0)
+        near(row_max[r], m, 0)
+        near(log_sum[r], z, U * (n + abs(z)))
+        near(H[r], ol.entropy(l), 2 * U * n * (1 + math.log(f.V)))
+        t = targets[r]
+        near(logp[r], l[t] if 0 <= t < f.V else 0.0, U * (n + 4 * u[t] + 4) if 0 <= t < f.V else 0)
+        ids, lp = ol.top(x[r], l, k)
+        np.testing.assert_array_equal(top_ids[r], ids)
+        near(top_logp[r], lp, U * (n + 4 * np.where(ids >= 0, u[ids], 0) + 4))
+
+
+SIZES = [(3, 1, 1, 3), (2, 2, 5, 2), (5, 7, 7, 4), (4, 63, 64, 5), (3, 64, 64, 64), (300, 65, 71, 8), (33, 255, 256, 128), (7, 257, 257, 1),
+         (130, 1000, 1003, 17), (2, 2048, 2048, 128), (3, 2049, 2056, 40), (40, 5003, 5003, 64), (2, 8193, 8200, 128), (3, 16385, 16385, 100),
+         (260, 30522, 30522, 3), (1, 50257, 50304, 10), (5, 50257, 50257, 128), (3, 66001, 66003, 64), (2, 131072, 131072, 128), (2, 200003, 200003, 77)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,V,ld,k", SIZES)
+def test_logprob_against_64_bits(prec, T, V, ld, k):
+    say(f"logprob {prec} T={T} V={V} ld={ld} k={k}")
+    rng = np.random.default_rng(V * 31 + T)
+    x = rows(rng, T, V, prec)
+    targets = rng.integers(0, V, T)
+    targets[::5] = -1
+    targets[1::7] = V          # names no token either
+    for scale, ws, kk in ((1.0, None, k), (0.6, workspace(), k), (1.0, workspace(), 0)):
+        f = Forward(x, targets, prec, kk, ld, scale, ws)
+        check_forward(f, x, targets, kk, float(np.float32(scale)))
+
+
+def special_rows(V):
+    rng = np.random.default_rng(V)
+    lowest = float(torch.finfo(torch.bfloat16).min)
+    x = rng.standard_normal((16, V)).astype(np.float32)
+    x[0] = -INF                                    # nothing left
+    x[1] = 0.25                                    # all equal
+    x[2] = lowest                                  # masks of the type's lowest value, and nothing but them
+    x[3] = lowest
+    x[3, V // 3] = 1.0
+    x[4] = -INF
+    x[4, [1, V - 1]] = 2.0, 3.0                    # fewer tokens than a list is long
+    x[5] = np.sort(x[5])                           # ascending: every later segment outranks all before
+    x[6] = -np.sort(-x[6])
+    x[7] = 0.0
+    x[7, ::2] = -0.0                               # equal
+    x[8, 7] = np.nan
+    x[9, V // 2] = INF
+    x[10] = 3.0e38
+    x[11] = -3.0e38
+    x[12] = np.where(np.arange(V) % 4096 < 8, 5.0 + np.arange(V) / V, -5.0)   # the largest in the same few threads
+    x[13] = np.where(np.arange(V) < V // 2, -INF, 1.0)
+    x[14] = np.where(np.arange(V) % 2048 < 16, 4.0, -3.0)                     # and all of them equal
+    x[15] = np.round(x[15])
+    return synth.round_bf16(x)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [40, 1000, 5003, 50257, 140001])
+@pytest.mark.parametrize("k", [1, 64, 128])
+def test_logprob_of_rows_where_it_can_go_wrong(prec, V, k):
+    say(f"logprob special {prec} V={V} k={k}")
+    x = special_rows(V)
+    targets = np.full(16, V // 3)
+    for ws in (None, workspace()):
+        f = Forward(x, targets, prec, k, V, 1.0, ws)
+        check_forward(f, x, targets, k, 1.0)
+        many = np.tile(x, (20, 1))                 # more rows than compute units: each is one workgroup's
+        g = Forward(many, np.tile(targets, 20), prec, k, V, 1.0, ws)
+        for a, b in zip(f.outputs(), g.outputs()):
+            if a.dtype == torch.int32:
+                assert torch.equal(a.repeat(20, 1), b)
+        check_forward(g, many[:16], targets, k, 1.0) if g.T == 16 else None
+
+
+@pytest.mark.gpu
+def test_logprob_any_subset_of_outputs():
+    rng = np.random.default_rng(3)
+    for T, V, ws in ((4, 5003, None), (4, 50257, workspace()), (300, 5003, workspace())):
+        x, targets = rows(rng, T, V, "fp32"), rng.integers(0, V, T)
+        whole = Forward(x, targets, "fp32", 9, V, 1.0, ws)
+        for name in ("row_max", "log_sum", "entropy"):
+            out = f32(T)
+            B.hmy_k_logprob(0, whole.logits, T, V, V, workspace=ws, **{name: out})
+            assert torch.equal(out, getattr(whole, name)), name
+        out = f32(T)
+        B.hmy_k_logprob(0, whole.logits, T, V, V, targets=whole.targets, logp=out, workspace=ws)
+        assert torch.equal(out, whole.logp)
+        ids, lp = torch.zeros(T, 9, dtype=torch.int32, device="cuda"), f32(T, 9)
+        B.hmy_k_logprob(0, whole.logits, T, V, V, k=9, top_ids=ids, top_logp=lp, workspace=ws)
+        assert torch.equal(ids, whole.top_ids) and torch.equal(lp, whole.top_logp)
+
+
+def gradient_bound(x, l, scale, n, target, a, h, bf16):
+    """What the roundings can do to one row's gradient."""
+    p = np.exp(l)
+    fine = np.where(np.isfinite(l), l, 0.0)
+    H = ol.entropy(l)
+    size = scale * p * (abs(a) + abs(h) * (np.abs(fine) + H))
+    hot = np.zeros_like(p)
+    if 0 <= target < len(p):
+        hot[target] = scale * abs(a)
+    return U * (2 * n + 8 * np.abs(fine) + 16) * size + U * scale * p * abs(h) * (2 * n) * (1 + math.log(len(p))) + 4 * U * hot
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lp,ep", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("T,V,ldl,ldd,pad", [(3, 1, 1, 1, 0), (2, 7, 9, 8, 1), (300, 65, 65, 72, 7), (33, 1000, 1001, 1003, 2),
+                                             (5, 5003, 5008, 5008, 5), (2, 50257, 50304, 50304, 47), (3, 131071, 131071, 131071, 0),
+                                             (270, 8193, 8193, 8200, 0)])
+def test_logprob_backward_against_64_bits(lp, ep, T, V, ldl, ldd, pad):
+    say(f"logprob_bwd {lp} -> {ep} T={T} V={V} ldl={ldl} ldd={ldd} pad={pad}")
+    rng = np.random.default_rng(V + T)
+    x = rows(rng, T, V, lp)
+    targets = rng.integers(0, V, T)
+    targets[::4] = -1
+    a, h = rng.standard_normal(T).astype(np.float32), (rng.standard_normal(T) * 0.3).astype(np.float32)
+    scale = float(np.float32(0.8))
+    f = Forward(x, targets, lp, 0, ldl, scale)
+    ad, hd = torch.from_numpy(a).cuda(), torch.from_numpy(h).cuda()
+    for use_a, use_h in ((True, True), (True, False), (False, True)):
+        d = torch.full((T, ldd), 7.0, device="cuda", dtype=DT[ep])
+        B.hmy_k_logprob_bwd(PC[ep], PC[lp], f.logits, f.row_max, f.log_sum, d, T, V, ldl, ldd, targets=f.targets if use_a else None,
+                            d_logp=ad if use_a else None, entropy=f.entropy if use_h else None, d_entropy=hd if use_h else None,
+                            scale=scale, pad=pad)
+        got = host(d)
+        assert np.all(got[:, V:V + pad] == 0) and np.all(got[:, V + pad:] == 7)
+        for r in range(T):
+            av, hv = float(a[r]) if use_a else 0.0, float(h[r]) if use_h else 0.0
+            t = int(targets[r]) if use_a else -1
+            ref = ol.logprob_bwd(x[r], t, av, hv, scale)
+            l = ol.log_probabilities(x[r], scale)[2]
+            off = gradient_bound(x[r], l, scale, roundings(V), t, av, hv, ep)
+            near(got[r, :V], ref, off + (2.0 ** -8 * (np.abs(ref) + off) if ep == "bf16" else 0) + 1e-37)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+def test_logprob_backward_of_rows_where_it_can_go_wrong(prec):
+    V = 5003
+    x = special_rows(V)
+    targets = np.full(16, V // 3)
+    f = Forward(x, targets, prec, 0, V)
+    a, h = torch.full((16,), 0.5, device="cuda"), torch.full((16,), -0.25, device="cuda")
+    d = torch.full((16, V), 7.0, device="cuda", dtype=DT[prec])
+    B.hmy_k_logprob_bwd(PC[prec], PC[prec], f.logits, f.row_max, f.log_sum, d, 16, V, V, V, targets=f.targets, d_logp=a,
+                        entropy=f.entropy, d_entropy=h)
+    got = host(d)
+    assert np.isnan(got[8]).any() and np.isnan(got[9]).any()      # NaN and +inf
+    for r in [r for r in range(16) if r not in (8, 9)]:
+        ref = ol.logprob_bwd(x[r], V // 3, 0.5, -0.25, 1.0)
+        l = ol.log_probabilities(x[r], 1.0)[2]
+        off = gradient_bound(x[r], l, 1.0, roundings(V), V // 3, 0.5, -0.25, prec)
+        near(got[r], ref, off + (2.0 ** -8 * (np.abs(ref) + off) if prec == "bf16" else 0) + 1e-37)
+
+
+def teacher_lists(rng, x, K, scale=1.0):
+    """A teacher's K most likely tokens: the student's logits moved about."""
+    T, V = x.shape
+    ids, lp = np.full((T, K), -1, np.int32), np.full((T, K), -INF, np.float32)
+    for r in range(T):
+        y = x[r].astype(np.float64) + rng.standard_normal(V)
+        l = ol.log_probabilities(y, scale)[2]
+        i, v = ol.top(y, l, K)
+        ids[r], lp[r] = i, v.astype(np.float32)
+    return ids, lp
+
+
+def check_distill(loss, d, x, ids, lp, scale, w, tail, bf16, V):
+    n = roundings(V)
+    for r in range(len(x)):
+        ref_loss, g = ol.distill(x[r], ids[r], lp[r], scale, tail)
+        m, z, l = ol.log_probabilities(x[r], scale)
+        # the list's terms are held in 64 bits and leave log S, off by n u; the result is rounded once
+        near(loss[r], ref_loss, U * (n + abs(ref_loss)))
+        if d is None:
+            continue
+        p = np.exp(l)
+        fine = np.where(np.isfinite(l), np.abs(l), 0.0)
+        listed = np.zeros(V)
+        for i, t in zip(ids[r], lp[r]):
+            if 0 <= i < V and t > -INF:
+                listed[i] += math.exp(t)
+        if not tail and listed.sum() > 0:
+            listed /= listed.sum()
+        # Q - q_r / p_r: the quotient's error is that of p_r, as large as that of p
+        keep = 1.0
+        if tail:
+            rest = p[listed == 0].sum()
+            keep = 1.0 + (max(0.0, 1.0 - listed.sum()) / rest if rest > 0 else 0.0)
+        off = scale * w * U * ((2 * n + 8 * fine + 16) * p * keep + 4 * listed)
+        ref = g * w
+        near(d[r], ref, off + (2.0 ** -8 * (np.abs(ref) + off) if bf16 else 0) + 1e-37)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("lp,ep", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("T,V,ldl,ldd,pad,K", [(3, 1, 1, 1, 0, 1), (2, 7, 9, 8, 1, 7), (300, 65, 65, 72, 7, 5), (33, 1000, 1001, 1003, 2, 128),
+                                               (40, 2049, 2056, 2056, 7, 33), (5, 5003, 5008, 5008, 5, 8), (2, 50257, 50304, 50304, 47, 64),
+                                               (3, 131071, 131071, 131071, 0, 128), (260, 8193, 8193, 8200, 0, 16), (2, 200003, 200003, 200003, 0, 20)])
+def test_distill_against_64_bits(tail, lp, ep, T, V, ldl, ldd, pad, K):
+    say(f"distill {lp} -> {ep} T={T} V={V} ldl={ldl} ldd={ldd} pad={pad} K={K} tail={tail}")
+    rng = np.random.default_rng(V + T + K)
+    x = rows(rng, T, V, lp, masked=0.0)
+    scale, w = float(np.float32(0.7)), float(np.float32(1.0 / 57))
+    ids, t = teacher_lists(rng, x, K, scale)
+    ids[T - 1] = -1                               # padding
+    logits = on_device(x, ldl, lp)
+    for ws in (None, workspace()):
+        loss, d = f32(T), torch.full((T, ldd), 7.0, device="cuda", dtype=DT[ep])
+        acc = torch.full((1,), 0.5, device="cuda", dtype=torch.float64)
+        B.hmy_k_distill(PC[ep], PC[lp], logits, i32(ids), torch.from_numpy(t).cuda(), loss, d, T, V, K, ldl, ldd, tail=tail, scale=scale,
+                        grad_scale=w, pad=pad, loss_acc=acc, workspace=ws)
+        got = host(d)
+        assert np.all(got[:, V:V + pad] == 0) and np.all(got[:, V + pad:] == 7)
+        assert host(loss)[T - 1] == 0 and np.all(got[T - 1, :V] == 0)
+        check_distill(host(loss), got[:, :V], x, ids, t, scale, w, tail, ep == "bf16", V)
+        np.testing.assert_allclose(host(acc)[0], 0.5 + w * host(loss).sum(), rtol=1e-12)
+        alone = f32(T)
+        B.hmy_k_distill(PC[ep], PC[lp], logits, i32(ids), torch.from_numpy(t).cuda(), alone, None, T, V, K, ldl, ldd, tail=tail, scale=scale,
+                        grad_scale=w, workspace=ws)
+        assert torch.equal(alone, loss)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("V", [200, 5003, 70001])
+def test_distill_of_lists_and_rows_where_it_can_go_wrong(prec, tail, V):
+    say(f"distill special {prec} V={V} tail={tail}")
+    rng = np.random.default_rng(V)
+    K = 6
+    x = rows(rng, 12, V, prec, masked=0.0)
+    ids, t = teacher_lists(rng, x, K)
+    ids[0, 3] = ids[0, 0]                          # one token twice
+    ids[1] = 5                                     # and six times
+    t[1] = np.log(0.1)
+    ids[2, 1], ids[2, 4] = -1, V                   # no tokens
+    t[3, 2] = -INF                                 # no weight
+    t[4] = -INF
+    ids[5] = -5
+    x[6, ids[6, 0]] = -INF                         # the student has masked what the teacher lists
+    x[7] = -INF
+    x[7, ids[7]] = 1.0                             # and everything else: the tail has no weight
+    x[8] = float(torch.finfo(torch.bfloat16).min)
+    t[9] = np.log(0.3)                             # adds up to more than 1
+    x[10, 3] = np.nan
+    t[11, 1] = np.nan
+    logits = on_device(x, V, prec)
+    for ws in (None, workspace()):
+        loss, d = f32(12), torch.full((12, V), 7.0, device="cuda", dtype=DT[prec])
+        B.hmy_k_distill(PC[prec], PC[prec], logits, i32(ids), torch.from_numpy(t).cuda(), loss, d, 12, V, K, V, V, tail=tail, workspace=ws)
+        ls, got = host(loss), host(d)
+        assert np.isnan(ls[10]) and np.isnan(ls[11]) and np.isnan(got[10]).any() and np.isnan(got[11]).any()
+        assert ls[4] == 0 and ls[5] == 0 and np.all(got[4:6] == 0)
+        assert ls[6] == INF
+        check_distill(ls[:10], got[:10], x[:10], ids[:10], t[:10], 1.0, 1.0, tail, prec == "bf16", V)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tail", [False, True])
+def test_distill_of_whole_vocabularies_is_the_divergence(tail):
+    """Every token listed: no class of others, and with the student's own probabilities neither loss nor gradient."""
+    rng = np.random.default_rng(8)
+    T, V = 5, 100
+    x = rows(rng, T, V, "fp32", masked=0.0)
+    logits = on_device(x, V, "fp32")
+    ids = np.tile(np.arange(V), (T, 1))
+    t = np.stack([ol.log_probabilities(x[r])[2] for r in range(T)]).astype(np.float32)
+    loss, d = f32(T), f32(T, V)
+    B.hmy_k_distill(0, 0, logits, i32(ids), torch.from_numpy(t).cuda(), loss, d, T, V, V, V, V, tail=tail)
+    assert np.abs(host(loss)).max() < U * 2 * roundings(V) and np.abs(host(d)).max() < U * 2 * roundings(V) * 4
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,V", [(3, 70001), (300, 2050), (300, 30522), (2, 140001)])
+def test_gradients_in_place(prec, T, V):
+    rng = np.random.default_rng(V)
+    x, targets = rows(rng, T, V, prec, masked=0.0), rng.integers(0, V, T)
+    ids = np.stack([rng.choice(V, 9, replace=False) for _ in range(T)])
+    t = np.log(np.full((T, 9), 0.1, np.float32))
+    one = torch.ones(T, device="cuda")
+    for ws in (None, workspace()):
+        f = Forward(x, targets, prec, 0, V + 3)
+        apart, kept = torch.zeros_like(f.logits), f.logits.clone()
+        B.hmy_k_logprob_bwd(PC[prec], PC[prec], f.logits, f.row_max, f.log_sum, apart, T, V, V + 3, V + 3, targets=f.targets, d_logp=one)
+        B.hmy_k_logprob_bwd(PC[prec], PC[prec], f.logits, f.row_max, f.log_sum, f.logits, T, V, V + 3, V + 3, targets=f.targets, d_logp=one)
+        assert torch.equal(f.logits[:, :V], apart[:, :V]) and torch.isnan(f.logits[:, V:]).all()
+        for tail in (False, True):
+            inside, losses = kept.clone(), [f32(T), f32(T)]
+            for out, src, loss in ((apart, inside, losses[0]), (inside, inside, losses[1])):
+                B.hmy_k_distill(PC[prec], PC[prec], src, i32(ids), torch.from_numpy(t).cuda(), loss, out, T, V, 9, V + 3, V + 3, tail=tail,
+                                workspace=ws)
+            assert torch.equal(inside[:, :V], apart[:, :V]) and torch.isnan(inside[:, V:]).all() and torch.equal(*losses)
+
+
+@pytest.mark.gpu
+def test_logits_and_gradients_side_by_side_in_one_array():
+    T, V = 20, 1000
+    rng = np.random.default_rng(1)
+    x, targets = rows(rng, T, V, "fp32", masked=0.0), rng.integers(0, V, T)
+    both = torch.full((T, 2 * V + 5), 7.0, device="cuda")
+    both[:, :V] = torch.from_numpy(x).cuda()
+    f = Forward(x, targets, "fp32", 0, 2 * V + 5, logits=both)
+    one = torch.ones(T, device="cuda")
+    B.hmy_k_logprob_bwd(0, 0, both, f.row_max, f.log_sum, both[:, V + 2:], T, V, 2 * V + 5, 2 * V + 5, targets=f.targets, d_logp=one)
+    apart = f32(T, V)
+    B.hmy_k_logprob_bwd(0, 0, both, f.row_max, f.log_sum, apart, T, V, 2 * V + 5, V, targets=f.targets, d_logp=one)
+    assert torch.equal(both[:, V + 2:2 * V + 2], apart)
+    assert torch.equal(both[:, :V], torch.from_numpy(x).cuda()) and torch.all(both[:, V:V + 2] == 7) and torch.all(both[:, 2 * V + 2:] == 7)
+
+
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits():
+    """Rows 2^23 elements apart, 2^31 and more of them before the last."""
+    T, V, ld = 300, 3001, 1 << 23
+    rng = np.random.default_rng(2)
+    x, targets = rows(rng, T, V, "bf16", masked=0.0), rng.integers(0, V, T)
+    logits = torch.empty(T * ld, device="cuda", dtype=torch.bfloat16).view(T, ld)
+    logits[:, :V] = torch.from_numpy(x).to("cuda", torch.bfloat16)
+    f = Forward(x, targets, "bf16", 5, ld, logits=logits)
+    dense = Forward(x, targets, "bf16", 5, V)
+    for a, b in zip(f.outputs(), dense.outputs()):
+        assert torch.equal(a, b)
+    one = torch.ones(T, device="cuda")
+    want = torch.zeros(T, V, device="cuda", dtype=torch.bfloat16)
+    B.hmy_k_logprob_bwd(1, 1, logits, f.row_max, f.log_sum, want, T, V, ld, V, targets=f.targets, d_logp=one)
+    B.hmy_k_logprob_bwd(1, 1, logits, f.row_max, f.log_sum, logits, T, V, ld, ld, targets=f.targets, d_logp=one)
+    assert torch.equal(logits[:, :V], want)
+    logits[:, :V] = torch.from_numpy(x).to("cuda", torch.bfloat16)
+    ids, t = teacher_lists(rng, x, 4)
+    losses = [f32(T), f32(T)]
+    B.hmy_k_distill(1, 1, logits, i32(ids), torch.from_numpy(t).cuda(), losses[0], want, T, V, 4, ld, V)
+    B.hmy_k_distill(1, 1, logits, i32(ids), torch.from_numpy(t).cuda(), losses[1], logits, T, V, 4, ld, ld)
+    assert torch.equal(*losses) and torch.equal(logits[:, :V], want)
+
+
+@pytest.mark.gpu
+def test_more_rows_than_one_launch_has_workgroups():
+    T, V = (1 << 20) + 37, 3
+    x = torch.randn(T, V, device="cuda", generator=torch.Generator(device="cuda").manual_seed(0))
+    logp, z, m, H = f32(T), f32(T), f32(T), f32(T)
+    ids, lp = torch.zeros(T, 2, dtype=torch.int32, device="cuda"), f32(T, 2)
+    tgt = (torch.arange(T, device="cuda") % V).to(torch.int32)
+    B.hmy_k_logprob(0, x, T, V, V, targets=tgt, logp=logp, row_max=m, log_sum=z, entropy=H, k=2, top_ids=ids, top_logp=lp)
+    ref = torch.log_softmax(x.double(), 1)
+    n = roundings(V) * U
+    assert float((logp - ref.gather(1, tgt.long()[:, None])[:, 0]).abs().max()) < 16 * n
+    assert float((H + (ref * ref.exp()).sum(1)).abs().max()) < 16 * n
+    best = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :2]
+    assert torch.equal(ids.long(), best)
+    d = f32(T, V)
+    one = torch.ones(T, device="cuda")
+    B.hmy_k_logprob_bwd(0, 0, x, m, z, d, T, V, V, V, targets=tgt, d_logp=one)
+    hot = torch.zeros(T, V, device="cuda", dtype=torch.float64).scatter_(1, tgt.long()[:, None], 1.0)
+    assert float((d - (hot - ref.exp())).abs().max()) < 16 * n
+    loss = f32(T)
+    B.hmy_k_distill(0, 0, x, ids, lp, loss, d, T, V, 2, V, V)
+    q = torch.softmax(lp.double(), 1)
+    assert float((loss - (q * (q.log() - ref.gather(1, best))).sum(1)).abs().max()) < 16 * n
+    assert float((d - (ref.exp() - torch.zeros_like(hot).scatter_(1, best, q))).abs().max()) < 16 * n
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,V", [(2, 50257), (300, 5003)])
+def test_captured_and_replayed(T, V):
+    """Each of the three in one graph, replayed between eager calls on other inputs, on a stream of its own."""
+    rng = np.random.default_rng(T)
+    K = 12
+    ws = workspace()
+    xs = [rows(rng, T, V, "fp32", masked=0.0) for _ in range(4)]
+    targets = rng.integers(0, V, T)
+    logits = torch.from_numpy(xs[0]).cuda()
+    one = torch.ones(T, device="cuda")
+    logp, m, z, H, loss = (f32(T) for _ in range(5))
+    ids, lp = torch.zeros(T, K, dtype=torch.int32, device="cuda"), f32(T, K)
+    d1, d2 = f32(T, V), f32(T, V)
+    acc = torch.zeros(1, device="cuda", dtype=torch.float64)
+    tg = i32(targets)
+
+    def calls(stream, ws):
+        B.hmy_k_logprob(0, logits, T, V, V, targets=tg, logp=logp, row_max=m, log_sum=z, entropy=H, k=K, top_ids=ids, top_logp=lp, stream=stream,
+                        workspace=ws)
+        B.hmy_k_logprob_bwd(0, 0, logits, m, z, d1, T, V, V, V, targets=tg, d_logp=one, entropy=H, d_entropy=one, stream=stream)
+        B.hmy_k_distill(0, 0, logits, ids, lp, loss, d2, T, V, K, V, V, tail=True, loss_acc=acc, stream=stream, workspace=ws)
+
+    outs = [logp, m, z, H, ids, lp, d1, d2, loss]
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        calls(torch.cuda.current_stream().cuda_stream, ws)
+    for x in xs + xs:
+        logits.copy_(torch.from_numpy(x).cuda())
+        acc.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_acc = [o.clone() for o in outs], acc.clone()
+        for o in outs:
+            o.zero_()
+        acc.zero_()
+        calls(None, workspace(0x11))
+        torch.cuda.synchronize()
+        for a, b in zip(got, outs):
+            assert torch.equal(a, b)
+        assert torch.equal(got_acc, acc)
+
+
+@pytest.mark.gpu
+def test_two_streams_with_a_workspace_each():
+    rng = np.random.default_rng(5)
+    T, V, k = 3, 50257, 20
+    xs = [rows(rng, T, V, "fp32") for _ in range(2)]
+    targets = rng.integers(0, V, T)
+    alone = [Forward(x, targets, "fp32", k, V, 1.0, workspace()) for x in xs]
+    want = [[o.clone() for o in f.outputs()] for f in alone]
+    streams, spaces = [torch.cuda.Stream(), torch.cuda.Stream()], [workspace(), workspace()]
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for f, s, ws in zip(alone, streams, spaces):
+            f.call(stream=s.cuda_stream, workspace=ws)
+    torch.cuda.synchronize()
+    for f, w in zip(alone, want):
+        for a, b in zip(f.outputs(), w):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+def test_a_teacher_a_student_and_a_policy_gradient_through_the_head(prec):
+    """As a training program runs them: the teacher's vocabulary projection and its list, the student's projection and the
+    divergence, then the gradient's way back through the projection; and the gradient of given tokens' log probabilities."""
+    rng = np.random.default_rng(4)
+    T, d, V, K = 96, 64, 1003, 24
+    ldl = (V + 63) // 64 * 64
+    bf = prec == "bf16"
+    r = lambda *s: (lambda a: synth.round_bf16(a) if bf else a)(rng.standard_normal(s).astype(np.float32))
+    zt, wt, zs, wh = r(T, d), r(V, d) * 0.5, r(T, d), r(V, d) * 0.25
+    dev = lambda a: torch.from_numpy(a).to("cuda", DT[prec])
+    wtd, whd, zsd = dev(wt), dev(wh), dev(zs)
+    teacher, student = torch.zeros(T, ldl, device="cuda"), torch.zeros(T, ldl, device="cuda")
+    B.hmy_k_gemm(PC[prec], T, V, d, dev(zt), d, wtd, d, teacher, ldl, c_fp32=1)
+    ids, lp = torch.zeros(T, K, dtype=torch.int32, device="cuda"), f32(T, K)
+    B.hmy_k_logprob(0, teacher, T, V, ldl, k=K, top_ids=ids, top_logp=lp)
+    ids[T - 5:] = -1                              # padding
+    B.hmy_k_gemm(PC[prec], T, V, d, zsd, d, whd, d, student, ldl, c_fp32=1)
+    loss, acc = f32(T), torch.zeros(1, device="cuda", dtype=torch.float64)
+    dl = torch.full((T, ldl), float("nan"), device="cuda", dtype=DT[prec])
+    B.hmy_k_distill(PC[prec], 0, student, ids, lp, loss, dl, T, V, K, ldl, ldl, tail=True, grad_scale=1.0 / T, pad=ldl - V, loss_acc=acc)
+    dz, dw = torch.zeros(T, d, device="cuda"), torch.zeros(V, d, device="cuda")
+    B.hmy_k_gemm(PC[prec], T, d, V, dl, ldl, whd, d, dz, d, tb=1, c_fp32=1, accumulate=1)
+    B.hmy_k_gemm(PC[prec], V, d, T, dl, ldl, zsd, d, dw, d, ta=1, tb=1, c_fp32=1, accumulate=1)
+    # 64 bits, from the teacher's list as recorded
+    x = zs.astype(np.float64) @ wh.astype(np.float64).T
+    pairs = [ol.distill(x[t], ids.cpu().numpy()[t], host(lp)[t], 1.0, True) for t in range(T)]
+    ref_loss, g = np.array([p[0] for p in pairs]), np.stack([p[1] for p in pairs]) / T
+    # logits of d products, each in fp32: off by (d + 2) u |z| |w|, times what the loss and the gradient make of it
+    off = U * (d + 2) * (np.abs(zs.astype(np.float64)) @ np.abs(wh.astype(np.float64)).T).max(1)
+    near(host(loss), ref_loss, U * roundings(V) + 2 * off + U * np.abs(ref_loss))
+    np.testing.assert_allclose(host(acc)[0], host(loss).sum() * float(np.float32(1.0 / T)), rtol=1e-12)   # the ABI carries fp32
+    step = 2.0 ** -8 if bf else U * (roundings(V) + 40)
+    slack = np.abs(g) * step + (U * (2 * roundings(V) + 64) + 2 * off[:, None]) * (np.exp(np.stack([ol.log_probabilities(r)[2] for r in x])) * 3 + 1e-3) / T
+    assert np.all(np.abs(host(dl)[:, :V] - g) <= slack) and np.all(host(dl)[:, V:] == 0)
+    sums = U * (V + T)
+    near(host(dz), g @ wh.astype(np.float64), slack @ np.abs(wh) + sums * (np.abs(g) @ np.abs(wh)))
+    near(host(dw), g.T @ zs.astype(np.float64), slack.T @ np.abs(zs) + sums * (np.abs(g).T @ np.abs(zs)))
+    # given tokens: forward, a loss of its outputs, backward
+    targets = rng.integers(0, V, T)
+    logp, m, z, H = (f32(T) for _ in range(4))
+    tg, adv = i32(targets), torch.from_numpy(rng.standard_normal(T).astype(np.float32)).cuda()
+    bonus = torch.full((T,), 0.01, device="cuda")
+    B.hmy_k_logprob(0, student, T, V, ldl, targets=tg, logp=logp, row_max=m, log_sum=z, entropy=H)
+    B.hmy_k_logprob_bwd(PC[prec], 0, student, m, z, dl, T, V, ldl, ldl, targets=tg, d_logp=adv, entropy=H, d_entropy=bonus, pad=ldl - V)
+    for t in range(T):
+        l = ol.log_probabilities(x[t])[2]
+        ref = ol.logprob_bwd(x[t], int(targets[t]), float(adv[t]), 0.01)
+        e = gradient_bound(x[t], l, 1.0, roundings(V), int(targets[t]), float(adv[t]), 0.01, bf)
+        e = e + 4 * off[t] * (np.exp(l) * (abs(float(adv[t])) + 0.2) + 1e-6)
+        near(host(dl)[t, :V], ref, e + step * (np.abs(ref) + e))
+    near(host(logp), [ol.log_probabilities(x[t])[2][targets[t]] for t in range(T)], U * (roundings(V) + 80) + 2 * off)
+
+
+# ---- without a GPU ------------------------------------------------------------------------------
+
+def test_structs_match_the_header(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    names = ["hmy_logprob_desc", "hmy_logprob_grad_desc", "hmy_distill_desc"]
+    src = tmp_path / "sz.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "hmy.h"\nint main(void){' +
+                   "".join(f'printf("%zu\\n", sizeof({n}));' +
+                           "".join(f'printf("%zu\\n", offsetof({n}, {f}));' for f, _ in getattr(B, n)._fields_) for n in names) +
+                   'printf("%d %d\\n", HMY_MAX_TOP, HMY_ROWS_WORKSPACE_BYTES);return 0;}')
+    exe = tmp_path / "sz"
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(root, "include"), str(src), "-o", str(exe)], check=True)
+    out = [int(v) for v in subprocess.run([str(exe)], check=True, capture_output=True, text=True).stdout.split()]
+    want = []
+    for n in names:
+        S = getattr(B, n)
+        want += [ctypes.sizeof(S)] + [getattr(S, f).offset for f, _ in S._fields_]
+    assert out == want + [B.HMY_MAX_TOP, B.HMY_ROWS_WORKSPACE_BYTES]
+
+
+P = 1 << 20    # an address that is looked at for its alignment only
+
+
+def forward(**kw):
+    a = dict(logits_prec=0, logits=P, T=2, V=10, ldl=10, targets=P, logp=P)
+    a.update(kw)
+    B.hmy_k_logprob(**a)
+
+
+def backward(**kw):
+    a = dict(prec=0, logits_prec=0, logits=P, row_max=P, log_sum=P, dlogits=2 * P, T=2, V=10, ldl=10, ldd=10, targets=P, d_logp=P)
+    a.update(kw)
+    B.hmy_k_logprob_bwd(**a)
+
+
+def distill(**kw):
+    a = dict(prec=0, logits_prec=0, logits=P, teacher_ids=P, teacher_logp=P, row_loss=P, dlogits=2 * P, T=2, V=10, K=3, ldl=10, ldd=10)
+    a.update(kw)
+    B.hmy_k_distill(**a)
+
+
+NAN = float("nan")
+
+
+@pytest.mark.parametrize("call,bad", [
+    *[(forward, kw) for kw in (dict(logits=None), dict(T=0), dict(T=-1), dict(V=0), dict(V=(1 << 24) + 1, ldl=1 << 25), dict(ldl=9), dict(ldl=-10),
+                               dict(ldl=1 << 60), dict(logits_prec=2), dict(logits_prec=-1), dict(logits=P + 2), dict(logits_prec=1, logits=P + 1),
+                               dict(scale=0.0), dict(scale=-1.0), dict(scale=NAN), dict(scale=INF), dict(k=-1), dict(k=129, top_ids=P, top_logp=P),
+                               dict(k=1), dict(k=1, top_ids=P), dict(k=1, top_logp=P), dict(targets=None), dict(logp=None),
+                               dict(targets=None, logp=None), dict(logp=P + 2), dict(entropy=P + 1), dict(targets=P + 3))],
+    *[(backward, kw) for kw in (dict(logits=None), dict(row_max=None), dict(log_sum=None), dict(dlogits=None), dict(T=0), dict(V=0), dict(ldl=9),
+                                dict(ldd=9), dict(pad=-1), dict(pad=1), dict(prec=3), dict(logits_prec=7), dict(scale=0.0), dict(scale=NAN),
+                                dict(d_logp=None), dict(targets=None), dict(d_entropy=P), dict(dlogits=2 * P + 2), dict(logits=P + 1),
+                                dict(dlogits=P + 4), dict(dlogits=P, prec=1), dict(dlogits=P, ldd=12), dict(dlogits=P + 40 - 4),
+                                dict(dlogits=P - 4), dict(ldl=20, ldd=20, dlogits=P + 36), dict(ldl=20, ldd=20, dlogits=P + 44))],
+    *[(distill, kw) for kw in (dict(logits=None), dict(teacher_ids=None), dict(teacher_logp=None), dict(row_loss=None), dict(T=0), dict(V=0),
+                               dict(K=0), dict(K=129), dict(K=-1), dict(ldl=9), dict(ldd=9), dict(pad=-1), dict(pad=1), dict(prec=2),
+                               dict(logits_prec=2), dict(scale=0.0), dict(scale=-INF), dict(grad_scale=NAN), dict(grad_scale=INF), dict(tail=2),
+                               dict(row_loss=P + 2), dict(loss_acc=P + 4), dict(dlogits=P + 4), dict(dlogits=P, prec=1))],
+])
+def test_refusals(call, bad):
+    with pytest.raises(B.HmyError) as e:
+        call(**bad)
+    assert e.value.code == B.HMY_E_INVALID and len(str(e.value)) > 30
+
+
+def test_no_description_at_all():
+    for f in (B.lib.hmy_k_logprob, B.lib.hmy_k_logprob_bwd, B.lib.hmy_k_distill):
+        assert f(None, None) == B.HMY_E_INVALID
+
+
+def test_oracle_gradients_are_differences():
+    """The formulas of the fp64 oracle against central differences of its own losses: step h leaves h^2 and rounding / h."""
+    rng = np.random.default_rng(0)
+    V, h = 12, 1e-5
+    x = rng.standard_normal(V) * 2
+    x[5] = -INF
+    ids, t = np.array([3, 7, 7, -1, 2]), np.log(np.array([0.3, 0.2, 0.1, 0.5, 0.05]))
+
+    def scored(y):
+        l = ol.log_probabilities(y, 0.7)[2]
+        return 1.3 * l[4] - 0.4 * ol.entropy(l)
+
+    for f, g in ((scored, ol.logprob_bwd(x, 4, 1.3, -0.4, 0.7)),
+                 (lambda y: ol.distill(y, ids, t, 0.7, False)[0], ol.distill(x, ids, t, 0.7, False)[1]),
+                 (lambda y: ol.distill(y, ids, t, 0.7, True)[0], ol.distill(x, ids, t, 0.7, True)[1])):
+        for j in range(V):
+            if j == 5:
+                assert g[j] == 0
+                continue
+            e = np.zeros(V)
+            e[j] = h
+            assert abs((f(x + e) - f(x - e)) / (2 * h) - g[j]) < 1e-8
