@@ -1,0 +1,392 @@
+// The divergence of a student's rows of logits from a teacher's listed tokens, and its gradient.
+//
+// With u_j = s (x_j - m), S = sum exp u_j, l_j = u_j - log S, p_j = exp l_j, the teacher's q_k of listed tokens and, with a tail,
+// q_r = 1 - sum q_k of all others together (the student's: p_r):
+//   loss = sum q_k (log q_k - l_k) + q_r (log q_r - log p_r),  Q = sum q_k + q_r,
+//   dloss/dz_j = Q p_j - q_j for listed tokens, p_j (Q - q_r / p_r) for the others (z = s x; without a tail q_r = 0, Q = 1).
+// A divergence is small beside the logarithms that it is the difference of: the list's terms are held in 64 bits.  With a tail
+// the row's sum is taken as that of the others (listed tokens are set to -inf where they are loaded) and that of the list, so
+// that p_r of a student who is sure of listed tokens is no difference of two sums.
+#include "logit_rows.h"
+
+namespace hmy {
+
+namespace {
+
+struct DistillArgs {
+  const int32_t *ids;
+  const float *logp;
+  float *row_loss;
+  int T, V, K, pad;
+  int64_t ldl, ldd;
+  float scale, grad_scale;
+  bool tail;
+};
+
+// A row's list, in LDS: written and read by one wave, entries lane and lane + 64 a lane's own.  An entry that names no token or
+// has no weight is not there.
+struct List {
+  int id[HMY_MAX_TOP];      // -1: not there
+  float t[HMY_MAX_TOP];     // the teacher's log probability
+  float x[HMY_MAX_TOP];     // the student's logit
+  double q[HMY_MAX_TOP];    // the teacher's probability, before it is divided by q_norm
+  float gq[HMY_MAX_TOP];    // what the token's gradient is lowered by: grad_scale * scale * its q, all entries that name it together
+};
+// What the rest of the workgroup wants of it
+struct ListSum {
+  double q_sum, q_norm;   // sum of q_k, what they are divided by
+  double sum;             // sum over the tokens, each once, of exp(s (x - max))
+  float t_max;            // q = exp(t - t_max) / q_norm
+  float max;              // largest logit, -inf if there is none
+  int any;
+};
+
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// exp in 64 bits on few registers: x = n ln 2 + r with |r| <= ln 2 / 2, Taylor's series up to r^11 (the next term is 6e-15)
+__device__ __forceinline__ double exp64(double x) {
+  x = x < -2000. ? -2000. : x;
+  const double n = rint(x * 1.4426950408889634074), r = fma(n, -1.9082149292705877e-10, fma(n, -0.6931471803691238, x));
+  double p = 1. / 39916800.;
+  p = fma(p, r, 1. / 3628800.);
+  p = fma(p, r, 1. / 362880.);
+  p = fma(p, r, 1. / 40320.);
+  p = fma(p, r, 1. / 5040.);
+  p = fma(p, r, 1. / 720.);
+  p = fma(p, r, 1. / 120.);
+  p = fma(p, r, 1. / 24.);
+  p = fma(p, r, 1. / 6.);
+  p = fma(p, r, 0.5);
+  p = fma(p, r, 1.);
+  p = fma(p, r, 1.);
+  return ldexp(p, int(n));
+}
+__device__ __forceinline__ void lds_of_own_wave() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// by one wave: the list's entries and sums
+template <typename L>
+__device__ __forceinline__ void read_list(const L *x, const DistillArgs &a, int row, int lane, List &l, ListSum &z) {
+  float tm = -INFINITY, m = -INFINITY;
+#pragma unroll
+  for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
+    int id = -1;
+    float t = -INFINITY;
+    if (k < a.K) {
+      id = a.ids[int64_t(row) * a.K + k];
+      t = a.logp[int64_t(row) * a.K + k];
+      if (uint32_t(id) >= uint32_t(a.V) || t == -INFINITY) id = -1;
+    }
+    const float v = id >= 0 ? to_f32(x[id]) : -INFINITY;
+    l.id[k] = id;
+    l.t[k] = t;
+    l.x[k] = v;
+    if (id >= 0) tm = fmaxf(tm, t);
+    m = fmaxf(m, v);
+  }
+  m = wave_max(m);
+  tm = a.tail ? 0.f : wave_max(tm);
+  if (tm == -INFINITY) tm = 0.f;
+  lds_of_own_wave();
+  const double ref = m == -INFINITY ? 0. : double(m), s = a.scale, w = s * double(a.grad_scale);
+  double qs = 0., sum = 0.;
+  bool any = false, again = false;
+#pragma unroll 1
+  for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
+    const int id = l.id[k];
+    bool first = id >= 0;
+    for (int o = 0; o < a.K; o += 4) {   // entries from K on are -1
+      const int4 other = *reinterpret_cast<const int4 *>(l.id + o);
+      const bool same[4] = {other.x == id && o != k, other.y == id && o + 1 != k, other.z == id && o + 2 != k, other.w == id && o + 3 != k};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (id >= 0 && same[j]) {
+          again = true;
+          if (o + j < k) first = false;
+        }
+    }
+    double q = 0.;
+    if (id >= 0) {
+      q = exp64(double(l.t[k]) - double(tm));
+      if (first) sum += exp64((double(l.x[k]) - ref) * s);
+      any = true;
+    }
+    l.q[k] = q;
+    qs += q;
+  }
+  qs = wave_sum64(qs);
+  sum = wave_sum64(sum);
+  const double norm = a.tail ? 1. : qs, lower = w / norm;
+  lds_of_own_wave();
+#pragma unroll 1
+  for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
+    double q = l.q[k];
+    if (__any(again)) {   // one token more than once: all of its q
+      const int id = l.id[k];
+      q = 0.;
+      for (int o = 0; o < a.K; ++o)
+        if (l.id[o] == id) q += l.q[o];
+    }
+    l.gq[k] = float(lower * q);
+  }
+  if (lane == 0) {
+    z.q_sum = a.tail ? qs : qs / norm;
+    z.q_norm = norm;
+    z.sum = sum;
+    z.t_max = tm;
+    z.max = m;
+    z.any = 0;
+  }
+  if (__any(any) && lane == 0) z.any = 1;
+}
+
+// What a row's gradient is made of once its sums are known
+struct RowTerms {
+  float m;                // the row's maximum, 0 where nothing has any weight
+  float c_list, c_rest;   // what exp(s (x - m)) of a listed token and of any other is multiplied with
+};
+// rest, m_rest: the sum of exp(s (x - m_rest)) over the tokens that are not listed (over all without a tail) and its reference
+__device__ __forceinline__ RowTerms row_terms(float m_rest, float rest, const ListSum &z, const DistillArgs &a) {
+  const float m = a.tail ? fmaxf(m_rest, z.max) : m_rest;
+  const float S_rest = rest * rebase(m_rest, m, a.scale), S = S_rest + (a.tail ? float(z.sum) * rebase(z.max, m, a.scale) : 0.f);
+  const float q_rest = a.tail && !(S_rest == 0.f) ? float(fmax(1. - z.q_sum, 0.)) : 0.f;
+  const float w = a.scale * a.grad_scale, Q = float(z.q_sum) + q_rest;
+  RowTerms r;
+  r.m = m == -INFINITY ? 0.f : m;
+  const float inv = S == 0.f ? 0.f : 1.f / S;
+  r.c_list = w * (Q * inv);
+  r.c_rest = q_rest > 0.f ? w * (Q * inv - q_rest / S_rest) : r.c_list;
+  return r;
+}
+// by one wave, the result in all lanes
+__device__ __forceinline__ float row_loss(float m_rest, float rest, const List &l, const ListSum &z, const DistillArgs &a, int lane) {
+  if (!z.any) return 0.f;
+  const double s = a.scale, mr = m_rest == -INFINITY ? 0. : double(m_rest);
+  // relative to the others' maximum; a list far above it has its own sum scaled down instead
+  const double up = z.max == -INFINITY ? 0. : (double(z.max) - mr) * s, top = a.tail && up > 0. ? up : 0.;
+  const double S_rest = double(rest) * exp64(-top), S = S_rest + (a.tail && z.max != -INFINITY ? z.sum * exp64(up - top) : 0.);
+  if (S == 0.) return z.q_sum > 0. ? INFINITY : 0.f;   // the student gives nothing any weight
+  const double log_S = log(S) + top, log_n = double(z.t_max) + (a.tail ? 0. : log(z.q_norm));
+  double loss = 0.;
+#pragma unroll 1
+  for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
+    const double q = l.q[k];
+    if (!(q == 0.)) loss += q * ((double(l.t[k]) - log_n) - ((double(l.x[k]) - mr) * s - log_S));
+  }
+  loss = wave_sum64(loss) / z.q_norm;
+  if (a.tail && !(S_rest == 0.)) {
+    const double q_rest = fmax(1. - z.q_sum, 0.);
+    if (q_rest > 0.) loss += q_rest * (log(q_rest) - log(S_rest / S));
+  }
+  return float(loss);
+}
+
+// One workgroup per row.  The row stays in registers between its sums and its gradient, as exponentials in fp32, as loaded in
+// bf16; of a row beyond NT * NG groups of eight columns the last so many do, and those in front are read again.
+template <typename L, typename E, int NT, int NG, bool TAIL, int WPE>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void k_distill(const L *logits, E *dlogits, DistillArgs a) {
+  constexpr int kWaves = NT / kWave, kSegment = NT * NG, kWords = (NG + 3) / 4;
+  constexpr bool kHold = sizeof(L) == 4;
+  __shared__ uint32_t listed[TAIL ? NT * kWords : 1];   // a bit for each of a thread's columns
+  __shared__ uint32_t listed_behind;                    // and for the columns behind the whole groups
+  __shared__ float wave_m[kWaves], wave_s[kWaves];
+  __shared__ ListSum z;
+  __shared__ __attribute__((aligned(16))) List list;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const float c = a.scale * kLog2e;
+  // segments of the row's groups: a short one first, if any, then whole ones, the last of which stays
+  const int groups = a.V / 8, segments = max(1, (groups + kSegment - 1) / kSegment), lead = groups - (segments - 1) * kSegment;
+  const int behind = groups * 8 + tid;   // this thread's column behind the groups, if it is less than V
+  const int row = blockIdx.x;
+  const L *x = logits + int64_t(row) * a.ldl;
+  if (wave == 0) read_list(x, a, row, lane, list, z);
+  Eight<L> v[NG];
+  float xb = behind < a.V ? to_f32(x[behind]) : -INFINITY, m = -INFINITY, sum = 0.f;
+  for (int seg = 0; seg < segments; ++seg) {
+    const int g0 = seg == 0 ? 0 : lead + (seg - 1) * kSegment, g1 = lead + seg * kSegment;
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int g = g0 + i * NT + tid;
+      if (g < g1) load_whole(v[i], x + uint32_t(g) * 8);
+      else v[i].all_no_weight();
+    }
+    if constexpr (TAIL) {
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) listed[w * NT + tid] = 0;
+      if (tid == 0) listed_behind = 0;
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll 1
+        for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
+          const int id = list.id[k], g = id / 8;
+          if (id >= 0 && g >= g0 && g < g1) {
+            const int slot = ((g - g0) / NT) * 8 + id % 8;
+            atomicOr(&listed[(slot / 32) * NT + (g - g0) % NT], 1u << (slot % 32));
+          } else if (id >= groups * 8) {
+            atomicOr(&listed_behind, 1u << (id % 8));
+          }
+        }
+      }
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) {
+        const uint32_t bits = listed[w * NT + tid];
+        if (bits) {
+#pragma unroll
+          for (int i = 4 * w; i < 4 * w + 4 && i < NG; ++i)
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+              if (bits >> (8 * (i % 4) + k) & 1) v[i].set_no_weight(k);
+        }
+      }
+      if (tid < 8 && (listed_behind >> tid & 1)) xb = -INFINITY;
+    }
+    float sm = fmaxf(m, xb);
+#pragma unroll
+    for (int i = 0; i < NG; ++i)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sm = fmaxf(sm, v[i].at(k));
+    const float ref = sm == -INFINITY ? 0.f : sm;
+    sum *= fast_exp2((m - ref) * c);
+    m = sm;
+    if (seg == 0) sum += fast_exp2((xb - ref) * c);
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      v[i].forget_floats();
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float e = fast_exp2((v[i].at(k) - ref) * c);
+        sum += e;
+        if constexpr (kHold) v[i].w[k] = __float_as_uint(e);
+      }
+      v[i].forget_floats();
+    }
+  }
+  // the row's sum: of a wave, then of the workgroup, one barrier
+  const float wm = wave_max(m), ws = wave_sum(sum == 0.f ? 0.f : sum * rebase(m, wm, a.scale));
+  if (lane == 0) {
+    wave_m[wave] = wm;
+    wave_s[wave] = ws;
+  }
+  __syncthreads();
+  const float om = lane < kWaves ? wave_m[lane] : -INFINITY, m_rest = wave_max(om);
+  const float os = lane < kWaves ? wave_s[lane] : 0.f, rest = wave_sum(os == 0.f ? 0.f : os * rebase(om, m_rest, a.scale));
+  if (dlogits) {
+    E *d = dlogits + int64_t(row) * a.ldd;
+    const RowTerms r = row_terms(m_rest, rest, z, a);
+    const bool any = z.any;
+    const float mine = r.c_rest * rebase(m, r.m, a.scale);
+    auto grad = [&](float xj) { return any ? fast_exp2((xj - r.m) * c) * r.c_rest : 0.f; };
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      const int g = (segments == 1 ? 0 : lead + (segments - 2) * kSegment) + i * NT + tid;
+      if (g < groups) {
+        float o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = kHold ? (any ? v[i].at(k) * mine : 0.f) : grad(v[i].at(k));
+        store_whole(d + uint32_t(g) * 8, o);
+      }
+    }
+    if (behind < a.V) d[behind] = from_f32<E>(grad(xb));
+    for (int seg = segments - 2; seg >= 0; --seg) {
+      const int g0 = seg == 0 ? 0 : lead + (seg - 1) * kSegment, g1 = lead + seg * kSegment;
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const int g = g0 + i * NT + tid;
+        if (g < g1) load_whole(v[i], x + uint32_t(g) * 8);
+      }
+#pragma unroll
+      for (int i = 0; i < NG; ++i) {
+        const int g = g0 + i * NT + tid;
+        if (g < g1) {
+          float o[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) o[k] = grad(v[i].at(k));
+          store_whole(d + uint32_t(g) * 8, o);
+        }
+      }
+    }
+    zero_padding(d, a.V, a.pad, tid, NT);
+    __syncthreads();   // behind the stores of the columns around
+    if (wave == 0) {
+#pragma unroll 1
+      for (int k = lane; k < HMY_MAX_TOP; k += kWave)
+        if (list.id[k] >= 0) d[list.id[k]] = from_f32<E>(fmaf(rebase(list.x[k], r.m, a.scale), r.c_list, -list.gq[k]));
+    }
+  }
+  if (wave == 0) {
+    const float loss = row_loss(m_rest, rest, list, z, a, lane);
+    if (lane == 0) a.row_loss[row] = loss;
+  }
+}
+
+// loss[0] += scale * the sum of the rows' losses, in one order whatever the launch
+constexpr int kSumThreads = 256;
+__global__ __launch_bounds__(kSumThreads) void k_loss_sum(const float *row_loss, double *loss, int T, double scale) {
+  __shared__ double scratch[kSumThreads / kWave];
+  double v = 0.;
+  for (int i = threadIdx.x; i < T; i += kSumThreads) v += double(row_loss[i]);
+  v = wave_sum64(v);
+  if (threadIdx.x % kWave == 0) scratch[threadIdx.x / kWave] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kSumThreads / kWave; ++w) v += scratch[w];
+    loss[0] += v * scale;
+  }
+}
+
+template <typename L, typename E, int NT, int NG, int WPE>
+void launch_rows(const L *x, E *d, DistillArgs a, hipStream_t s) {
+  for (int rows = a.T; rows > 0; rows -= kMaxGrid) {   // a launch has a limited number of workgroups
+    const dim3 grid(rows < kMaxGrid ? rows : kMaxGrid);
+    if (a.tail) hipLaunchKernelGGL((k_distill<L, E, NT, NG, true, WPE>), grid, dim3(NT), 0, s, x, d, a);
+    else hipLaunchKernelGGL((k_distill<L, E, NT, NG, false, WPE>), grid, dim3(NT), 0, s, x, d, a);
+    x += int64_t(kMaxGrid) * a.ldl;
+    if (d) d += int64_t(kMaxGrid) * a.ldd;
+    a.ids += int64_t(kMaxGrid) * a.K;
+    a.logp += int64_t(kMaxGrid) * a.K;
+    a.row_loss += kMaxGrid;
+  }
+}
+
+}  // namespace
+
+int launch_distill(const hmy_distill_desc &g, stream_t st) {
+  int rc = check_rows("distill", g.logits_prec, g.logits, g.T, g.V, 0, g.ldl);
+  if (!rc && g.dlogits) rc = check_rows("distill", g.prec, g.dlogits, g.T, g.V, g.pad, g.ldd);
+  if (rc) return rc;
+  if (!positive(g.scale)) return fail(HMY_E_INVALID, "distill: the scale must be positive and finite");
+  if (!std::isfinite(g.grad_scale)) return fail(HMY_E_INVALID, "distill: the gradient's scale must be finite");
+  if (g.K < 1 || g.K > HMY_MAX_TOP) return fail(HMY_E_INVALID, "distill: K = %d is not in 1..%d", g.K, HMY_MAX_TOP);
+  if (g.tail != 0 && g.tail != 1) return fail(HMY_E_INVALID, "distill: tail is 0 or 1");
+  const void *words[] = {g.teacher_ids, g.teacher_logp, g.row_loss};
+  for (const void *p : words)
+    if (misaligned(p, 4)) return fail(HMY_E_INVALID, "distill: misaligned array");
+  if (misaligned(g.loss_acc, 8)) return fail(HMY_E_INVALID, "distill: misaligned loss_acc");
+  const int el = bytes_of(g.logits_prec), ee = bytes_of(g.prec);
+  if (g.dlogits && rows_clash(g.logits, int64_t(g.V) * el, g.ldl * el, g.dlogits, (int64_t(g.V) + g.pad) * ee, g.ldd * ee, g.T, g.logits_prec == g.prec))
+    return fail(HMY_E_INVALID, "distill: dlogits overlaps logits other than in place");
+  const DistillArgs a = {g.teacher_ids, g.teacher_logp, g.row_loss, g.T, g.V, g.K, g.pad, g.ldl, g.ldd, g.scale, g.grad_scale, g.tail == 1};
+  const hipStream_t s = (hipStream_t)st;
+  DISPATCH_ROWS(g.logits_prec, g.prec, {
+    const L *x = (const L *)g.logits;
+    E *d = (E *)g.dlogits;
+    if (g.V <= 2048) launch_rows<L, E, 256, 1, 4>(x, d, a, s);
+    else if (g.V <= 8192) launch_rows<L, E, 256, 4, 4>(x, d, a, s);
+    else if (g.V <= 32768) launch_rows<L, E, 1024, 4, 4>(x, d, a, s);
+    else if (sizeof(L) == 4) launch_rows<L, E, 1024, 7, 4>(x, d, a, s);
+    else if (g.V <= 65536) launch_rows<L, E, 1024, 8, 4>(x, d, a, s);
+    else launch_rows<L, E, 1024, sizeof(L) == 4 ? 7 : 16, 4>(x, d, a, s);
+  });
+  if (g.loss_acc)
+    hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(kSumThreads), 0, s, g.row_loss, g.loss_acc, g.T, double(g.grad_scale));
+  return check_launch("distill");
+}
+
+}  // namespace hmy

@@ -43,6 +43,14 @@ template <typename E> struct alignas(16) Eight {
     if constexpr (sizeof(E) == 4) w[k] = 0xff800000u;
     else w[k / 2] = k & 1 ? (w[k / 2] & 0xffffu) | 0xff800000u : (w[k / 2] & 0xffff0000u) | 0xff80u;
   }
+  // keeps the compiler from holding on to values that were taken apart before this point: a bf16 row fits the registers as loaded,
+  // but not as floats
+  __device__ __forceinline__ void forget_floats() {
+    if constexpr (sizeof(E) == 2) {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) asm volatile("" : "+v"(w[i]));
+    }
+  }
   __device__ __forceinline__ void all_no_weight() {
 #pragma unroll
     for (int i = 0; i < WORDS; ++i) w[i] = sizeof(E) == 4 ? 0xff800000u : 0xff80ff80u;
@@ -56,57 +64,32 @@ template <typename E> __device__ __forceinline__ void load_whole(Eight<E> &v, co
     v.w[i] = a.x; v.w[i + 1] = a.y; v.w[i + 2] = a.z; v.w[i + 3] = a.w;
   }
 }
-// columns col .. col+7 of a row of V; those at and beyond V are -inf
-template <typename E> __device__ __forceinline__ void load_columns(Eight<E> &v, const E *row, int col, int V) {
-  if (col + 8 <= V) {
-    load_whole(v, row + col);
-  } else {
-    v.all_no_weight();
+template <typename E> __device__ __forceinline__ void store_whole(E *p, const float (&g)[8]) {
+  typedef typename Unaligned<E>::type unaligned;
+  Eight<E> o;
+  if constexpr (sizeof(E) == 4) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (col + k < V) {
-        if constexpr (sizeof(E) == 4) {
-          v.w[k] = *reinterpret_cast<const uint32_t *>(row + col + k);
-        } else {
-          const uint32_t h = *reinterpret_cast<const uint16_t *>(row + col + k);
-          v.w[k / 2] = k & 1 ? (v.w[k / 2] & 0xffffu) | (h << 16) : (v.w[k / 2] & 0xffff0000u) | h;
-        }
-      }
+    for (int k = 0; k < 8; ++k) o.w[k] = __float_as_uint(g[k]);
+  } else {
+    typedef E pair __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int k = 0; k < 8; k += 2) {
+      pair t;
+      t.x = from_f32<E>(g[k]);
+      t.y = from_f32<E>(g[k + 1]);
+      o.w[k / 2] = __builtin_bit_cast(uint32_t, t);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < Eight<E>::WORDS; i += 4) {
+    u32x4 a;
+    a.x = o.w[i]; a.y = o.w[i + 1]; a.z = o.w[i + 2]; a.w = o.w[i + 3];
+    *reinterpret_cast<unaligned *>(reinterpret_cast<char *>(p) + 4 * i) = a;
   }
 }
-// columns col .. col+7, zeros from V on, nothing from `end` on
-template <typename E> __device__ __forceinline__ void store_columns(E *row, int col, int V, int end, const float (&g)[8]) {
-  if (col + 8 <= V) {
-    typedef typename Unaligned<E>::type unaligned;
-    Eight<E> o;
-    if constexpr (sizeof(E) == 4) {
-#pragma unroll
-      for (int k = 0; k < 8; ++k) o.w[k] = __float_as_uint(g[k]);
-    } else {
-      typedef E pair __attribute__((ext_vector_type(2)));
-#pragma unroll
-      for (int k = 0; k < 8; k += 2) {
-        pair t;
-        t.x = from_f32<E>(g[k]);
-        t.y = from_f32<E>(g[k + 1]);
-        o.w[k / 2] = __builtin_bit_cast(uint32_t, t);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < Eight<E>::WORDS; i += 4) {
-      u32x4 a;
-      a.x = o.w[i]; a.y = o.w[i + 1]; a.z = o.w[i + 2]; a.w = o.w[i + 3];
-      *reinterpret_cast<unaligned *>(reinterpret_cast<char *>(row + col) + 4 * i) = a;
-    }
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (col + k < end) row[col + k] = from_f32<E>(col + k < V ? g[k] : 0.f);
-  }
-}
-// the padding behind the last eight columns that hold some of the row
+// A row is its V / 8 whole groups of eight columns, and the V % 8 columns behind them, one thread's each.
 template <typename E> __device__ __forceinline__ void zero_padding(E *row, int V, int pad, int tid, int nt) {
-  for (int j = (V + 7) / 8 * 8 + tid; j < V + pad; j += nt) row[j] = from_f32<E>(0.f);
+  for (int j = V + tid; j < V + pad; j += nt) row[j] = from_f32<E>(0.f);
 }
 
 // ---- on the host ----

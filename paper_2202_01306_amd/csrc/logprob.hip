@@ -1,5 +1,5 @@
-// Operators on rows of logits x[T,V]: log probabilities of given tokens with entropy and the most likely tokens, their
-// gradient, and the divergence from a teacher's listed tokens with its gradient.
+// Operators on rows of logits x[T,V]: log probabilities of given tokens with entropy and the most likely tokens, and their
+// gradient.
 //
 // With the scale s, m = max x, u_j = s (x_j - m), S = sum exp u_j:  log p_j = u_j - log S,
 //   H = log S - (sum u_j exp u_j) / S.
@@ -35,19 +35,6 @@ __device__ __forceinline__ float block_max(float v, float *scratch) {
   for (int w = 1; w < NT / kWave; ++w) r = fmaxf(r, scratch[w]);
   return r;
 }
-template <int NT>
-__device__ __forceinline__ double block_sum(double v, double *scratch) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-  __syncthreads();
-  if (threadIdx.x % kWave == 0) scratch[threadIdx.x / kWave] = v;
-  __syncthreads();
-  double r = 0.;
-#pragma unroll
-  for (int w = 0; w < NT / kWave; ++w) r += scratch[w];
-  return r;
-}
-
 // A token's rank as one number: the larger logit first, of equal ones the lower column.  +0 and -0 are equal.  A key is never
 // 0, which stands for "none".
 __device__ __forceinline__ uint64_t rank_key(float x, int col) {
@@ -144,134 +131,47 @@ struct LogprobGradArgs {
 template <typename L, typename E, int NT, int U>
 __global__ __launch_bounds__(NT) void k_logprob_bwd(const L *logits, E *dlogits, LogprobGradArgs g, int tiles) {
   const int64_t n = int64_t(g.T) * tiles;
+  const uint32_t whole = uint32_t(g.V) & ~7u;
   for (int64_t wg = blockIdx.x; wg < n; wg += gridDim.x) {
-    const int row = int(wg / tiles), tile = int(wg % tiles), c0 = (tile * NT * U + int(threadIdx.x)) * 8;
+    const int row = int(wg / tiles), tile = int(wg % tiles);
+    const uint32_t c0 = (uint32_t(tile) * NT * U + threadIdx.x) * 8;
     const L *x = logits + int64_t(row) * g.ldl;
     E *d = dlogits + int64_t(row) * g.ldd;
     Eight<L> v[U];
 #pragma unroll
     for (int i = 0; i < U; ++i)
-      if (c0 + i * NT * 8 < g.V) load_columns(v[i], x, c0 + i * NT * 8, g.V);
+      if (c0 + i * NT * 8 < whole) load_whole(v[i], x + (c0 + i * NT * 8));
     const float m = g.row_max[row], z = g.log_sum[row];
     const int tgt = g.targets ? g.targets[row] : -1;
     const float a = g.d_logp && tgt >= 0 && tgt < g.V ? g.d_logp[row] : 0.f;
     const float h = g.d_entropy ? g.d_entropy[row] : 0.f, H = g.d_entropy ? g.entropy[row] : 0.f;
     const float na = -g.scale * fmaf(h, H, a), nh = -g.scale * h;
     const bool empty = z == -INFINITY;   // no token has any weight: p = 0 throughout
+    auto grad = [&](float xj) {
+      const float l = fmaf(xj - m, g.scale, -z);
+      return empty ? 0.f : fast_exp2(l * kLog2e) * fmaf(nh, fmaxf(l, kNoWeight), na);
+    };
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int col = c0 + i * NT * 8;
-      if (col < g.V) {
+      const uint32_t col = c0 + i * NT * 8;
+      if (col < whole) {
         float o[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float l = fmaf(v[i].at(k) - m, g.scale, -z);
-          o[k] = empty ? 0.f : fast_exp2(l * kLog2e) * fmaf(nh, fmaxf(l, kNoWeight), na);
-        }
-        if (uint32_t(tgt - col) < 8u) {
+        for (int k = 0; k < 8; ++k) o[k] = grad(v[i].at(k));
+        if (uint32_t(tgt) - col < 8u) {
 #pragma unroll
           for (int k = 0; k < 8; ++k)
-            if (col + k == tgt) o[k] = fmaf(g.scale, a, o[k]);
+            if (int(col) + k == tgt) o[k] = fmaf(g.scale, a, o[k]);
         }
-        store_columns(d, col, g.V, g.V + g.pad, o);
+        store_whole(d + col, o);
       }
     }
-    if (tile == tiles - 1) zero_padding(d, g.V, g.pad, threadIdx.x, NT);
+    if (tile == tiles - 1) {
+      const int col = int(whole) + int(threadIdx.x);
+      if (col < g.V) d[col] = from_f32<E>(fmaf(g.scale, col == tgt ? a : 0.f, grad(to_f32(x[col]))));
+      zero_padding(d, g.V, g.pad, threadIdx.x, NT);
+    }
   }
-}
-
-struct DistillArgs {
-  const int32_t *ids;
-  const float *logp;
-  float *row_loss;
-  int T, V, K, tail, pad;
-  int64_t ldl, ldd;
-  float scale, grad_scale;
-};
-
-// Loss and gradient of one row; the list's terms in 64 bits (a divergence is small beside the logarithms that it is the
-// difference of), the row's exponentials in 32.  With a tail the row's sum is that of the listed tokens and that of the others.
-template <typename L, typename E>
-__global__ __launch_bounds__(kRowThreads) void k_distill(const L *logits, E *dlogits, DistillArgs a) {
-  __shared__ float scratch[kRowThreads / kWave];
-  __shared__ double dscratch[kRowThreads / kWave];
-  __shared__ int ids[HMY_MAX_TOP];
-  __shared__ double q_of[HMY_MAX_TOP];
-  const int tid = threadIdx.x;
-  const float c = a.scale * kLog2e;
-  for (int row = blockIdx.x; row < a.T; row += gridDim.x) {
-    const L *x = logits + int64_t(row) * a.ldl;
-    E *d = dlogits ? dlogits + int64_t(row) * a.ldd : nullptr;
-    // the list: thread k has entry k; an entry that names no token or has no weight is not there
-    int id = -1;
-    double t = -INFINITY;
-    float xk = 0.f;
-    if (tid < a.K) {
-      id = a.ids[int64_t(row) * a.K + tid];
-      t = a.logp[int64_t(row) * a.K + tid];
-      if (id < 0 || id >= a.V || t == -INFINITY) id = -1;
-      if (id >= 0) xk = to_f32(x[id]);
-    }
-    __syncthreads();
-    if (tid < HMY_MAX_TOP) ids[tid] = id;
-    const bool there = id >= 0, any = block_sum<kRowThreads>(there ? 1.f : 0.f, scratch) > 0.f;
-    double q;
-    if (a.tail) {
-      q = there ? exp(t) : 0.;
-    } else {
-      const float tm = block_max<kRowThreads>(there ? float(t) : -INFINITY, scratch);
-      const double e = there ? exp(t - double(tm)) : 0.;
-      const double n = block_sum<kRowThreads>(e, dscratch);
-      q = e / n;
-      t = t - double(tm) - log(n);
-    }
-    const double q_sum = block_sum<kRowThreads>(there ? q : 0., dscratch);
-    float m = -INFINITY;
-    for (int j = tid; j < a.V; j += kRowThreads) m = fmaxf(m, to_f32(x[j]));
-    m = block_max<kRowThreads>(m, scratch);
-    const float ref = m == -INFINITY ? 0.f : m;
-    float rest = 0.f, listed = 0.f;
-    for (int j = tid; j < a.V; j += kRowThreads) {
-      const float e = fast_exp2((to_f32(x[j]) - ref) * c);
-      bool in = false;
-      for (int k = 0; k < a.K; ++k) in |= ids[k] == j;
-      if (in) listed += e;
-      else rest += e;
-    }
-    const double S_rest = block_sum<kRowThreads>(rest, scratch), S = S_rest + block_sum<kRowThreads>(listed, scratch);
-    const double u = (double(xk) - double(ref)) * a.scale;
-    double loss = there && q > 0. ? q * (t - (u - log(S))) : (there ? q * 0. : 0.);
-    loss = block_sum<kRowThreads>(loss, dscratch);
-    double q_rest = a.tail && any && !(S_rest == 0.) ? fmax(1. - q_sum, 0.) : 0.;
-    if (q_rest > 0.) loss += q_rest * (log(q_rest) - log(S_rest / S));
-    if (tid == 0) a.row_loss[row] = any ? float(loss) : 0.f;
-    if (!d) continue;
-    const double w = double(a.scale) * double(a.grad_scale), inv = S == 0. || !any ? 0. : 1. / S;
-    const float c_list = float(w * (q_sum + q_rest) * inv);
-    const float c_rest = q_rest > 0. ? float(w * (q_sum + q_rest - q_rest * S / S_rest) * inv) : c_list;
-    if (tid < HMY_MAX_TOP) q_of[tid] = q;
-    __syncthreads();
-    double same = 0.;
-    if (there)
-      for (int k = 0; k < a.K; ++k)
-        if (ids[k] == id) same += q_of[k];
-    for (int j = tid; j < a.V + a.pad; j += kRowThreads) {
-      bool in = false;
-      for (int k = 0; k < a.K; ++k) in |= ids[k] == j;
-      if (!in) d[j] = from_f32<E>(j < a.V && any ? fast_exp2((to_f32(x[j]) - ref) * c) * c_rest : 0.f);
-    }
-    if (there) d[id] = from_f32<E>(float(double(fast_exp2((xk - ref) * c)) * double(c_list) - w * same));
-    __syncthreads();
-  }
-}
-
-// loss[0] += scale * the sum of the rows' losses, in one order whatever the launch
-__global__ __launch_bounds__(kRowThreads) void k_loss_sum(const float *row_loss, double *loss, int T, double scale) {
-  __shared__ double scratch[kRowThreads / kWave];
-  double v = 0.;
-  for (int i = threadIdx.x; i < T; i += kRowThreads) v += double(row_loss[i]);
-  v = block_sum<kRowThreads>(v, scratch);
-  if (threadIdx.x == 0) loss[0] += v * scale;
 }
 
 }  // namespace
@@ -325,31 +225,6 @@ int launch_logprob_bwd(const hmy_logprob_grad_desc &g, stream_t st) {
     else hipLaunchKernelGGL((k_logprob_bwd<L, E, 256, 2>), grid, dim3(256), 0, s, x, d, a, tiles);
   });
   return check_launch("logprob_bwd");
-}
-
-int launch_distill(const hmy_distill_desc &g, stream_t st) {
-  int rc = check_rows("distill", g.logits_prec, g.logits, g.T, g.V, 0, g.ldl);
-  if (!rc && g.dlogits) rc = check_rows("distill", g.prec, g.dlogits, g.T, g.V, g.pad, g.ldd);
-  if (rc) return rc;
-  if (!positive(g.scale)) return fail(HMY_E_INVALID, "distill: the scale must be positive and finite");
-  if (!std::isfinite(g.grad_scale)) return fail(HMY_E_INVALID, "distill: the gradient's scale must be finite");
-  if (g.K < 1 || g.K > HMY_MAX_TOP) return fail(HMY_E_INVALID, "distill: K = %d is not in 1..%d", g.K, HMY_MAX_TOP);
-  if (g.tail != 0 && g.tail != 1) return fail(HMY_E_INVALID, "distill: tail is 0 or 1");
-  const void *words[] = {g.teacher_ids, g.teacher_logp, g.row_loss};
-  for (const void *p : words)
-    if (misaligned(p, 4)) return fail(HMY_E_INVALID, "distill: misaligned array");
-  if (misaligned(g.loss_acc, 8)) return fail(HMY_E_INVALID, "distill: misaligned loss_acc");
-  const int el = bytes_of(g.logits_prec), ee = bytes_of(g.prec);
-  if (g.dlogits && rows_clash(g.logits, int64_t(g.V) * el, g.ldl * el, g.dlogits, (int64_t(g.V) + g.pad) * ee, g.ldd * ee, g.T, g.logits_prec == g.prec))
-    return fail(HMY_E_INVALID, "distill: dlogits overlaps logits other than in place");
-  const DistillArgs a = {g.teacher_ids, g.teacher_logp, g.row_loss, g.T, g.V, g.K, g.tail, g.pad, g.ldl, g.ldd, g.scale, g.grad_scale};
-  const dim3 grid(g.T < kMaxGrid ? g.T : kMaxGrid);
-  DISPATCH_ROWS(g.logits_prec, g.prec, {
-    hipLaunchKernelGGL((k_distill<L, E>), grid, dim3(kRowThreads), 0, (hipStream_t)st, (const L *)g.logits, (E *)g.dlogits, a);
-  });
-  if (g.loss_acc)
-    hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(kRowThreads), 0, (hipStream_t)st, g.row_loss, g.loss_acc, g.T, double(g.grad_scale));
-  return check_launch("distill");
 }
 
 }  // namespace hmy
