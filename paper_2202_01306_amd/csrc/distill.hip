@@ -70,24 +70,32 @@ __device__ __forceinline__ void lds_of_own_wave() {
   __builtin_amdgcn_wave_barrier();
 }
 
-// by one wave: the list's entries and sums
+// this lane's two entries: the tokens, -1 where there is none, and the teacher's log probabilities
+__device__ __forceinline__ void list_entries(const DistillArgs &a, int row, int lane, int (&id)[2], float (&tl)[2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int k = lane + i * kWave;
+    id[i] = -1;
+    tl[i] = -INFINITY;
+    if (k < a.K) {
+      id[i] = a.ids[int64_t(row) * a.K + k];
+      tl[i] = a.logp[int64_t(row) * a.K + k];
+    }
+    if (uint32_t(id[i]) >= uint32_t(a.V) || tl[i] == -INFINITY) id[i] = -1;
+  }
+}
+// by one wave: the list and its sums
 template <typename L>
-__device__ __forceinline__ void read_list(const L *x, const DistillArgs &a, int row, int lane, List &l, ListSum &z) {
+__device__ __forceinline__ void read_list(const L *x, const DistillArgs &a, int lane, const int (&id)[2], const float (&tl)[2], List &l, ListSum &z) {
   float tm = -INFINITY, m = -INFINITY;
 #pragma unroll
-  for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
-    int id = -1;
-    float t = -INFINITY;
-    if (k < a.K) {
-      id = a.ids[int64_t(row) * a.K + k];
-      t = a.logp[int64_t(row) * a.K + k];
-      if (uint32_t(id) >= uint32_t(a.V) || t == -INFINITY) id = -1;
-    }
-    const float v = id >= 0 ? to_f32(x[id]) : -INFINITY;
-    l.id[k] = id;
-    l.t[k] = t;
+  for (int i = 0; i < 2; ++i) {
+    const int k = lane + i * kWave;
+    const float v = id[i] >= 0 ? to_f32(x[id[i]]) : -INFINITY;
+    l.id[k] = id[i];
+    l.t[k] = tl[i];
     l.x[k] = v;
-    if (id >= 0) tm = fmaxf(tm, t);
+    if (id[i] >= 0) tm = fmaxf(tm, tl[i]);
     m = fmaxf(m, v);
   }
   m = wave_max(m);
@@ -100,16 +108,16 @@ __device__ __forceinline__ void read_list(const L *x, const DistillArgs &a, int 
 #pragma unroll 1
   for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
     const int id = l.id[k];
-    bool first = id >= 0;
+    int same = 0;
+#pragma unroll 2
     for (int o = 0; o < a.K; o += 4) {   // entries from K on are -1
       const int4 other = *reinterpret_cast<const int4 *>(l.id + o);
-      const bool same[4] = {other.x == id && o != k, other.y == id && o + 1 != k, other.z == id && o + 2 != k, other.w == id && o + 3 != k};
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (id >= 0 && same[j]) {
-          again = true;
-          if (o + j < k) first = false;
-        }
+      same += (other.x == id) + (other.y == id) + (other.z == id) + (other.w == id);
+    }
+    bool first = id >= 0;
+    if (first && same > 1) {
+      again = true;
+      for (int o = 0; o < k; ++o) first &= l.id[o] != id;
     }
     double q = 0.;
     if (id >= 0) {
@@ -194,7 +202,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
   constexpr int kWaves = NT / kWave, kSegment = NT * NG, kWords = (NG + 3) / 4;
   constexpr bool kHold = sizeof(L) == 4;
   __shared__ uint32_t listed[TAIL ? NT * kWords : 1];   // a bit for each of a thread's columns
-  __shared__ uint32_t listed_behind;                    // and for the columns behind the whole groups
+  __shared__ uint32_t listed_behind[kWaves];            // and for the columns behind the whole groups
   __shared__ float wave_m[kWaves], wave_s[kWaves];
   __shared__ ListSum z;
   __shared__ __attribute__((aligned(16))) List list;
@@ -205,7 +213,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
   const int behind = groups * 8 + tid;   // this thread's column behind the groups, if it is less than V
   const int row = blockIdx.x;
   const L *x = logits + int64_t(row) * a.ldl;
-  if (wave == 0) read_list(x, a, row, lane, list, z);
+  int id[2];
+  float tl[2];
+  if (TAIL || wave == 0) list_entries(a, row, lane, id, tl);
+  if (wave == 0) read_list(x, a, lane, id, tl, list, z);
   Eight<L> v[NG];
   float xb = behind < a.V ? to_f32(x[behind]) : -INFINITY, m = -INFINITY, sum = 0.f;
   for (int seg = 0; seg < segments; ++seg) {
@@ -216,36 +227,29 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
       if (g < g1) load_whole(v[i], x + uint32_t(g) * 8);
       else v[i].all_no_weight();
     }
-    if constexpr (TAIL) {
+    if constexpr (TAIL) {   // a wave finds the listed tokens among its own columns: no barrier
 #pragma unroll
       for (int w = 0; w < kWords; ++w) listed[w * NT + tid] = 0;
-      if (tid == 0) listed_behind = 0;
-      __syncthreads();
-      if (wave == 0) {
-#pragma unroll 1
-        for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
-          const int id = list.id[k], g = id / 8;
-          if (id >= 0 && g >= g0 && g < g1) {
-            const int slot = ((g - g0) / NT) * 8 + id % 8;
-            atomicOr(&listed[(slot / 32) * NT + (g - g0) % NT], 1u << (slot % 32));
-          } else if (id >= groups * 8) {
-            atomicOr(&listed_behind, 1u << (id % 8));
-          }
+      if (seg == 0 && lane == 0) listed_behind[wave] = 0;
+      lds_of_own_wave();
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int off = id[i] / 8 - g0, owner = off % NT;
+        if (id[i] >= 0 && off >= 0 && off < g1 - g0 && owner / kWave == wave) {
+          const int slot = (off / NT) * 8 + id[i] % 8;
+          atomicOr(&listed[(slot / 32) * NT + owner], 1u << (slot % 32));
         }
+        if (seg == 0 && id[i] >= groups * 8) atomicOr(&listed_behind[wave], 1u << (id[i] % 8));
       }
-      __syncthreads();
+      lds_of_own_wave();
 #pragma unroll
       for (int w = 0; w < kWords; ++w) {
         const uint32_t bits = listed[w * NT + tid];
-        if (bits) {
 #pragma unroll
-          for (int i = 4 * w; i < 4 * w + 4 && i < NG; ++i)
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              if (bits >> (8 * (i % 4) + k) & 1) v[i].set_no_weight(k);
-        }
+        for (int i = 4 * w; i < 4 * w + 4 && i < NG; ++i)
+          if (bits >> (8 * (i % 4)) & 0xff) v[i].set_no_weight(bits >> (8 * (i % 4)));
       }
-      if (tid < 8 && (listed_behind >> tid & 1)) xb = -INFINITY;
+      if (seg == 0 && tid < 8 && (listed_behind[wave] >> tid & 1)) xb = -INFINITY;
     }
     float sm = fmaxf(m, xb);
 #pragma unroll
@@ -280,16 +284,23 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
   if (dlogits) {
     E *d = dlogits + int64_t(row) * a.ldd;
     const RowTerms r = row_terms(m_rest, rest, z, a);
-    const bool any = z.any;
+    if (!z.any) {   // a row of padding: zeros whatever its logits are
+      const float none[8] = {};
+      for (int g = tid; g < groups; g += NT) store_whole(d + uint32_t(g) * 8, none);
+      if (behind < a.V) d[behind] = from_f32<E>(0.f);
+      zero_padding(d, a.V, a.pad, tid, NT);
+      if (tid == 0) a.row_loss[row] = 0.f;
+      return;
+    }
     const float mine = r.c_rest * rebase(m, r.m, a.scale);
-    auto grad = [&](float xj) { return any ? fast_exp2((xj - r.m) * c) * r.c_rest : 0.f; };
+    auto grad = [&](float xj) { return fast_exp2((xj - r.m) * c) * r.c_rest; };
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
       const int g = (segments == 1 ? 0 : lead + (segments - 2) * kSegment) + i * NT + tid;
       if (g < groups) {
         float o[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = kHold ? (any ? v[i].at(k) * mine : 0.f) : grad(v[i].at(k));
+        for (int k = 0; k < 8; ++k) o[k] = kHold ? v[i].at(k) * mine : grad(v[i].at(k));
         store_whole(d + uint32_t(g) * 8, o);
       }
     }

@@ -39,9 +39,18 @@ template <typename E> struct alignas(16) Eight {
     if constexpr (sizeof(E) == 4) return __uint_as_float(w[k]);
     else return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
   }
-  __device__ __forceinline__ void set_no_weight(int k) {   // -inf
-    if constexpr (sizeof(E) == 4) w[k] = 0xff800000u;
-    else w[k / 2] = k & 1 ? (w[k / 2] & 0xffffu) | 0xff800000u : (w[k / 2] & 0xffff0000u) | 0xff80u;
+  // -inf in the columns whose bits are set
+  __device__ __forceinline__ void set_no_weight(uint32_t bits) {
+    auto all = [&](int k) { return uint32_t(int32_t(bits << (31 - k)) >> 31); };
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if constexpr (sizeof(E) == 4) {
+        w[k] = (w[k] & ~all(k)) | (all(k) & 0xff800000u);
+      } else if (k % 2 == 0) {
+        const uint32_t m = (all(k) & 0xffffu) | (all(k + 1) & 0xffff0000u);
+        w[k / 2] = (w[k / 2] & ~m) | (m & 0xff80ff80u);
+      }
+    }
   }
   // keeps the compiler from holding on to values that were taken apart before this point: a bf16 row fits the registers as loaded,
   // but not as floats
@@ -72,12 +81,13 @@ template <typename E> __device__ __forceinline__ void store_whole(E *p, const fl
     for (int k = 0; k < 8; ++k) o.w[k] = __float_as_uint(g[k]);
   } else {
     typedef E pair __attribute__((ext_vector_type(2)));
+    typedef float floats __attribute__((ext_vector_type(2)));
 #pragma unroll
-    for (int k = 0; k < 8; k += 2) {
-      pair t;
-      t.x = from_f32<E>(g[k]);
-      t.y = from_f32<E>(g[k + 1]);
-      o.w[k / 2] = __builtin_bit_cast(uint32_t, t);
+    for (int k = 0; k < 8; k += 2) {   // both halves of a word by one instruction
+      floats f;
+      f.x = g[k];
+      f.y = g[k + 1];
+      o.w[k / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, pair));
     }
   }
 #pragma unroll
