@@ -35,17 +35,11 @@ struct List {
 // What the rest of the workgroup wants of it
 struct ListSum {
   double q_sum, q_norm;   // sum of q_k, what they are divided by
-  double sum;             // sum over the tokens, each once, of exp(s (x - max))
+  double sum;             // with a tail: sum over the tokens, each once, of exp(s (x - max))
   float t_max;            // q = exp(t - t_max) / q_norm
   float max;              // largest logit, -inf if there is none
   int any;
 };
-
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
-}
 
 // exp in 64 bits on few registers: x = n ln 2 + r with |r| <= ln 2 / 2, Taylor's series up to r^11 (the next term is 6e-15)
 __device__ __forceinline__ double exp64(double x) {
@@ -64,6 +58,13 @@ __device__ __forceinline__ double exp64(double x) {
   p = fma(p, r, 1.);
   p = fma(p, r, 1.);
   return ldexp(p, int(n));
+}
+// log of a positive number in 64 bits: y from the 32-bit logarithm, off by d < 1e-6, then d from x exp(-y) = exp d
+__device__ __forceinline__ double log64(double x) {
+  int e;
+  const double f = frexp(x, &e), y = (double(__builtin_amdgcn_logf(float(f))) + double(e)) * 0.69314718055994530942;
+  const double d = fma(x, exp64(-y), -1.);
+  return y + fma(-0.5 * d, d, d);
 }
 __device__ __forceinline__ void lds_of_own_wave() {
   __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -98,15 +99,15 @@ __device__ __forceinline__ void read_list(const L *x, const DistillArgs &a, int 
     if (id[i] >= 0) tm = fmaxf(tm, tl[i]);
     m = fmaxf(m, v);
   }
-  m = wave_max(m);
-  tm = a.tail ? 0.f : wave_max(tm);
+  m = wave_top(m);
+  tm = a.tail ? 0.f : wave_top(tm);
   if (tm == -INFINITY) tm = 0.f;
   lds_of_own_wave();
   const double ref = m == -INFINITY ? 0. : double(m), s = a.scale, w = s * double(a.grad_scale);
   double qs = 0., sum = 0.;
   bool any = false, again = false;
 #pragma unroll 1
-  for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
+  for (int k = lane; k < a.K; k += kWave) {
     const int id = l.id[k];
     int same = 0;
 #pragma unroll 2
@@ -122,18 +123,18 @@ __device__ __forceinline__ void read_list(const L *x, const DistillArgs &a, int 
     double q = 0.;
     if (id >= 0) {
       q = exp64(double(l.t[k]) - double(tm));
-      if (first) sum += exp64((double(l.x[k]) - ref) * s);
+      if (first && a.tail) sum += exp64((double(l.x[k]) - ref) * s);
       any = true;
     }
     l.q[k] = q;
     qs += q;
   }
-  qs = wave_sum64(qs);
-  sum = wave_sum64(sum);
-  const double norm = a.tail ? 1. : qs, lower = w / norm;
+  qs = wave_total(qs);
+  sum = wave_total(sum);
+  const double inv = a.tail ? 1. : 1. / qs, lower = w * inv;
   lds_of_own_wave();
 #pragma unroll 1
-  for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
+  for (int k = lane; k < a.K; k += kWave) {
     double q = l.q[k];
     if (__any(again)) {   // one token more than once: all of its q
       const int id = l.id[k];
@@ -143,15 +144,15 @@ __device__ __forceinline__ void read_list(const L *x, const DistillArgs &a, int 
     }
     l.gq[k] = float(lower * q);
   }
+  const bool any_there = __any(any);
   if (lane == 0) {
-    z.q_sum = a.tail ? qs : qs / norm;
-    z.q_norm = norm;
+    z.q_sum = a.tail || qs != qs || !any_there ? qs : 1.;
+    z.q_norm = a.tail ? 1. : qs;
     z.sum = sum;
     z.t_max = tm;
     z.max = m;
-    z.any = 0;
+    z.any = any_there;
   }
-  if (__any(any) && lane == 0) z.any = 1;
 }
 
 // What a row's gradient is made of once its sums are known
@@ -180,17 +181,18 @@ __device__ __forceinline__ float row_loss(float m_rest, float rest, const List &
   const double up = z.max == -INFINITY ? 0. : (double(z.max) - mr) * s, top = a.tail && up > 0. ? up : 0.;
   const double S_rest = double(rest) * exp64(-top), S = S_rest + (a.tail && z.max != -INFINITY ? z.sum * exp64(up - top) : 0.);
   if (S == 0.) return z.q_sum > 0. ? INFINITY : 0.f;   // the student gives nothing any weight
-  const double log_S = log(S) + top, log_n = double(z.t_max) + (a.tail ? 0. : log(z.q_norm));
   double loss = 0.;
 #pragma unroll 1
-  for (int k = lane; k < HMY_MAX_TOP; k += kWave) {
+  for (int k = lane; k < a.K; k += kWave) {
     const double q = l.q[k];
-    if (!(q == 0.)) loss += q * ((double(l.t[k]) - log_n) - ((double(l.x[k]) - mr) * s - log_S));
+    if (!(q == 0.)) loss += q * ((double(l.t[k]) - double(z.t_max)) - (double(l.x[k]) - mr) * s);
   }
-  loss = wave_sum64(loss) / z.q_norm;
-  if (a.tail && !(S_rest == 0.)) {
+  loss = wave_total(loss);
+  if (!a.tail) return float(loss / z.q_norm + (log64(S / z.q_norm) + top));
+  loss += z.q_sum * (log64(S) + top);
+  if (!(S_rest == 0.)) {
     const double q_rest = fmax(1. - z.q_sum, 0.);
-    if (q_rest > 0.) loss += q_rest * (log(q_rest) - log(S_rest / S));
+    if (q_rest > 0.) loss += q_rest * log64(q_rest * (S / S_rest));
   }
   return float(loss);
 }
@@ -273,14 +275,14 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
     }
   }
   // the row's sum: of a wave, then of the workgroup, one barrier
-  const float wm = wave_max(m), ws = wave_sum(sum == 0.f ? 0.f : sum * rebase(m, wm, a.scale));
+  const float wm = wave_top(m), ws = wave_total(sum == 0.f ? 0.f : sum * rebase(m, wm, a.scale));
   if (lane == 0) {
     wave_m[wave] = wm;
     wave_s[wave] = ws;
   }
   __syncthreads();
-  const float om = lane < kWaves ? wave_m[lane] : -INFINITY, m_rest = wave_max(om);
-  const float os = lane < kWaves ? wave_s[lane] : 0.f, rest = wave_sum(os == 0.f ? 0.f : os * rebase(om, m_rest, a.scale));
+  const float om = lane < kWaves ? wave_m[lane] : -INFINITY, m_rest = wave_top(om);
+  const float os = lane < kWaves ? wave_s[lane] : 0.f, rest = wave_total(os == 0.f ? 0.f : os * rebase(om, m_rest, a.scale));
   if (dlogits) {
     E *d = dlogits + int64_t(row) * a.ldd;
     const RowTerms r = row_terms(m_rest, rest, z, a);
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
     __syncthreads();   // behind the stores of the columns around
     if (wave == 0) {
 #pragma unroll 1
-      for (int k = lane; k < HMY_MAX_TOP; k += kWave)
+      for (int k = lane; k < a.K; k += kWave)
         if (list.id[k] >= 0) d[list.id[k]] = from_f32<E>(fmaf(rebase(list.x[k], r.m, a.scale), r.c_list, -list.gq[k]));
     }
   }
@@ -343,7 +345,7 @@ __global__ __launch_bounds__(kSumThreads) void k_loss_sum(const float *row_loss,
   __shared__ double scratch[kSumThreads / kWave];
   double v = 0.;
   for (int i = threadIdx.x; i < T; i += kSumThreads) v += double(row_loss[i]);
-  v = wave_sum64(v);
+  v = wave_total(v);
   if (threadIdx.x % kWave == 0) scratch[threadIdx.x / kWave] = v;
   __syncthreads();
   if (threadIdx.x == 0) {
@@ -388,12 +390,20 @@ int launch_distill(const hmy_distill_desc &g, stream_t st) {
   DISPATCH_ROWS(g.logits_prec, g.prec, {
     const L *x = (const L *)g.logits;
     E *d = (E *)g.dlogits;
-    if (g.V <= 2048) launch_rows<L, E, 256, 1, 4>(x, d, a, s);
+    // As few waves as hold the row in up to four groups of eight columns a thread, while a workgroup has at most 256 threads: the
+    // first wave's work on the list, which the others wait for, is then a smaller part.  Beyond, what a compute unit's registers
+    // hold of rows, two or more at a time as far as they fit.
+    constexpr bool wide = sizeof(L) == 4;
+    if (g.V <= 512) launch_rows<L, E, 64, 1, 4>(x, d, a, s);
+    else if (g.V <= 2048) launch_rows<L, E, 64, 4, 4>(x, d, a, s);
+    else if (g.V <= 4096) launch_rows<L, E, 128, 4, 4>(x, d, a, s);
     else if (g.V <= 8192) launch_rows<L, E, 256, 4, 4>(x, d, a, s);
-    else if (g.V <= 32768) launch_rows<L, E, 1024, 4, 4>(x, d, a, s);
-    else if (sizeof(L) == 4) launch_rows<L, E, 1024, 7, 4>(x, d, a, s);
-    else if (g.V <= 65536) launch_rows<L, E, 1024, 8, 4>(x, d, a, s);
-    else launch_rows<L, E, 1024, sizeof(L) == 4 ? 7 : 16, 4>(x, d, a, s);
+    else if (g.V <= 14336) launch_rows<L, E, 256, 7, 4>(x, d, a, s);
+    else if (g.V <= 28672) launch_rows<L, E, 512, 7, 4>(x, d, a, s);
+    else if (wide) launch_rows<L, E, 1024, 7, 4>(x, d, a, s);
+    else if (g.V <= 32768) launch_rows<L, E, 512, wide ? 7 : 8, 4>(x, d, a, s);
+    else if (g.V <= 110000) launch_rows<L, E, 1024, 7, wide ? 4 : 8>(x, d, a, s);
+    else launch_rows<L, E, 1024, wide ? 7 : 16, 4>(x, d, a, s);
   });
   if (g.loss_acc)
     hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(kSumThreads), 0, s, g.row_loss, g.loss_acc, g.T, double(g.grad_scale));

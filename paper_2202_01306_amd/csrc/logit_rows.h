@@ -25,6 +25,48 @@ __device__ __forceinline__ float rebase(float a, float m, float scale) {
   return fast_exp2(hi) * fmaf(lo, kLn2, 1.f);
 }
 
+// Reductions over a wave by moves between neighbouring lanes, without LDS; the result is the same scalar for all lanes.  Lanes
+// that a move gives nothing take the operation's neutral element.
+template <int CTRL, int ROWS> __device__ __forceinline__ float lane_move(float x, float neutral) {
+  return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(neutral), __float_as_uint(x), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float x) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), 63)); }
+__device__ __forceinline__ float wave_total(float x) {
+  x += lane_move<0x111, 0xf>(x, 0.f);   // within rows of sixteen lanes: from 1, 2, 4 and 8 lanes before
+  x += lane_move<0x112, 0xf>(x, 0.f);
+  x += lane_move<0x114, 0xf>(x, 0.f);
+  x += lane_move<0x118, 0xf>(x, 0.f);
+  x += lane_move<0x142, 0xa>(x, 0.f);   // a row's last lane to the next row
+  x += lane_move<0x143, 0xc>(x, 0.f);   // lane 31 to the upper half
+  return last_lane(x);
+}
+__device__ __forceinline__ float wave_top(float x) {
+  x = fmaxf(x, lane_move<0x111, 0xf>(x, -INFINITY));
+  x = fmaxf(x, lane_move<0x112, 0xf>(x, -INFINITY));
+  x = fmaxf(x, lane_move<0x114, 0xf>(x, -INFINITY));
+  x = fmaxf(x, lane_move<0x118, 0xf>(x, -INFINITY));
+  x = fmaxf(x, lane_move<0x142, 0xa>(x, -INFINITY));
+  x = fmaxf(x, lane_move<0x143, 0xc>(x, -INFINITY));
+  return last_lane(x);
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ double lane_move(double x) {
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, uint32_t(b), CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, uint32_t(b >> 32), CTRL, ROWS, 0xf, false);
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+__device__ __forceinline__ double wave_total(double x) {
+  x += lane_move<0x111, 0xf>(x);
+  x += lane_move<0x112, 0xf>(x);
+  x += lane_move<0x114, 0xf>(x);
+  x += lane_move<0x118, 0xf>(x);
+  x += lane_move<0x142, 0xa>(x);
+  x += lane_move<0x143, 0xc>(x);
+  const uint64_t b = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_readlane(uint32_t(b), 63), hi = __builtin_amdgcn_readlane(uint32_t(b >> 32), 63);
+  return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+
 // Eight columns as they are stored.  The accesses are 16 bytes wide and aligned to the element only: rows of any stride take
 // the same path (the device splits what crosses a cache line).
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
