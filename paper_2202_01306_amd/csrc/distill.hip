@@ -176,10 +176,10 @@ __device__ __forceinline__ RowTerms row_terms(float m_rest, float rest, const Li
 // by one wave, the result in all lanes
 __device__ __forceinline__ float row_loss(float m_rest, float rest, const List &l, const ListSum &z, const DistillArgs &a, int lane) {
   if (!z.any) return 0.f;
-  const double s = a.scale, mr = m_rest == -INFINITY ? 0. : double(m_rest);
-  // relative to the others' maximum; a list far above it has its own sum scaled down instead
-  const double up = z.max == -INFINITY ? 0. : (double(z.max) - mr) * s, top = a.tail && up > 0. ? up : 0.;
-  const double S_rest = double(rest) * exp64(-top), S = S_rest + (a.tail && z.max != -INFINITY ? z.sum * exp64(up - top) : 0.);
+  const float m = a.tail ? fmaxf(m_rest, z.max) : m_rest;
+  const double s = a.scale, mr = m == -INFINITY ? 0. : double(m);
+  const double S_rest = m_rest == -INFINITY ? double(rest) : double(rest) * exp64((double(m_rest) - mr) * s);
+  const double S = S_rest + (a.tail && z.max != -INFINITY ? z.sum * exp64((double(z.max) - mr) * s) : 0.);
   if (S == 0.) return z.q_sum > 0. ? INFINITY : 0.f;   // the student gives nothing any weight
   double loss = 0.;
 #pragma unroll 1
@@ -188,8 +188,8 @@ __device__ __forceinline__ float row_loss(float m_rest, float rest, const List &
     if (!(q == 0.)) loss += q * ((double(l.t[k]) - double(z.t_max)) - (double(l.x[k]) - mr) * s);
   }
   loss = wave_total(loss);
-  if (!a.tail) return float(loss / z.q_norm + (log64(S / z.q_norm) + top));
-  loss += z.q_sum * (log64(S) + top);
+  if (!a.tail) return float(loss / z.q_norm + log64(S / z.q_norm));
+  loss += z.q_sum * log64(S);
   if (!(S_rest == 0.)) {
     const double q_rest = fmax(1. - z.q_sum, 0.);
     if (q_rest > 0.) loss += q_rest * log64(q_rest * (S / S_rest));

@@ -17,10 +17,11 @@ constexpr float kNoWeight = -1e4f;
 __device__ __forceinline__ float fast_exp2(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // exp(s (a - m)) to the last bits, for what whole partial sums are multiplied with: the product with s log2(e) rounds, which
-// costs |s (a - m)| 2^-24 relative; here the rounded part is carried along.  a <= m; a = -inf gives 0.
+// costs |s (a - m)| 2^-24 relative; here the rounded part is carried along.  a <= m; a = -inf gives 0, and so does the type's
+// lowest value beside an ordinary one, whose products here are no longer finite.
 __device__ __forceinline__ float rebase(float a, float m, float scale) {
-  if (a == -INFINITY) return 0.f;
   const float d = (a - m) * scale, hi = d * kLog2e;
+  if (a == -INFINITY || d < -200.f) return 0.f;
   const float lo = fmaf(d, kLog2e, -hi) + d * kLog2eLow;
   return fast_exp2(hi) * fmaf(lo, kLn2, 1.f);
 }

@@ -344,7 +344,7 @@ def test_distill_of_lists_and_rows_where_it_can_go_wrong(prec, tail, V):
     say(f"distill special {prec} V={V} tail={tail}")
     rng = np.random.default_rng(V)
     K = 6
-    x = rows(rng, 12, V, prec, masked=0.0)
+    x = rows(rng, 16, V, prec, masked=0.0)
     ids, t = teacher_lists(rng, x, K)
     ids[0, 3] = ids[0, 0]                          # one token twice
     ids[1] = 5                                     # and six times
@@ -360,15 +360,25 @@ def test_distill_of_lists_and_rows_where_it_can_go_wrong(prec, tail, V):
     t[9] = np.log(0.3)                             # adds up to more than 1
     x[10, 3] = np.nan
     t[11, 1] = np.nan
+    # masks of the type's lowest value: on most of a row; on all that is not listed; on all but one token, not a listed one
+    lowest = float(torch.finfo(torch.bfloat16).min)
+    x[12, V // 20:] = lowest
+    x[13] = lowest
+    x[13, ids[13]] = 1.0
+    x[14] = lowest
+    x[14, V - 1] = -2.0
+    ids[14], t[14] = np.arange(K), np.log(1e-3)
+    x[15] = -INF                                   # nothing left
     logits = on_device(x, V, prec)
     for ws in (None, workspace()):
-        loss, d = f32(12), torch.full((12, V), 7.0, device="cuda", dtype=DT[prec])
-        B.hmy_k_distill(PC[prec], PC[prec], logits, i32(ids), torch.from_numpy(t).cuda(), loss, d, 12, V, K, V, V, tail=tail, workspace=ws)
+        loss, d = f32(16), torch.full((16, V), 7.0, device="cuda", dtype=DT[prec])
+        B.hmy_k_distill(PC[prec], PC[prec], logits, i32(ids), torch.from_numpy(t).cuda(), loss, d, 16, V, K, V, V, tail=tail, workspace=ws)
         ls, got = host(loss), host(d)
         assert np.isnan(ls[10]) and np.isnan(ls[11]) and np.isnan(got[10]).any() and np.isnan(got[11]).any()
         assert ls[4] == 0 and ls[5] == 0 and np.all(got[4:6] == 0)
         assert ls[6] == INF
-        check_distill(ls[:10], got[:10], x[:10], ids[:10], t[:10], 1.0, 1.0, tail, prec == "bf16", V)
+        rows_ = [r for r in range(16) if r not in (10, 11)]
+        check_distill(ls[rows_], got[rows_], x[rows_], ids[rows_], t[rows_], 1.0, 1.0, tail, prec == "bf16", V)
 
 
 @pytest.mark.gpu
