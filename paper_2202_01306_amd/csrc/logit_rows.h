@@ -50,6 +50,18 @@ __device__ __forceinline__ float wave_top(float x) {
   x = fmaxf(x, lane_move<0x143, 0xc>(x, -INFINITY));
   return last_lane(x);
 }
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t lane_move(uint32_t x, uint32_t neutral) {
+  return __builtin_amdgcn_update_dpp(neutral, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ uint32_t wave_top(uint32_t x) {
+  x = max(x, lane_move<0x111, 0xf>(x, 0u));
+  x = max(x, lane_move<0x112, 0xf>(x, 0u));
+  x = max(x, lane_move<0x114, 0xf>(x, 0u));
+  x = max(x, lane_move<0x118, 0xf>(x, 0u));
+  x = max(x, lane_move<0x142, 0xa>(x, 0u));
+  x = max(x, lane_move<0x143, 0xc>(x, 0u));
+  return __builtin_amdgcn_readlane(x, 63);
+}
 template <int CTRL, int ROWS> __device__ __forceinline__ double lane_move(double x) {
   const uint64_t b = __builtin_bit_cast(uint64_t, x);
   const uint32_t lo = __builtin_amdgcn_update_dpp(0, uint32_t(b), CTRL, ROWS, 0xf, false);

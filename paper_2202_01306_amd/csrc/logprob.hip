@@ -23,39 +23,28 @@ __device__ __forceinline__ uint64_t rank_key(float x, int col) { return (uint64_
 __device__ __forceinline__ int key_column(uint64_t key) { return int(~uint32_t(key)); }
 constexpr uint32_t kLowestOrdered = 0x00800000u;   // of the lowest finite value: -inf and "none" are below
 
-// Candidates for a row's list, in LDS.  What is not among them is outranked by at least k that are.
+// What a workgroup finds a row's list with, in LDS.
 constexpr int kCandidates = 2048;
-constexpr int kRanked = 512;       // as many are ranked by comparing all with all
+constexpr int kRanked = 512;       // as many candidates are ranked by comparing all with all
+constexpr int kSlots = 8;          // the row's segments fall into so many slots, of which each thread knows its largest logit
+constexpr int kHits = 1024;
 template <int NT> struct Candidates {
   uint64_t key[kCandidates];
-  uint32_t group[NT];              // maxima of the threads' columns
-  uint32_t n, floor, count[2];     // floor: `ordered` of the least logit that can still be among the k
+  uint32_t rank[kRanked + kWave];
+  float top[kSlots * NT];          // a thread's largest logit in a slot
+  uint32_t hit[kHits];             // slot * NT + thread of those that reach the floor
+  uint32_t n, n_hits, floor, count[2];
 };
 
-// by one wave: some t with at least k of the values at or above it, and not many more if it can be had: the bisection ends at
-// k + k / 8 + 2.  kLowestOrdered if fewer than k are at or above that.
-template <int P>
-__device__ __forceinline__ uint32_t threshold(const uint32_t (&v)[P], int k) {
-  auto count = [&](uint32_t t) {
-    int c = 0;
-#pragma unroll
-    for (int i = 0; i < P; ++i) c += __popcll(__ballot(v[i] >= t));
-    return c;
-  };
+// by one wave: some t with at least k of its values at or above it, and not many more if it can be had: the bisection ends at
+// k + k / 8 + 2.  kLowestOrdered if fewer than k are at or above that.  count(t): how many are; each lane's smallest (of those
+// from kLowestOrdered on) and largest in lo and hi.
+template <typename F>
+__device__ __forceinline__ uint32_t threshold(uint32_t lo, uint32_t hi, int k, F count) {
   if (count(kLowestOrdered) < k) return kLowestOrdered;
-  uint32_t lo = ~0u, hi = 0;
-#pragma unroll
-  for (int i = 0; i < P; ++i) {
-    hi = max(hi, v[i]);
-    if (v[i] >= kLowestOrdered) lo = min(lo, v[i]);
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    hi = max(hi, uint32_t(__shfl_xor(int(hi), o, kWave)));
-    lo = min(lo, uint32_t(__shfl_xor(int(lo), o, kWave)));
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);   // at or above lo: at least k; above hi: none
+  hi = wave_top(hi);   // at or above lo: at least k; above hi: none
+  lo = ~wave_top(~lo);
+#pragma unroll 1
   while (lo < hi) {
     const uint32_t mid = lo + (hi - lo + 1) / 2;
     const int c = count(mid);
@@ -83,60 +72,118 @@ __device__ __forceinline__ int hits(Candidates<NT> &c, int mine, int &turn) {
   return r;
 }
 
-// by the workgroup: leaves only candidates that the k largest can be among, at most `most` of them.  Barriers on both sides.
+// by the workgroup: leaves only those of n > k candidates that the k largest can be among, at most `most` of them, and says how
+// many.  Wants a barrier in front.  The first wave does it: there is little to do, and the others keep their registers.
 template <int NT>
-__device__ __forceinline__ void thin_out(Candidates<NT> &c, int k, int most, int &turn) {
-  constexpr int P = kCandidates / 2 / kWave, PT = (kCandidates + NT - 1) / NT;
-  const int tid = threadIdx.x, n = min(int(c.n), kCandidates);
-  if (n <= k) return;
-  uint64_t mine[PT], least = 0;
-#pragma unroll
-  for (int i = 0; i < PT; ++i) mine[i] = tid + i * NT < n ? c.key[tid + i * NT] : 0;
-  if (n <= P * kWave) {
-    if (tid < kWave) {
-      uint32_t v[P];
-#pragma unroll
-      for (int i = 0; i < P; ++i) v[i] = tid + i * kWave < n ? uint32_t(c.key[tid + i * kWave] >> 32) : 0;
-      const uint32_t t = threshold(v, k);
-      if (tid == 0) c.floor = t;
+__device__ __forceinline__ int thin_out(Candidates<NT> &c, int n, int k, int most) {
+  const int lane = threadIdx.x;
+  if (lane < kWave) {
+    uint32_t lo = ~0u, hi = 0;
+#pragma unroll 1
+    for (int i = lane; i < n; i += kWave) {
+      const uint32_t v = uint32_t(c.key[i] >> 32);   // at or above kLowestOrdered: -inf is no candidate
+      lo = min(lo, v);
+      hi = max(hi, v);
     }
-    __syncthreads();
-    least = uint64_t(c.floor) << 32;
+    auto count = [&](uint64_t t) {
+      int r = 0;
+#pragma unroll 4
+      for (int i = 0; i < n; i += kWave) r += __popcll(__ballot(i + lane < n && c.key[i + lane] >= t));
+      return r;
+    };
+    uint64_t least = uint64_t(threshold(lo, hi, k, [&](uint32_t t) { return count(uint64_t(t) << 32); })) << 32;
+    if (count(least) > most) {   // many equal logits: the k-th largest key itself, bit by bit
+      least = 0;
+#pragma unroll 1
+      for (int bit = 63; bit >= 0; --bit)
+        if (count(least | uint64_t(1) << bit) >= k) least |= uint64_t(1) << bit;
+    }
     int kept = 0;
-#pragma unroll
-    for (int i = 0; i < PT; ++i) kept += mine[i] >= least && mine[i];
-    if (hits<NT>(c, kept, turn) > most) least = 0;   // many equal logits
-  }
-  if (least == 0) {   // the k-th largest key itself, bit by bit
-    for (int bit = 63; bit >= 0; --bit) {
-      const uint64_t t = least | uint64_t(1) << bit;
-      int above = 0;
-#pragma unroll
-      for (int i = 0; i < PT; ++i) above += mine[i] >= t;
-      if (hits<NT>(c, above, turn) >= k) least = t;
+#pragma unroll 1
+    for (int i = 0; i < n; i += kWave) {   // to places that have been read already
+      const uint64_t key = i + lane < n ? c.key[i + lane] : 0;
+      const uint64_t keep = __ballot(key >= least && key != 0);
+      if (key >= least && key != 0) c.key[kept + __popcll(keep & ((uint64_t(1) << lane) - 1))] = key;
+      kept += __popcll(keep);
     }
-    if (tid == 0) c.floor = max(uint32_t(least >> 32), kLowestOrdered);
+    if (lane == 0) c.n = kept;
   }
   __syncthreads();
-  if (tid == 0) c.n = 0;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < PT; ++i)
-    if (mine[i] && mine[i] >= least) c.key[atomicAdd(&c.n, 1u)] = mine[i];
-  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(c.n);
 }
 
-// by the workgroup: the k first of the candidates, `put(rank, key)` for each; barriers in front
-template <int NT, typename F>
-__device__ __forceinline__ void rank_candidates(Candidates<NT> &c, int k, int &turn, F put) {
-  if (int(c.n) > 2 * k + 64) thin_out<NT>(c, k, kRanked, turn);
-  const int n = int(c.n), tid = threadIdx.x;
-  for (int i = tid; i < n; i += NT) {
-    const uint64_t mine = c.key[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += c.key[j] > mine;
-    if (rank < k) put(rank, mine);
+// by the workgroup, where there are more candidates than there is room for (the largest logits are those of few threads, or very
+// many are equal): the k first of the `cols` >= k columns from x[first] on, which are read again for every bit.  The k-th largest
+// logit bit by bit, then of those that equal it the lowest columns.
+template <int NT, typename L>
+__device__ __forceinline__ int keep_first(Candidates<NT> &c, const L *x, int first, int cols, int k) {
+  const int tid = threadIdx.x;
+  int turn = 0;
+  uint32_t t = 0;
+  if (tid == 0) c.n = c.count[0] = c.count[1] = 0;
+  __syncthreads();
+#pragma unroll 1
+  for (int bit = 31; bit >= 0; --bit) {
+    const uint32_t to = t | 1u << bit;
+    int above = 0;
+#pragma unroll 1
+    for (int j = tid; j < cols; j += NT) {
+      const float v = to_f32(x[first + j]);
+      above += v == v && ordered(v) >= to;
+    }
+    if (hits<NT>(c, above, turn) >= k) t = to;
   }
+  int above = 0;
+#pragma unroll 1
+  for (int j = tid; j < cols; j += NT) {
+    const float v = to_f32(x[first + j]);
+    above += v == v && ordered(v) > t;
+  }
+  const int want = k - hits<NT>(c, above, turn);   // of those that equal it
+  int last = 0;
+#pragma unroll 1
+  for (int bit = 24; bit >= 0; --bit) {
+    const int to = last | 1 << bit;
+    int equal = 0;
+#pragma unroll 1
+    for (int j = tid; j < cols && j < to; j += NT) {
+      const float v = to_f32(x[first + j]);
+      equal += v == v && ordered(v) == t;
+    }
+    if (hits<NT>(c, equal, turn) <= want) last = to;
+  }
+#pragma unroll 1
+  for (int j = tid; j < cols; j += NT) {
+    const float v = to_f32(x[first + j]);
+    if (v == v && (ordered(v) > t || (ordered(v) == t && j < last))) c.key[atomicAdd(&c.n, 1u)] = rank_key(v, first + j);
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(c.n);
+}
+
+// by the workgroup: the k first of n candidates, `put(rank, key)` for each.  Wants a barrier in front.
+template <int NT, typename F>
+__device__ __forceinline__ void rank_candidates(Candidates<NT> &c, int n, int k, F put) {
+  const int tid = threadIdx.x;
+  if (n > 2 * k + 64) n = thin_out<NT>(c, n, k, kRanked);
+  // n is at most kRanked now.  All compared with all: `parts` threads share the comparisons of one candidate.
+  const int wide = (n + kWave - 1) / kWave * kWave, parts = max(1, NT / max(wide, 1)), share = ((n + parts - 1) / parts + 7) / 8 * 8;
+  for (int i = tid; i < wide; i += NT) c.rank[i] = 0;
+  if (tid < 8) c.key[n + tid] = 0;
+  __syncthreads();
+  for (int i = tid; i < wide * parts; i += NT) {
+    const int own = i % wide, first = i / wide * share;
+    const uint64_t mine = own < n ? c.key[own] : ~uint64_t(0);
+    int above = 0;
+    for (int j = first; j < min(first + share, n); j += 8) {
+#pragma unroll
+      for (int o = 0; o < 8; ++o) above += c.key[j + o] > mine;
+    }
+    if (above) atomicAdd(&c.rank[own], uint32_t(above));
+  }
+  __syncthreads();
+  for (int i = tid; i < n; i += NT)
+    if (int(c.rank[i]) < k) put(int(c.rank[i]), c.key[i]);
   for (int i = n + tid; i < k; i += NT) put(i, uint64_t(0));
 }
 
@@ -177,31 +224,97 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int row, const Sum
   if (a.entropy) a.entropy[row] = z.S == 0.f ? 0.f : log_sum - z.A * kLn2 / z.S;
 }
 
+// by the workgroup: the k first of a row's tokens, `put(rank, key)` for each.  `mine`: this thread's largest logit, c.top its
+// largest per slot of `per_slot` segments; xb: the logit of column `behind`, -inf where the thread has none.
+// A floor that at least k logits reach: the k-th largest, or a little less, of the maxima of 256 groups of threads.  What reaches
+// it is in the slots of few threads (k of 256 groups at least; as many as the row's largest logits fall into), and those columns
+// are read again: a second reading of a small part of the row, where looking for candidates in the first one costs every segment a
+// comparison and a barrier (2048 x 131072 bf16, k = 128: 192 us; 512 x 50257 fp32, k = 64: 39 us).
+template <typename L, int NT, int NG, typename F>
+__device__ __forceinline__ void list_row(Candidates<NT> &c, const L *x, int first, int groups, int cols, int per_slot, int k, float mine, float xb, int behind, F put) {
+  constexpr int kSegment = NT * NG;
+  const int tid = threadIdx.x, lane = tid % kWave;
+  const int slots = ((groups + kSegment - 1) / kSegment + per_slot - 1) / per_slot;
+  uint32_t *group = reinterpret_cast<uint32_t *>(c.key);   // free until there are candidates
+  group[tid] = ordered(fmaxf(mine, xb));
+  if (tid == 0) c.n = c.n_hits = 0;
+  __syncthreads();
+  if (tid < kWave) {
+    uint32_t g[4] = {0, 0, 0, 0}, lo = ~0u, hi = 0;
+#pragma unroll
+    for (int i = 0; i < NT / kWave; ++i) g[i % 4] = max(g[i % 4], group[lane + i * kWave]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      hi = max(hi, g[i]);
+      if (g[i] >= kLowestOrdered) lo = min(lo, g[i]);
+    }
+    const uint32_t t = threshold(lo, hi, k, [&](uint32_t to) {
+      int r = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r += __popcll(__ballot(g[i] >= to));
+      return r;
+    });
+    if (lane == 0) c.floor = t;
+  }
+  __syncthreads();
+  const float floor = unordered(__builtin_amdgcn_readfirstlane(c.floor));
+  if (mine >= floor) {
+    for (int s = 0; s < slots; ++s)
+      if (c.top[s * NT + tid] >= floor) {
+        const uint32_t at = atomicAdd(&c.n_hits, 1u);
+        if (at < kHits) c.hit[at] = s * NT + tid;
+      }
+  }
+  __syncthreads();
+  if (xb >= floor) c.key[atomicAdd(&c.n, 1u)] = rank_key(xb, behind);   // at most seven
+  const int n_hits = int(c.n_hits);
+  if (n_hits <= kHits) {
+    for (int s = 0; s < per_slot; ++s)
+      for (int i = tid; i < n_hits * NG; i += NT) {
+        const uint32_t h = c.hit[i / NG];
+        const int g = ((h / NT) * per_slot + s) * kSegment + (i % NG) * NT + h % NT;
+        if (g < groups) {
+          Eight<L> v;
+          load_whole(v, x + first + uint32_t(g) * 8);
+          int above = 0;
+#pragma unroll
+          for (int o = 0; o < 8; ++o) above += v.at(o) >= floor;
+          if (above) {
+            uint32_t at = atomicAdd(&c.n, uint32_t(above));
+#pragma unroll
+            for (int o = 0; o < 8; ++o)
+              if (v.at(o) >= floor) {
+                if (at < kCandidates) c.key[at] = rank_key(v.at(o), first + g * 8 + o);
+                ++at;
+              }
+          }
+        }
+      }
+  }
+  __syncthreads();
+  int n = __builtin_amdgcn_readfirstlane(c.n);
+  __syncthreads();   // all have read c.n, which is written again
+  if (n > kCandidates - 8 || n_hits > kHits) n = keep_first<NT>(c, x, first, cols, k);   // (eight keys more are written behind n)
+  rank_candidates<NT>(c, n, k, put);
+}
+
 // One workgroup per row, NT * NG groups of eight columns at a time, the next ones' loads on their way meanwhile.  One reading
-// of the row: each thread keeps a running maximum and sums relative to it.  The list: the first columns give a floor that at
-// least k of them reach (a bisection over the maxima of 256 groups of threads), from then on only what reaches the floor is
-// looked at; the candidates are thinned out, and the floor raised, when there are many.
-template <typename L, int NT, int NG, bool TOP>
-__global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a) {
+// of the row: each thread keeps a running maximum and sums relative to it, and its largest logit per slot for the list.
+template <typename L, int NT, int NG, bool TOP, int WPE>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void k_logprob(const L *logits, LogprobArgs a) {
   constexpr int kWaves = NT / kWave, kSegment = NT * NG;
   __shared__ Sums part[kWaves];
-  __shared__ Candidates<TOP ? NT : 1> cand_;
+  __shared__ Candidates<TOP ? NT : 1> cand;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), row = blockIdx.x;
   const float c = a.scale * kLog2e;
   const L *x = logits + int64_t(row) * a.ldl;
-  const int groups = a.V / 8, segments = (groups + kSegment - 1) / kSegment;
+  const int groups = a.V / 8, segments = (groups + kSegment - 1) / kSegment, per_slot = (segments + kSlots - 1) / kSlots;
   const int tgt = a.targets ? a.targets[row] : -1;
   const bool has_target = tgt >= 0 && tgt < a.V;
   const float target_logit = has_target ? to_f32(x[tgt]) : 0.f;
-  Sums z = no_sums();
-  int turn = 0;
-  if constexpr (TOP) {
-    if (tid == 0) {
-      cand_.n = cand_.count[0] = cand_.count[1] = 0;
-      cand_.floor = 0;
-    }
-    __syncthreads();
-  }
+  // the column behind the groups, if there is one for this thread
+  const int behind = groups * 8 + tid;
+  const float xb = behind < a.V ? to_f32(x[behind]) : -INFINITY;
   auto load = [&](Eight<L> (&v)[NG], int seg) {
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
@@ -210,23 +323,35 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a) 
       else v[i].all_no_weight();
     }
   };
-  auto take = [&](Eight<L> (&v)[NG], int seg) {
-    float top[NG], sm = z.m;
+  Eight<L> v[NG], next[NG];
+  if (segments > 0) load(v, 0);
+  Sums z = {fmaxf(xb, -INFINITY), 0.f, 0.f};
+  if (behind < a.V) z.S = fast_exp2((xb - (xb == -INFINITY ? 0.f : xb)) * c);   // 1, 0 for -inf, NaN
+  float in_slot = -INFINITY;
+  for (int seg = 0, of_slot = 0; seg < segments; ++seg) {
+    if (seg + 1 < segments) load(next, seg + 1);
+    float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
-      top[i] = v[i].at(0);
 #pragma unroll
-      for (int k = 1; k < 8; ++k) top[i] = fmaxf(top[i], v[i].at(k));
-      sm = fmaxf(sm, top[i]);
+      for (int k = 0; k < 8; ++k) top = fmaxf(top, v[i].at(k));
       v[i].forget_floats();
     }
-    if (sm > z.m) {
-      const float d = fmaxf((z.m - sm) * c, kNoWeight), f = fast_exp2(d);
+    if constexpr (TOP) {
+      in_slot = fmaxf(in_slot, top);
+      if (++of_slot == per_slot || seg + 1 == segments) {
+        cand.top[(seg / per_slot) * NT + tid] = in_slot;
+        in_slot = -INFINITY;
+        of_slot = 0;
+      }
+    }
+    if (top > z.m) {
+      const float d = fmaxf((z.m - top) * c, kNoWeight), f = fast_exp2(d);
       z.A = f * fmaf(d, z.S, z.A);
       z.S *= f;
-      z.m = sm;
+      z.m = top;
     }
-    const float ref = sm == -INFINITY ? 0.f : sm;
+    const float ref = z.m == -INFINITY ? 0.f : z.m;
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
 #pragma unroll
@@ -235,114 +360,9 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a) 
         z.S += e;
         z.A = fmaf(e, fmaxf(u, kNoWeight), z.A);
       }
-      v[i].forget_floats();
     }
-    if constexpr (TOP) {
-      auto &cand = cand_;
-      if (seg == 0) {
-        float mine = top[0];
 #pragma unroll
-        for (int i = 1; i < NG; ++i) mine = fmaxf(mine, top[i]);
-        cand.group[tid] = ordered(mine);
-        __syncthreads();
-        if (wave == 0) {
-          uint32_t g[4] = {0, 0, 0, 0};
-#pragma unroll
-          for (int i = 0; i < NT / kWave; ++i) g[i % 4] = max(g[i % 4], cand.group[lane + i * kWave]);
-          const uint32_t t = threshold(g, a.k);
-          if (lane == 0) cand.floor = t;
-        }
-        __syncthreads();
-      }
-      const int before = int(cand.n);
-      const float floor = unordered(__builtin_amdgcn_readfirstlane(cand.floor));
-      __syncthreads();
-#pragma unroll
-      for (int i = 0; i < NG; ++i)
-        if (top[i] >= floor) {
-          const int col = (seg * kSegment + i * NT + tid) * 8;
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (v[i].at(k) >= floor) {
-              const uint32_t at = atomicAdd(&cand.n, 1u);
-              if (at < kCandidates) cand.key[at] = rank_key(v[i].at(k), col + k);
-            }
-        }
-      __syncthreads();
-      const int n = int(cand.n);
-      if (n > kCandidates) {
-        // too many to keep (the largest logits are those of few threads, or very many are equal): the k-th largest of these
-        // columns, bit by bit, and of those that equal it the lowest columns
-        uint32_t t = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-          const float f = unordered(t | 1u << bit);
-          const bool can = (t | 1u << bit) >= kLowestOrdered;
-          int above = 0;
-#pragma unroll
-          for (int i = 0; i < NG; ++i)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) above += can ? v[i].at(k) >= f : v[i].at(k) > -INFINITY;
-          if (hits<TOP ? NT : 1>(cand, above, turn) >= a.k) t |= 1u << bit;
-        }
-        t = max(t, kLowestOrdered);
-        const float f = unordered(t);
-        int above = 0;
-#pragma unroll
-        for (int i = 0; i < NG; ++i)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) above += v[i].at(k) > f;
-        const int want = a.k - hits<TOP ? NT : 1>(cand, above, turn);   // of those that equal f
-        int last = 0;                                        // how many columns from this segment's first on
-        for (int bit = 31 - __builtin_clz(kSegment * 8); bit >= 0; --bit) {
-          const int to = last | 1 << bit;
-          int equal = 0;
-#pragma unroll
-          for (int i = 0; i < NG; ++i)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) equal += v[i].at(k) == f && (i * NT + tid) * 8 + k < to;
-          if (hits<TOP ? NT : 1>(cand, equal, turn) <= want) last = to;
-        }
-        if (tid == 0) cand.n = before;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < NG; ++i)
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            const int off = (i * NT + tid) * 8 + k;
-            if (v[i].at(k) > f || (v[i].at(k) == f && off < last))
-              cand.key[atomicAdd(&cand.n, 1u)] = rank_key(v[i].at(k), seg * kSegment * 8 + off);
-          }
-        __syncthreads();
-      }
-      if (int(cand.n) > kCandidates / 4) thin_out<TOP ? NT : 1>(cand, a.k, kRanked, turn);
-    }
-  };
-  Eight<L> v[NG], w[NG];
-  if (segments > 0) load(v, 0);
-  for (int seg = 0; seg < segments; seg += 2) {
-    if (seg + 1 < segments) load(w, seg + 1);
-    take(v, seg);
-    if (seg + 1 < segments) {
-      if (seg + 2 < segments) load(v, seg + 2);
-      take(w, seg + 1);
-    }
-  }
-  // the columns behind the groups
-  const int behind = groups * 8 + tid;
-  if (behind < a.V) {
-    const float xb = to_f32(x[behind]);
-    if (xb > z.m) {
-      const float d = fmaxf((z.m - xb) * c, kNoWeight), f = fast_exp2(d);
-      z.A = f * fmaf(d, z.S, z.A);
-      z.S *= f;
-      z.m = xb;
-    }
-    const float u = (xb - (z.m == -INFINITY ? 0.f : z.m)) * c, e = fast_exp2(u);
-    z.S += e;
-    z.A = fmaf(e, fmaxf(u, kNoWeight), z.A);
-    if constexpr (TOP) {
-      if (xb > -INFINITY) cand_.key[atomicAdd(&cand_.n, 1u)] = rank_key(xb, behind);   // at most seven more
-    }
+    for (int i = 0; i < NG; ++i) v[i] = next[i];
   }
   const Sums ws = wave_sums(z, a.scale);
   if (lane == 0) part[wave] = ws;
@@ -352,7 +372,7 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a) 
   if (tid == 0) put_row(a, row, all, target_logit, has_target);
   if constexpr (TOP) {
     const float log_sum = logf(all.S);
-    rank_candidates<TOP ? NT : 1>(cand_, a.k, turn, [&](int rank, uint64_t key) {
+    list_row<L, NT, NG>(cand, x, 0, groups, a.V, per_slot, a.k, z.m, xb, behind, [&](int rank, uint64_t key) {
       a.top_ids[int64_t(row) * a.k + rank] = key ? key_column(key) : -1;
       a.top_logp[int64_t(row) * a.k + rank] = key ? (unordered(uint32_t(key >> 32)) - all.m) * a.scale - log_sum : -INFINITY;
     });
@@ -419,12 +439,12 @@ __global__ __launch_bounds__(NT) void k_logprob_bwd(const L *logits, E *dlogits,
   }
 }
 
-template <typename L, int NT, int NG>
+template <typename L, int NT, int NG, int WPE>
 void launch_rows(const L *x, LogprobArgs a, int rows, hipStream_t s) {
   for (; rows > 0; rows -= kMaxGrid) {   // a launch has a limited number of workgroups
     const dim3 grid(rows < kMaxGrid ? rows : kMaxGrid);
-    if (a.k) hipLaunchKernelGGL((k_logprob<L, NT, NG, true>), grid, dim3(NT), 0, s, x, a);
-    else hipLaunchKernelGGL((k_logprob<L, NT, NG, false>), grid, dim3(NT), 0, s, x, a);
+    if (a.k) hipLaunchKernelGGL((k_logprob<L, NT, NG, true, WPE>), grid, dim3(NT), 0, s, x, a);
+    else hipLaunchKernelGGL((k_logprob<L, NT, NG, false, WPE>), grid, dim3(NT), 0, s, x, a);
     x += int64_t(kMaxGrid) * a.ldl;
     for (float **p : {&a.logp, &a.row_max, &a.log_sum, &a.entropy})
       if (*p) *p += kMaxGrid;
@@ -437,8 +457,8 @@ void launch_rows(const L *x, LogprobArgs a, int rows, hipStream_t s) {
 }
 template <typename L>
 void launch_rows(const L *x, const LogprobArgs &a, int rows, hipStream_t s) {
-  if (a.V <= 16384) launch_rows<L, 256, 2>(x, a, rows, s);
-  else launch_rows<L, 1024, 2>(x, a, rows, s);
+  if (a.V <= 16384) launch_rows<L, 256, 2, 4>(x, a, rows, s);
+  else launch_rows<L, 1024, 2, 8>(x, a, rows, s);
 }
 
 }  // namespace
