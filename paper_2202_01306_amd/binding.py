@@ -482,31 +482,34 @@ def hmy_k_xent(prec, logits, targets, loss_acc, dlogits, T, V, ldl, inv_ntgt, st
                           C.c_float(inv_ntgt), _p(stream)))
 
 
-def _workspace(w):
-    return (_p(w), w.numel() * w.element_size() if w is not None else 0)
+def _at(x):
+    """_p for a struct's field, which takes the plain number."""
+    return x if x is None or isinstance(x, int) else x.data_ptr()
 
 
 def hmy_k_logprob(logits_prec, logits, T, V, ldl, targets=None, logp=None, row_max=None, log_sum=None, entropy=None, k=0,
                   top_ids=None, top_logp=None, scale=1.0, stream=None, workspace=None):
-    """workspace: a tensor of HMY_ROWS_WORKSPACE_BYTES, which lets a call of few rows use the whole device."""
-    g = hmy_logprob_desc(logits_prec, T, V, k, _p(logits), ldl, _p(targets), _p(logp), _p(row_max), _p(log_sum),
-                         _p(entropy), _p(top_ids), _p(top_logp), *_workspace(workspace), scale, 0)
+    """workspace: a tensor of HMY_ROWS_WORKSPACE_BYTES, which lets a call of few, long rows use the whole device."""
+    g = hmy_logprob_desc(logits_prec, T, V, k, _at(logits), ldl, _at(targets), _at(logp), _at(row_max), _at(log_sum),
+                         _at(entropy), _at(top_ids), _at(top_logp), _at(workspace),
+                         0 if workspace is None else workspace.numel() * workspace.element_size(), scale, 0)
     _check(lib.hmy_k_logprob(C.byref(g), _p(stream)))
 
 
 def hmy_k_logprob_bwd(prec, logits_prec, logits, row_max, log_sum, dlogits, T, V, ldl, ldd, targets=None, d_logp=None,
                       entropy=None, d_entropy=None, scale=1.0, pad=0, stream=None):
     """prec: type of dlogits, whose columns V .. V+pad-1 are zeroed."""
-    g = hmy_logprob_grad_desc(prec, logits_prec, T, V, _p(logits), ldl, _p(row_max), _p(log_sum), _p(targets), _p(d_logp),
-                              _p(entropy), _p(d_entropy), _p(dlogits), ldd, scale, pad)
+    g = hmy_logprob_grad_desc(prec, logits_prec, T, V, _at(logits), ldl, _at(row_max), _at(log_sum), _at(targets), _at(d_logp),
+                              _at(entropy), _at(d_entropy), _at(dlogits), ldd, scale, pad)
     _check(lib.hmy_k_logprob_bwd(C.byref(g), _p(stream)))
 
 
 def hmy_k_distill(prec, logits_prec, logits, teacher_ids, teacher_logp, row_loss, dlogits, T, V, K, ldl, ldd, tail=False,
                   scale=1.0, grad_scale=1.0, pad=0, loss_acc=None, stream=None, workspace=None):
     """prec: type of dlogits (None: the loss alone); workspace as for hmy_k_logprob."""
-    g = hmy_distill_desc(prec, logits_prec, T, V, K, int(tail), _p(logits), ldl, _p(teacher_ids), _p(teacher_logp),
-                         _p(row_loss), _p(loss_acc), _p(dlogits), ldd, *_workspace(workspace), scale, grad_scale, pad, 0)
+    g = hmy_distill_desc(prec, logits_prec, T, V, K, int(tail), _at(logits), ldl, _at(teacher_ids), _at(teacher_logp),
+                         _at(row_loss), _at(loss_acc), _at(dlogits), ldd, _at(workspace),
+                         0 if workspace is None else workspace.numel() * workspace.element_size(), scale, grad_scale, pad, 0)
     _check(lib.hmy_k_distill(C.byref(g), _p(stream)))
 
 

@@ -5,6 +5,8 @@
 //   H = log S - (sum u_j exp u_j) / S.
 // u is taken from the difference to the maximum, so rows of the type's lowest value, or of very large values, lose nothing; a
 // token at -inf has no weight (0 times its u counts as 0), a row of nothing else has m = -inf and S = 0.
+#include <algorithm>
+
 #include "logit_rows.h"
 
 namespace hmy {
@@ -23,18 +25,22 @@ __device__ __forceinline__ uint64_t rank_key(float x, int col) { return (uint64_
 __device__ __forceinline__ int key_column(uint64_t key) { return int(~uint32_t(key)); }
 constexpr uint32_t kLowestOrdered = 0x00800000u;   // of the lowest finite value: -inf and "none" are below
 
-// What a workgroup finds a row's list with, in LDS.
-constexpr int kCandidates = 2048;
-constexpr int kRanked = 512;       // as many candidates are ranked by comparing all with all
-constexpr int kSlots = 8;          // the row's segments fall into so many slots, of which each thread knows its largest logit
-constexpr int kHits = 1024;
-template <int NT> struct Candidates {
-  uint64_t key[kCandidates];
-  uint32_t rank[kRanked + kWave];
-  float top[kSlots * NT];          // a thread's largest logit in a slot
-  uint32_t hit[kHits];             // slot * NT + thread of those that reach the floor
+// What a workgroup finds a list with, in LDS: `keys` candidates at most; as many as `ranked` are ranked by comparing all with all;
+// the segments of a row fall into `slots` slots, of which each thread knows its largest logit.
+template <int NT_, int KEYS, int RANKED, int SLOTS, int HITS> struct Candidates {
+  static constexpr int NT = NT_, keys = KEYS, ranked = RANKED, slots = SLOTS, hits = HITS;
+  uint64_t key[KEYS];
+  uint32_t rank[RANKED + kWave];
+  float top[SLOTS * NT];           // a thread's largest logit in a slot
+  uint32_t hit[HITS];              // slot * NT + thread of those that reach the floor
   uint32_t n, n_hits, floor, count[2];
 };
+// For rows (and parts of rows) of one slot, which are many at a time, and for longer ones.  On 64 threads for short lists only:
+// there are but 64 maxima to take the floor from.
+template <int NT, bool ONE_SLOT> struct CandidatesOf { typedef Candidates<NT, 2048, 512, 8, 1024> type; };
+template <int NT> struct CandidatesOf<NT, true> { typedef Candidates<NT, 1024, 512, 1, NT> type; };
+template <> struct CandidatesOf<64, true> { typedef Candidates<64, 512, 256, 1, 64> type; };
+constexpr int kShortList = 24;
 
 // by one wave: some t with at least k of its values at or above it, and not many more if it can be had: the bisection ends at
 // k + k / 8 + 2.  kLowestOrdered if fewer than k are at or above that.  count(t): how many are; each lane's smallest (of those
@@ -59,8 +65,8 @@ __device__ __forceinline__ uint32_t threshold(uint32_t lo, uint32_t hi, int k, F
 }
 
 // by the workgroup: the number of its threads' hits, all together
-template <int NT>
-__device__ __forceinline__ int hits(Candidates<NT> &c, int mine, int &turn) {
+template <typename C>
+__device__ __forceinline__ int hits(C &c, int mine, int &turn) {
   // two counters in turn: the next is cleared while this one is read
   const int total = int(wave_total(float(mine)));   // below 2^24: exact
   if (threadIdx.x % kWave == 0 && total) atomicAdd(&c.count[turn], uint32_t(total));
@@ -74,8 +80,8 @@ __device__ __forceinline__ int hits(Candidates<NT> &c, int mine, int &turn) {
 
 // by the workgroup: leaves only those of n > k candidates that the k largest can be among, at most `most` of them, and says how
 // many.  Wants a barrier in front.  The first wave does it: there is little to do, and the others keep their registers.
-template <int NT>
-__device__ __forceinline__ int thin_out(Candidates<NT> &c, int n, int k, int most) {
+template <typename C>
+__device__ __forceinline__ int thin_out(C &c, int n, int k, int most) {
   const int lane = threadIdx.x;
   if (lane < kWave) {
     uint32_t lo = ~0u, hi = 0;
@@ -87,8 +93,14 @@ __device__ __forceinline__ int thin_out(Candidates<NT> &c, int n, int k, int mos
     }
     auto count = [&](uint64_t t) {
       int r = 0;
-#pragma unroll 4
-      for (int i = 0; i < n; i += kWave) r += __popcll(__ballot(i + lane < n && c.key[i + lane] >= t));
+#pragma unroll 1
+      for (int i = lane; i - lane < n; i += 4 * kWave) {
+        bool in[4];
+#pragma unroll
+        for (int o = 0; o < 4; ++o) in[o] = c.key[min(i + o * kWave, n - 1)] >= t && i + o * kWave < n;
+#pragma unroll
+        for (int o = 0; o < 4; ++o) r += __popcll(__ballot(in[o]));
+      }
       return r;
     };
     uint64_t least = uint64_t(threshold(lo, hi, k, [&](uint32_t t) { return count(uint64_t(t) << 32); })) << 32;
@@ -113,10 +125,11 @@ __device__ __forceinline__ int thin_out(Candidates<NT> &c, int n, int k, int mos
 }
 
 // by the workgroup, where there are more candidates than there is room for (the largest logits are those of few threads, or very
-// many are equal): the k first of the `cols` >= k columns from x[first] on, which are read again for every bit.  The k-th largest
+// many are equal): the k first of the `cols` >= k columns x[0 .. cols-1], numbered from `first` on, which are read again for every bit.  The k-th largest
 // logit bit by bit, then of those that equal it the lowest columns.
-template <int NT, typename L>
-__device__ __forceinline__ int keep_first(Candidates<NT> &c, const L *x, int first, int cols, int k) {
+template <typename C, typename L>
+__device__ __forceinline__ int keep_first(C &c, const L *x, int first, int cols, int k) {
+  constexpr int NT = C::NT;
   const int tid = threadIdx.x;
   int turn = 0;
   uint32_t t = 0;
@@ -128,18 +141,18 @@ __device__ __forceinline__ int keep_first(Candidates<NT> &c, const L *x, int fir
     int above = 0;
 #pragma unroll 1
     for (int j = tid; j < cols; j += NT) {
-      const float v = to_f32(x[first + j]);
+      const float v = to_f32(x[j]);
       above += v == v && ordered(v) >= to;
     }
-    if (hits<NT>(c, above, turn) >= k) t = to;
+    if (hits(c, above, turn) >= k) t = to;
   }
   int above = 0;
 #pragma unroll 1
   for (int j = tid; j < cols; j += NT) {
-    const float v = to_f32(x[first + j]);
+    const float v = to_f32(x[j]);
     above += v == v && ordered(v) > t;
   }
-  const int want = k - hits<NT>(c, above, turn);   // of those that equal it
+  const int want = k - hits(c, above, turn);   // of those that equal it
   int last = 0;
 #pragma unroll 1
   for (int bit = 24; bit >= 0; --bit) {
@@ -147,14 +160,14 @@ __device__ __forceinline__ int keep_first(Candidates<NT> &c, const L *x, int fir
     int equal = 0;
 #pragma unroll 1
     for (int j = tid; j < cols && j < to; j += NT) {
-      const float v = to_f32(x[first + j]);
+      const float v = to_f32(x[j]);
       equal += v == v && ordered(v) == t;
     }
-    if (hits<NT>(c, equal, turn) <= want) last = to;
+    if (hits(c, equal, turn) <= want) last = to;
   }
 #pragma unroll 1
   for (int j = tid; j < cols; j += NT) {
-    const float v = to_f32(x[first + j]);
+    const float v = to_f32(x[j]);
     if (v == v && (ordered(v) > t || (ordered(v) == t && j < last))) c.key[atomicAdd(&c.n, 1u)] = rank_key(v, first + j);
   }
   __syncthreads();
@@ -162,11 +175,12 @@ __device__ __forceinline__ int keep_first(Candidates<NT> &c, const L *x, int fir
 }
 
 // by the workgroup: the k first of n candidates, `put(rank, key)` for each.  Wants a barrier in front.
-template <int NT, typename F>
-__device__ __forceinline__ void rank_candidates(Candidates<NT> &c, int n, int k, F put) {
+template <typename C, typename F>
+__device__ __forceinline__ void rank_candidates(C &c, int n, int k, F put) {
+  constexpr int NT = C::NT;
   const int tid = threadIdx.x;
-  if (n > 2 * k + 64) n = thin_out<NT>(c, n, k, kRanked);
-  // n is at most kRanked now.  All compared with all: `parts` threads share the comparisons of one candidate.
+  if (n > min(2 * k + 64, C::ranked)) n = thin_out(c, n, k, C::ranked);
+  // n is at most C::ranked now.  All compared with all: `parts` threads share the comparisons of one candidate.
   const int wide = (n + kWave - 1) / kWave * kWave, parts = max(1, NT / max(wide, 1)), share = ((n + parts - 1) / parts + 7) / 8 * 8;
   for (int i = tid; i < wide; i += NT) c.rank[i] = 0;
   if (tid < 8) c.key[n + tid] = 0;
@@ -216,6 +230,24 @@ __device__ __forceinline__ Sums wave_sums(const Sums &z, float scale) {
   r.A = wave_total(r.A);
   return r;
 }
+// Few, long rows: per_row <= 64 workgroups each take `cols` (a multiple of eight) of a row's columns.
+struct RowParts {
+  Sums *sums;          // [rows * per_row]
+  uint64_t *keys;      // [rows * per_row, k]
+  int per_row, cols;
+};
+// one entry of a row's list
+struct PutEntry {
+  int32_t *ids;
+  float *logp;
+  float m, scale, log_sum;
+  __device__ __forceinline__ PutEntry(const LogprobArgs &a, int row, const Sums &z)
+      : ids(a.top_ids + int64_t(row) * a.k), logp(a.top_logp + int64_t(row) * a.k), m(z.m), scale(a.scale), log_sum(logf(z.S)) {}
+  __device__ __forceinline__ void operator()(int rank, uint64_t key) const {
+    ids[rank] = key ? key_column(key) : -1;
+    logp[rank] = key ? (unordered(uint32_t(key >> 32)) - m) * scale - log_sum : -INFINITY;
+  }
+};
 __device__ __forceinline__ void put_row(const LogprobArgs &a, int row, const Sums &z, float target_logit, bool has_target) {
   const float log_sum = logf(z.S), ref = z.m == -INFINITY ? 0.f : z.m;
   if (a.logp) a.logp[row] = !has_target ? 0.f : z.S == 0.f ? -INFINITY : (target_logit - ref) * a.scale - log_sum;
@@ -224,15 +256,15 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int row, const Sum
   if (a.entropy) a.entropy[row] = z.S == 0.f ? 0.f : log_sum - z.A * kLn2 / z.S;
 }
 
-// by the workgroup: the k first of a row's tokens, `put(rank, key)` for each.  `mine`: this thread's largest logit, c.top its
+// by the workgroup: the k first of the columns x[0 .. cols-1], numbered from `first` on, `put(rank, key)` for each.  `mine`: this thread's largest logit, c.top its
 // largest per slot of `per_slot` segments; xb: the logit of column `behind`, -inf where the thread has none.
 // A floor that at least k logits reach: the k-th largest, or a little less, of the maxima of 256 groups of threads.  What reaches
 // it is in the slots of few threads (k of 256 groups at least; as many as the row's largest logits fall into), and those columns
 // are read again: a second reading of a small part of the row, where looking for candidates in the first one costs every segment a
 // comparison and a barrier (2048 x 131072 bf16, k = 128: 192 us; 512 x 50257 fp32, k = 64: 39 us).
-template <typename L, int NT, int NG, typename F>
-__device__ __forceinline__ void list_row(Candidates<NT> &c, const L *x, int first, int groups, int cols, int per_slot, int k, float mine, float xb, int behind, F put) {
-  constexpr int kSegment = NT * NG;
+template <int NG, typename C, typename L, typename F>
+__device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups, int cols, int per_slot, int k, float mine, float xb, int behind, F put) {
+  constexpr int NT = C::NT, kSegment = NT * NG;
   const int tid = threadIdx.x, lane = tid % kWave;
   const int slots = ((groups + kSegment - 1) / kSegment + per_slot - 1) / per_slot;
   uint32_t *group = reinterpret_cast<uint32_t *>(c.key);   // free until there are candidates
@@ -262,20 +294,20 @@ __device__ __forceinline__ void list_row(Candidates<NT> &c, const L *x, int firs
     for (int s = 0; s < slots; ++s)
       if (c.top[s * NT + tid] >= floor) {
         const uint32_t at = atomicAdd(&c.n_hits, 1u);
-        if (at < kHits) c.hit[at] = s * NT + tid;
+        if (at < C::hits) c.hit[at] = s * NT + tid;
       }
   }
   __syncthreads();
-  if (xb >= floor) c.key[atomicAdd(&c.n, 1u)] = rank_key(xb, behind);   // at most seven
+  if (xb >= floor) c.key[atomicAdd(&c.n, 1u)] = rank_key(xb, first + behind);   // at most seven
   const int n_hits = int(c.n_hits);
-  if (n_hits <= kHits) {
+  if (n_hits <= C::hits) {
     for (int s = 0; s < per_slot; ++s)
       for (int i = tid; i < n_hits * NG; i += NT) {
         const uint32_t h = c.hit[i / NG];
         const int g = ((h / NT) * per_slot + s) * kSegment + (i % NG) * NT + h % NT;
         if (g < groups) {
           Eight<L> v;
-          load_whole(v, x + first + uint32_t(g) * 8);
+          load_whole(v, x + uint32_t(g) * 8);
           int above = 0;
 #pragma unroll
           for (int o = 0; o < 8; ++o) above += v.at(o) >= floor;
@@ -284,7 +316,7 @@ __device__ __forceinline__ void list_row(Candidates<NT> &c, const L *x, int firs
 #pragma unroll
             for (int o = 0; o < 8; ++o)
               if (v.at(o) >= floor) {
-                if (at < kCandidates) c.key[at] = rank_key(v.at(o), first + g * 8 + o);
+                if (at < C::keys) c.key[at] = rank_key(v.at(o), first + g * 8 + o);
                 ++at;
               }
           }
@@ -294,27 +326,33 @@ __device__ __forceinline__ void list_row(Candidates<NT> &c, const L *x, int firs
   __syncthreads();
   int n = __builtin_amdgcn_readfirstlane(c.n);
   __syncthreads();   // all have read c.n, which is written again
-  if (n > kCandidates - 8 || n_hits > kHits) n = keep_first<NT>(c, x, first, cols, k);   // (eight keys more are written behind n)
-  rank_candidates<NT>(c, n, k, put);
+  if (n > C::keys - 8 || n_hits > C::hits) n = keep_first(c, x, first, cols, k);   // (eight keys more are written behind n)
+  rank_candidates(c, n, k, put);
 }
 
-// One workgroup per row, NT * NG groups of eight columns at a time, the next ones' loads on their way meanwhile.  One reading
-// of the row: each thread keeps a running maximum and sums relative to it, and its largest logit per slot for the list.
-template <typename L, int NT, int NG, bool TOP, int WPE>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void k_logprob(const L *logits, LogprobArgs a) {
+// One workgroup per row (PARTS: per part of a row, of which the workspace gets the sums and the list), NT * NG groups of eight
+// columns at a time, the next ones' loads on their way meanwhile.  One reading: each thread keeps a running maximum and sums
+// relative to it, and its largest logit per slot for the list.
+template <typename L, int NT, int NG, bool TOP, bool ONE_SLOT, bool PARTS>
+__global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, RowParts p) {
   constexpr int kWaves = NT / kWave, kSegment = NT * NG;
+  typedef typename CandidatesOf<NT, ONE_SLOT>::type Cands;
   __shared__ Sums part[kWaves];
-  __shared__ Candidates<TOP ? NT : 1> cand;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), row = blockIdx.x;
+  __shared__ __attribute__((aligned(16))) char cand_[TOP ? sizeof(Cands) : 1];
+  Cands &cand = *reinterpret_cast<Cands *>(cand_);
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int row = PARTS ? blockIdx.x / p.per_row : blockIdx.x, piece = PARTS ? blockIdx.x % p.per_row : 0;
   const float c = a.scale * kLog2e;
-  const L *x = logits + int64_t(row) * a.ldl;
-  const int groups = a.V / 8, segments = (groups + kSegment - 1) / kSegment, per_slot = (segments + kSlots - 1) / kSlots;
-  const int tgt = a.targets ? a.targets[row] : -1;
+  // columns first .. first+cols-1
+  const int first = PARTS ? piece * p.cols : 0, cols = PARTS ? min(p.cols, a.V - first) : a.V;
+  const L *x = logits + int64_t(row) * a.ldl + first;
+  const int groups = cols / 8, segments = (groups + kSegment - 1) / kSegment, per_slot = (segments + Cands::slots - 1) / Cands::slots;
+  const int tgt = !PARTS && a.targets ? a.targets[row] : -1;
   const bool has_target = tgt >= 0 && tgt < a.V;
   const float target_logit = has_target ? to_f32(x[tgt]) : 0.f;
   // the column behind the groups, if there is one for this thread
   const int behind = groups * 8 + tid;
-  const float xb = behind < a.V ? to_f32(x[behind]) : -INFINITY;
+  const float xb = behind < cols ? to_f32(x[behind]) : -INFINITY;
   auto load = [&](Eight<L> (&v)[NG], int seg) {
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
@@ -326,7 +364,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
   Eight<L> v[NG], next[NG];
   if (segments > 0) load(v, 0);
   Sums z = {fmaxf(xb, -INFINITY), 0.f, 0.f};
-  if (behind < a.V) z.S = fast_exp2((xb - (xb == -INFINITY ? 0.f : xb)) * c);   // 1, 0 for -inf, NaN
+  if (behind < cols) z.S = fast_exp2((xb - (xb == -INFINITY ? 0.f : xb)) * c);   // 1, 0 for -inf, NaN
   float in_slot = -INFINITY;
   for (int seg = 0, of_slot = 0; seg < segments; ++seg) {
     if (seg + 1 < segments) load(next, seg + 1);
@@ -369,14 +407,61 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
   __syncthreads();
   Sums all = lane < kWaves ? part[lane] : no_sums();
   all = wave_sums(all, a.scale);
-  if (tid == 0) put_row(a, row, all, target_logit, has_target);
-  if constexpr (TOP) {
-    const float log_sum = logf(all.S);
-    list_row<L, NT, NG>(cand, x, 0, groups, a.V, per_slot, a.k, z.m, xb, behind, [&](int rank, uint64_t key) {
-      a.top_ids[int64_t(row) * a.k + rank] = key ? key_column(key) : -1;
-      a.top_logp[int64_t(row) * a.k + rank] = key ? (unordered(uint32_t(key >> 32)) - all.m) * a.scale - log_sum : -INFINITY;
-    });
+  if constexpr (PARTS) {
+    if (tid == 0) p.sums[blockIdx.x] = all;
+    if constexpr (TOP)
+      list_row<NG>(cand, x, first, groups, cols, per_slot, a.k, z.m, xb, behind, [&](int rank, uint64_t key) { p.keys[int64_t(blockIdx.x) * a.k + rank] = key; });
+  } else {
+    if (tid == 0) put_row(a, row, all, target_logit, has_target);
+    if constexpr (TOP) list_row<NG>(cand, x, 0, groups, cols, per_slot, a.k, z.m, xb, behind, PutEntry(a, row, all));
   }
+}
+
+// The rows of few, long rows whose parts have been taken by a workgroup each: sums of the parts' sums, and the first of the
+// parts' lists.
+constexpr int kJoinThreads = 256;
+template <typename L>
+__global__ __launch_bounds__(kJoinThreads) void k_logprob_join(const L *logits, LogprobArgs a, RowParts p) {
+  typedef Candidates<kJoinThreads, 2048, 512, 1, 1> Cands;
+  __shared__ __attribute__((aligned(16))) Cands cand;
+  const int tid = threadIdx.x, lane = tid % kWave, row = blockIdx.x;
+  const Sums all = wave_sums(lane < p.per_row ? p.sums[row * p.per_row + lane] : no_sums(), a.scale);   // per_row <= 64
+  if (tid == 0) {
+    const int tgt = a.targets ? a.targets[row] : -1;
+    const bool has_target = tgt >= 0 && tgt < a.V;
+    put_row(a, row, all, has_target ? to_f32(logits[int64_t(row) * a.ldl + tgt]) : 0.f, has_target);
+  }
+  if (!a.k) return;
+  // What at least k of the parts' keys reach: each part's j-th with j parts >= k, or the k-th of one part.  0: none
+  const uint64_t *keys = p.keys + int64_t(row) * p.per_row * a.k;
+  const int total = p.per_row * a.k, j = (a.k + p.per_row - 1) / p.per_row;
+  uint64_t each = lane < p.per_row ? keys[lane * a.k + j - 1] : ~uint64_t(0), one = lane < p.per_row ? keys[lane * a.k + a.k - 1] : 0;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    each = min(each, uint64_t(__shfl_xor((unsigned long long)each, o, kWave)));
+    one = max(one, uint64_t(__shfl_xor((unsigned long long)one, o, kWave)));
+  }
+  uint64_t least = max(max(each, one), uint64_t(1));
+  if (tid == 0) cand.n = cand.count[0] = cand.count[1] = 0;
+  __syncthreads();
+  int turn = 0;
+  auto reach = [&](uint64_t t) {
+    int r = 0;
+    for (int i = tid; i < total; i += kJoinThreads) r += keys[i] >= t;
+    return hits(cand, r, turn);
+  };
+  if (reach(least) > Cands::keys - 8) {   // most of the list in one or two parts: the k-th largest key itself, bit by bit
+    least = 0;
+#pragma unroll 1
+    for (int bit = 63; bit >= 0; --bit)
+      if (reach(least | uint64_t(1) << bit) >= a.k) least |= uint64_t(1) << bit;
+  }
+  for (int i = tid; i < total; i += kJoinThreads)
+    if (keys[i] >= least) cand.key[atomicAdd(&cand.n, 1u)] = keys[i];
+  __syncthreads();
+  const int n = __builtin_amdgcn_readfirstlane(cand.n);
+  __syncthreads();
+  rank_candidates(cand, n, a.k, PutEntry(a, row, all));
 }
 
 struct LogprobGradArgs {
@@ -439,12 +524,13 @@ __global__ __launch_bounds__(NT) void k_logprob_bwd(const L *logits, E *dlogits,
   }
 }
 
-template <typename L, int NT, int NG, int WPE>
+template <typename L, int NT, int NG, bool ONE_SLOT>
 void launch_rows(const L *x, LogprobArgs a, int rows, hipStream_t s) {
+  const RowParts none = {};
   for (; rows > 0; rows -= kMaxGrid) {   // a launch has a limited number of workgroups
     const dim3 grid(rows < kMaxGrid ? rows : kMaxGrid);
-    if (a.k) hipLaunchKernelGGL((k_logprob<L, NT, NG, true, WPE>), grid, dim3(NT), 0, s, x, a);
-    else hipLaunchKernelGGL((k_logprob<L, NT, NG, false, WPE>), grid, dim3(NT), 0, s, x, a);
+    if (a.k) hipLaunchKernelGGL((k_logprob<L, NT, NG, true, ONE_SLOT, false>), grid, dim3(NT), 0, s, x, a, none);
+    else hipLaunchKernelGGL((k_logprob<L, NT, NG, false, true, false>), grid, dim3(NT), 0, s, x, a, none);
     x += int64_t(kMaxGrid) * a.ldl;
     for (float **p : {&a.logp, &a.row_max, &a.log_sum, &a.entropy})
       if (*p) *p += kMaxGrid;
@@ -455,10 +541,31 @@ void launch_rows(const L *x, LogprobArgs a, int rows, hipStream_t s) {
     }
   }
 }
+
+constexpr int kPartRows = 32, kPartLaunch = 512, kPartMinCols = 16384, kPartMaxCols = 65536, kPartsMax = 64;
+static_assert(kPartLaunch * (sizeof(Sums) + 4 + HMY_MAX_TOP * 8) <= HMY_ROWS_WORKSPACE_BYTES, "the parts' sums and lists fit the workspace");
+
 template <typename L>
-void launch_rows(const L *x, const LogprobArgs &a, int rows, hipStream_t s) {
-  if (a.V <= 16384) launch_rows<L, 256, 2, 4>(x, a, rows, s);
-  else launch_rows<L, 1024, 2, 8>(x, a, rows, s);
+void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hipStream_t s) {
+  const int room = rows <= kPartRows ? kPartLaunch / rows : 1;
+  const int parts = std::min(std::min(room, kPartsMax), a.V / kPartMinCols);
+  if (workspace && parts >= 4 && a.V / parts <= kPartMaxCols) {
+    RowParts p;
+    p.cols = (a.V + parts - 1) / parts + 7 & ~7;
+    p.per_row = (a.V + p.cols - 1) / p.cols;
+    p.keys = static_cast<uint64_t *>(workspace);
+    p.sums = reinterpret_cast<Sums *>(p.keys + int64_t(rows) * p.per_row * a.k);
+    const dim3 grid(rows * p.per_row);
+    if (a.k) hipLaunchKernelGGL((k_logprob<L, 512, sizeof(L) == 4 ? 2 : 4, true, true, true>), grid, dim3(512), 0, s, x, a, p);
+    else hipLaunchKernelGGL((k_logprob<L, 512, sizeof(L) == 4 ? 2 : 4, false, true, true>), grid, dim3(512), 0, s, x, a, p);
+    hipLaunchKernelGGL(k_logprob_join<L>, dim3(rows), dim3(kJoinThreads), 0, s, x, a, p);
+  } else if (a.V <= 2048 && a.k <= kShortList) {
+    launch_rows<L, 64, 4, true>(x, a, rows, s);
+  } else if (a.V <= 8192) {
+    launch_rows<L, 256, 4, true>(x, a, rows, s);
+  } else {
+    launch_rows<L, 512, sizeof(L) == 4 ? 2 : 4, false>(x, a, rows, s);
+  }
 }
 
 }  // namespace
@@ -476,8 +583,10 @@ int launch_logprob(const hmy_logprob_desc &g, stream_t st) {
     if (misaligned(p, 4)) return fail(HMY_E_INVALID, "logprob: misaligned array");
   const LogprobArgs a = {g.targets, g.logp, g.row_max, g.log_sum, g.entropy, g.top_ids, g.top_logp, g.V, g.k, g.ldl, g.scale};
   const hipStream_t s = (hipStream_t)st;
-  if (g.logits_prec == HMY_PREC_BF16) launch_rows((const bf16_t *)g.logits, a, g.T, s);
-  else launch_rows((const float *)g.logits, a, g.T, s);
+  void *ws = has_workspace(g.workspace, g.workspace_bytes) ? g.workspace : nullptr;
+  if (misaligned(ws, 16)) return fail(HMY_E_INVALID, "logprob: workspace not aligned to 16 bytes");
+  if (g.logits_prec == HMY_PREC_BF16) launch_rows((const bf16_t *)g.logits, a, g.T, ws, s);
+  else launch_rows((const float *)g.logits, a, g.T, ws, s);
   return check_launch("logprob");
 }
 
