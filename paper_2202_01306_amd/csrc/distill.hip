@@ -7,6 +7,8 @@
 // A divergence is small beside the logarithms that it is the difference of: the list's terms are held in 64 bits.  With a tail
 // the row's sum is taken as that of the others (listed tokens are set to -inf where they are loaded) and that of the list, so
 // that p_r of a student who is sure of listed tokens is no difference of two sums.
+#include <algorithm>
+
 #include "logit_rows.h"
 
 namespace hmy {
@@ -197,15 +199,102 @@ __device__ __forceinline__ float row_loss(float m_rest, float rest, const List &
   return float(loss);
 }
 
+// Sets the listed tokens among a wave's own columns (groups g0 .. g1-1 of the row, dealt out over NT threads) to -inf: a wave looks
+// for itself, with a bit in LDS for each of a thread's columns, and needs no barrier.  id: this lane's two entries.
+template <int NT, int NG, typename L>
+__device__ __forceinline__ void drop_listed(Eight<L> (&v)[NG], uint32_t *listed, const int (&id)[2], int g0, int g1, int wave) {
+  constexpr int kWords = (NG + 3) / 4;
+  const int tid = threadIdx.x;
+#pragma unroll
+  for (int w = 0; w < kWords; ++w) listed[w * NT + tid] = 0;
+  lds_of_own_wave();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int off = id[i] / 8 - g0, owner = off % NT;
+    if (id[i] >= 0 && off >= 0 && off < g1 - g0 && owner / kWave == wave) {
+      const int slot = (off / NT) * 8 + id[i] % 8;
+      atomicOr(&listed[(slot / 32) * NT + owner], 1u << (slot % 32));
+    }
+  }
+  lds_of_own_wave();
+#pragma unroll
+  for (int w = 0; w < kWords; ++w) {
+    const uint32_t bits = listed[w * NT + tid];
+#pragma unroll
+    for (int i = 4 * w; i < 4 * w + 4 && i < NG; ++i)
+      if (bits >> (8 * (i % 4)) & 0xff) v[i].set_no_weight(bits >> (8 * (i % 4)));
+  }
+  lds_of_own_wave();   // the next columns' bits come behind the reads
+}
+// whether column `behind`, of the row's last V % 8, is listed: those are the first wave's
+__device__ __forceinline__ bool is_listed_behind(const int (&id)[2], int V, int behind) {
+  bool listed = false;
+  for (int c = V / 8 * 8; c < V; ++c) {
+    const bool any = __any(id[0] == c || id[1] == c);
+    listed |= any && c == behind;
+  }
+  return listed;
+}
+// a thread's running maximum and sum of exp(s (x - m)) with more columns; HOLD: their exponentials stay in their place
+template <bool HOLD, int NG, typename L>
+__device__ __forceinline__ void add_columns(Eight<L> (&v)[NG], float xb, float &m, float &sum, float c) {
+  float sm = fmaxf(m, xb);
+#pragma unroll
+  for (int i = 0; i < NG; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sm = fmaxf(sm, v[i].at(k));
+  const float ref = sm == -INFINITY ? 0.f : sm;
+  sum *= fast_exp2((m - ref) * c);
+  m = sm;
+  sum += fast_exp2((xb - ref) * c);   // 0 for -inf
+#pragma unroll
+  for (int i = 0; i < NG; ++i) {
+    v[i].forget_floats();
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const float e = fast_exp2((v[i].at(k) - ref) * c);
+      sum += e;
+      if constexpr (HOLD) v[i].w[k] = __float_as_uint(e);
+    }
+    v[i].forget_floats();
+  }
+}
+// m and sum of a wave's lanes, the same for all of them
+__device__ __forceinline__ void wave_sums(float &m, float &sum, float scale) {
+  const float wm = wave_top(m);
+  sum = wave_total(sum == 0.f ? 0.f : sum * rebase(m, wm, scale));
+  m = wm;
+}
+template <int NT>
+__device__ __forceinline__ void block_sums(float &m, float &sum, float scale, float *scratch) {
+  constexpr int kWaves = NT / kWave;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  wave_sums(m, sum, scale);
+  if (lane == 0) {
+    scratch[wave] = m;
+    scratch[kWaves + wave] = sum;
+  }
+  __syncthreads();
+  m = lane < kWaves ? scratch[lane] : -INFINITY;
+  sum = lane < kWaves ? scratch[kWaves + lane] : 0.f;
+  wave_sums(m, sum, scale);
+}
+// gradient of one row's listed tokens, by one wave, behind the stores of the columns around them
+template <typename E>
+__device__ __forceinline__ void put_listed(E *d, const List &l, const RowTerms &r, const DistillArgs &a, int lane, int c0, int c1) {
+#pragma unroll 1
+  for (int k = lane; k < a.K; k += kWave)
+    if (l.id[k] >= c0 && l.id[k] < c1) d[l.id[k]] = from_f32<E>(fmaf(rebase(l.x[k], r.m, a.scale), r.c_list, -l.gq[k]));
+}
+
 // One workgroup per row.  The row stays in registers between its sums and its gradient, as exponentials in fp32, as loaded in
 // bf16; of a row beyond NT * NG groups of eight columns the last so many do, and those in front are read again.
 template <typename L, typename E, int NT, int NG, bool TAIL, int WPE>
 __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void k_distill(const L *logits, E *dlogits, DistillArgs a) {
-  constexpr int kWaves = NT / kWave, kSegment = NT * NG, kWords = (NG + 3) / 4;
+  constexpr int kSegment = NT * NG;
   constexpr bool kHold = sizeof(L) == 4;
-  __shared__ uint32_t listed[TAIL ? NT * kWords : 1];   // a bit for each of a thread's columns
-  __shared__ uint32_t listed_behind[kWaves];            // and for the columns behind the whole groups
-  __shared__ float wave_m[kWaves], wave_s[kWaves];
+  __shared__ uint32_t listed[TAIL ? NT * ((NG + 3) / 4) : 1];
+  __shared__ float scratch[2 * NT / kWave];
   __shared__ ListSum z;
   __shared__ __attribute__((aligned(16))) List list;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -221,6 +310,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
   if (wave == 0) read_list(x, a, lane, id, tl, list, z);
   Eight<L> v[NG];
   float xb = behind < a.V ? to_f32(x[behind]) : -INFINITY, m = -INFINITY, sum = 0.f;
+  if (TAIL && wave == 0 && is_listed_behind(id, a.V, behind)) xb = -INFINITY;
   for (int seg = 0; seg < segments; ++seg) {
     const int g0 = seg == 0 ? 0 : lead + (seg - 1) * kSegment, g1 = lead + seg * kSegment;
 #pragma unroll
@@ -229,60 +319,11 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
       if (g < g1) load_whole(v[i], x + uint32_t(g) * 8);
       else v[i].all_no_weight();
     }
-    if constexpr (TAIL) {   // a wave finds the listed tokens among its own columns: no barrier
-#pragma unroll
-      for (int w = 0; w < kWords; ++w) listed[w * NT + tid] = 0;
-      if (seg == 0 && lane == 0) listed_behind[wave] = 0;
-      lds_of_own_wave();
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int off = id[i] / 8 - g0, owner = off % NT;
-        if (id[i] >= 0 && off >= 0 && off < g1 - g0 && owner / kWave == wave) {
-          const int slot = (off / NT) * 8 + id[i] % 8;
-          atomicOr(&listed[(slot / 32) * NT + owner], 1u << (slot % 32));
-        }
-        if (seg == 0 && id[i] >= groups * 8) atomicOr(&listed_behind[wave], 1u << (id[i] % 8));
-      }
-      lds_of_own_wave();
-#pragma unroll
-      for (int w = 0; w < kWords; ++w) {
-        const uint32_t bits = listed[w * NT + tid];
-#pragma unroll
-        for (int i = 4 * w; i < 4 * w + 4 && i < NG; ++i)
-          if (bits >> (8 * (i % 4)) & 0xff) v[i].set_no_weight(bits >> (8 * (i % 4)));
-      }
-      if (seg == 0 && tid < 8 && (listed_behind[wave] >> tid & 1)) xb = -INFINITY;
-    }
-    float sm = fmaxf(m, xb);
-#pragma unroll
-    for (int i = 0; i < NG; ++i)
-#pragma unroll
-      for (int k = 0; k < 8; ++k) sm = fmaxf(sm, v[i].at(k));
-    const float ref = sm == -INFINITY ? 0.f : sm;
-    sum *= fast_exp2((m - ref) * c);
-    m = sm;
-    if (seg == 0) sum += fast_exp2((xb - ref) * c);
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      v[i].forget_floats();
-#pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float e = fast_exp2((v[i].at(k) - ref) * c);
-        sum += e;
-        if constexpr (kHold) v[i].w[k] = __float_as_uint(e);
-      }
-      v[i].forget_floats();
-    }
+    if constexpr (TAIL) drop_listed<NT>(v, listed, id, g0, g1, wave);
+    add_columns<kHold>(v, seg == 0 ? xb : -INFINITY, m, sum, c);
   }
-  // the row's sum: of a wave, then of the workgroup, one barrier
-  const float wm = wave_top(m), ws = wave_total(sum == 0.f ? 0.f : sum * rebase(m, wm, a.scale));
-  if (lane == 0) {
-    wave_m[wave] = wm;
-    wave_s[wave] = ws;
-  }
-  __syncthreads();
-  const float om = lane < kWaves ? wave_m[lane] : -INFINITY, m_rest = wave_top(om);
-  const float os = lane < kWaves ? wave_s[lane] : 0.f, rest = wave_total(os == 0.f ? 0.f : os * rebase(om, m_rest, a.scale));
+  float m_rest = m, rest = sum;
+  block_sums<NT>(m_rest, rest, a.scale, scratch);
   if (dlogits) {
     E *d = dlogits + int64_t(row) * a.ldd;
     const RowTerms r = row_terms(m_rest, rest, z, a);
@@ -327,14 +368,106 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
     }
     zero_padding(d, a.V, a.pad, tid, NT);
     __syncthreads();   // behind the stores of the columns around
-    if (wave == 0) {
-#pragma unroll 1
-      for (int k = lane; k < a.K; k += kWave)
-        if (list.id[k] >= 0) d[list.id[k]] = from_f32<E>(fmaf(rebase(list.x[k], r.m, a.scale), r.c_list, -list.gq[k]));
-    }
+    if (wave == 0) put_listed(d, list, r, a, lane, 0, a.V);
   }
   if (wave == 0) {
     const float loss = row_loss(m_rest, rest, list, z, a, lane);
+    if (lane == 0) a.row_loss[row] = loss;
+  }
+}
+
+// Few, long rows: workgroups each take `groups` of a row's groups of eight columns, once for the row's sums and once for the
+// gradient.
+struct RowParts {
+  ListSum *z;        // [rows]
+  List *list;        // [rows]
+  float2 *sums;      // [rows * per_row]: maximum, sum relative to it
+  int per_row, groups;
+};
+constexpr int kPartThreads = 512;
+
+template <typename L, int NG, bool TAIL>
+__global__ __launch_bounds__(kPartThreads) void k_distill_parts(const L *logits, DistillArgs a, RowParts p) {
+  constexpr int NT = kPartThreads;
+  __shared__ uint32_t listed[TAIL ? NT * ((NG + 3) / 4) : 1];
+  __shared__ float scratch[2 * NT / kWave];
+  __shared__ ListSum z;
+  __shared__ __attribute__((aligned(16))) List list;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int row = blockIdx.x / p.per_row, piece = blockIdx.x % p.per_row;
+  const float c = a.scale * kLog2e;
+  const L *x = logits + int64_t(row) * a.ldl;
+  const int first = piece * p.groups, last = min(first + p.groups, a.V / 8), behind = a.V / 8 * 8 + tid;
+  int id[2];
+  float tl[2];
+  list_entries(a, row, lane, id, tl);
+  float xb = piece == p.per_row - 1 && behind < a.V ? to_f32(x[behind]) : -INFINITY, m = -INFINITY, sum = 0.f;
+  if (TAIL && wave == 0 && is_listed_behind(id, a.V, behind)) xb = -INFINITY;
+  Eight<L> v[NG];
+  for (int g0 = first; g0 < last; g0 += NT * NG) {
+#pragma unroll
+    for (int i = 0; i < NG; ++i) {
+      if (g0 + i * NT + tid < last) load_whole(v[i], x + uint32_t(g0 + i * NT + tid) * 8);
+      else v[i].all_no_weight();
+    }
+    if constexpr (TAIL) drop_listed<NT>(v, listed, id, g0, min(g0 + NT * NG, last), wave);
+    add_columns<false>(v, -INFINITY, m, sum, c);
+  }
+  if (xb > -INFINITY || xb != xb) {
+    const float sm = fmaxf(m, xb), ref = sm == -INFINITY ? 0.f : sm;
+    sum = sum * fast_exp2((m - ref) * c) + fast_exp2((xb - ref) * c);
+    m = sm;
+  }
+  block_sums<NT>(m, sum, a.scale, scratch);
+  if (tid == 0) p.sums[blockIdx.x] = make_float2(m, sum);
+  if (piece == 0 && wave == 0) {
+    read_list(x, a, lane, id, tl, list, z);
+    lds_of_own_wave();
+    for (int i = lane; i < int(sizeof(List) / 4); i += kWave) reinterpret_cast<uint32_t *>(p.list + row)[i] = reinterpret_cast<const uint32_t *>(&list)[i];
+    if (lane == 0) p.z[row] = z;
+  }
+}
+template <typename L, typename E>
+__global__ __launch_bounds__(kPartThreads) void k_distill_finish(const L *logits, E *dlogits, DistillArgs a, RowParts p) {
+  constexpr int NT = kPartThreads, NG = 2;
+  const int tid = threadIdx.x, lane = tid % kWave;
+  const int row = blockIdx.x / p.per_row, piece = blockIdx.x % p.per_row;
+  const float2 part = lane < p.per_row ? p.sums[row * p.per_row + lane] : make_float2(-INFINITY, 0.f);   // per_row <= 64
+  float m_rest = part.x, rest = part.y;
+  wave_sums(m_rest, rest, a.scale);
+  const ListSum z = p.z[row];
+  if (dlogits) {
+    const RowTerms r = row_terms(m_rest, rest, z, a);
+    const float c = a.scale * kLog2e;
+    auto grad = [&](float xj) { return z.any ? fast_exp2((xj - r.m) * c) * r.c_rest : 0.f; };
+    const L *x = logits + int64_t(row) * a.ldl;
+    E *d = dlogits + int64_t(row) * a.ldd;
+    const int first = piece * p.groups, last = min(first + p.groups, a.V / 8);
+    for (int g0 = first + tid; g0 < last; g0 += NT * NG) {
+      Eight<L> v[NG];
+#pragma unroll
+      for (int i = 0; i < NG; ++i)
+        if (g0 + i * NT < last) load_whole(v[i], x + uint32_t(g0 + i * NT) * 8);
+#pragma unroll
+      for (int i = 0; i < NG; ++i)
+        if (g0 + i * NT < last) {
+          float o[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) o[k] = grad(v[i].at(k));
+          store_whole(d + uint32_t(g0 + i * NT) * 8, o);
+        }
+    }
+    const bool ends = piece == p.per_row - 1;
+    const int behind = a.V / 8 * 8 + tid;
+    if (ends) {
+      if (behind < a.V) d[behind] = from_f32<E>(grad(to_f32(x[behind])));
+      zero_padding(d, a.V, a.pad, tid, NT);
+    }
+    __syncthreads();   // behind the stores of the columns around
+    if (tid < kWave) put_listed(d, p.list[row], r, a, lane, first * 8, ends ? a.V : last * 8);
+  }
+  if (piece == 0 && tid < kWave) {
+    const float loss = row_loss(m_rest, rest, p.list[row], z, a, lane);
     if (lane == 0) a.row_loss[row] = loss;
   }
 }
@@ -368,6 +501,24 @@ void launch_rows(const L *x, E *d, DistillArgs a, hipStream_t s) {
   }
 }
 
+constexpr int kPartRows = 32, kPartLaunch = 512, kPartMinCols = 16384, kPartsMax = 64;
+static_assert(kPartRows * (sizeof(List) + sizeof(ListSum)) + kPartLaunch * sizeof(float2) <= HMY_ROWS_WORKSPACE_BYTES, "the parts' sums and the lists fit the workspace");
+
+template <typename L, typename E>
+void launch_parts(const L *x, E *d, const DistillArgs &a, int parts, void *workspace, hipStream_t s) {
+  RowParts p;
+  p.groups = (a.V / 8 + parts - 1) / parts;
+  p.per_row = (a.V / 8 + p.groups - 1) / p.groups;
+  p.list = static_cast<List *>(workspace);
+  p.z = reinterpret_cast<ListSum *>(p.list + a.T);
+  p.sums = reinterpret_cast<float2 *>(p.z + a.T);
+  const dim3 grid(a.T * p.per_row);
+  constexpr int NG = sizeof(L) == 4 ? 2 : 4;
+  if (a.tail) hipLaunchKernelGGL((k_distill_parts<L, NG, true>), grid, dim3(kPartThreads), 0, s, x, a, p);
+  else hipLaunchKernelGGL((k_distill_parts<L, NG, false>), grid, dim3(kPartThreads), 0, s, x, a, p);
+  hipLaunchKernelGGL((k_distill_finish<L, E>), grid, dim3(kPartThreads), 0, s, x, d, a, p);
+}
+
 }  // namespace
 
 int launch_distill(const hmy_distill_desc &g, stream_t st) {
@@ -387,6 +538,9 @@ int launch_distill(const hmy_distill_desc &g, stream_t st) {
     return fail(HMY_E_INVALID, "distill: dlogits overlaps logits other than in place");
   const DistillArgs a = {g.teacher_ids, g.teacher_logp, g.row_loss, g.T, g.V, g.K, g.pad, g.ldl, g.ldd, g.scale, g.grad_scale, g.tail == 1};
   const hipStream_t s = (hipStream_t)st;
+  void *ws = has_workspace(g.workspace, g.workspace_bytes) ? g.workspace : nullptr;
+  if (misaligned(ws, 16)) return fail(HMY_E_INVALID, "distill: workspace not aligned to 16 bytes");
+  const int parts = ws && g.T <= kPartRows ? std::min(std::min(kPartLaunch / g.T, kPartsMax), g.V / kPartMinCols) : 1;
   DISPATCH_ROWS(g.logits_prec, g.prec, {
     const L *x = (const L *)g.logits;
     E *d = (E *)g.dlogits;
@@ -394,7 +548,8 @@ int launch_distill(const hmy_distill_desc &g, stream_t st) {
     // first wave's work on the list, which the others wait for, is then a smaller part.  Beyond, what a compute unit's registers
     // hold of rows, two or more at a time as far as they fit.
     constexpr bool wide = sizeof(L) == 4;
-    if (g.V <= 512) launch_rows<L, E, 64, 1, 4>(x, d, a, s);
+    if (parts >= 4) launch_parts(x, d, a, parts, ws, s);
+    else if (g.V <= 512) launch_rows<L, E, 64, 1, 4>(x, d, a, s);
     else if (g.V <= 2048) launch_rows<L, E, 64, 4, 4>(x, d, a, s);
     else if (g.V <= 4096) launch_rows<L, E, 128, 4, 4>(x, d, a, s);
     else if (g.V <= 8192) launch_rows<L, E, 256, 4, 4>(x, d, a, s);
