@@ -501,7 +501,7 @@ void launch_rows(const L *x, E *d, DistillArgs a, hipStream_t s) {
   }
 }
 
-constexpr int kPartRows = 32, kPartLaunch = 512, kPartMinCols = 16384, kPartsMax = 64;
+constexpr int kPartRows = 64, kPartLaunch = 512, kPartMinCols = 16384, kPartsMax = 64;
 static_assert(kPartRows * (sizeof(List) + sizeof(ListSum)) + kPartLaunch * sizeof(float2) <= HMY_ROWS_WORKSPACE_BYTES, "the parts' sums and the lists fit the workspace");
 
 template <typename L, typename E>

@@ -542,14 +542,14 @@ void launch_rows(const L *x, LogprobArgs a, int rows, hipStream_t s) {
   }
 }
 
-constexpr int kPartRows = 32, kPartLaunch = 512, kPartMinCols = 16384, kPartMaxCols = 65536, kPartsMax = 64;
+constexpr int kPartLaunch = 512, kPartMinCols = 16384, kPartMaxCols = 65536, kPartsMax = 64;
 static_assert(kPartLaunch * (sizeof(Sums) + 4 + HMY_MAX_TOP * 8) <= HMY_ROWS_WORKSPACE_BYTES, "the parts' sums and lists fit the workspace");
 
 template <typename L>
 void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hipStream_t s) {
-  const int room = rows <= kPartRows ? kPartLaunch / rows : 1;
+  const int room = rows <= (a.k > kShortList ? 16 : 64) ? kPartLaunch / rows : 1;
   const int parts = std::min(std::min(room, kPartsMax), a.V / kPartMinCols);
-  if (workspace && parts >= 4 && a.V / parts <= kPartMaxCols) {
+  if (workspace && parts >= 6 && a.V / parts <= kPartMaxCols) {
     RowParts p;
     p.cols = (a.V + parts - 1) / parts + 7 & ~7;
     p.per_row = (a.V + p.cols - 1) / p.cols;
