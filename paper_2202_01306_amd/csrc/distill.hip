@@ -265,12 +265,13 @@ __device__ __forceinline__ void wave_sums(float &m, float &sum, float scale) {
   sum = wave_total(sum == 0.f ? 0.f : sum * rebase(m, wm, scale));
   m = wm;
 }
+// the same of a workgroup's first NT threads, for all of its threads
 template <int NT>
 __device__ __forceinline__ void block_sums(float &m, float &sum, float scale, float *scratch) {
   constexpr int kWaves = NT / kWave;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   wave_sums(m, sum, scale);
-  if (lane == 0) {
+  if (lane == 0 && wave < kWaves) {
     scratch[wave] = m;
     scratch[kWaves + wave] = sum;
   }
@@ -289,8 +290,10 @@ __device__ __forceinline__ void put_listed(E *d, const List &l, const RowTerms &
 
 // One workgroup per row.  The row stays in registers between its sums and its gradient, as exponentials in fp32, as loaded in
 // bf16; of a row beyond NT * NG groups of eight columns the last so many do, and those in front are read again.
-template <typename L, typename E, int NT, int NG, bool TAIL, int WPE>
-__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void k_distill(const L *logits, E *dlogits, DistillArgs a) {
+// The list is the first wave's (short rows, of which many are at work at a time), or with LIST_WAVE one wave's more than the NT
+// threads of the columns: the list is a chain of dependent loads and 64-bit arithmetic, and its wave's columns would wait for it.
+template <typename L, typename E, int NT, int NG, bool TAIL, bool LIST_WAVE, int WPE>
+__global__ __launch_bounds__(NT + (LIST_WAVE ? kWave : 0)) __attribute__((amdgpu_waves_per_eu(WPE))) void k_distill(const L *logits, E *dlogits, DistillArgs a) {
   constexpr int kSegment = NT * NG;
   constexpr bool kHold = sizeof(L) == 4;
   __shared__ uint32_t listed[TAIL ? NT * ((NG + 3) / 4) : 1];
@@ -298,6 +301,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
   __shared__ ListSum z;
   __shared__ __attribute__((aligned(16))) List list;
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const bool lists = wave == (LIST_WAVE ? NT / kWave : 0), columns = !LIST_WAVE || !lists;
   const float c = a.scale * kLog2e;
   // segments of the row's groups: a short one first, if any, then whole ones, the last of which stays
   const int groups = a.V / 8, segments = max(1, (groups + kSegment - 1) / kSegment), lead = groups - (segments - 1) * kSegment;
@@ -306,71 +310,82 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(WPE))) void 
   const L *x = logits + int64_t(row) * a.ldl;
   int id[2];
   float tl[2];
-  if (TAIL || wave == 0) list_entries(a, row, lane, id, tl);
-  if (wave == 0) read_list(x, a, lane, id, tl, list, z);
+  if (TAIL || lists) list_entries(a, row, lane, id, tl);
+  if (lists) read_list(x, a, lane, id, tl, list, z);
   Eight<L> v[NG];
-  float xb = behind < a.V ? to_f32(x[behind]) : -INFINITY, m = -INFINITY, sum = 0.f;
-  if (TAIL && wave == 0 && is_listed_behind(id, a.V, behind)) xb = -INFINITY;
-  for (int seg = 0; seg < segments; ++seg) {
-    const int g0 = seg == 0 ? 0 : lead + (seg - 1) * kSegment, g1 = lead + seg * kSegment;
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      const int g = g0 + i * NT + tid;
-      if (g < g1) load_whole(v[i], x + uint32_t(g) * 8);
-      else v[i].all_no_weight();
-    }
-    if constexpr (TAIL) drop_listed<NT>(v, listed, id, g0, g1, wave);
-    add_columns<kHold>(v, seg == 0 ? xb : -INFINITY, m, sum, c);
-  }
-  float m_rest = m, rest = sum;
-  block_sums<NT>(m_rest, rest, a.scale, scratch);
-  if (dlogits) {
-    E *d = dlogits + int64_t(row) * a.ldd;
-    const RowTerms r = row_terms(m_rest, rest, z, a);
-    if (!z.any) {   // a row of padding: zeros whatever its logits are
-      const float none[8] = {};
-      for (int g = tid; g < groups; g += NT) store_whole(d + uint32_t(g) * 8, none);
-      if (behind < a.V) d[behind] = from_f32<E>(0.f);
-      zero_padding(d, a.V, a.pad, tid, NT);
-      if (tid == 0) a.row_loss[row] = 0.f;
-      return;
-    }
-    const float mine = r.c_rest * rebase(m, r.m, a.scale);
-    auto grad = [&](float xj) { return fast_exp2((xj - r.m) * c) * r.c_rest; };
-#pragma unroll
-    for (int i = 0; i < NG; ++i) {
-      const int g = (segments == 1 ? 0 : lead + (segments - 2) * kSegment) + i * NT + tid;
-      if (g < groups) {
-        float o[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = kHold ? v[i].at(k) * mine : grad(v[i].at(k));
-        store_whole(d + uint32_t(g) * 8, o);
-      }
-    }
-    if (behind < a.V) d[behind] = from_f32<E>(grad(xb));
-    for (int seg = segments - 2; seg >= 0; --seg) {
+  float xb = -INFINITY, m = -INFINITY, sum = 0.f;
+  if (columns) {
+    if (behind < a.V) xb = to_f32(x[behind]);
+    if (TAIL && wave == 0 && is_listed_behind(id, a.V, behind)) xb = -INFINITY;
+    for (int seg = 0; seg < segments; ++seg) {
       const int g0 = seg == 0 ? 0 : lead + (seg - 1) * kSegment, g1 = lead + seg * kSegment;
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         const int g = g0 + i * NT + tid;
         if (g < g1) load_whole(v[i], x + uint32_t(g) * 8);
+        else v[i].all_no_weight();
       }
+      if constexpr (TAIL) drop_listed<NT>(v, listed, id, g0, g1, wave);
+      add_columns<kHold>(v, seg == 0 ? xb : -INFINITY, m, sum, c);
+    }
+  }
+  float m_rest = m, rest = sum;
+  block_sums<NT>(m_rest, rest, a.scale, scratch);
+  if (dlogits) {
+    E *d = dlogits + int64_t(row) * a.ldd;
+    if (!z.any) {   // a row of padding: zeros whatever its logits are
+      const float none[8] = {};
+      if (columns) {
+        for (int g = tid; g < groups; g += NT) store_whole(d + uint32_t(g) * 8, none);
+        if (behind < a.V) d[behind] = from_f32<E>(0.f);
+        zero_padding(d, a.V, a.pad, tid, NT);
+      }
+      if (tid == 0) a.row_loss[row] = 0.f;
+      return;
+    }
+    const RowTerms r = row_terms(m_rest, rest, z, a);
+    if (columns) {
+      const float mine = r.c_rest * rebase(m, r.m, a.scale);
+      auto grad = [&](float xj) { return fast_exp2((xj - r.m) * c) * r.c_rest; };
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
-        const int g = g0 + i * NT + tid;
-        if (g < g1) {
+        const int g = (segments == 1 ? 0 : lead + (segments - 2) * kSegment) + i * NT + tid;
+        if (g < groups) {
           float o[8];
 #pragma unroll
-          for (int k = 0; k < 8; ++k) o[k] = grad(v[i].at(k));
+          for (int k = 0; k < 8; ++k) o[k] = kHold ? v[i].at(k) * mine : grad(v[i].at(k));
           store_whole(d + uint32_t(g) * 8, o);
         }
       }
+      if (behind < a.V) d[behind] = from_f32<E>(grad(xb));
+      for (int seg = segments - 2; seg >= 0; --seg) {
+        const int g0 = seg == 0 ? 0 : lead + (seg - 1) * kSegment, g1 = lead + seg * kSegment;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const int g = g0 + i * NT + tid;
+          if (g < g1) load_whole(v[i], x + uint32_t(g) * 8);
+        }
+#pragma unroll
+        for (int i = 0; i < NG; ++i) {
+          const int g = g0 + i * NT + tid;
+          if (g < g1) {
+            float o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = grad(v[i].at(k));
+            store_whole(d + uint32_t(g) * 8, o);
+          }
+        }
+      }
+      zero_padding(d, a.V, a.pad, tid, NT);
     }
-    zero_padding(d, a.V, a.pad, tid, NT);
+    if (LIST_WAVE && lists) {   // while the others store
+      const float loss = row_loss(m_rest, rest, list, z, a, lane);
+      if (lane == 0) a.row_loss[row] = loss;
+    }
     __syncthreads();   // behind the stores of the columns around
-    if (wave == 0) put_listed(d, list, r, a, lane, 0, a.V);
+    if (lists) put_listed(d, list, r, a, lane, 0, a.V);
   }
-  if (wave == 0) {
+  if (lists && !(LIST_WAVE && dlogits)) {
     const float loss = row_loss(m_rest, rest, list, z, a, lane);
     if (lane == 0) a.row_loss[row] = loss;
   }
@@ -487,12 +502,12 @@ __global__ __launch_bounds__(kSumThreads) void k_loss_sum(const float *row_loss,
   }
 }
 
-template <typename L, typename E, int NT, int NG, int WPE>
+template <typename L, typename E, int NT, int NG, bool LIST_WAVE, int WPE>
 void launch_rows(const L *x, E *d, DistillArgs a, hipStream_t s) {
   for (int rows = a.T; rows > 0; rows -= kMaxGrid) {   // a launch has a limited number of workgroups
-    const dim3 grid(rows < kMaxGrid ? rows : kMaxGrid);
-    if (a.tail) hipLaunchKernelGGL((k_distill<L, E, NT, NG, true, WPE>), grid, dim3(NT), 0, s, x, d, a);
-    else hipLaunchKernelGGL((k_distill<L, E, NT, NG, false, WPE>), grid, dim3(NT), 0, s, x, d, a);
+    const dim3 grid(rows < kMaxGrid ? rows : kMaxGrid), block(NT + (LIST_WAVE ? kWave : 0));
+    if (a.tail) hipLaunchKernelGGL((k_distill<L, E, NT, NG, true, LIST_WAVE, WPE>), grid, block, 0, s, x, d, a);
+    else hipLaunchKernelGGL((k_distill<L, E, NT, NG, false, LIST_WAVE, WPE>), grid, block, 0, s, x, d, a);
     x += int64_t(kMaxGrid) * a.ldl;
     if (d) d += int64_t(kMaxGrid) * a.ldd;
     a.ids += int64_t(kMaxGrid) * a.K;
@@ -545,20 +560,24 @@ int launch_distill(const hmy_distill_desc &g, stream_t st) {
     const L *x = (const L *)g.logits;
     E *d = (E *)g.dlogits;
     // As few waves as hold the row in up to four groups of eight columns a thread, while a workgroup has at most 256 threads: the
-    // first wave's work on the list, which the others wait for, is then a smaller part.  Beyond, what a compute unit's registers
-    // hold of rows, two or more at a time as far as they fit.
+    // first wave's work on the list, which the others wait for, is then a smaller part (us, 8192 rows of 1000 columns in bf16 on
+    // 64, 128, 256 threads: 19.5, 25, 36; the floor is 6.5).  Beyond, what a compute unit's registers hold of rows, two at a
+    // time as far as they fit: 448 threads and a list wave (20000 columns 83, on 512 threads without one 90; the floor is 81), in
+    // bf16 1024 threads of 64 registers although a part of the row is read twice then (80000 columns 102, on 110 registers
+    // 110), and only beyond 110000 one row at a time (131072 columns 230 against 246).
     constexpr bool wide = sizeof(L) == 4;
     if (parts >= 4) launch_parts(x, d, a, parts, ws, s);
-    else if (g.V <= 512) launch_rows<L, E, 64, 1, 4>(x, d, a, s);
-    else if (g.V <= 2048) launch_rows<L, E, 64, 4, 4>(x, d, a, s);
-    else if (g.V <= 4096) launch_rows<L, E, 128, 4, 4>(x, d, a, s);
-    else if (g.V <= 8192) launch_rows<L, E, 256, 4, 4>(x, d, a, s);
-    else if (g.V <= 14336) launch_rows<L, E, 256, 7, 4>(x, d, a, s);
-    else if (g.V <= 28672) launch_rows<L, E, 512, 7, 4>(x, d, a, s);
-    else if (wide) launch_rows<L, E, 1024, 7, 4>(x, d, a, s);
-    else if (g.V <= 32768) launch_rows<L, E, 512, wide ? 7 : 8, 4>(x, d, a, s);
-    else if (g.V <= 110000) launch_rows<L, E, 1024, 7, wide ? 4 : 8>(x, d, a, s);
-    else launch_rows<L, E, 1024, wide ? 7 : 16, 4>(x, d, a, s);
+    else if (g.V <= 512) launch_rows<L, E, 64, 1, false, 4>(x, d, a, s);
+    else if (g.V <= 2048) launch_rows<L, E, 64, 4, false, 4>(x, d, a, s);
+    else if (g.V <= 4096) launch_rows<L, E, 128, 4, false, 4>(x, d, a, s);
+    else if (g.V <= 8192) launch_rows<L, E, 256, 4, false, 4>(x, d, a, s);
+    else if (g.V <= 14336) launch_rows<L, E, 256, 7, false, 4>(x, d, a, s);
+    else if (g.V <= (wide ? 32768 : 25088)) launch_rows<L, E, 448, 7, true, 4>(x, d, a, s);
+    else if (wide) launch_rows<L, E, 1024, 7, false, 4>(x, d, a, s);
+    else if (g.V <= 35840) launch_rows<L, E, 448, wide ? 7 : 10, true, 4>(x, d, a, s);
+    else if (g.V <= 50176) launch_rows<L, E, 448, wide ? 7 : 14, true, 4>(x, d, a, s);
+    else if (g.V <= 110000) launch_rows<L, E, 1024, 7, false, wide ? 4 : 8>(x, d, a, s);
+    else launch_rows<L, E, 1024, wide ? 7 : 16, false, 4>(x, d, a, s);
   });
   if (g.loss_acc)
     hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(kSumThreads), 0, s, g.row_loss, g.loss_acc, g.T, double(g.grad_scale));
