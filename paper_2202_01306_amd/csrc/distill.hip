@@ -540,8 +540,8 @@ int launch_distill(const hmy_distill_desc &g, stream_t st) {
   int rc = check_rows("distill", g.logits_prec, g.logits, g.T, g.V, 0, g.ldl);
   if (!rc && g.dlogits) rc = check_rows("distill", g.prec, g.dlogits, g.T, g.V, g.pad, g.ldd);
   if (rc) return rc;
-  if (!positive(g.scale)) return fail(HMY_E_INVALID, "distill: the scale must be positive and finite");
-  if (!std::isfinite(g.grad_scale)) return fail(HMY_E_INVALID, "distill: the gradient's scale must be finite");
+  if (!usable_scale(g.scale)) return fail(HMY_E_INVALID, "distill: the scale must be positive and finite");
+  if (!std::isfinite(g.scale * g.grad_scale)) return fail(HMY_E_INVALID, "distill: the gradient's scale, and its product with the logits', must be finite");
   if (g.K < 1 || g.K > HMY_MAX_TOP) return fail(HMY_E_INVALID, "distill: K = %d is not in 1..%d", g.K, HMY_MAX_TOP);
   if (g.tail != 0 && g.tail != 1) return fail(HMY_E_INVALID, "distill: tail is 0 or 1");
   const void *words[] = {g.teacher_ids, g.teacher_logp, g.row_loss};

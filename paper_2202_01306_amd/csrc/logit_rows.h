@@ -163,7 +163,7 @@ constexpr int kMaxColumns = 1 << 24;
 
 inline bool misaligned(const void *p, int to) { return (reinterpret_cast<uintptr_t>(p) & uintptr_t(to - 1)) != 0; }
 inline int bytes_of(int prec) { return prec == HMY_PREC_BF16 ? 2 : 4; }
-inline bool positive(float s) { return s > 0.f && std::isfinite(s); }
+inline bool usable_scale(float s) { return s > 0.f && std::isfinite(s * kLog2e); }
 inline bool has_workspace(const void *p, uint64_t bytes) { return p && bytes >= uint64_t(HMY_ROWS_WORKSPACE_BYTES); }
 
 inline int check_launch(const char *what) {

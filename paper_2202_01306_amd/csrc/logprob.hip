@@ -124,54 +124,71 @@ __device__ __forceinline__ int thin_out(C &c, int n, int k, int most) {
   return __builtin_amdgcn_readfirstlane(c.n);
 }
 
-// by the workgroup, where there are more candidates than there is room for (the largest logits are those of few threads, or very
-// many are equal): the k first of the `cols` >= k columns x[0 .. cols-1], numbered from `first` on, which are read again for every bit.  The k-th largest
-// logit bit by bit, then of those that equal it the lowest columns.
+// by the workgroup, where more than there is room for reach a floor that at least k of the columns x[0 .. cols-1] (numbered from
+// `first` on) reach: very many are equal, as in the rows of an untrained model or under masks of a finite value, or the largest
+// logits are those of few threads.  All columns are read again: those above the floor, and while there is no room for them
+// either, for what the k-th of an arbitrary part of them gives as a floor; then the lowest columns that equal it.  Says how many
+// candidates there are.  Wants a barrier in front.
 template <typename C, typename L>
-__device__ __forceinline__ int keep_first(C &c, const L *x, int first, int cols, int k) {
-  constexpr int NT = C::NT;
-  const int tid = threadIdx.x;
-  int turn = 0;
-  uint32_t t = 0;
-  if (tid == 0) c.n = c.count[0] = c.count[1] = 0;
-  __syncthreads();
+__device__ __forceinline__ int list_ties(C &c, const L *x, int first, int cols, int k, float floor) {
+  constexpr int NT = C::NT, kRoom = C::keys - 8;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  int n;
 #pragma unroll 1
-  for (int bit = 31; bit >= 0; --bit) {
-    const uint32_t to = t | 1u << bit;
-    int above = 0;
+  while (true) {
+    if (tid == 0) c.n = 0;
+    __syncthreads();
 #pragma unroll 1
-    for (int j = tid; j < cols; j += NT) {
-      const float v = to_f32(x[j]);
-      above += v == v && ordered(v) >= to;
+    for (int j0 = 0; j0 < cols; j0 += NT) {
+      const int j = j0 + tid;
+      const float v = j < cols ? to_f32(x[j]) : -INFINITY;
+      const uint64_t above = __ballot(v > floor);
+      if (above) {
+        int at = 0;
+        if (lane == 0) at = int(atomicAdd(&c.n, uint32_t(__popcll(above))));
+        at = __builtin_amdgcn_readfirstlane(at) + __popcll(above & ((uint64_t(1) << lane) - 1));
+        if (v > floor && at < kRoom) c.key[at] = rank_key(v, first + j);
+      }
     }
-    if (hits(c, above, turn) >= k) t = to;
-  }
-  int above = 0;
-#pragma unroll 1
-  for (int j = tid; j < cols; j += NT) {
-    const float v = to_f32(x[j]);
-    above += v == v && ordered(v) > t;
-  }
-  const int want = k - hits(c, above, turn);   // of those that equal it
-  int last = 0;
-#pragma unroll 1
-  for (int bit = 24; bit >= 0; --bit) {
-    const int to = last | 1 << bit;
-    int equal = 0;
-#pragma unroll 1
-    for (int j = tid; j < cols && j < to; j += NT) {
-      const float v = to_f32(x[j]);
-      equal += v == v && ordered(v) == t;
+    __syncthreads();
+    n = __builtin_amdgcn_readfirstlane(c.n);
+    if (n <= kRoom) break;
+    if (tid < kWave) {
+      uint32_t lo = ~0u, hi = 0;
+      for (int i = lane; i < kRoom; i += kWave) {
+        const uint32_t v = uint32_t(c.key[i] >> 32);
+        lo = min(lo, v);
+        hi = max(hi, v);
+      }
+      const uint32_t t = threshold(lo, hi, k, [&](uint32_t to) {
+        int r = 0;
+        for (int i = 0; i < kRoom; i += kWave) r += __popcll(__ballot(i + lane < kRoom && uint32_t(c.key[min(i + lane, kRoom - 1)] >> 32) >= to));
+        return r;
+      });
+      if (lane == 0) c.floor = t;
     }
-    if (hits(c, equal, turn) <= want) last = to;
+    __syncthreads();
+    floor = unordered(__builtin_amdgcn_readfirstlane(c.floor));   // above the one before
   }
+  const int wanted = k - n;   // of those that equal the floor, the lowest columns first
+  int taken = 0;
 #pragma unroll 1
-  for (int j = tid; j < cols; j += NT) {
-    const float v = to_f32(x[j]);
-    if (v == v && (ordered(v) > t || (ordered(v) == t && j < last))) c.key[atomicAdd(&c.n, 1u)] = rank_key(v, first + j);
+  for (int j0 = 0; j0 < cols && taken < wanted; j0 += NT) {
+    const int j = j0 + tid;
+    const bool equal = j < cols && to_f32(x[j]) == floor;
+    const uint64_t equals = __ballot(equal);
+    if (lane == 0) c.rank[wave] = uint32_t(__popcll(equals));
+    __syncthreads();
+    int before = taken;
+    for (int w = 0; w < NT / kWave; ++w) {
+      if (w < wave) before += int(c.rank[w]);
+      taken += int(c.rank[w]);
+    }
+    before += __popcll(equals & ((uint64_t(1) << lane) - 1));
+    if (equal && before < wanted) c.key[n + before] = rank_key(floor, first + j);
+    __syncthreads();
   }
-  __syncthreads();
-  return __builtin_amdgcn_readfirstlane(c.n);
+  return n + max(0, min(taken, wanted));
 }
 
 // by the workgroup: the k first of n candidates, `put(rank, key)` for each.  Wants a barrier in front.
@@ -326,7 +343,7 @@ __device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups
   __syncthreads();
   int n = __builtin_amdgcn_readfirstlane(c.n);
   __syncthreads();   // all have read c.n, which is written again
-  if (n > C::keys - 8 || n_hits > C::hits) n = keep_first(c, x, first, cols, k);   // (eight keys more are written behind n)
+  if (n > C::keys - 8 || n_hits > C::hits) n = list_ties(c, x, first, cols, k, floor);   // (eight keys more are written behind n)
   rank_candidates(c, n, k, put);
 }
 
@@ -347,9 +364,6 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, 
   const int first = PARTS ? piece * p.cols : 0, cols = PARTS ? min(p.cols, a.V - first) : a.V;
   const L *x = logits + int64_t(row) * a.ldl + first;
   const int groups = cols / 8, segments = (groups + kSegment - 1) / kSegment, per_slot = (segments + Cands::slots - 1) / Cands::slots;
-  const int tgt = !PARTS && a.targets ? a.targets[row] : -1;
-  const bool has_target = tgt >= 0 && tgt < a.V;
-  const float target_logit = has_target ? to_f32(x[tgt]) : 0.f;
   // the column behind the groups, if there is one for this thread
   const int behind = groups * 8 + tid;
   const float xb = behind < cols ? to_f32(x[behind]) : -INFINITY;
@@ -363,6 +377,10 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, 
   };
   Eight<L> v[NG], next[NG];
   if (segments > 0) load(v, 0);
+  // behind the columns' loads: the first of these two is waited for before the second is issued
+  const int tgt = !PARTS && a.targets ? a.targets[row] : -1;
+  const bool has_target = tgt >= 0 && tgt < a.V;
+  const float target_logit = has_target ? to_f32(x[tgt]) : 0.f;
   Sums z = {fmaxf(xb, -INFINITY), 0.f, 0.f};
   if (behind < cols) z.S = fast_exp2((xb - (xb == -INFINITY ? 0.f : xb)) * c);   // 1, 0 for -inf, NaN
   float in_slot = -INFINITY;
@@ -563,6 +581,8 @@ void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hi
     launch_rows<L, 64, 4, true>(x, a, rows, s);
   } else if (a.V <= 8192) {
     launch_rows<L, 256, 4, true>(x, a, rows, s);
+  } else if (a.V <= 32768) {
+    launch_rows<L, 256, 4, false>(x, a, rows, s);
   } else {
     launch_rows<L, 512, sizeof(L) == 4 ? 2 : 4, false>(x, a, rows, s);
   }
@@ -573,7 +593,7 @@ void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hi
 int launch_logprob(const hmy_logprob_desc &g, stream_t st) {
   int rc = check_rows("logprob", g.logits_prec, g.logits, g.T, g.V, 0, g.ldl);
   if (rc) return rc;
-  if (!positive(g.scale)) return fail(HMY_E_INVALID, "logprob: the scale must be positive and finite");
+  if (!usable_scale(g.scale)) return fail(HMY_E_INVALID, "logprob: the scale must be positive and finite");
   if (g.k < 0 || g.k > HMY_MAX_TOP) return fail(HMY_E_INVALID, "logprob: k = %d is not in 0..%d", g.k, HMY_MAX_TOP);
   if (g.k > 0 && (!g.top_ids || !g.top_logp)) return fail(HMY_E_INVALID, "logprob: k > 0 needs top_ids and top_logp");
   if (!g.targets != !g.logp) return fail(HMY_E_INVALID, "logprob: targets and logp come together");
@@ -594,7 +614,7 @@ int launch_logprob_bwd(const hmy_logprob_grad_desc &g, stream_t st) {
   int rc = check_rows("logprob_bwd", g.logits_prec, g.logits, g.T, g.V, 0, g.ldl);
   if (!rc) rc = check_rows("logprob_bwd", g.prec, g.dlogits, g.T, g.V, g.pad, g.ldd);
   if (rc) return rc;
-  if (!positive(g.scale)) return fail(HMY_E_INVALID, "logprob_bwd: the scale must be positive and finite");
+  if (!usable_scale(g.scale)) return fail(HMY_E_INVALID, "logprob_bwd: the scale must be positive and finite");
   if (!g.d_logp && !g.d_entropy) return fail(HMY_E_INVALID, "logprob_bwd: d_logp, d_entropy or both wanted");
   if (g.d_logp && !g.targets) return fail(HMY_E_INVALID, "logprob_bwd: d_logp needs targets");
   if (g.d_entropy && !g.entropy) return fail(HMY_E_INVALID, "logprob_bwd: d_entropy needs the rows' entropy");
