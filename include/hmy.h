@@ -567,8 +567,9 @@ int hmy_k_adam(int32_t prec, const float *grad, float *master, float *m, float *
  *   - dlogits[T,V] with row stride ldd: columns V .. V+pad-1 of each row are written as zeros (the padding that
  *     hmy_k_xent zeroes is pad = ldl - V), columns beyond are left as they are.  dlogits may be the logits themselves (same
  *     address, type and stride); otherwise the two must not overlap (HMY_E_INVALID where their rows do).
- *   - workspace: HMY_ROWS_WORKSPACE_BYTES of device memory, aligned to 16 bytes, lets a call of few rows use the whole device;
- *     without it (NULL, or smaller) each row is one workgroup's.  Nothing in it has to be cleared.  Calls that may overlap
+ *   - scale (and its product with log2 e, and in hmy_k_distill that with grad_scale) must be finite.
+ *   - workspace: HMY_ROWS_WORKSPACE_BYTES of device memory, aligned to 16 bytes, lets a call of few, long rows use the whole
+ *     device; without it (NULL, or smaller) each row is one workgroup's.  Nothing in it has to be cleared.  Calls that may overlap
  *     need one each.  Nothing is allocated, and every call can be captured into a graph. */
 #define HMY_MAX_TOP 128
 #define HMY_ROWS_WORKSPACE_BYTES (1 << 20)
@@ -617,8 +618,8 @@ int hmy_k_logprob_bwd(const hmy_logprob_grad_desc *g, void *stream);
  *     dL/dx_j = w s (Q p_j - q_j) for listed tokens, w s p_j (Q - q_r / p_r) for the others.  Where the student gives the class
  *     no weight at all (p_r = 0) it is dropped: q_r = 0.
  * (A token listed twice counts q_k (log q_k - l_k) for each entry.)  w = grad_scale, which also scales what loss_acc (may be
- * NULL) gets: loss_acc[0] += w sum_t row_loss[t], added up in one order by a launch of its own.  row_loss[T] itself is not
- * scaled.  A row with no entry at all (padding) has loss 0 and gradient 0.  dlogits NULL: the loss alone. */
+ * NULL) gets: loss_acc[0] += w sum_t row_loss[t], added up in one order by a launch of its own, to which one atomic addition
+ * belongs, so that calls that overlap may share it (as in hmy_k_xent).  row_loss[T] itself is not scaled.  A row with no entry at all (padding) has loss 0 and gradient 0.  dlogits NULL: the loss alone. */
 typedef struct hmy_distill_desc {
   int32_t prec, logits_prec, T, V, K, tail;  /* 1 <= K <= HMY_MAX_TOP         */
   const void *logits; int64_t ldl;

@@ -506,7 +506,7 @@ def hmy_k_logprob_bwd(prec, logits_prec, logits, row_max, log_sum, dlogits, T, V
 
 def hmy_k_distill(prec, logits_prec, logits, teacher_ids, teacher_logp, row_loss, dlogits, T, V, K, ldl, ldd, tail=False,
                   scale=1.0, grad_scale=1.0, pad=0, loss_acc=None, stream=None, workspace=None):
-    """prec: type of dlogits (None: the loss alone); workspace as for hmy_k_logprob."""
+    """prec: type of dlogits; dlogits None: the loss alone; workspace as for hmy_k_logprob."""
     g = hmy_distill_desc(prec, logits_prec, T, V, K, int(tail), _at(logits), ldl, _at(teacher_ids), _at(teacher_logp),
                          _at(row_loss), _at(loss_acc), _at(dlogits), ldd, _at(workspace),
                          0 if workspace is None else workspace.numel() * workspace.element_size(), scale, grad_scale, pad, 0)

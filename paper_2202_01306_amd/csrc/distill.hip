@@ -292,6 +292,10 @@ __device__ __forceinline__ void put_listed(E *d, const List &l, const RowTerms &
 // bf16; of a row beyond NT * NG groups of eight columns the last so many do, and those in front are read again.
 // The list is the first wave's (short rows, of which many are at work at a time), or with LIST_WAVE one wave's more than the NT
 // threads of the columns: the list is a chain of dependent loads and 64-bit arithmetic, and its wave's columns would wait for it.
+// Bound by HBM, one reading and one writing, where there are rows for all compute units: 512 x 50257 fp32 into bf16 37 us (4.2
+// TB/s: all of its rows are at work at once, two per compute unit, so that all read and then all write), 2048 x 50257 123 (5.0),
+// 2048 x 131072 bf16 243 (4.4; one row per compute unit).  A few short rows: 6 us for 5003 columns, launch and one chain of
+// latencies (ids, their logits, 64-bit sums, barrier, stores, barrier, the listed columns).
 template <typename L, typename E, int NT, int NG, bool TAIL, bool LIST_WAVE, int WPE>
 __global__ __launch_bounds__(NT + (LIST_WAVE ? kWave : 0)) __attribute__((amdgpu_waves_per_eu(WPE))) void k_distill(const L *logits, E *dlogits, DistillArgs a) {
   constexpr int kSegment = NT * NG;
@@ -391,8 +395,8 @@ __global__ __launch_bounds__(NT + (LIST_WAVE ? kWave : 0)) __attribute__((amdgpu
   }
 }
 
-// Few, long rows: workgroups each take `groups` of a row's groups of eight columns, once for the row's sums and once for the
-// gradient.
+// Few, long rows: workgroups each take `groups` of a row's groups of eight columns, once for the row's sums and once, in a second
+// launch, for the gradient.  The list is the first part's.
 struct RowParts {
   ListSum *z;        // [rows]
   List *list;        // [rows]
@@ -487,7 +491,7 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_finish(const L *logits
   }
 }
 
-// loss[0] += scale * the sum of the rows' losses, in one order whatever the launch
+// loss[0] += scale * the sum of the rows' losses, in one order whatever the launch; calls on other streams may add to it meanwhile
 constexpr int kSumThreads = 256;
 __global__ __launch_bounds__(kSumThreads) void k_loss_sum(const float *row_loss, double *loss, int T, double scale) {
   __shared__ double scratch[kSumThreads / kWave];
@@ -498,7 +502,7 @@ __global__ __launch_bounds__(kSumThreads) void k_loss_sum(const float *row_loss,
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < kSumThreads / kWave; ++w) v += scratch[w];
-    loss[0] += v * scale;
+    atomicAdd(loss, v * scale);
   }
 }
 
@@ -565,6 +569,8 @@ int launch_distill(const hmy_distill_desc &g, stream_t st) {
     // time as far as they fit: 448 threads and a list wave (20000 columns 83, on 512 threads without one 90; the floor is 81), in
     // bf16 1024 threads of 64 registers although a part of the row is read twice then (80000 columns 102, on 110 registers
     // 110), and only beyond 110000 one row at a time (131072 columns 230 against 246).
+    // Few rows by parts, two launches, from four parts on, which read twice but on the whole device.  us by parts / by rows, fp32:
+    // one row of 131072 columns 10.2 / 23.5, 64 rows of 80000 17.4 / 19.6, but 128 rows 25.6 / 21.6.
     constexpr bool wide = sizeof(L) == 4;
     if (parts >= 4) launch_parts(x, d, a, parts, ws, s);
     else if (g.V <= 512) launch_rows<L, E, 64, 1, false, 4>(x, d, a, s);

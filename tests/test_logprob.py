@@ -189,6 +189,19 @@ def test_logprob_of_rows_where_it_can_go_wrong(prec, V, k):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [2049, 3001, 4096, 4097])
+@pytest.mark.parametrize("k", [0, 24, 64, 65])
+def test_logprob_of_rows_on_workgroups_of_two_waves(prec, V, k):
+    rng = np.random.default_rng(V + k)
+    x = np.concatenate([special_rows(V), rows(rng, 300, V, "fp32")])
+    if prec == "bf16":
+        x = synth.round_bf16(x)
+    targets = rng.integers(-1, V, len(x))
+    check_forward(Forward(x, targets, prec, k, V + 1), x, targets, k, 1.0)
+
+
+@pytest.mark.gpu
 def test_logprob_any_subset_of_outputs():
     rng = np.random.default_rng(3)
     for T, V, ws in ((4, 5003, None), (4, 50257, workspace()), (300, 5003, workspace())):
@@ -552,6 +565,26 @@ def test_two_streams_with_a_workspace_each():
     for f, w in zip(alone, want):
         for a, b in zip(f.outputs(), w):
             assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+def test_two_streams_that_add_to_one_loss():
+    rng = np.random.default_rng(6)
+    T, V, K, times = 40, 300, 8, 50
+    x = on_device(rows(rng, T, V, "fp32"), V, "fp32")
+    ids, lp, loss = i32(rng.permuted(np.tile(np.arange(V), (T, 1)), axis=1)[:, :K]), f32(T, K), f32(T)
+    lp.fill_(-3.0)
+    alone = torch.zeros(1, device="cuda", dtype=torch.float64)
+    B.hmy_k_distill(0, 0, x, ids, lp, loss, None, T, V, K, V, V, tail=True, loss_acc=alone)
+    both, losses = torch.zeros(1, device="cuda", dtype=torch.float64), [f32(T), f32(T)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(times):
+        for s, l in zip(streams, losses):
+            B.hmy_k_distill(0, 0, x, ids, lp, l, None, T, V, K, V, V, tail=True, loss_acc=both, stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    # 2 * times additions of one positive number, each off by 2^-53 of a sum
+    np.testing.assert_allclose(host(both)[0], 2 * times * host(alone)[0], rtol=2 * times * 2.0 ** -53)
 
 
 @pytest.mark.gpu
