@@ -35,12 +35,13 @@ template <int NT_, int KEYS, int RANKED, int SLOTS, int HITS> struct Candidates 
   uint32_t hit[HITS];              // slot * NT + thread of those that reach the floor
   uint32_t n, n_hits, floor, count[2];
 };
-// For rows (and parts of rows) of one slot, which are many at a time, and for longer ones.  On 64 threads for short lists only:
-// there are but 64 maxima to take the floor from.
+// For rows (and parts of rows) of one slot, which are many at a time, and for longer ones.  On 64 threads for lists of up to
+// kList64 entries only, on 128 of up to kList128: there are but as many maxima to take the floor from as threads, and the floor
+// has to be far above the lowest of them for few columns to pass.
 template <int NT, bool ONE_SLOT> struct CandidatesOf { typedef Candidates<NT, 2048, 512, 8, 1024> type; };
 template <int NT> struct CandidatesOf<NT, true> { typedef Candidates<NT, 1024, 512, 1, NT> type; };
 template <> struct CandidatesOf<64, true> { typedef Candidates<64, 512, 256, 1, 64> type; };
-constexpr int kShortList = 24;
+constexpr int kList64 = 24, kList128 = 64;
 
 // by one wave: some t with at least k of its values at or above it, and not many more if it can be had: the bisection ends at
 // k + k / 8 + 2.  kLowestOrdered if fewer than k are at or above that.  count(t): how many are; each lane's smallest (of those
@@ -277,8 +278,10 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int row, const Sum
 // largest per slot of `per_slot` segments; xb: the logit of column `behind`, -inf where the thread has none.
 // A floor that at least k logits reach: the k-th largest, or a little less, of the maxima of 256 groups of threads.  What reaches
 // it is in the slots of few threads (k of 256 groups at least; as many as the row's largest logits fall into), and those columns
-// are read again: a second reading of a small part of the row, where looking for candidates in the first one costs every segment a
-// comparison and a barrier (2048 x 131072 bf16, k = 128: 192 us; 512 x 50257 fp32, k = 64: 39 us).
+// are read again: a second reading of a small part of the row (counted: 7 % of 512 x 50257 fp32 at k = 64, 30 % of 2048 x 131072
+// bf16 at k = 128, whose 128 entries are in 128 of 4096 slots), where looking for candidates in the first one costs every segment a
+// comparison and a barrier.  us, with the floor's columns read again / looked for in the one reading: 2048 x 131072 bf16, k = 128,
+// 122 / 192; 512 x 50257 fp32, k = 64, 24.3 / 39; without a list 102 and 18.5.
 template <int NG, typename C, typename L, typename F>
 __device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups, int cols, int per_slot, int k, float mine, float xb, int behind, F put) {
   constexpr int NT = C::NT, kSegment = NT * NG;
@@ -349,7 +352,10 @@ __device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups
 
 // One workgroup per row (PARTS: per part of a row, of which the workspace gets the sums and the list), NT * NG groups of eight
 // columns at a time, the next ones' loads on their way meanwhile.  One reading: each thread keeps a running maximum and sums
-// relative to it, and its largest logit per slot for the list.
+// relative to it, and its largest logit per slot for the list.  Bound by HBM where there are rows for all compute units: 512 x
+// 50257 fp32 18.5 us (5.5 TB/s), 2048 x 131072 bf16 102 (5.3); a large copy runs at 5.06, a reading sum at 3.97.  Few or short
+// rows are a chain of latencies: launch, ids, one round of loads, one barrier, and with a list four more (6 us for a row of 260
+// columns and 10 for one of 50257, with a list each).
 template <typename L, int NT, int NG, bool TOP, bool ONE_SLOT, bool PARTS>
 __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, RowParts p) {
   constexpr int kWaves = NT / kWave, kSegment = NT * NG;
@@ -493,9 +499,9 @@ struct LogprobGradArgs {
 
 // g_j = s (a (1[j = target] - p_j) - h p_j (log p_j + H)) with a = dL/dlogp, h = dL/dH.  Every column on its own: a stream over
 // the logits and the gradient, bound by HBM.  A workgroup takes NT * U * 8 columns of one row, all of a thread's loads in flight
-// before its first store.  us (TB/s), rows x columns, U = 1 / 2 / 4: fp32 into bf16, 512 x 50257 31.2 / 30.7 (5.0) / 32.6; bf16,
-// 1111 x 131071 134 / 112 (5.2) / 114, x 131072 119 / 105 (5.5) / 106: rows that start off any alignment cost 6 %.  A large copy
-// runs at 5.06.
+// before its first store.  us (TB/s), rows x columns, U = 2: fp32 into bf16, 512 x 50257 30.0 (5.1); bf16, 1111 x 131071 99.5
+// (5.9), x 131072 102.6 (5.7): rows that start off any alignment cost nothing.  A large copy runs at 5.06.  U = 1 took 2 % and 19 %
+// more, U = 4 6 % and 2 %.
 template <typename L, typename E, int NT, int U>
 __global__ __launch_bounds__(NT) void k_logprob_bwd(const L *logits, E *dlogits, LogprobGradArgs g, int tiles) {
   const int64_t n = int64_t(g.T) * tiles;
@@ -565,8 +571,16 @@ static_assert(kPartLaunch * (sizeof(Sums) + 4 + HMY_MAX_TOP * 8) <= HMY_ROWS_WOR
 
 template <typename L>
 void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hipStream_t s) {
-  const int room = rows <= (a.k > kShortList ? 16 : 64) ? kPartLaunch / rows : 1;
+  // Parts: two launches, the second of which waits for the first and ranks the parts' lists, so a row has to be long enough for
+  // six parts, rows few, fewer with long lists, and parts short, for their list is ranked on one slot.  us by parts / by rows, fp32:
+  // one row of 131072, k = 10, 11.6 / 16.3; of 80000 (four parts) 12.5 / 12.4; 32 rows of 131072, k = 128, 21.8 / 20.5.
+  const int room = rows <= (a.k > kList64 ? 16 : 64) ? kPartLaunch / rows : 1;
   const int parts = std::min(std::min(room, kPartsMax), a.V / kPartMinCols);
+  // Short rows are bound by what a workgroup does once, not by the columns: fewer threads, more workgroups at a time.  us on 64 /
+  // 128 / 256 threads, bf16, 8192 rows: 2000 columns, k = 20, 21.7 / - / 40.4, k = 48, 42.7 / 37.5 / 44.7, 4000 columns, k = 0, 17.3 /
+  // 16.8 / 25.2, k = 20, 31.2 / 29.4 / 40.3, k = 64, - / 46.1 / 51.3, k = 128, - / 122 / 79, 8000 columns, k = 20, 51.5 / 44.5 / 41.9.
+  // One slot while a thread has but one: 8000 columns, k = 20, 42.6, with eight (twice the LDS) 51.8.  256 against 512 threads:
+  // 4096 rows of 20000 columns, k = 20, 51.1 / 64.0, of 12000 36.9 / 47.2; 1024 rows of 131072, k = 128, 75.8 / 70.2 (fp32 117 / 104).
   if (workspace && parts >= 6 && a.V / parts <= kPartMaxCols) {
     RowParts p;
     p.cols = (a.V + parts - 1) / parts + 7 & ~7;
@@ -577,8 +591,10 @@ void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hi
     if (a.k) hipLaunchKernelGGL((k_logprob<L, 512, sizeof(L) == 4 ? 2 : 4, true, true, true>), grid, dim3(512), 0, s, x, a, p);
     else hipLaunchKernelGGL((k_logprob<L, 512, sizeof(L) == 4 ? 2 : 4, false, true, true>), grid, dim3(512), 0, s, x, a, p);
     hipLaunchKernelGGL(k_logprob_join<L>, dim3(rows), dim3(kJoinThreads), 0, s, x, a, p);
-  } else if (a.V <= 2048 && a.k <= kShortList) {
+  } else if (a.V <= 2048 && a.k <= kList64) {
     launch_rows<L, 64, 4, true>(x, a, rows, s);
+  } else if (a.V <= 4096 && a.k <= kList128) {
+    launch_rows<L, 128, 4, true>(x, a, rows, s);
   } else if (a.V <= 8192) {
     launch_rows<L, 256, 4, true>(x, a, rows, s);
   } else if (a.V <= 32768) {
@@ -625,7 +641,8 @@ int launch_logprob_bwd(const hmy_logprob_grad_desc &g, stream_t st) {
   if (rows_clash(g.logits, int64_t(g.V) * el, g.ldl * el, g.dlogits, (int64_t(g.V) + g.pad) * ee, g.ldd * ee, g.T, g.logits_prec == g.prec))
     return fail(HMY_E_INVALID, "logprob_bwd: dlogits overlaps logits other than in place");
   const LogprobGradArgs a = {g.row_max, g.log_sum, g.targets, g.d_logp, g.entropy, g.d_entropy, g.T, g.V, g.pad, g.ldl, g.ldd, g.scale};
-  // one group of eight columns per thread while the row gives a workgroup of 64, 128 or 256 threads no more, two beyond
+  // one group of eight columns per thread while the row gives a workgroup of 64, 128 or 256 threads no more, two beyond: us, 8192
+  // rows of 300 columns 5.3 on 64 threads, 9.0 on 256; of 1000 in bf16 8.5 on 128, 10.0 on 256
   const int nt = g.V <= 512 ? 64 : g.V <= 1024 ? 128 : 256, per_wg = 8 * nt * (g.V <= 2048 ? 1 : 2);
   const int tiles = (g.V + per_wg - 1) / per_wg;
   const int64_t n = int64_t(g.T) * tiles;
