@@ -248,6 +248,32 @@ __device__ __forceinline__ Sums wave_sums(const Sums &z, float scale) {
   r.A = wave_total(r.A);
   return r;
 }
+// A thread's sums while it reads.  Exponents in log2 units, u = c x - R with R near c m, take one instruction, and one rounding;
+// what R is beside c m, d = c m - R, is taken out at the end.  Where c m itself is beyond kLargest, d is no small number: a thread's
+// tokens that are that far down have no weight beside a row's maximum that is not, and for a row whose maximum is, the sums are
+// taken once more, from c (x - m).  bf16 is bound by what it computes, too: us, with c (x - m) throughout / as it is, 1027 x 30522,
+// k = 20, 22.3 / 21.7; 2048 x 131072, k = 128, 123.8 / 121.4.
+constexpr float kLargest = 1 << 20;
+struct Running {
+  float m, R, S, A;
+  __device__ __forceinline__ static float reference(float mc) { return fminf(fmaxf(mc, -kLargest), kLargest); }
+  __device__ __forceinline__ void raise(float to, float c) {   // to > m
+    const float next = reference(to * c), by = R - next, f = fast_exp2(by);
+    A = f * fmaf(by, S, A);
+    S *= f;
+    m = to;
+    R = next;
+  }
+  __device__ __forceinline__ void add(float u) {
+    const float e = fast_exp2(u);
+    S += e;
+    A = fmaf(e, fmaxf(u, kNoWeight), A);
+  }
+  __device__ __forceinline__ Sums sums(float c) const {
+    const float d = fmaf(m, c, -R), down = d > -126.f ? d : 0.f, f = d > -126.f ? fast_exp2(-d) : 0.f;
+    return {m, f * S, fmaf(-down, f * S, f * A)};
+  }
+};
 // Few, long rows: per_row <= 64 workgroups each take `cols` (a multiple of eight) of a row's columns.
 struct RowParts {
   Sums *sums;          // [rows * per_row]
@@ -387,8 +413,8 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, 
   const int tgt = !PARTS && a.targets ? a.targets[row] : -1;
   const bool has_target = tgt >= 0 && tgt < a.V;
   const float target_logit = has_target ? to_f32(x[tgt]) : 0.f;
-  Sums z = {fmaxf(xb, -INFINITY), 0.f, 0.f};
-  if (behind < cols) z.S = fast_exp2((xb - (xb == -INFINITY ? 0.f : xb)) * c);   // 1, 0 for -inf, NaN
+  Running z = {fmaxf(xb, -INFINITY), Running::reference(xb * c), 0.f, 0.f};
+  z.add(fmaf(xb, c, -z.R));   // nothing for -inf, NaN for what is no number
   float in_slot = -INFINITY;
   for (int seg = 0, of_slot = 0; seg < segments; ++seg) {
     if (seg + 1 < segments) load(next, seg + 1);
@@ -407,30 +433,35 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, 
         of_slot = 0;
       }
     }
-    if (top > z.m) {
-      const float d = fmaxf((z.m - top) * c, kNoWeight), f = fast_exp2(d);
-      z.A = f * fmaf(d, z.S, z.A);
-      z.S *= f;
-      z.m = top;
-    }
-    const float ref = z.m == -INFINITY ? 0.f : z.m;
+    if (top > z.m) z.raise(top, c);
 #pragma unroll
-    for (int i = 0; i < NG; ++i) {
+    for (int i = 0; i < NG; ++i)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float u = (v[i].at(k) - ref) * c, e = fast_exp2(u);
-        z.S += e;
-        z.A = fmaf(e, fmaxf(u, kNoWeight), z.A);
-      }
-    }
+      for (int k = 0; k < 8; ++k) z.add(fmaf(v[i].at(k), c, -z.R));
 #pragma unroll
     for (int i = 0; i < NG; ++i) v[i] = next[i];
   }
-  const Sums ws = wave_sums(z, a.scale);
+  const Sums ws = wave_sums(z.sums(c), a.scale);
   if (lane == 0) part[wave] = ws;
   __syncthreads();
   Sums all = lane < kWaves ? part[lane] : no_sums();
   all = wave_sums(all, a.scale);
+  if (all.m != -INFINITY && !(fabsf(all.m * c) <= kLargest)) {
+    Running r = {all.m, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int g = tid; g < groups; g += NT) {
+      Eight<L> w;
+      load_whole(w, x + uint32_t(g) * 8);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r.add((w.at(k) - all.m) * c);
+    }
+    if (behind < cols) r.add((xb - all.m) * c);
+    __syncthreads();   // all have read the waves' sums
+    const Sums again = wave_sums({all.m, r.S, r.A}, a.scale);
+    if (lane == 0) part[wave] = again;
+    __syncthreads();
+    all = wave_sums(lane < kWaves ? part[lane] : no_sums(), a.scale);
+  }
   if constexpr (PARTS) {
     if (tid == 0) p.sums[blockIdx.x] = all;
     if constexpr (TOP)

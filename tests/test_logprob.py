@@ -202,6 +202,29 @@ def test_logprob_of_rows_on_workgroups_of_two_waves(prec, V, k):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [37, 3001, 50257, 140001])
+@pytest.mark.parametrize("scale", [1.0, 0.25, 1e-30])
+def test_logprob_of_rows_far_from_zero(prec, V, scale):
+    """Logits around a value of any size: the exponents' reference is a number of 24 bits, too."""
+    rng = np.random.default_rng(V)
+    at = [7.26e5, -7.26e5, 7.2681e5, -7.2683e5, 2.9e6, -2.9e6, 1e9, -1e9, 1e30, -1e30, 3e38, -3e38]
+    x = np.stack([(a + rng.standard_normal(V) * 3 / scale if scale > 1e-20 else a * (1 + rng.standard_normal(V) * 0.01)) for a in at]).astype(np.float32)
+    x[np.isinf(x)] = np.float32(3.3e38)
+    mixed = rows(rng, 3, V, "fp32")
+    mixed[0, ::2] = -1e30                              # ordinary ones among them, in every thread and in some
+    mixed[1, :V // 2] = -7.3e5
+    mixed[2, V // 3] = 8e5
+    x = np.concatenate([x, mixed])
+    if prec == "bf16":
+        x = synth.round_bf16(x)
+        x[np.isinf(x) & (x > 0)] = np.float32(2.0 ** 127)
+    targets = x.argmax(1)
+    for ws in (None, workspace()):
+        check_forward(Forward(x, targets, prec, 10, V, scale, ws), x, targets, 10, float(np.float32(scale)))
+
+
+@pytest.mark.gpu
 def test_logprob_any_subset_of_outputs():
     rng = np.random.default_rng(3)
     for T, V, ws in ((4, 5003, None), (4, 50257, workspace()), (300, 5003, workspace())):
