@@ -302,34 +302,43 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int row, const Sum
 
 // by the workgroup: the k first of the columns x[0 .. cols-1], numbered from `first` on, `put(rank, key)` for each.  `mine`: this thread's largest logit, c.top its
 // largest per slot of `per_slot` segments; xb: the logit of column `behind`, -inf where the thread has none.
-// A floor that at least k logits reach: the k-th largest, or a little less, of the maxima of 256 groups of threads.  What reaches
+// A floor that at least k logits reach: the k-th largest, or a little less, of the maxima of 256 groups of threads (FINE = 4: `fine`
+// holds this thread's largest of each fourth of its columns, and there are 512 groups, at a cost of 0.6 us; 2048 rows of 512 columns
+// in fp32, us on one maximum / four: k = 64 on 128 threads 21.3 / 12.9, k = 128 on 256 31.1 / 21.7, but k = 32 of 4000 13.6 / 14.5).  What reaches
 // it is in the slots of few threads (k of 256 groups at least; as many as the row's largest logits fall into), and those columns
 // are read again: a second reading of a small part of the row (counted: 7 % of 512 x 50257 fp32 at k = 64, 30 % of 2048 x 131072
 // bf16 at k = 128, whose 128 entries are in 128 of 4096 slots), where looking for candidates in the first one costs every segment a
 // comparison and a barrier.  us, with the floor's columns read again / looked for in the one reading: 2048 x 131072 bf16, k = 128,
 // 122 / 192; 512 x 50257 fp32, k = 64, 24.3 / 39; without a list 102 and 18.5.
-template <int NG, typename C, typename L, typename F>
-__device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups, int cols, int per_slot, int k, float mine, float xb, int behind, F put) {
-  constexpr int NT = C::NT, kSegment = NT * NG;
+template <int NG, int FINE, typename C, typename L, typename F>
+__device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups, int cols, int per_slot, int k, const float (&fine)[FINE], float mine, float xb, int behind, F put) {
+  constexpr int NT = C::NT, kSegment = NT * NG, kGroups = FINE == 1 ? 4 : 8;   // a lane's
   const int tid = threadIdx.x, lane = tid % kWave;
   const int slots = ((groups + kSegment - 1) / kSegment + per_slot - 1) / per_slot;
   uint32_t *group = reinterpret_cast<uint32_t *>(c.key);   // free until there are candidates
-  group[tid] = ordered(fmaxf(mine, xb));
+  static_assert(FINE * NT * sizeof(uint32_t) <= sizeof(c.key), "the maxima fit");
+#pragma unroll
+  for (int f = 0; f < FINE; ++f) group[f * NT + tid] = ordered(f == 0 ? fmaxf(fine[f], xb) : fine[f]);
   if (tid == 0) c.n = c.n_hits = 0;
   __syncthreads();
   if (tid < kWave) {
-    uint32_t g[4] = {0, 0, 0, 0}, lo = ~0u, hi = 0;
+    uint32_t g[kGroups] = {}, lo = ~0u, hi = 0;
 #pragma unroll
-    for (int i = 0; i < NT / kWave; ++i) g[i % 4] = max(g[i % 4], group[lane + i * kWave]);
+    for (int f = 0; f < FINE; ++f)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+      for (int w = 0; w < NT / kWave; ++w) {
+        uint32_t &to = g[f * (kGroups / FINE) + w % (kGroups / FINE)];
+        to = max(to, group[f * NT + w * kWave + lane]);
+      }
+#pragma unroll
+    for (int i = 0; i < kGroups; ++i) {
       hi = max(hi, g[i]);
       if (g[i] >= kLowestOrdered) lo = min(lo, g[i]);
     }
     const uint32_t t = threshold(lo, hi, k, [&](uint32_t to) {
       int r = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) r += __popcll(__ballot(g[i] >= to));
+      for (int i = 0; i < kGroups; ++i) r += __popcll(__ballot(g[i] >= to));
       return r;
     });
     if (lane == 0) c.floor = t;
@@ -378,16 +387,17 @@ __device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups
 
 // One workgroup per row (PARTS: per part of a row, of which the workspace gets the sums and the list), NT * NG groups of eight
 // columns at a time, the next ones' loads on their way meanwhile.  One reading: each thread keeps a running maximum and sums
-// relative to it, and its largest logit per slot for the list.  Bound by HBM where there are rows for all compute units: 512 x
+// relative to it, and its largest logit per slot for the list (LIST = 4: of each fourth of its columns, in rows of one slot, where
+// a long list is to be taken from few threads' maxima; LIST = 0: no list).  Bound by HBM where there are rows for all compute units: 512 x
 // 50257 fp32 18.5 us (5.5 TB/s), 2048 x 131072 bf16 102 (5.3); a large copy runs at 5.06, a reading sum at 3.97.  Few or short
 // rows are a chain of latencies: launch, ids, one round of loads, one barrier, and with a list four more (6 us for a row of 260
 // columns and 10 for one of 50257, with a list each).
-template <typename L, int NT, int NG, bool TOP, bool ONE_SLOT, bool PARTS>
+template <typename L, int NT, int NG, int LIST, bool ONE_SLOT, bool PARTS>
 __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, RowParts p) {
   constexpr int kWaves = NT / kWave, kSegment = NT * NG;
   typedef typename CandidatesOf<NT, ONE_SLOT>::type Cands;
   __shared__ Sums part[kWaves];
-  __shared__ __attribute__((aligned(16))) char cand_[TOP ? sizeof(Cands) : 1];
+  __shared__ __attribute__((aligned(16))) char cand_[LIST ? sizeof(Cands) : 1];
   Cands &cand = *reinterpret_cast<Cands *>(cand_);
   const int tid = threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int row = PARTS ? blockIdx.x / p.per_row : blockIdx.x, piece = PARTS ? blockIdx.x % p.per_row : 0;
@@ -415,17 +425,27 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, 
   const float target_logit = has_target ? to_f32(x[tgt]) : 0.f;
   Running z = {fmaxf(xb, -INFINITY), Running::reference(xb * c), 0.f, 0.f};
   z.add(fmaf(xb, c, -z.R));   // nothing for -inf, NaN for what is no number
-  float in_slot = -INFINITY;
+  constexpr int kFine = LIST ? LIST : 1;
+  static_assert(LIST <= 1 || ONE_SLOT, "several maxima a thread in one slot");
+  float in_slot = -INFINITY, fine[kFine];
+#pragma unroll
+  for (int f = 0; f < kFine; ++f) fine[f] = -INFINITY;
   for (int seg = 0, of_slot = 0; seg < segments; ++seg) {
     if (seg + 1 < segments) load(next, seg + 1);
     float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < NG; ++i) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) top = fmaxf(top, v[i].at(k));
+      for (int k = 0; k < 8; ++k) {
+        if constexpr (kFine > 1) fine[k / 2] = fmaxf(fine[k / 2], v[i].at(k));
+        else top = fmaxf(top, v[i].at(k));
+      }
       v[i].forget_floats();
     }
-    if constexpr (TOP) {
+    if constexpr (kFine > 1) {
+      top = fmaxf(fmaxf(fine[0], fine[1]), fmaxf(fine[2], fine[3]));   // of all segments so far
+      if (seg + 1 == segments) cand.top[tid] = top;
+    } else if constexpr (LIST) {
       in_slot = fmaxf(in_slot, top);
       if (++of_slot == per_slot || seg + 1 == segments) {
         cand.top[(seg / per_slot) * NT + tid] = in_slot;
@@ -441,6 +461,7 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, 
 #pragma unroll
     for (int i = 0; i < NG; ++i) v[i] = next[i];
   }
+  if constexpr (kFine == 1) fine[0] = z.m;
   const Sums ws = wave_sums(z.sums(c), a.scale);
   if (lane == 0) part[wave] = ws;
   __syncthreads();
@@ -464,11 +485,11 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, 
   }
   if constexpr (PARTS) {
     if (tid == 0) p.sums[blockIdx.x] = all;
-    if constexpr (TOP)
-      list_row<NG>(cand, x, first, groups, cols, per_slot, a.k, z.m, xb, behind, [&](int rank, uint64_t key) { p.keys[int64_t(blockIdx.x) * a.k + rank] = key; });
+    if constexpr (LIST)
+      list_row<NG>(cand, x, first, groups, cols, per_slot, a.k, fine, z.m, xb, behind, [&](int rank, uint64_t key) { p.keys[int64_t(blockIdx.x) * a.k + rank] = key; });
   } else {
     if (tid == 0) put_row(a, row, all, target_logit, has_target);
-    if constexpr (TOP) list_row<NG>(cand, x, 0, groups, cols, per_slot, a.k, z.m, xb, behind, PutEntry(a, row, all));
+    if constexpr (LIST) list_row<NG>(cand, x, 0, groups, cols, per_slot, a.k, fine, z.m, xb, behind, PutEntry(a, row, all));
   }
 }
 
@@ -584,8 +605,10 @@ void launch_rows(const L *x, LogprobArgs a, int rows, hipStream_t s) {
   const RowParts none = {};
   for (; rows > 0; rows -= kMaxGrid) {   // a launch has a limited number of workgroups
     const dim3 grid(rows < kMaxGrid ? rows : kMaxGrid);
-    if (a.k) hipLaunchKernelGGL((k_logprob<L, NT, NG, true, ONE_SLOT, false>), grid, dim3(NT), 0, s, x, a, none);
-    else hipLaunchKernelGGL((k_logprob<L, NT, NG, false, true, false>), grid, dim3(NT), 0, s, x, a, none);
+    constexpr int kFine = ONE_SLOT && NT > 64 ? 4 : 1;   // 64 threads have no such lists
+    if (a.k > NT / 4 && kFine > 1) hipLaunchKernelGGL((k_logprob<L, NT, NG, kFine, ONE_SLOT, false>), grid, dim3(NT), 0, s, x, a, none);
+    else if (a.k) hipLaunchKernelGGL((k_logprob<L, NT, NG, 1, ONE_SLOT, false>), grid, dim3(NT), 0, s, x, a, none);
+    else hipLaunchKernelGGL((k_logprob<L, NT, NG, 0, true, false>), grid, dim3(NT), 0, s, x, a, none);
     x += int64_t(kMaxGrid) * a.ldl;
     for (float **p : {&a.logp, &a.row_max, &a.log_sum, &a.entropy})
       if (*p) *p += kMaxGrid;
@@ -619,8 +642,8 @@ void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hi
     p.keys = static_cast<uint64_t *>(workspace);
     p.sums = reinterpret_cast<Sums *>(p.keys + int64_t(rows) * p.per_row * a.k);
     const dim3 grid(rows * p.per_row);
-    if (a.k) hipLaunchKernelGGL((k_logprob<L, 512, sizeof(L) == 4 ? 2 : 4, true, true, true>), grid, dim3(512), 0, s, x, a, p);
-    else hipLaunchKernelGGL((k_logprob<L, 512, sizeof(L) == 4 ? 2 : 4, false, true, true>), grid, dim3(512), 0, s, x, a, p);
+    if (a.k) hipLaunchKernelGGL((k_logprob<L, 512, sizeof(L) == 4 ? 2 : 4, 1, true, true>), grid, dim3(512), 0, s, x, a, p);
+    else hipLaunchKernelGGL((k_logprob<L, 512, sizeof(L) == 4 ? 2 : 4, 0, true, true>), grid, dim3(512), 0, s, x, a, p);
     hipLaunchKernelGGL(k_logprob_join<L>, dim3(rows), dim3(kJoinThreads), 0, s, x, a, p);
   } else if (a.V <= 2048 && a.k <= kList64) {
     launch_rows<L, 64, 4, true>(x, a, rows, s);
