@@ -36,8 +36,8 @@ template <int NT_, int KEYS, int RANKED, int SLOTS, int HITS> struct Candidates 
   uint32_t n, n_hits, floor, count[2];
 };
 // For rows (and parts of rows) of one slot, which are many at a time, and for longer ones.  On 64 threads for lists of up to
-// kList64 entries only, on 128 of up to kList128: there are but as many maxima to take the floor from as threads, and the floor
-// has to be far above the lowest of them for few columns to pass.
+// kList64 entries only: there are but as many maxima to take the floor from as threads, and the floor has to be far above the
+// lowest of them for few columns to pass.
 template <int NT, bool ONE_SLOT> struct CandidatesOf { typedef Candidates<NT, 2048, 512, 8, 1024> type; };
 template <int NT> struct CandidatesOf<NT, true> { typedef Candidates<NT, 1024, 512, 1, NT> type; };
 template <> struct CandidatesOf<64, true> { typedef Candidates<64, 512, 256, 1, 64> type; };
@@ -631,8 +631,10 @@ void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hi
   const int room = rows <= (a.k > kList64 ? 16 : 64) ? kPartLaunch / rows : 1;
   const int parts = std::min(std::min(room, kPartsMax), a.V / kPartMinCols);
   // Short rows are bound by what a workgroup does once, not by the columns: fewer threads, more workgroups at a time.  us on 64 /
-  // 128 / 256 threads, bf16, 8192 rows: 2000 columns, k = 20, 21.7 / - / 40.4, k = 48, 42.7 / 37.5 / 44.7, 4000 columns, k = 0, 17.3 /
-  // 16.8 / 25.2, k = 20, 31.2 / 29.4 / 40.3, k = 64, - / 46.1 / 51.3, k = 128, - / 122 / 79, 8000 columns, k = 20, 51.5 / 44.5 / 41.9.
+  // 128 / 256 threads, bf16, 8192 rows: 2000 columns, k = 20, 21.7 / - / 40.4, 4000 columns, k = 0, 17.3 / 16.8 / 25.2, k = 20, 31.2 /
+  // 29.4 / 40.3, 8000 columns, k = 20, 51.5 / 44.5 / 41.9.  Where rows are few a long list is quicker on more threads: 1000 columns,
+  // k = 64, on 64 / 128, one row 11.8 / 9.1, 2048 rows 15.1 / 13.7; k = 128 on 128 / 256 (fp32), 512 rows 16.0 / 11.9, 1024 15.9 /
+  // 14.1, 2048 19.9 / 24.9, 8192 62 / 78.
   // One slot while a thread has but one: 8000 columns, k = 20, 42.6, with eight (twice the LDS) 51.8.  256 against 512 threads:
   // 4096 rows of 20000 columns, k = 20, 51.1 / 64.0, of 12000 36.9 / 47.2; 1024 rows of 131072, k = 128, 75.8 / 70.2 (fp32 117 / 104).
   if (workspace && parts >= 6 && a.V / parts <= kPartMaxCols) {
@@ -647,7 +649,7 @@ void launch_rows(const L *x, const LogprobArgs &a, int rows, void *workspace, hi
     hipLaunchKernelGGL(k_logprob_join<L>, dim3(rows), dim3(kJoinThreads), 0, s, x, a, p);
   } else if (a.V <= 2048 && a.k <= kList64) {
     launch_rows<L, 64, 4, true>(x, a, rows, s);
-  } else if (a.V <= 4096 && a.k <= kList128) {
+  } else if (a.V <= 4096 && (a.k <= kList128 || rows >= 2048)) {
     launch_rows<L, 128, 4, true>(x, a, rows, s);
   } else if (a.V <= 8192) {
     launch_rows<L, 256, 4, true>(x, a, rows, s);

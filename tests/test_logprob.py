@@ -203,6 +203,25 @@ def test_logprob_of_rows_on_workgroups_of_two_waves(prec, V, k):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [300, 1023, 4096, 4500])
+@pytest.mark.parametrize("k", [33, 65, 128])
+def test_long_lists_of_many_short_rows(prec, V, k):
+    rng = np.random.default_rng(V + k)
+    T, known = 2100, 60
+    x = np.concatenate([special_rows(V), rows(rng, known - 18, V, "fp32")])
+    if prec == "bf16":
+        x = synth.round_bf16(x)
+    targets = rng.integers(0, V, known)
+    all_rows, all_targets = np.tile(x, (T // known, 1)), np.tile(targets, T // known)
+    f, many = Forward(x, targets, prec, k, V), Forward(all_rows, all_targets, prec, k, V)
+    check_forward(f, x, targets, k, 1.0)
+    assert torch.equal(many.top_ids, f.top_ids.repeat(T // known, 1))
+    many.T = known
+    check_forward(many, x, targets, k, 1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
 @pytest.mark.parametrize("V", [37, 3001, 50257, 140001])
 @pytest.mark.parametrize("scale", [1.0, 0.25, 1e-30])
 def test_logprob_of_rows_far_from_zero(prec, V, scale):
