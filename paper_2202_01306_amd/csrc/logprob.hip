@@ -309,7 +309,7 @@ __device__ __forceinline__ void put_row(const LogprobArgs &a, int row, const Sum
 // are read again: a second reading of a small part of the row (counted: 7 % of 512 x 50257 fp32 at k = 64, 30 % of 2048 x 131072
 // bf16 at k = 128, whose 128 entries are in 128 of 4096 slots), where looking for candidates in the first one costs every segment a
 // comparison and a barrier.  us, with the floor's columns read again / looked for in the one reading: 2048 x 131072 bf16, k = 128,
-// 122 / 192; 512 x 50257 fp32, k = 64, 24.3 / 39; without a list 102 and 18.5.
+// 119 / 192; 512 x 50257 fp32, k = 64, 24.2 / 39; without a list 98 and 18.5.
 template <int NG, int FINE, typename C, typename L, typename F>
 __device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups, int cols, int per_slot, int k, const float (&fine)[FINE], float mine, float xb, int behind, F put) {
   constexpr int NT = C::NT, kSegment = NT * NG, kGroups = FINE == 1 ? 4 : 8;   // a lane's
@@ -389,7 +389,7 @@ __device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups
 // columns at a time, the next ones' loads on their way meanwhile.  One reading: each thread keeps a running maximum and sums
 // relative to it, and its largest logit per slot for the list (LIST = 4: of each fourth of its columns, in rows of one slot, where
 // a long list is to be taken from few threads' maxima; LIST = 0: no list).  Bound by HBM where there are rows for all compute units: 512 x
-// 50257 fp32 18.5 us (5.5 TB/s), 2048 x 131072 bf16 102 (5.3); a large copy runs at 5.06, a reading sum at 3.97.  Few or short
+// 50257 fp32 18.5 us (5.5 TB/s), 2048 x 131072 bf16 98 (5.5); a large copy runs at 5.06, a reading sum at 3.97.  Few or short
 // rows are a chain of latencies: launch, ids, one round of loads, one barrier, and with a list four more (6 us for a row of 260
 // columns and 10 for one of 50257, with a list each).
 template <typename L, int NT, int NG, int LIST, bool ONE_SLOT, bool PARTS>
