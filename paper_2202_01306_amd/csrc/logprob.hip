@@ -390,8 +390,8 @@ __device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups
 // relative to it, and its largest logit per slot for the list (LIST = 4: of each fourth of its columns, in rows of one slot, where
 // a long list is to be taken from few threads' maxima; LIST = 0: no list).  Bound by HBM where there are rows for all compute units: 512 x
 // 50257 fp32 18.5 us (5.5 TB/s), 2048 x 131072 bf16 98 (5.5); a large copy runs at 5.06, a reading sum at 3.97.  Few or short
-// rows are a chain of latencies: launch, ids, one round of loads, one barrier, and with a list four more (6 us for a row of 260
-// columns and 10 for one of 50257, with a list each).
+// rows are a chain of latencies: launch, ids, one round of loads, one barrier, and with a list four more (6 us for 64 rows of 512
+// columns, 9.5 for one of 50257, with a list each).
 template <typename L, int NT, int NG, int LIST, bool ONE_SLOT, bool PARTS>
 __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, RowParts p) {
   constexpr int kWaves = NT / kWave, kSegment = NT * NG;
