@@ -353,7 +353,10 @@ __device__ __forceinline__ void list_row(C &c, const L *x, int first, int groups
       }
   }
   __syncthreads();
-  if (xb >= floor) c.key[atomicAdd(&c.n, 1u)] = rank_key(xb, first + behind);   // at most seven
+  if (xb >= floor) {   // other waves may be counting what they find below by now: there may be no room left
+    const uint32_t at = atomicAdd(&c.n, 1u);
+    if (at < C::keys) c.key[at] = rank_key(xb, first + behind);
+  }
   const int n_hits = int(c.n_hits);
   if (n_hits <= C::hits) {
     for (int s = 0; s < per_slot; ++s)

@@ -244,6 +244,28 @@ def test_logprob_of_rows_far_from_zero(prec, V, scale):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,k", [(1001, 20), (1002, 64), (4093, 24), (4094, 128), (8189, 20), (30522, 20), (30523, 128), (50257, 64),
+                                 (50260, 1), (140005, 20)])
+def test_lists_of_equal_logits_with_columns_behind_the_last_eight(prec, V, k):
+    """Far more columns reach the floor than a workgroup has room for, those behind the last whole eight among them, which one
+    wave alone looks at, whenever it comes to it."""
+    say(f"logprob equal {prec} V={V} k={k}")
+    x = np.full((6, V), 0.25, np.float32)
+    x[1, V // 8 * 8:] = 0.5                        # the largest of all behind the eight
+    x[2, V - 1] = 0.5
+    x[3, V // 8 * 8:] = -1.0
+    x[4, ::3] = -INF
+    x[5, :V // 2] = -1.0
+    targets = np.full(6, V - 1)
+    for ws in (None, workspace()):
+        f = Forward(x, targets, prec, k, V, 1.0, ws)
+        check_forward(f, x, targets, k, 1.0)
+        many = Forward(np.tile(x, (50, 1)), np.tile(targets, 50), prec, k, V, 1.0, ws)
+        assert torch.equal(many.top_ids, f.top_ids.repeat(50, 1)) and torch.equal(many.logp, many.logp[:6].repeat(50))
+
+
+@pytest.mark.gpu
 def test_logprob_any_subset_of_outputs():
     rng = np.random.default_rng(3)
     for T, V, ws in ((4, 5003, None), (4, 50257, workspace()), (300, 5003, workspace())):
