@@ -171,6 +171,7 @@ __device__ __forceinline__ int list_ties(C &c, const L *x, int first, int cols, 
     __syncthreads();
     floor = unordered(__builtin_amdgcn_readfirstlane(c.floor));   // above the one before
   }
+  __syncthreads();   // all have read c.n, which thin_out writes: no column that equals the floor may be wanted
   const int wanted = k - n;   // of those that equal the floor, the lowest columns first
   int taken = 0;
 #pragma unroll 1

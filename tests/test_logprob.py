@@ -266,6 +266,27 @@ def test_lists_of_equal_logits_with_columns_behind_the_last_eight(prec, V, k):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("V,k", [(2000, 1), (2000, 24), (4096, 64), (8185, 128), (30522, 20), (50257, 1), (50257, 64), (140005, 128)])
+def test_lists_whose_candidates_are_taken_from_a_second_floor(prec, V, k):
+    """More columns above the floor than there is room for, all of them unlike or nearly so: a second floor leaves more than the
+    list is long, and none that equals it is wanted.  Many rows at once, so that their waves come to it at all times."""
+    say(f"logprob second floor {prec} V={V} k={k}")
+    rng = np.random.default_rng(V + k)
+    at = np.arange(V)
+    x = np.stack([np.where(at // 8 % 64 < 2, 5.0 + rng.permutation(V) / V, -5.0), np.where(at // 8 % 512 < 24, 5.0 + rng.permutation(V) / V, -5.0),
+                  np.where(at % 16 < 8, at / V, -1.0), 1.0 + rng.integers(0, 100, V) / 128]).astype(np.float32)
+    if prec == "bf16":
+        x = synth.round_bf16(x)
+    targets = rng.integers(0, V, 4)
+    for ws in (None, workspace()):
+        f = Forward(x, targets, prec, k, V, 1.0, ws)
+        check_forward(f, x, targets, k, 1.0)
+        many = Forward(np.tile(x, (100, 1)), np.tile(targets, 100), prec, k, V, 1.0, ws)
+        assert torch.equal(many.top_ids, f.top_ids.repeat(100, 1)) and torch.equal(many.top_logp, many.top_logp[:4].repeat(100, 1))
+
+
+@pytest.mark.gpu
 def test_logprob_any_subset_of_outputs():
     rng = np.random.default_rng(3)
     for T, V, ws in ((4, 5003, None), (4, 50257, workspace()), (300, 5003, workspace())):
