@@ -409,7 +409,8 @@ __global__ __launch_bounds__(NT) void k_logprob(const L *logits, LogprobArgs a, 
   // columns first .. first+cols-1
   const int first = PARTS ? piece * p.cols : 0, cols = PARTS ? min(p.cols, a.V - first) : a.V;
   const L *x = logits + int64_t(row) * a.ldl + first;
-  const int groups = cols / 8, segments = (groups + kSegment - 1) / kSegment, per_slot = (segments + Cands::slots - 1) / Cands::slots;
+  const int groups = cols / 8, segments = (groups + kSegment - 1) / kSegment;
+  const int per_slot = max(1, (segments + Cands::slots - 1) / Cands::slots);   // list_row divides by it, also for rows of no group
   // the column behind the groups, if there is one for this thread
   const int behind = groups * 8 + tid;
   const float xb = behind < cols ? to_f32(x[behind]) : -INFINITY;

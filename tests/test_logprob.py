@@ -287,6 +287,28 @@ def test_lists_whose_candidates_are_taken_from_a_second_floor(prec, V, k):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", range(1, 10))
+def test_lists_of_rows_without_eight_columns(prec, V):
+    """Rows of no whole group of eight columns, and of one, on each number of threads that a list of their length gets."""
+    say(f"logprob without eight {prec} V={V}")
+    rng = np.random.default_rng(V)
+    x = rows(rng, 9, V, prec)
+    x[1] = -INF
+    x[2] = 0.25
+    x[3] = float(torch.finfo(torch.bfloat16).min)
+    x[4] = -np.arange(V)
+    targets = rng.integers(-1, V, 9)
+    for k in (1, 7, 24, 25, 33, 65, 128):
+        f = Forward(x, targets, prec, k, V, 1.0, workspace())
+        check_forward(f, x, targets, k, 1.0)
+        many = Forward(np.tile(x, (250, 1)), np.tile(targets, 250), prec, k, V)
+        assert torch.equal(many.top_ids, f.top_ids.repeat(250, 1))
+        many.T = 9
+        check_forward(many, x, targets, k, 1.0)
+
+
+@pytest.mark.gpu
 def test_logprob_any_subset_of_outputs():
     rng = np.random.default_rng(3)
     for T, V, ws in ((4, 5003, None), (4, 50257, workspace()), (300, 5003, workspace())):
