@@ -616,7 +616,8 @@ int hmy_k_logprob_bwd(const hmy_logprob_grad_desc *g, void *stream);
  *     q_r = max(0, 1 - sum q_k) and the student's p_r = the sum of their p_j:
  *     row_loss = sum_k q_k (teacher_logp_k - l_k) + q_r (log q_r - log p_r); with Q = sum q_k + q_r,
  *     dL/dx_j = w s (Q p_j - q_j) for listed tokens, w s p_j (Q - q_r / p_r) for the others.  Where the student gives the class
- *     no weight at all (p_r = 0) it is dropped: q_r = 0.
+ *     no weight at all it is dropped, q_r = 0: where s times its largest logit is more than 745 below s times the row's (e^-745 is
+ *     the least number of 64 bits), or is -inf.
  * (A token listed twice counts q_k (log q_k - l_k) for each entry.)  w = grad_scale, which also scales what loss_acc (may be
  * NULL) gets: loss_acc[0] += w sum_t row_loss[t], added up in one order by a launch of its own, to which one atomic addition
  * belongs, so that calls that overlap may share it (as in hmy_k_xent).  row_loss[T] itself is not scaled.  A row with no entry at all (padding) has loss 0 and gradient 0.  dlogits NULL: the loss alone. */

@@ -6,7 +6,8 @@
 //   dloss/dz_j = Q p_j - q_j for listed tokens, p_j (Q - q_r / p_r) for the others (z = s x; without a tail q_r = 0, Q = 1).
 // A divergence is small beside the logarithms that it is the difference of: the list's terms are held in 64 bits.  With a tail
 // the row's sum is taken as that of the others (listed tokens are set to -inf where they are loaded) and that of the list, so
-// that p_r of a student who is sure of listed tokens is no difference of two sums.
+// that p_r of a student who is sure of listed tokens is no difference of two sums.  The others' sum and exponentials stay relative to
+// their own largest logit: p_j / p_r is a quotient of numbers of ordinary size however little weight the class has.
 #include <algorithm>
 
 #include "logit_rows.h"
@@ -157,22 +158,28 @@ __device__ __forceinline__ void read_list(const L *x, const DistillArgs &a, int 
   }
 }
 
+// Whether the tokens that are not listed have any weight: exp(-745) is the least number of 64 bits.  One rule for loss and gradient.
+// m_rest, rest: the sum of exp(s (x - m_rest)) over them (over all without a tail) and its reference, their largest logit, so that
+// rest is at least 1 unless none of them has a logit above -inf; m: the row's largest logit
+__device__ __forceinline__ bool others_weigh(float m_rest, float rest, float m, float scale) {
+  return !(rest == 0.f) && !((double(m_rest) - double(m)) * double(scale) < -745.);
+}
 // What a row's gradient is made of once its sums are known
 struct RowTerms {
-  float m;                // the row's maximum, 0 where nothing has any weight
-  float c_list, c_rest;   // what exp(s (x - m)) of a listed token and of any other is multiplied with
-};
-// rest, m_rest: the sum of exp(s (x - m_rest)) over the tokens that are not listed (over all without a tail) and its reference
+  float m, c_list;        // the row's maximum, and what exp(s (x - m)) of a listed token is multiplied with
+  float m_rest, c_rest;   // the others' maximum, and what exp(s (x - m_rest)) of any other is multiplied with
+};                        // (maxima: 0 where nothing has any weight)
 __device__ __forceinline__ RowTerms row_terms(float m_rest, float rest, const ListSum &z, const DistillArgs &a) {
-  const float m = a.tail ? fmaxf(m_rest, z.max) : m_rest;
-  const float S_rest = rest * rebase(m_rest, m, a.scale), S = S_rest + (a.tail ? float(z.sum) * rebase(z.max, m, a.scale) : 0.f);
-  const float q_rest = a.tail && !(S_rest == 0.f) ? float(fmax(1. - z.q_sum, 0.)) : 0.f;
+  const float m = a.tail ? fmaxf(m_rest, z.max) : m_rest, f = rebase(m_rest, m, a.scale);
+  const float S = rest * f + (a.tail ? float(z.sum) * rebase(z.max, m, a.scale) : 0.f);
+  const float q_rest = a.tail && others_weigh(m_rest, rest, m, a.scale) ? float(fmax(1. - z.q_sum, 0.)) : 0.f;
   const float w = a.scale * a.grad_scale, Q = float(z.q_sum) + q_rest;
   RowTerms r;
   r.m = m == -INFINITY ? 0.f : m;
+  r.m_rest = m_rest == -INFINITY ? 0.f : m_rest;
   const float inv = S == 0.f ? 0.f : 1.f / S;
   r.c_list = w * (Q * inv);
-  r.c_rest = q_rest > 0.f ? w * (Q * inv - q_rest / S_rest) : r.c_list;
+  r.c_rest = w * (Q * inv * f - (q_rest > 0.f ? q_rest / rest : 0.f));
   return r;
 }
 // by one wave, the result in all lanes
@@ -192,7 +199,7 @@ __device__ __forceinline__ float row_loss(float m_rest, float rest, const List &
   loss = wave_total(loss);
   if (!a.tail) return float(loss / z.q_norm + log64(S / z.q_norm));
   loss += z.q_sum * log64(S);
-  if (!(S_rest == 0.)) {
+  if (others_weigh(m_rest, rest, m, a.scale)) {
     const double q_rest = fmax(1. - z.q_sum, 0.);
     if (q_rest > 0.) loss += q_rest * log64(q_rest * (S / S_rest));
   }
@@ -349,8 +356,9 @@ __global__ __launch_bounds__(NT + (LIST_WAVE ? kWave : 0)) __attribute__((amdgpu
     }
     const RowTerms r = row_terms(m_rest, rest, z, a);
     if (columns) {
-      const float mine = r.c_rest * rebase(m, r.m, a.scale);
-      auto grad = [&](float xj) { return fast_exp2((xj - r.m) * c) * r.c_rest; };
+      const float mine = r.c_rest * rebase(m, r.m_rest, a.scale);
+      // (listed tokens may come out as anything: theirs is stored behind)
+      auto grad = [&](float xj) { return fast_exp2((xj - r.m_rest) * c) * r.c_rest; };
 #pragma unroll
       for (int i = 0; i < NG; ++i) {
         const int g = (segments == 1 ? 0 : lead + (segments - 2) * kSegment) + i * NT + tid;
@@ -458,7 +466,7 @@ __global__ __launch_bounds__(kPartThreads) void k_distill_finish(const L *logits
   if (dlogits) {
     const RowTerms r = row_terms(m_rest, rest, z, a);
     const float c = a.scale * kLog2e;
-    auto grad = [&](float xj) { return z.any ? fast_exp2((xj - r.m) * c) * r.c_rest : 0.f; };
+    auto grad = [&](float xj) { return z.any ? fast_exp2((xj - r.m_rest) * c) * r.c_rest : 0.f; };
     const L *x = logits + int64_t(row) * a.ldl;
     E *d = dlogits + int64_t(row) * a.ldd;
     const int first = piece * p.groups, last = min(first + p.groups, a.V / 8);

@@ -504,6 +504,57 @@ def test_distill_of_lists_and_rows_where_it_can_go_wrong(prec, tail, V):
         check_distill(ls[rows_], got[rows_], x[rows_], ids[rows_], t[rows_], 1.0, 1.0, tail, prec == "bf16", V)
 
 
+def check_class_of_little_weight(lp, ep, x, ids, t, scale, w, ws):
+    """Loss and gradient with a tail of rows that leave the others next to nothing, each token once in its list.
+
+    What is not listed is w s (Q p_j - q_r p_j / p_r): p_j / p_r is the exponential of the distance to the others' own log sum,
+    d_j, so it is off by (n + 4 |d_j| + 4) u relative and 4 u more for the products with it, and p_j by the same with |l_j|.
+    Numbers below the least normal one of fp32 count as 0."""
+    (T, V), K = x.shape, ids.shape[1]
+    n = roundings(V)
+    loss, d = f32(T), f32(T, V).to(DT[ep])
+    B.hmy_k_distill(PC[ep], PC[lp], on_device(x, V, lp), i32(ids), torch.from_numpy(t).cuda(), loss, d, T, V, K, V, V, tail=True, scale=scale,
+                    grad_scale=w, workspace=ws)
+    got, got_loss = host(d), host(loss)
+    for r in range(T):
+        ref_loss, g = ol.distill(x[r], ids[r], t[r], scale, True)
+        near(got_loss[r], ref_loss, U * (n + abs(ref_loss)))
+        l = ol.log_probabilities(x[r], scale)[2]
+        listed = np.zeros(V)
+        listed[ids[r]] = np.exp(t[r].astype(np.float64))
+        others, q_r = listed == 0, 1 - listed.sum()
+        dist = l - l[others].max() - np.log(np.exp(l[others] - l[others].max()).sum())
+        share = np.where(others, q_r * np.exp(np.where(others, dist, 0)) * (2 * n + 8 * np.abs(dist) + 16), 4 * listed)
+        off = scale * w * (U * ((2 * n + 8 * np.abs(l) + 16) * np.exp(l) + share) + 4 * 2.0 ** -126)
+        ref = g * w
+        near(got[r], ref, off + (2.0 ** -8 * (np.abs(ref) + off) if ep == "bf16" else 0) + 2.0 ** -126)
+
+
+LITTLE = np.log([0.3, 0.2, 0.1, 0.1, 0.05, 0.05])    # a teacher's list that leaves a fifth to the others
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lp,ep", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("V", [200, 5003, 30522, 70001])
+def test_distill_where_the_student_leaves_the_others_next_to_nothing(lp, ep, V):
+    """A class of others whose probability is far below what fp32 holds keeps its share of the gradient, as it does of the loss."""
+    say(f"distill of a class of little weight {lp} -> {ep} V={V}")
+    rng = np.random.default_rng(V)
+    gaps = [-100, 10, 60, 80, 86, 87, 88, 90, 100, 104, 150, 300, 400, 540]
+    T, K = len(gaps) + 1, len(LITTLE)
+    ids = np.stack([rng.choice(V - 1, K, replace=False) for _ in range(T)]).astype(np.int32)
+    ids[:, 0] = V - 1                              # behind the last whole eight, where there is something
+    t = np.tile(LITTLE, (T, 1)).astype(np.float32)
+    x = rng.standard_normal((T, V)).astype(np.float32) * 2 - np.array(gaps + [0], np.float32)[:, None]
+    x[T - 1] = -rng.uniform(95, 400, V)
+    np.put_along_axis(x, ids.astype(np.int64), rng.standard_normal((T, K)).astype(np.float32), 1)
+    if lp == "bf16":
+        x = synth.round_bf16(x)
+    for scale, w in ((1.0, 1.0), (1.0, 1024.0), (1.25, 1e30)):
+        for ws in (None, workspace()):
+            check_class_of_little_weight(lp, ep, x, ids, t, scale, float(np.float32(w)), ws)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("tail", [False, True])
 def test_distill_of_whole_vocabularies_is_the_divergence(tail):
