@@ -55,6 +55,14 @@ def logprob_bwd(x, target, d_logp, d_entropy, scale=1.0):
     return scale * g
 
 
+def has_weight(x, of, scale=1.0):
+    """Whether the tokens `of` a row weigh anything: their largest logit is above -inf and at most 745 (the logarithm of the least
+    number of 64 bits) below the row's, times the scale."""
+    x = np.asarray(x, F64)
+    m = np.fmax.reduce(x[of], initial=NINF)
+    return m > NINF and not scale * (m - np.fmax.reduce(x)) < -745
+
+
 def distill(x, ids, t, scale=1.0, tail=False):
     """(loss, its gradient with respect to x) of one row against listed tokens and the teacher's log probabilities of them."""
     V = len(x)
@@ -76,14 +84,16 @@ def distill(x, ids, t, scale=1.0, tail=False):
     listed = np.zeros(V, bool)
     listed[[i for i, _ in there]] = True
     Q, rest = q.sum(), 0.0
-    p_rest = p[~listed].sum()
-    if tail and not p_rest == 0:
+    if tail and has_weight(x, ~listed, scale):
         rest = max(0.0, 1.0 - Q)
-        if rest > 0:
-            loss += rest * (np.log(rest) - np.log(p_rest))
+    if rest > 0:
+        # log p of the class as a whole: p itself has few bits left, or none, where the student gives it next to nothing
+        n = np.fmax.reduce(l[~listed])
+        log_p_rest = n + np.log(np.exp(l[~listed] - n).sum())
+        loss += rest * (np.log(rest) - log_p_rest)
     g = (Q + rest) * p
     if rest > 0:
-        g[~listed] = p[~listed] * (Q + rest - rest / p_rest)
+        g[~listed] -= rest * np.exp(l[~listed] - log_p_rest)
     for (i, _), qk in zip(there, q):
         g[i] -= qk
     return loss, scale * g

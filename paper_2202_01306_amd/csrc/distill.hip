@@ -201,7 +201,8 @@ __device__ __forceinline__ float row_loss(float m_rest, float rest, const List &
   loss += z.q_sum * log64(S);
   if (others_weigh(m_rest, rest, m, a.scale)) {
     const double q_rest = fmax(1. - z.q_sum, 0.);
-    if (q_rest > 0.) loss += q_rest * log64(q_rest * (S / S_rest));
+    // p_r = exp(u) rest / S with u down to -745, where exp(u) keeps few bits: u is added outside of the logarithm
+    if (q_rest > 0.) loss += q_rest * (log64(q_rest * (S / double(rest))) - (double(m_rest) - mr) * s);
   }
   return float(loss);
 }

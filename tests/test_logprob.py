@@ -556,6 +556,29 @@ def test_distill_where_the_student_leaves_the_others_next_to_nothing(lp, ep, V):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lp,ep", [("fp32", "fp32"), ("fp32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("V", [200, 5003, 30522, 70001])
+@pytest.mark.parametrize("scale", [1.0, 0.5])
+def test_distill_of_a_class_at_the_edge_of_64_bits(lp, ep, V, scale):
+    """The others' probability has few bits of 64 left, then none: the loss is a number throughout, on either side of the 745 below
+    the row's largest logit from which on the class is dropped.  All values are multiples of four (bf16 keeps them)."""
+    say(f"distill of a class at the edge {lp} -> {ep} V={V} scale={scale}")
+    rng = np.random.default_rng(V)
+    gaps = np.array([640, 700, 708, 712, 720, 724, 736, 744, 748, 760, 1000], np.float32) / scale
+    T, K = len(gaps), len(LITTLE)
+    ids = np.stack([rng.choice(V - 1, K, replace=False) for _ in range(T)]).astype(np.int32)
+    ids[:, 1] = V - 1
+    t = np.tile(LITTLE, (T, 1)).astype(np.float32)
+    x = np.repeat(-gaps[:, None], V, 1)
+    x[:, ::5] = -1024.0 / scale
+    np.put_along_axis(x, ids.astype(np.int64), np.float32(0.0), 1)
+    x[np.arange(T), ids[:, 3]] = -2.0
+    assert np.array_equal(synth.round_bf16(x), x)
+    for ws in (None, workspace()):
+        check_class_of_little_weight(lp, ep, x, ids, t, scale, 1.0, ws)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("tail", [False, True])
 def test_distill_of_whole_vocabularies_is_the_divergence(tail):
     """Every token listed: no class of others, and with the student's own probabilities neither loss nor gradient."""
@@ -911,3 +934,35 @@ def test_oracle_gradients_are_differences():
             e = np.zeros(V)
             e[j] = h
             assert abs((f(x + e) - f(x - e)) / (2 * h) - g[j]) < 1e-8
+
+
+@pytest.mark.parametrize("gap", [1, 30, 100, 400, 700, 720, 744, 748, 1000])
+def test_oracle_of_a_class_of_little_weight(gap):
+    """The fp64 oracle against the same formulas in decimal numbers of 60 digits, whose exponents have no such edge."""
+    from decimal import Decimal, localcontext
+    rng = np.random.default_rng(gap)
+    V, ids = 40, [3, 39, 8, 21, 5, 30]
+    t = LITTLE.astype(np.float32)
+    x = (-gap - rng.random(V) * 4).astype(np.float32)
+    x[11] = -gap
+    x[17] = -INF
+    x[ids] = -rng.random(6)
+    x[ids[0]] = 0.0
+    loss, g = ol.distill(x, ids, t, 1.0, True)
+    with localcontext() as c:
+        c.prec = 60
+        D = [None if v == -INF else Decimal(float(v)) for v in x]
+        z = sum(v.exp() for v in D if v is not None).ln()
+        l = [None if v is None else v - z for v in D]
+        p = [Decimal(0) if v is None else v.exp() for v in l]
+        tk = [Decimal(float(v)) for v in t]
+        q = [v.exp() for v in tk]
+        q_r = 1 - sum(q) if gap <= 745 else Decimal(0)
+        p_r = sum(p[j] for j in range(V) if j not in ids)
+        ref_loss = sum(qk * (tv - l[i]) for i, tv, qk in zip(ids, tk, q)) + (q_r * (q_r.ln() - p_r.ln()) if q_r > 0 else 0)
+        Q = sum(q) + q_r
+        ref = [Q * p[j] - q[ids.index(j)] if j in ids else p[j] * (Q - q_r / p_r) for j in range(V)]
+        ref_loss, ref = float(ref_loss), np.array([float(v) for v in ref])
+    # l and log p_r carry half a step of 64 bits of |l| for each of a few operations, exponentials as much relative
+    assert abs(loss - ref_loss) <= 2.0 ** -53 * 8 * (gap + 8)
+    assert np.all(np.abs(g - ref) <= 2.0 ** -53 * 8 * (gap + 8) * np.abs(ref).max())
