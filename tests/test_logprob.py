@@ -579,6 +579,37 @@ def test_distill_of_a_class_at_the_edge_of_64_bits(lp, ep, V, scale):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("lp", ["fp32", "bf16"])
+@pytest.mark.parametrize("V", [200, 5003, 30522, 70001])
+def test_distill_of_a_student_near_its_teacher(lp, V):
+    """The others' gradient is p_r - q_r, two nearly equal numbers, over their number.  All of their logits are 0, so that sums and
+    exponentials are exact; what is left are the roundings of the factor to fp32 and of its product with 1, and of numbers near 1
+    to 64 bits beside a difference of 2e-8 or more.  The list's sum, 1 - p_r of the whole, is brought from its largest logit to 0 by
+    an exponential in fp32: 2 u of the unit, u of its correction and u of their product, and S in Q p_r = Q rest / S is off by as
+    much of its part: 4 u Q p_r (1 - p_r) / rest, of any number of listed tokens."""
+    rng = np.random.default_rng(V)
+    T, K = 9, 6
+    ids = np.stack([rng.choice(V, K, replace=False) for _ in range(T)]).astype(np.int32)
+    x = np.zeros((T, V), np.float32)
+    np.put_along_axis(x, ids.astype(np.int64), -rng.random((T, K)).astype(np.float32), 1)
+    if lp == "bf16":
+        x = synth.round_bf16(x)
+    l = np.stack([ol.log_probabilities(r)[2] for r in x])
+    t = (np.take_along_axis(l, ids.astype(np.int64), 1) + 0.001 + 0.01 * rng.random((T, K))).astype(np.float32)
+    for ws in (None, workspace()):
+        loss, d = f32(T), f32(T, V)
+        B.hmy_k_distill(0, PC[lp], on_device(x, V, lp), i32(ids), torch.from_numpy(t).cuda(), loss, d, T, V, K, V, V, tail=True, workspace=ws)
+        got = host(d)
+        for r in range(T):
+            g = ol.distill(x[r], ids[r], t[r], 1.0, True)[1]
+            others = np.ones(V, bool)
+            others[ids[r]] = False
+            p_r, q_r = np.exp(l[r])[others].sum(), 1 - np.exp(t[r].astype(np.float64)).sum()
+            assert 2e-8 < abs(p_r - q_r)
+            near(got[r][others], g[others], 4 * U * (np.abs(g[others]) + p_r * (1 - p_r) / others.sum()))
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("tail", [False, True])
 def test_distill_of_whole_vocabularies_is_the_divergence(tail):
     """Every token listed: no class of others, and with the student's own probabilities neither loss nor gradient."""
