@@ -487,12 +487,22 @@ def _at(x):
     return x if x is None or isinstance(x, int) else x.data_ptr()
 
 
+def _size_of(workspace, workspace_bytes):
+    if workspace_bytes is not None:
+        return workspace_bytes
+    if workspace is None:
+        return 0
+    if isinstance(workspace, int):
+        raise HmyError(HMY_E_INVALID, "a workspace given by its address wants its size, workspace_bytes")
+    return workspace.numel() * workspace.element_size()
+
+
 def hmy_k_logprob(logits_prec, logits, T, V, ldl, targets=None, logp=None, row_max=None, log_sum=None, entropy=None, k=0,
-                  top_ids=None, top_logp=None, scale=1.0, stream=None, workspace=None):
-    """workspace: a tensor of HMY_ROWS_WORKSPACE_BYTES, which lets a call of few, long rows use the whole device."""
+                  top_ids=None, top_logp=None, scale=1.0, stream=None, workspace=None, workspace_bytes=None):
+    """workspace: a tensor of HMY_ROWS_WORKSPACE_BYTES, or an address with its size in workspace_bytes, which lets a call of few, long
+    rows use the whole device; one that is smaller is not used."""
     g = hmy_logprob_desc(logits_prec, T, V, k, _at(logits), ldl, _at(targets), _at(logp), _at(row_max), _at(log_sum),
-                         _at(entropy), _at(top_ids), _at(top_logp), _at(workspace),
-                         0 if workspace is None else workspace.numel() * workspace.element_size(), scale, 0)
+                         _at(entropy), _at(top_ids), _at(top_logp), _at(workspace), _size_of(workspace, workspace_bytes), scale, 0)
     _check(lib.hmy_k_logprob(C.byref(g), _p(stream)))
 
 
@@ -505,11 +515,11 @@ def hmy_k_logprob_bwd(prec, logits_prec, logits, row_max, log_sum, dlogits, T, V
 
 
 def hmy_k_distill(prec, logits_prec, logits, teacher_ids, teacher_logp, row_loss, dlogits, T, V, K, ldl, ldd, tail=False,
-                  scale=1.0, grad_scale=1.0, pad=0, loss_acc=None, stream=None, workspace=None):
-    """prec: type of dlogits; dlogits None: the loss alone; workspace as for hmy_k_logprob."""
+                  scale=1.0, grad_scale=1.0, pad=0, loss_acc=None, stream=None, workspace=None, workspace_bytes=None):
+    """prec: type of dlogits; dlogits None: the loss alone; workspace and workspace_bytes as for hmy_k_logprob."""
     g = hmy_distill_desc(prec, logits_prec, T, V, K, int(tail), _at(logits), ldl, _at(teacher_ids), _at(teacher_logp),
-                         _at(row_loss), _at(loss_acc), _at(dlogits), ldd, _at(workspace),
-                         0 if workspace is None else workspace.numel() * workspace.element_size(), scale, grad_scale, pad, 0)
+                         _at(row_loss), _at(loss_acc), _at(dlogits), ldd, _at(workspace), _size_of(workspace, workspace_bytes),
+                         scale, grad_scale, pad, 0)
     _check(lib.hmy_k_distill(C.byref(g), _p(stream)))
 
 

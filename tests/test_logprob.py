@@ -938,6 +938,33 @@ def test_refusals(call, bad):
     assert e.value.code == B.HMY_E_INVALID and len(str(e.value)) > 30
 
 
+@pytest.mark.parametrize("call", [forward, distill])
+def test_a_workspace_by_its_address(call):
+    """Its size comes with it: without one it is refused, and the size is what the library looks at (an address that is not aligned
+    to 16 bytes is refused only where it would be used)."""
+    with pytest.raises(B.HmyError, match="workspace_bytes") as e:
+        call(workspace=P)
+    assert e.value.code == B.HMY_E_INVALID
+    with pytest.raises(B.HmyError, match="16 bytes"):
+        call(workspace=P + 8, workspace_bytes=B.HMY_ROWS_WORKSPACE_BYTES)
+
+
+@pytest.mark.gpu
+def test_a_workspace_by_its_address_is_used():
+    rng = np.random.default_rng(9)
+    T, V, k = 2, 140001, 9
+    x, ws = rows(rng, T, V, "fp32"), workspace(0x5a)
+    by_tensor = Forward(x, [3, 4], "fp32", k, V, 1.0, workspace())
+    f = Forward(x, [3, 4], "fp32", k, V, 1.0, ws, logits=by_tensor.logits)
+    before = ws.fill_(0x5a).clone()
+    f.call(workspace=ws.data_ptr(), workspace_bytes=ws.numel() - 1)
+    assert torch.equal(ws, before)                 # too small: not used
+    f.call(workspace=ws.data_ptr(), workspace_bytes=ws.numel())
+    assert not torch.equal(ws, before)
+    for a, b in zip(f.outputs(), by_tensor.outputs()):
+        assert torch.equal(a, b)
+
+
 def test_no_description_at_all():
     for f in (B.lib.hmy_k_logprob, B.lib.hmy_k_logprob_bwd, B.lib.hmy_k_distill):
         assert f(None, None) == B.HMY_E_INVALID
