@@ -557,11 +557,13 @@ int hmy_k_adam(int32_t prec, const float *grad, float *master, float *m, float *
 /* ---- operators on rows of logits (all pointers DEVICE, stream as above) ----
  * logits[T,V], row stride ldl >= V, in fp32 or bf16 (logits_prec: HMY_PREC_*); rows may start at any element.  With a scale
  * s > 0 (an inverse temperature), m = the row's largest logit and S = sum exp(s (x_j - m)), the log probability of token j is
- * l_j = s (x_j - m) - log S, p_j = exp l_j.  Sums are held in fp32, a list's terms of hmy_k_distill in fp64; results do not
- * depend on the order in which workgroups run.
+ * l_j = s (x_j - m) - log S, p_j = exp l_j.  Sums over a row are held in fp32, a list's terms of hmy_k_distill and what its
+ * gradient's factors are made of in fp64; results do not depend on the order in which workgroups run.
  *   - A logit of -inf is a token without weight: l = -inf, p = 0, in no list.  A row of nothing else has row_max = log_sum =
  *     -inf, entropy 0 and l = -inf throughout.  A row that holds a NaN or +inf has NaN results (its list still ranks the
  *     tokens that are no NaN).
+ *   - x_j - m is taken in fp32 and then scaled: a finite logit more than 3.4e38 below the row's largest counts as infinitely far
+ *     below it (with s < 1e-36, where it would have weight, S of hmy_k_logprob may hold that or not).
  *   - An id outside of [0, V) names no token.
  *   - T >= 1, 1 <= V <= 2^24.  Arrays are aligned to their elements.
  *   - dlogits[T,V] with row stride ldd: columns V .. V+pad-1 of each row are written as zeros (the padding that
@@ -620,7 +622,8 @@ int hmy_k_logprob_bwd(const hmy_logprob_grad_desc *g, void *stream);
  *     the least number of 64 bits), or is -inf.
  * (A token listed twice counts q_k (log q_k - l_k) for each entry.)  w = grad_scale, which also scales what loss_acc (may be
  * NULL) gets: loss_acc[0] += w sum_t row_loss[t], added up in one order by a launch of its own, to which one atomic addition
- * belongs, so that calls that overlap may share it (as in hmy_k_xent).  row_loss[T] itself is not scaled.  A row with no entry at all (padding) has loss 0 and gradient 0.  dlogits NULL: the loss alone. */
+ * belongs, so that calls that overlap may share it (as in hmy_k_xent).  row_loss[T] itself is not scaled.  A row with no entry
+ * at all (padding) has loss 0 and gradient 0.  dlogits NULL: the loss alone. */
 typedef struct hmy_distill_desc {
   int32_t prec, logits_prec, T, V, K, tail;  /* 1 <= K <= HMY_MAX_TOP         */
   const void *logits; int64_t ldl;

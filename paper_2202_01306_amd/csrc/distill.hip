@@ -307,7 +307,8 @@ __device__ __forceinline__ void put_listed(E *d, const List &l, const RowTerms &
 // Bound by HBM, one reading and one writing, where there are rows for all compute units: 512 x 50257 fp32 into bf16 37 us (4.2
 // TB/s: all of its rows are at work at once, two per compute unit, so that all read and then all write), 2048 x 50257 123 (5.0),
 // 2048 x 131072 bf16 243 (4.4; one row per compute unit).  A few short rows: 6 us for 5003 columns, launch and one chain of
-// latencies (ids, their logits, 64-bit sums, barrier, stores, barrier, the listed columns).
+// latencies (ids, their logits, 64-bit sums, barrier, stores, barrier, the listed columns).  The loss alone takes the same way as far
+// as the sums: 512 x 50257 fp32 21.3 us without a tail (4.8 TB/s), 22.7 with one; 2048 x 131072 bf16 116 (4.6) and 129.
 template <typename L, typename E, int NT, int NG, bool TAIL, bool LIST_WAVE, int WPE>
 __global__ __launch_bounds__(NT + (LIST_WAVE ? kWave : 0)) __attribute__((amdgpu_waves_per_eu(WPE))) void k_distill(const L *logits, E *dlogits, DistillArgs a) {
   constexpr int kSegment = NT * NG;
@@ -590,6 +591,9 @@ int launch_distill(const hmy_distill_desc &g, stream_t st) {
     // time as far as they fit: 448 threads and a list wave (20000 columns 83, on 512 threads without one 90; the floor is 81), in
     // bf16 1024 threads of 64 registers although a part of the row is read twice then (80000 columns 102, on 110 registers
     // 110), and only beyond 110000 one row at a time (131072 columns 230 against 246).
+    // fp32 rows of 25089 to 32768 columns stay there although their first columns, beyond 448 x 7 groups, are read twice; us so / on
+    // 1024 threads without a list wave, a tail in fp32: 30522 columns, 6 rows 8.6 / 8.8, 256 15.7 / 15.9, 512 29.1 / 34.6, 3372 176 /
+    // 183; 32768 columns, 512 rows 30.9 / 35.1, 3372 186 / 187 (into bf16 without a tail 133 / 129); 36000 columns, 3372 rows 211 / 206.
     // Few rows by parts, two launches, from four parts on, which read twice but on the whole device.  us by parts / by rows, fp32:
     // one row of 131072 columns 10.2 / 23.5, 64 rows of 80000 17.4 / 19.6, but 128 rows 25.6 / 21.6.
     constexpr bool wide = sizeof(L) == 4;
