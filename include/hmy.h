@@ -557,8 +557,8 @@ int hmy_k_adam(int32_t prec, const float *grad, float *master, float *m, float *
 /* ---- operators on rows of logits (all pointers DEVICE, stream as above) ----
  * logits[T,V], row stride ldl >= V, in fp32 or bf16 (logits_prec: HMY_PREC_*); rows may start at any element.  With a scale
  * s > 0 (an inverse temperature), m = the row's largest logit and S = sum exp(s (x_j - m)), the log probability of token j is
- * l_j = s (x_j - m) - log S, p_j = exp l_j.  Sums over a row are held in fp32, a list's terms of hmy_k_distill and what its
- * gradient's factors are made of in fp64; results do not depend on the order in which workgroups run.
+ * l_j = s (x_j - m) - log S, p_j = exp l_j.  Sums over a row are held in fp32, a list's terms of hmy_k_distill and the
+ * differences that its gradient is made of in fp64; results do not depend on the order in which workgroups run.
  *   - A logit of -inf is a token without weight: l = -inf, p = 0, in no list.  A row of nothing else has row_max = log_sum =
  *     -inf, entropy 0 and l = -inf throughout.  A row that holds a NaN or +inf has NaN results (its list still ranks the
  *     tokens that are no NaN).

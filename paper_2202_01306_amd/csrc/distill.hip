@@ -171,19 +171,21 @@ struct RowTerms {
   float m, c_list;        // the row's maximum, and what exp(s (x - m)) of a listed token is multiplied with
   float m_rest, c_rest;   // the others' maximum, and what exp(s (x - m_rest)) of any other is multiplied with
 };                        // (maxima: 0 where nothing has any weight)
-// In 64 bits: where the student is near the teacher the others' factor is a difference of nearly equal numbers.  The sums of fp32
-// that it is made of are rounded once for both.
+// The others' factor Q f / S - q_r / rest is a difference of nearly equal numbers where the student is near the teacher: it is formed
+// in 64 bits, over a common denominator so that no division is (us with two of them / as it is, 8192 rows without a tail: 300 columns
+// 14.3 / 13.9, 8000 columns 55.9 / 55.3).
 __device__ __forceinline__ RowTerms row_terms(float m_rest, float rest, const ListSum &z, const DistillArgs &a) {
   const float m = a.tail ? fmaxf(m_rest, z.max) : m_rest, f = rebase(m_rest, m, a.scale);
   const double S = double(rest) * f + (a.tail ? z.sum * rebase(z.max, m, a.scale) : 0.);
   const double q_rest = a.tail && others_weigh(m_rest, rest, m, a.scale) ? fmax(1. - z.q_sum, 0.) : 0.;
-  const double w = double(a.scale) * a.grad_scale, Q = z.q_sum + q_rest;
+  const float w = a.scale * a.grad_scale;
+  const double Q = z.q_sum + q_rest;
   RowTerms r;
   r.m = m == -INFINITY ? 0.f : m;
   r.m_rest = m_rest == -INFINITY ? 0.f : m_rest;
-  const double inv = S == 0. ? 0. : 1. / S;
-  r.c_list = float(w * (Q * inv));
-  r.c_rest = float(w * (Q * inv * f - (q_rest > 0. ? q_rest / double(rest) : 0.)));
+  const float inv = S == 0. ? 0.f : 1.f / float(S);
+  r.c_list = w * (float(Q) * inv);
+  r.c_rest = q_rest > 0. ? w * (float(Q * (double(rest) * f) - q_rest * S) / float(double(rest) * S)) : r.c_list * f;
   return r;
 }
 // by one wave, the result in all lanes
