@@ -638,6 +638,109 @@ typedef struct hmy_distill_desc {
 } hmy_distill_desc;
 int hmy_k_distill(const hmy_distill_desc *g, void *stream);
 
+/* ---- the residual stream: what goes in, what is kept of it, what its gradient goes to (all pointers DEVICE, stream as above) ----
+ * Rows of T tokens and d columns in fp32 or bf16 (HMY_PREC_*), each array with a row stride of its own (in elements, >= d) and aligned
+ * to its elements only; columns behind the d-th are left as they are.  T >= 1, 1 <= d <= 2^24.  Nothing is allocated, results do not
+ * depend on the order in which workgroups run, and every call can be captured into a graph.  Outputs overlap neither each other nor
+ * an input (HMY_E_INVALID where a call's rows do), but where it is said. */
+
+/* x[t] (type out_prec) = scale * table[ids[t]] + pos_table[positions[t]], in fp32, rounded once.  An id outside of [0, V) names no
+ * token and a position outside of [0, P) no place: their term is left out, so that a token of padding with both at -1 has a row of
+ * zeros.  pos_table NULL (P = 0): no second term; positions NULL: token t is at place t mod P.  table and pos_table have type prec. */
+typedef struct hmy_embed_lookup_desc {
+  int32_t prec, out_prec, T, d, V, P;
+  const int32_t *ids;            /* [T]                                       */
+  const void *table; int64_t ldw;
+  const int32_t *positions;      /* [T] or NULL                               */
+  const void *pos_table; int64_t ldp;
+  void *x; int64_t ldx;
+  float scale;
+  int32_t reserved_;
+} hmy_embed_lookup_desc;
+int hmy_k_embed_lookup(const hmy_embed_lookup_desc *g, void *stream);
+
+/* dtable[v] = scale * sum over the t with ids[t] = v of dx[t] (dx of type prec, dtable fp32), with the tokens sorted by id: a row's
+ * sum runs over its tokens in ascending order in pieces that ids and T alone determine, without atomics.  accumulate = 0: all V rows
+ * are written, those that no token names with zeros; 1: the sums are added to the rows that tokens name, the others are not touched.
+ * Ids outside of [0, V) name no token.  The gradient of pos_table is the same call with the positions as ids and scale 1.
+ * workspace: HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d) of device memory, aligned to 16 bytes; calls that may overlap need one each, and
+ * a captured call's is written at each replay.  Nothing in it has to be cleared.  T <= HMY_MAX_SORTED; sizes that make more than 2^24
+ * workgroups (V / 64, T d / 2^14 each below that) are HMY_E_INVALID. */
+#define HMY_MAX_SORTED (1 << 24)
+#define HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d) (65536 + 32 * (uint64_t)(T) + 8 * (uint64_t)(d) * (((uint64_t)(T) + 15) / 16))
+typedef struct hmy_embed_grad_desc {
+  int32_t prec, T, d, V;
+  const int32_t *ids;            /* [T]                                       */
+  const void *dx; int64_t ldx;
+  float *dtable; int64_t ldt;
+  void *workspace; uint64_t workspace_bytes;
+  float scale;
+  int32_t accumulate;
+} hmy_embed_grad_desc;
+int hmy_k_embed_grad(const hmy_embed_grad_desc *g, void *stream);
+
+/* Rows held in 8 bits (a checkpoint of the stream at about a byte per element): each HMY_ROWS8_GROUP columns share a power of two.
+ * With a = the group's largest magnitude and e the least integer >= -126 for which a <= top 2^e, x_j is held as q_j = x_j / 2^e, rounded to
+ * the nearest of its format's numbers, to the even one of two:
+ *   HMY_CODE_INT8  whole numbers, top = 127: off by at most 2^(e-1), which is at most a / 127 (half that at best);
+ *   HMY_CODE_E4M3  floats of four bits of exponent and three of mantissa (1-4-3, bias 7, no infinities), top = 448: off by at most
+ *                  2^-4 of the value, from 2^(e-6) on.
+ * codes[T, ldc] holds q, scales[T, lds] one byte e + 127 per group (ceil(d / HMY_ROWS8_GROUP) of them in a row, the last one of the
+ * columns that are left); strides are in bytes.  A group that holds a NaN or an infinity has the byte 255 and codes 0.
+ * Reading gives q 2^e: exactly, in fp32, and in bf16 too down to 2^-126 (a magnitude that is rounded to 2^128 reads as infinity, as
+ * it does where fp32 is rounded to bf16).  The byte 255 reads as NaN throughout and 0, which is never
+ * written, as zeros; an INT8 code of -128 and the E4M3 codes of no number, never written either, read as -128 and NaN. */
+#define HMY_CODE_INT8 0
+#define HMY_CODE_E4M3 1
+#define HMY_ROWS8_GROUP 32
+typedef struct hmy_rows8_desc {
+  int32_t prec, code, T, d;      /* prec: of x                                */
+  void *x; int64_t ldx;
+  void *codes; int64_t ldc;
+  void *scales; int64_t lds;
+} hmy_rows8_desc;
+int hmy_k_pack8(const hmy_rows8_desc *g, void *stream);    /* x -> codes, scales */
+int hmy_k_unpack8(const hmy_rows8_desc *g, void *stream);  /* codes, scales -> x */
+
+/* hmy_k_layernorm_fwd of rows that are held in 8 bits, v: y (type prec) = gamma * (v - mean) * rstd + beta with the rows' mean and
+ * rstd = 1 / sqrt(variance + eps) in fp32 ([T]; each may be NULL).  x (may be NULL): v itself, fp32, which the residual connection of a
+ * block's recomputation adds to.  gamma and beta have type prec.  eps > 0.  d <= HMY_MAX_NORM8_COLUMNS. */
+#define HMY_MAX_NORM8_COLUMNS 8192
+typedef struct hmy_layernorm8_desc {
+  int32_t prec, code, T, d;
+  const void *codes; int64_t ldc;
+  const void *scales; int64_t lds;
+  const void *gamma, *beta;
+  void *y; int64_t ldy;
+  float *x; int64_t ldx;
+  float *mean, *rstd;
+  float eps;
+  int32_t reserved_;
+} hmy_layernorm8_desc;
+int hmy_k_layernorm8_fwd(const hmy_layernorm8_desc *g, void *stream);
+
+/* hmy_k_layernorm_bwd of such rows: the gradient with respect to v (and so, straight through the rounding, to what was packed):
+ *   dx (fp32) = (res ? res : 0) + LN'(dy);  dgamma[d] = sum of dy (v - mean) rstd over the rows, dbeta[d] = sum of dy, dres_sum[d] (may be
+ * NULL; needs res) = sum of res; dx_e (may be NULL): dx rounded to type prec, as is the type of dy.  accumulate = 1 adds the three sums
+ * to what is there.  dx may be res itself (same address and stride).  mean and rstd as hmy_k_layernorm8_fwd left them.
+ * workspace: HMY_NORM8_WORKSPACE_BYTES(d) of device memory, aligned to 16 bytes, as for hmy_k_embed_grad. */
+#define HMY_NORM8_WORKSPACE_BYTES(d) ((uint64_t)256 * 3 * 4 * (uint64_t)(d))
+typedef struct hmy_layernorm8_grad_desc {
+  int32_t prec, code, T, d;
+  const void *codes; int64_t ldc;
+  const void *scales; int64_t lds;
+  const float *mean, *rstd;
+  const void *gamma;
+  const void *dy; int64_t ldy;
+  const float *res; int64_t ldr;
+  float *dx; int64_t ldx;
+  void *dx_e; int64_t lde;
+  float *dgamma, *dbeta, *dres_sum;
+  void *workspace; uint64_t workspace_bytes;
+  int32_t accumulate, reserved_;
+} hmy_layernorm8_grad_desc;
+int hmy_k_layernorm8_bwd(const hmy_layernorm8_grad_desc *g, void *stream);
+
 /* ---- the host-side update on its own (all pointers HOST, no GPU needed) ----
  * What HMY_UPDATE_ON_HOST applies to each chunk of a pack (Section 4.4, update task on
  * the CPU): the arithmetic of hmy_k_adam, in place, over n elements, on `threads` CPU

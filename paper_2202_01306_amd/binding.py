@@ -26,6 +26,20 @@ HMY_SWAP_OUT_KERNEL, HMY_SWAP_OUT_MEMCPY = 0, 1
 HMY_MAX_WEIGHT_SLOTS = 4
 HMY_MAX_TOP = 128
 HMY_ROWS_WORKSPACE_BYTES = 1 << 20
+HMY_MAX_SORTED = 1 << 24
+HMY_CODE_INT8, HMY_CODE_E4M3 = 0, 1
+HMY_ROWS8_GROUP = 32
+HMY_MAX_NORM8_COLUMNS = 8192
+
+
+def HMY_EMBED_GRAD_WORKSPACE_BYTES(T: int, d: int) -> int:
+    return 65536 + 32 * T + 8 * d * ((T + 15) // 16)
+
+
+def HMY_NORM8_WORKSPACE_BYTES(d: int) -> int:
+    return 256 * 3 * 4 * d
+
+
 (HMY_OK, HMY_E_INVALID, HMY_E_BUDGET_TOO_SMALL, HMY_E_BAD_SCHEDULE, HMY_E_HIP,
  HMY_E_NOT_BOUND, HMY_E_NO_DEVICE) = (0, -1, -2, -3, -4, -5, -6)
 
@@ -169,13 +183,47 @@ class hmy_distill_desc(C.Structure):
                 ("grad_scale", C.c_float), ("pad", C.c_int32), ("reserved_", C.c_int32)]
 
 
+class hmy_embed_lookup_desc(C.Structure):
+    _fields_ = [("prec", C.c_int32), ("out_prec", C.c_int32), ("T", C.c_int32), ("d", C.c_int32), ("V", C.c_int32), ("P", C.c_int32),
+                ("ids", C.c_void_p), ("table", C.c_void_p), ("ldw", C.c_int64), ("positions", C.c_void_p), ("pos_table", C.c_void_p),
+                ("ldp", C.c_int64), ("x", C.c_void_p), ("ldx", C.c_int64), ("scale", C.c_float), ("reserved_", C.c_int32)]
+
+
+class hmy_embed_grad_desc(C.Structure):
+    _fields_ = [("prec", C.c_int32), ("T", C.c_int32), ("d", C.c_int32), ("V", C.c_int32), ("ids", C.c_void_p),
+                ("dx", C.c_void_p), ("ldx", C.c_int64), ("dtable", C.c_void_p), ("ldt", C.c_int64), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_uint64), ("scale", C.c_float), ("accumulate", C.c_int32)]
+
+
+class hmy_rows8_desc(C.Structure):
+    _fields_ = [("prec", C.c_int32), ("code", C.c_int32), ("T", C.c_int32), ("d", C.c_int32),
+                ("x", C.c_void_p), ("ldx", C.c_int64), ("codes", C.c_void_p), ("ldc", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64)]
+
+
+class hmy_layernorm8_desc(C.Structure):
+    _fields_ = [("prec", C.c_int32), ("code", C.c_int32), ("T", C.c_int32), ("d", C.c_int32),
+                ("codes", C.c_void_p), ("ldc", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64),
+                ("gamma", C.c_void_p), ("beta", C.c_void_p), ("y", C.c_void_p), ("ldy", C.c_int64), ("x", C.c_void_p),
+                ("ldx", C.c_int64), ("mean", C.c_void_p), ("rstd", C.c_void_p), ("eps", C.c_float), ("reserved_", C.c_int32)]
+
+
+class hmy_layernorm8_grad_desc(C.Structure):
+    _fields_ = [("prec", C.c_int32), ("code", C.c_int32), ("T", C.c_int32), ("d", C.c_int32),
+                ("codes", C.c_void_p), ("ldc", C.c_int64), ("scales", C.c_void_p), ("lds", C.c_int64),
+                ("mean", C.c_void_p), ("rstd", C.c_void_p), ("gamma", C.c_void_p), ("dy", C.c_void_p), ("ldy", C.c_int64),
+                ("res", C.c_void_p), ("ldr", C.c_int64), ("dx", C.c_void_p), ("ldx", C.c_int64), ("dx_e", C.c_void_p), ("lde", C.c_int64),
+                ("dgamma", C.c_void_p), ("dbeta", C.c_void_p), ("dres_sum", C.c_void_p),
+                ("workspace", C.c_void_p), ("workspace_bytes", C.c_uint64), ("accumulate", C.c_int32), ("reserved_", C.c_int32)]
+
+
 EXPORTS = [
     "hmy_strerror", "hmy_last_error", "hmy_model_size", "hmy_layout", "hmy_profile", "hmy_plan", "hmy_estimate", "hmy_arena",
     "hmy_arena_regions", "hmy_measure_profile",
     "hmy_count_swaps", "hmy_host_alloc", "hmy_host_free", "hmy_create", "hmy_get_schedule", "hmy_bind_state", "hmy_copies_on_engines", "hmy_resident_params", "hmy_sync_state",
     "hmy_iteration", "hmy_destroy", "hmy_set_profiling", "hmy_set_progress", "hmy_set_kernel_path", "hmy_k_embed_fwd", "hmy_k_embed_bwd",
     "hmy_k_layernorm_fwd", "hmy_k_layernorm_bwd", "hmy_k_layernorm_bwd_static", "hmy_k_gelu_fwd", "hmy_k_gelu_bwd", "hmy_k_gelu_bwd_colsum", "hmy_k_colsum",
-    "hmy_k_gemm", "hmy_gemm_tiles", "hmy_k_gemm_on_tiles", "hmy_k_attn_fwd", "hmy_k_attn_bwd", "hmy_k_xent", "hmy_k_logprob", "hmy_k_logprob_bwd", "hmy_k_distill", "hmy_k_adam", "hmy_host_adam",
+    "hmy_k_gemm", "hmy_gemm_tiles", "hmy_k_gemm_on_tiles", "hmy_k_attn_fwd", "hmy_k_attn_bwd", "hmy_k_xent", "hmy_k_logprob", "hmy_k_logprob_bwd", "hmy_k_distill",
+    "hmy_k_embed_lookup", "hmy_k_embed_grad", "hmy_k_pack8", "hmy_k_unpack8", "hmy_k_layernorm8_fwd", "hmy_k_layernorm8_bwd", "hmy_k_adam", "hmy_host_adam",
 ]
 
 lib.hmy_strerror.restype = C.c_char_p
@@ -521,6 +569,49 @@ def hmy_k_distill(prec, logits_prec, logits, teacher_ids, teacher_logp, row_loss
                          _at(row_loss), _at(loss_acc), _at(dlogits), ldd, _at(workspace), _size_of(workspace, workspace_bytes),
                          scale, grad_scale, pad, 0)
     _check(lib.hmy_k_distill(C.byref(g), _p(stream)))
+
+
+def hmy_k_embed_lookup(prec, out_prec, ids, table, x, T, d, V, ldw, ldx, scale=1.0, positions=None, pos_table=None, P=0, ldp=0,
+                       stream=None):
+    """prec: type of table and pos_table; positions None: token t is at place t mod P."""
+    g = hmy_embed_lookup_desc(prec, out_prec, T, d, V, P, _at(ids), _at(table), ldw, _at(positions), _at(pos_table), ldp, _at(x),
+                              ldx, scale, 0)
+    _check(lib.hmy_k_embed_lookup(C.byref(g), _p(stream)))
+
+
+def hmy_k_embed_grad(prec, ids, dx, dtable, T, d, V, ldx, ldt, scale=1.0, accumulate=False, stream=None, workspace=None,
+                     workspace_bytes=None):
+    """prec: type of dx; workspace: a tensor of HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d), or an address with its size."""
+    g = hmy_embed_grad_desc(prec, T, d, V, _at(ids), _at(dx), ldx, _at(dtable), ldt, _at(workspace),
+                            _size_of(workspace, workspace_bytes), scale, int(accumulate))
+    _check(lib.hmy_k_embed_grad(C.byref(g), _p(stream)))
+
+
+def hmy_k_pack8(prec, code, x, codes, scales, T, d, ldx, ldc, lds, stream=None):
+    """prec: type of x; code: HMY_CODE_*; ldc and lds in bytes."""
+    g = hmy_rows8_desc(prec, code, T, d, _at(x), ldx, _at(codes), ldc, _at(scales), lds)
+    _check(lib.hmy_k_pack8(C.byref(g), _p(stream)))
+
+
+def hmy_k_unpack8(prec, code, codes, scales, x, T, d, ldc, lds, ldx, stream=None):
+    g = hmy_rows8_desc(prec, code, T, d, _at(x), ldx, _at(codes), ldc, _at(scales), lds)
+    _check(lib.hmy_k_unpack8(C.byref(g), _p(stream)))
+
+
+def hmy_k_layernorm8_fwd(prec, code, codes, scales, gamma, beta, y, mean, rstd, T, d, ldc, lds, ldy, eps, x=None, ldx=0, stream=None):
+    """prec: type of gamma, beta and y; x: optional fp32 rows as they are read; mean and rstd may be None."""
+    g = hmy_layernorm8_desc(prec, code, T, d, _at(codes), ldc, _at(scales), lds, _at(gamma), _at(beta), _at(y), ldy, _at(x), ldx,
+                            _at(mean), _at(rstd), eps, 0)
+    _check(lib.hmy_k_layernorm8_fwd(C.byref(g), _p(stream)))
+
+
+def hmy_k_layernorm8_bwd(prec, code, dy, codes, scales, mean, rstd, gamma, dx, dgamma, dbeta, T, d, ldc, lds, ldy, ldx, res=None,
+                         ldr=0, dx_e=None, lde=0, dres_sum=None, accumulate=False, stream=None, workspace=None, workspace_bytes=None):
+    """prec: type of dy, gamma and dx_e; workspace: a tensor of HMY_NORM8_WORKSPACE_BYTES(d), or an address with its size."""
+    g = hmy_layernorm8_grad_desc(prec, code, T, d, _at(codes), ldc, _at(scales), lds, _at(mean), _at(rstd), _at(gamma), _at(dy), ldy,
+                                 _at(res), ldr, _at(dx), ldx, _at(dx_e), lde, _at(dgamma), _at(dbeta), _at(dres_sum), _at(workspace),
+                                 _size_of(workspace, workspace_bytes), int(accumulate), 0)
+    _check(lib.hmy_k_layernorm8_bwd(C.byref(g), _p(stream)))
 
 
 def hmy_host_adam(prec, grad_ptr, master_ptr, m_ptr, v_ptr, weights_ptr, n, lr, beta1, beta2, eps, step, threads=0):

@@ -277,6 +277,31 @@ int hmy_k_distill(const hmy_distill_desc *g, void *stream) {
   NOTNULL(g); NOTNULL(g->logits); NOTNULL(g->teacher_ids); NOTNULL(g->teacher_logp); NOTNULL(g->row_loss);
   return launch_distill(*g, stream);
 }
+int hmy_k_embed_lookup(const hmy_embed_lookup_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->ids); NOTNULL(g->table); NOTNULL(g->x);
+  return launch_embed_lookup(*g, stream);
+}
+int hmy_k_embed_grad(const hmy_embed_grad_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->ids); NOTNULL(g->dx); NOTNULL(g->dtable); NOTNULL(g->workspace);
+  return launch_embed_grad(*g, stream);
+}
+int hmy_k_pack8(const hmy_rows8_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->x); NOTNULL(g->codes); NOTNULL(g->scales);
+  return launch_pack8(*g, stream);
+}
+int hmy_k_unpack8(const hmy_rows8_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->x); NOTNULL(g->codes); NOTNULL(g->scales);
+  return launch_unpack8(*g, stream);
+}
+int hmy_k_layernorm8_fwd(const hmy_layernorm8_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->codes); NOTNULL(g->scales); NOTNULL(g->gamma); NOTNULL(g->beta); NOTNULL(g->y);
+  return launch_layernorm8_fwd(*g, stream);
+}
+int hmy_k_layernorm8_bwd(const hmy_layernorm8_grad_desc *g, void *stream) {
+  NOTNULL(g); NOTNULL(g->codes); NOTNULL(g->scales); NOTNULL(g->mean); NOTNULL(g->rstd); NOTNULL(g->gamma); NOTNULL(g->dy);
+  NOTNULL(g->dx); NOTNULL(g->dgamma); NOTNULL(g->dbeta); NOTNULL(g->workspace);
+  return launch_layernorm8_bwd(*g, stream);
+}
 int hmy_k_adam(int32_t prec, const float *grad, float *master, float *m, float *v, void *w_out, uint64_t n,
                const hmy_adam *hp, void *stream) {
   NOTNULL(grad); NOTNULL(m); NOTNULL(v); NOTNULL(w_out); NOTNULL(hp);

@@ -193,6 +193,12 @@ int launch_xent(int prec, const float *logits, const int32_t *targets, double *l
 int launch_logprob(const hmy_logprob_desc &g, stream_t st);
 int launch_logprob_bwd(const hmy_logprob_grad_desc &g, stream_t st);
 int launch_distill(const hmy_distill_desc &g, stream_t st);
+int launch_embed_lookup(const hmy_embed_lookup_desc &g, stream_t st);
+int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st);
+int launch_pack8(const hmy_rows8_desc &g, stream_t st);
+int launch_unpack8(const hmy_rows8_desc &g, stream_t st);
+int launch_layernorm8_fwd(const hmy_layernorm8_desc &g, stream_t st);
+int launch_layernorm8_bwd(const hmy_layernorm8_grad_desc &g, stream_t st);
 int launch_adam(int prec, const float *grad, float *master, float *m, float *v, void *w_out,
                 uint64_t n, const hmy_adam &hp, stream_t st);
 int launch_adam_out(int prec, const float *grad, const float *in_master, const float *in_m, const float *in_v,

@@ -1,0 +1,517 @@
+// Rows of the residual stream held in 8 bits with a power of two for each 32 columns, and the layer norm that reads them.
+//
+// A power of two as the scale makes every step but the one rounding exact: x 2^-e and q 2^e change no digit, so that what is read is
+// the same on every path, an 8-bit integer times a scale is a bf16 number as it stands, and a scale is one byte, which pays for groups
+// of 32 columns (3 % more bytes) where 32-bit scales would want 128.  What it costs is up to one bit of an INT8 group's range.
+// All kernels here are bound by HBM: 5.03 bytes per element for fp32 rows to or from 8 bits.
+#include <algorithm>
+
+#include "stream_rows.h"
+
+namespace hmy {
+
+namespace {
+
+constexpr int kGroup = HMY_ROWS8_GROUP;
+constexpr int kLanesPerGroup = kGroup / 8;
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_by1 __attribute__((aligned(1)));
+
+struct Rows8 {
+  const uint8_t *codes, *scales;
+  int64_t ldc, lds;
+};
+
+// The largest of four neighbouring lanes' values.
+__device__ __forceinline__ uint32_t quad_top(uint32_t x) {
+  x = max(x, uint32_t(__builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, false)));   // from lane ^ 1
+  x = max(x, uint32_t(__builtin_amdgcn_update_dpp(0, x, 0x4e, 0xf, 0xf, false)));   // from lane ^ 2
+  return x;
+}
+
+// The scale's byte for a group whose largest magnitude has these bits, e + 127 for the least e >= -126 with a <= top 2^e.  The
+// exponent's field of a, one more where the mantissa is above top's: an addition that carries into the field says so.
+template <int CODE> __device__ __forceinline__ uint32_t scale_byte(uint32_t a) {
+  constexpr uint32_t kCarry = CODE == HMY_CODE_INT8 ? 0x01ffffu : 0x1fffffu;   // 0x7fffff less the mantissa of 127, of 448
+  constexpr int kTop = CODE == HMY_CODE_INT8 ? 6 : 8;                          // their exponents
+  const int e = int((a + kCarry) >> 23) - kTop;
+  return a >= 0x7f800000u ? 255u : uint32_t(max(e, 1));
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return byte == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(byte << 23); }
+
+// Four columns to four codes.  INT8: adding 1.5 2^23 leaves the whole number, rounded to nearest even, in the sum's last bits, and the
+// multiply-add rounds once.
+template <int CODE> __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float inv) {
+  if constexpr (CODE == HMY_CODE_INT8) {
+    constexpr float kWhole = 12582912.f;
+    const uint32_t ia = __float_as_uint(fmaf(a, inv, kWhole)), ib = __float_as_uint(fmaf(b, inv, kWhole));
+    const uint32_t ic = __float_as_uint(fmaf(c, inv, kWhole)), id = __float_as_uint(fmaf(d, inv, kWhole));
+    const uint32_t lo = __builtin_amdgcn_perm(ib, ia, 0x0c0c0400u), hi = __builtin_amdgcn_perm(id, ic, 0x04000c0cu);
+    return lo | hi;
+  } else {
+    uint32_t w = __builtin_amdgcn_cvt_pk_fp8_f32(a * inv, b * inv, 0, false);
+    return __builtin_amdgcn_cvt_pk_fp8_f32(c * inv, d * inv, w, true);
+  }
+}
+template <int CODE> __device__ __forceinline__ void decode4(uint32_t w, float s, float *v) {
+  if constexpr (CODE == HMY_CODE_INT8) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = float(int8_t(w >> (8 * k))) * s;
+  } else {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+    v[0] = lo[0] * s;
+    v[1] = lo[1] * s;
+    v[2] = hi[0] * s;
+    v[3] = hi[1] * s;
+  }
+}
+
+// The first n of eight codes from p on.
+__device__ __forceinline__ u32x2 load_codes(const uint8_t *p, int n) {
+  if (n >= 8) return *reinterpret_cast<const u32x2_by1 *>(p);
+  u32x2 w = {0, 0};
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (k < n) w[k / 4] |= uint32_t(p[k]) << (8 * (k % 4));
+  return w;
+}
+__device__ __forceinline__ void store_codes(uint8_t *p, u32x2 w, int n) {
+  if (n >= 8) {
+    *reinterpret_cast<u32x2_by1 *>(p) = w;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < n) p[k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
+  }
+}
+// Eight columns of a row, from column c on, of which n exist; zeros behind them.
+template <int CODE> __device__ __forceinline__ void decode(u32x2 w, uint32_t byte, float (&v)[8]) {
+  const float s = scale_of(byte);
+  decode4<CODE>(w[0], s, v);
+  decode4<CODE>(w[1], s, v + 4);
+}
+
+// Rows are worked through as units of eight columns, rounded up to whole groups, numbered row by row: a workgroup takes kUnits of
+// them, and finds the row of each by one 32-bit division from that of its first.
+constexpr int kThreads = 256, kPerThread = 2, kUnits = kThreads * kPerThread;
+
+struct Units {
+  int d;
+  uint32_t per_row;
+  int64_t total, tiles;
+};
+inline Units units_of(int T, int d) {
+  Units u;
+  u.d = d;
+  u.per_row = uint32_t((d + kGroup - 1) / kGroup * kLanesPerGroup);
+  u.total = int64_t(T) * u.per_row;
+  u.tiles = (u.total + kUnits - 1) / kUnits;
+  return u;
+}
+
+template <typename E, int CODE>
+__global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, Units g) {
+  for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
+    const int64_t row0 = tile * kUnits / g.per_row;
+    const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
+    float v[kPerThread][8];
+    int64_t row[kPerThread];
+    int c[kPerThread], n[kPerThread];
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
+      row[i] = row0 + down;
+      c[i] = int(at - down * g.per_row) * 8;
+      n[i] = tile * kUnits + threadIdx.x + i * kThreads < g.total ? g.d - c[i] : -1;
+      load_columns(v[i], x + row[i] * ldx + c[i], n[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      uint32_t a = 0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) a = max(a, __float_as_uint(v[i][k]) & 0x7fffffffu);
+      a = quad_top(a);
+      const uint32_t byte = scale_byte<CODE>(a);
+      const float inv = __uint_as_float((254u - byte) << 23);
+      u32x2 w;
+      w[0] = encode4<CODE>(v[i][0], v[i][1], v[i][2], v[i][3], inv);
+      w[1] = encode4<CODE>(v[i][4], v[i][5], v[i][6], v[i][7], inv);
+      if (byte == 255u) w = 0;
+      store_codes(codes + row[i] * ldc + c[i], w, n[i]);
+      if (n[i] > 0 && c[i] % kGroup == 0) scales[row[i] * lds + c[i] / kGroup] = uint8_t(byte);
+    }
+  }
+}
+
+template <typename E, int CODE>
+__global__ __launch_bounds__(kThreads) void k_unpack8(Rows8 r, E *x, int64_t ldx, Units g) {
+  for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
+    const int64_t row0 = tile * kUnits / g.per_row;
+    const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
+    int64_t row[kPerThread];
+    int c[kPerThread], n[kPerThread];
+    u32x2 w[kPerThread];
+    uint32_t byte[kPerThread];
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
+      row[i] = row0 + down;
+      c[i] = int(at - down * g.per_row) * 8;
+      n[i] = tile * kUnits + threadIdx.x + i * kThreads < g.total ? g.d - c[i] : -1;
+      w[i] = load_codes(r.codes + row[i] * r.ldc + c[i], n[i]);
+      byte[i] = n[i] > 0 ? r.scales[row[i] * r.lds + c[i] / kGroup] : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      float v[8];
+      decode<CODE>(w[i], byte[i], v);
+      store_columns(x + row[i] * ldx + c[i], v, n[i]);
+    }
+  }
+}
+
+// ---- layer norm of rows in 8 bits -------------------------------------------------------------
+
+// A row is W waves', NJ units of eight columns a lane: wave w of it has columns 512 NJ w + 8 (lane + 64 j).  Sums over a row: within the
+// wave by lane moves, between waves through LDS, added in the same order by each of them.
+template <int W, int N> __device__ __forceinline__ void row_sums(float (&s)[N], float (*xch)[N], int wave) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) s[i] = wave_total(s[i]);
+  if constexpr (W > 1) {
+    if (threadIdx.x % kWave == 0)
+#pragma unroll
+      for (int i = 0; i < N; ++i) xch[wave][i] = s[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      s[i] = 0.f;
+#pragma unroll
+      for (int w = 0; w < W; ++w) s[i] += xch[wave / W * W + w][i];
+    }
+  }
+}
+
+struct Norm8 {
+  Rows8 r;
+  int T, d;
+  int64_t ldy, ldx;
+  float *mean, *rstd;
+  float eps;
+};
+
+template <typename E, int CODE, int W, int NJ>
+__global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma, const E *beta, E *y, float *x) {
+  constexpr int kSlots = 4 / W;
+  __shared__ float xch[2][2][4][1];   // of a round's two sums, and of the round before, which a wave may still read
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col0 = wave % W * NJ * 512 + 8 * lane;
+  int parity = 0;
+  for (int64_t base = int64_t(blockIdx.x) * kSlots; base < g.T; base += int64_t(gridDim.x) * kSlots, parity ^= 1) {
+    const int64_t row = base + wave / W;
+    const bool live = row < g.T;
+    float v[NJ][8], s[1] = {0.f};
+    u32x2 w[NJ];
+    uint32_t byte[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = col0 + 512 * j, n = live ? g.d - c : 0;
+      w[j] = load_codes(g.r.codes + row * g.r.ldc + c, n);
+      byte[j] = n > 0 ? g.r.scales[row * g.r.lds + c / kGroup] : 0;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      decode<CODE>(w[j], byte[j], v[j]);
+      const int n = g.d - (col0 + 512 * j);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[0] += k < n ? v[j][k] : 0.f;
+    }
+    row_sums<W>(s, xch[parity][0], wave);
+    const float mu = s[0] / float(g.d);
+    s[0] = 0.f;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int n = g.d - (col0 + 512 * j);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float t = v[j][k] - mu;
+        s[0] += k < n ? t * t : 0.f;
+      }
+    }
+    row_sums<W>(s, xch[parity][1], wave);
+    const float rs = 1.f / sqrtf(s[0] / float(g.d) + g.eps);
+    if (!live) continue;
+    if (lane == 0 && wave % W == 0) {
+      if (g.mean) g.mean[row] = mu;
+      if (g.rstd) g.rstd[row] = rs;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = col0 + 512 * j, n = g.d - c;
+      if (n > 0) {
+        float ga[8], be[8], o[8];
+        load_columns(ga, gamma + c, n);
+        load_columns(be, beta + c, n);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = fmaf(ga[k], (v[j][k] - mu) * rs, be[k]);
+        store_columns(y + row * g.ldy + c, o, n);
+        if (x) store_columns(x + row * g.ldx + c, v[j], n);
+      }
+    }
+  }
+}
+
+struct Norm8Grad {
+  Rows8 r;
+  int T, d;
+  int64_t ldy, ldr, ldx, lde;
+  const float *mean, *rstd;
+  const float *res;
+  float *dx;
+  float *sums[3];   // dgamma, dbeta, dres_sum
+  float *partial;
+  int accumulate;
+};
+
+// The rows of a workgroup's slots leave their column sums in registers; at the end the slots' meet in LDS and one row of sums per
+// workgroup goes to the workspace.
+template <typename E, int CODE, int W, int NJ>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_layernorm8_bwd(Norm8Grad g, const E *dy, const E *gamma, E *dx_e) {
+  constexpr int kWaves = 8, kSlots = kWaves / W;
+  extern __shared__ __align__(16) float lds[];   // kSlots > 1: per slot its sums' ns rows of d floats
+  __shared__ float xch[2][kWaves][2];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, slot = wave / W, col0 = wave % W * NJ * 512 + 8 * lane;
+  const int ns = g.sums[2] ? 3 : 2;
+  float ga[NJ][8], dg[NJ][8], db[NJ][8], dr[NJ][8];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    load_columns(ga[j], gamma + col0 + 512 * j, g.d - (col0 + 512 * j));
+#pragma unroll
+    for (int k = 0; k < 8; ++k) dg[j][k] = db[j][k] = dr[j][k] = 0.f;
+  }
+  int parity = 0;
+  for (int64_t base = int64_t(blockIdx.x) * kSlots; base < g.T; base += int64_t(gridDim.x) * kSlots, parity ^= 1) {
+    const int64_t row = base + slot;
+    const bool live = row < g.T;
+    const float mu = live ? g.mean[row] : 0.f, rs = live ? g.rstd[row] : 0.f;
+    float xh[NJ][8], gy[NJ][8], s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = col0 + 512 * j, n = live ? g.d - c : 0;
+      const u32x2 w = load_codes(g.r.codes + row * g.r.ldc + c, n);
+      const uint32_t byte = n > 0 ? g.r.scales[row * g.r.lds + c / kGroup] : 0;
+      load_columns(gy[j], dy + row * g.ldy + c, n);
+      decode<CODE>(w, byte, xh[j]);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        xh[j][k] = (xh[j][k] - mu) * rs;
+        if (k >= n) xh[j][k] = 0.f;
+        const float t = gy[j][k] * ga[j][k];
+        s[0] += t;
+        s[1] = fmaf(t, xh[j][k], s[1]);
+        dg[j][k] = fmaf(gy[j][k], xh[j][k], dg[j][k]);
+        db[j][k] += gy[j][k];
+      }
+    }
+    row_sums<W>(s, xch[parity], wave);
+    if (!live) continue;
+    const float m1 = s[0] / float(g.d), m2 = s[1] / float(g.d);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const int c = col0 + 512 * j, n = g.d - c;
+      if (n > 0) {
+        float o[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) o[k] = (gy[j][k] * ga[j][k] - m1 - xh[j][k] * m2) * rs;
+        if (g.res) {
+          float rv[8];
+          load_columns(rv, g.res + row * g.ldr + c, n);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            o[k] += rv[k];
+            dr[j][k] += rv[k];
+          }
+        }
+        store_columns(g.dx + row * g.ldx + c, o, n);
+        if (dx_e) store_columns(dx_e + row * g.lde + c, o, n);
+      }
+    }
+  }
+  float *out = g.partial + int64_t(blockIdx.x) * ns * g.d;
+  float *mine = kSlots > 1 ? lds + int64_t(slot) * ns * g.d : out;
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    const int c = col0 + 512 * j, n = g.d - c;
+    if (n > 0) {
+      store_columns(mine + c, dg[j], n);
+      store_columns(mine + g.d + c, db[j], n);
+      if (ns == 3) store_columns(mine + 2 * g.d + c, dr[j], n);
+    }
+  }
+  if constexpr (kSlots > 1) {
+    __syncthreads();
+    for (int c = threadIdx.x; c < ns * g.d; c += 512) {
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < kSlots; ++i) t += lds[int64_t(i) * ns * g.d + c];
+      out[c] = t;
+    }
+  }
+}
+
+// Sums of the workgroups' rows: 64 columns a workgroup, its 16 waves taking every 16th row, joined in one order.
+__global__ __launch_bounds__(1024) void k_layernorm8_sums(Norm8Grad g, int rows) {
+  __shared__ float part[16][64];
+  const int ns = g.sums[2] ? 3 : 2, lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const int c = blockIdx.x * 64 + lane, width = ns * g.d;
+  float t = 0.f;
+  if (c < width) {
+    float v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = wave + 16 * i < rows ? g.partial[int64_t(wave + 16 * i) * width + c] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t += v[i];
+  }
+  part[wave][lane] = t;
+  __syncthreads();
+  if (wave == 0 && c < width) {
+    t = 0.f;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) t += part[w][lane];
+    float *out = g.sums[c / g.d] + c % g.d;
+    *out = g.accumulate ? *out + t : t;
+  }
+}
+
+constexpr int kGradGroups = 256;   // workgroups of a backward pass: rows of the workspace
+
+int check_rows8(const char *who, int prec, int code, int T, int d, int most, const void *codes, int64_t ldc, const void *scales, int64_t lds) {
+  if (!known_prec(prec)) return fail(HMY_E_INVALID, "%s: unknown precision %d", who, prec);
+  if (code != HMY_CODE_INT8 && code != HMY_CODE_E4M3) return fail(HMY_E_INVALID, "%s: unknown code %d", who, code);
+  int rc = check_extent(who, T, d, most);
+  if (!rc) rc = check_array(who, "codes", codes, 1, T, d, ldc);
+  if (!rc) rc = check_array(who, "scales", scales, 1, T, (d + kGroup - 1) / kGroup, lds);
+  return rc;
+}
+Span span(const char *name, const void *p, int64_t bytes, int64_t T, int64_t d, int64_t ld, bool written) { return {name, p, d * bytes, ld * bytes, T, written}; }
+
+}  // namespace
+
+#define DISPATCH_ROWS8(prec, code, ...)                                                                            \
+  do {                                                                                                             \
+    if ((prec) == HMY_PREC_BF16) {                                                                                 \
+      typedef bf16_t E;                                                                                            \
+      if ((code) == HMY_CODE_INT8) { constexpr int CODE = HMY_CODE_INT8; __VA_ARGS__ } else { constexpr int CODE = HMY_CODE_E4M3; __VA_ARGS__ } \
+    } else {                                                                                                       \
+      typedef float E;                                                                                             \
+      if ((code) == HMY_CODE_INT8) { constexpr int CODE = HMY_CODE_INT8; __VA_ARGS__ } else { constexpr int CODE = HMY_CODE_E4M3; __VA_ARGS__ } \
+    }                                                                                                              \
+  } while (0)
+
+static int check_move8(const char *who, const hmy_rows8_desc &g, bool pack) {
+  int rc = check_rows8(who, g.prec, g.code, g.T, g.d, kMaxColumns, g.codes, g.ldc, g.scales, g.lds);
+  const int e = bytes_of(g.prec);
+  if (!rc) rc = check_array(who, "x", g.x, e, g.T, g.d, g.ldx);
+  if (rc) return rc;
+  const Span spans[] = {span("x", g.x, e, g.T, g.d, g.ldx, !pack), span("codes", g.codes, 1, g.T, g.d, g.ldc, pack),
+                        span("scales", g.scales, 1, g.T, (g.d + kGroup - 1) / kGroup, g.lds, pack)};
+  return check_apart(who, spans);
+}
+
+int launch_pack8(const hmy_rows8_desc &g, stream_t st) {
+  const int rc = check_move8("pack8", g, true);
+  if (rc) return rc;
+  const Units u = units_of(g.T, g.d);
+  const dim3 grid(uint32_t(std::min<int64_t>(u.tiles, kMaxGrid)));
+  DISPATCH_ROWS8(g.prec, g.code, {
+    hipLaunchKernelGGL((k_pack8<E, CODE>), grid, dim3(kThreads), 0, (hipStream_t)st, (const E *)g.x, g.ldx, (uint8_t *)g.codes, g.ldc,
+                       (uint8_t *)g.scales, g.lds, u);
+  });
+  return check_launch("pack8");
+}
+
+int launch_unpack8(const hmy_rows8_desc &g, stream_t st) {
+  const int rc = check_move8("unpack8", g, false);
+  if (rc) return rc;
+  const Units u = units_of(g.T, g.d);
+  const Rows8 r = {(const uint8_t *)g.codes, (const uint8_t *)g.scales, g.ldc, g.lds};
+  const dim3 grid(uint32_t(std::min<int64_t>(u.tiles, kMaxGrid)));
+  DISPATCH_ROWS8(g.prec, g.code, { hipLaunchKernelGGL((k_unpack8<E, CODE>), grid, dim3(kThreads), 0, (hipStream_t)st, r, (E *)g.x, g.ldx, u); });
+  return check_launch("unpack8");
+}
+
+int launch_layernorm8_fwd(const hmy_layernorm8_desc &g, stream_t st) {
+  const char *who = "layernorm8_fwd";
+  int rc = check_rows8(who, g.prec, g.code, g.T, g.d, HMY_MAX_NORM8_COLUMNS, g.codes, g.ldc, g.scales, g.lds);
+  const int e = bytes_of(g.prec);
+  if (!rc) rc = check_array(who, "y", g.y, e, g.T, g.d, g.ldy);
+  if (!rc && g.x) rc = check_array(who, "x", g.x, 4, g.T, g.d, g.ldx);
+  if (rc) return rc;
+  if (!(g.eps > 0.f) || !std::isfinite(g.eps)) return fail(HMY_E_INVALID, "%s: eps must be positive and finite", who);
+  if (misaligned(g.gamma, e) || misaligned(g.beta, e) || misaligned(g.mean, 4) || misaligned(g.rstd, 4))
+    return fail(HMY_E_INVALID, "%s: misaligned array", who);
+  const Span spans[] = {span("codes", g.codes, 1, g.T, g.d, g.ldc, false), span("scales", g.scales, 1, g.T, (g.d + kGroup - 1) / kGroup, g.lds, false),
+                        span("gamma", g.gamma, e, 1, g.d, g.d, false), span("beta", g.beta, e, 1, g.d, g.d, false), span("y", g.y, e, g.T, g.d, g.ldy, true),
+                        span("x", g.x, 4, g.T, g.d, g.ldx, true), span("mean", g.mean, 4, 1, g.T, g.T, true), span("rstd", g.rstd, 4, 1, g.T, g.T, true)};
+  rc = check_apart(who, spans);
+  if (rc) return rc;
+  const Norm8 a = {{(const uint8_t *)g.codes, (const uint8_t *)g.scales, g.ldc, g.lds}, g.T, g.d, g.ldy, g.ldx, g.mean, g.rstd, g.eps};
+  const int slots = g.d <= 2048 ? 4 : 1;
+  const dim3 grid(uint32_t(std::min<int64_t>((int64_t(g.T) + slots - 1) / slots, kMaxGrid)));
+  const hipStream_t s = (hipStream_t)st;
+#define NORM8_FWD(W, NJ) hipLaunchKernelGGL((k_layernorm8_fwd<E, CODE, W, NJ>), grid, dim3(256), 0, s, a, (const E *)g.gamma, (const E *)g.beta, (E *)g.y, g.x)
+  DISPATCH_ROWS8(g.prec, g.code, {
+    if (g.d <= 512) NORM8_FWD(1, 1);
+    else if (g.d <= 1024) NORM8_FWD(1, 2);
+    else if (g.d <= 2048) NORM8_FWD(1, 4);
+    else if (g.d <= 4096) NORM8_FWD(4, 2);
+    else NORM8_FWD(4, 4);
+  });
+#undef NORM8_FWD
+  return check_launch(who);
+}
+
+int launch_layernorm8_bwd(const hmy_layernorm8_grad_desc &g, stream_t st) {
+  const char *who = "layernorm8_bwd";
+  int rc = check_rows8(who, g.prec, g.code, g.T, g.d, HMY_MAX_NORM8_COLUMNS, g.codes, g.ldc, g.scales, g.lds);
+  const int e = bytes_of(g.prec);
+  if (!rc) rc = check_array(who, "dy", g.dy, e, g.T, g.d, g.ldy);
+  if (!rc) rc = check_array(who, "dx", g.dx, 4, g.T, g.d, g.ldx);
+  if (!rc && g.res) rc = check_array(who, "res", g.res, 4, g.T, g.d, g.ldr);
+  if (!rc && g.dx_e) rc = check_array(who, "dx_e", g.dx_e, e, g.T, g.d, g.lde);
+  if (rc) return rc;
+  if (g.accumulate != 0 && g.accumulate != 1) return fail(HMY_E_INVALID, "%s: accumulate must be 0 or 1", who);
+  if (g.dres_sum && !g.res) return fail(HMY_E_INVALID, "%s: column sums of a residual gradient that is not given", who);
+  if (g.workspace_bytes < HMY_NORM8_WORKSPACE_BYTES(g.d) || misaligned(g.workspace, 16))
+    return fail(HMY_E_INVALID, "%s: a workspace of %llu bytes, aligned to 16, wanted", who, (unsigned long long)HMY_NORM8_WORKSPACE_BYTES(g.d));
+  const void *words[] = {g.mean, g.rstd, g.dgamma, g.dbeta, g.dres_sum};
+  for (const void *p : words)
+    if (misaligned(p, 4)) return fail(HMY_E_INVALID, "%s: misaligned array", who);
+  if (misaligned(g.gamma, e)) return fail(HMY_E_INVALID, "%s: misaligned array", who);
+  const bool in_place = g.res == g.dx && g.ldr == g.ldx;
+  const Span spans[] = {span("codes", g.codes, 1, g.T, g.d, g.ldc, false), span("scales", g.scales, 1, g.T, (g.d + kGroup - 1) / kGroup, g.lds, false),
+                        span("gamma", g.gamma, e, 1, g.d, g.d, false), span("mean", g.mean, 4, 1, g.T, g.T, false), span("rstd", g.rstd, 4, 1, g.T, g.T, false),
+                        span("dy", g.dy, e, g.T, g.d, g.ldy, false), span("res", in_place ? nullptr : g.res, 4, g.T, g.d, g.ldr, false),
+                        span("dx", g.dx, 4, g.T, g.d, g.ldx, true), span("dx_e", g.dx_e, e, g.T, g.d, g.lde, true), span("dgamma", g.dgamma, 4, 1, g.d, g.d, true),
+                        span("dbeta", g.dbeta, 4, 1, g.d, g.d, true), span("dres_sum", g.dres_sum, 4, 1, g.d, g.d, true),
+                        span("workspace", g.workspace, 1, 1, int64_t(HMY_NORM8_WORKSPACE_BYTES(g.d)), int64_t(HMY_NORM8_WORKSPACE_BYTES(g.d)), true)};
+  rc = check_apart(who, spans);
+  if (rc) return rc;
+  const Norm8Grad a = {{(const uint8_t *)g.codes, (const uint8_t *)g.scales, g.ldc, g.lds}, g.T, g.d, g.ldy, g.ldr, g.ldx, g.lde, g.mean, g.rstd, g.res, g.dx,
+                       {g.dgamma, g.dbeta, g.dres_sum}, (float *)g.workspace, g.accumulate};
+  const int W = g.d <= 1024 ? 1 : g.d <= 2048 ? 2 : g.d <= 4096 ? 4 : 8, slots = 8 / W, ns = g.dres_sum ? 3 : 2;
+  const int groups = int(std::min<int64_t>((int64_t(g.T) + slots - 1) / slots, kGradGroups));
+  const size_t lds = slots > 1 ? size_t(slots) * ns * g.d * 4 : 0;
+  const hipStream_t s = (hipStream_t)st;
+#define NORM8_BWD(W, NJ) hipLaunchKernelGGL((k_layernorm8_bwd<E, CODE, W, NJ>), dim3(groups), dim3(512), lds, s, a, (const E *)g.dy, (const E *)g.gamma, (E *)g.dx_e)
+  DISPATCH_ROWS8(g.prec, g.code, {
+    if (g.d <= 512) NORM8_BWD(1, 1);
+    else if (g.d <= 1024) NORM8_BWD(1, 2);
+    else if (g.d <= 2048) NORM8_BWD(2, 2);
+    else if (g.d <= 4096) NORM8_BWD(4, 2);
+    else NORM8_BWD(8, 2);
+  });
+#undef NORM8_BWD
+  hipLaunchKernelGGL(k_layernorm8_sums, dim3((ns * g.d + 63) / 64), dim3(1024), 0, s, a, groups);
+  return check_launch(who);
+}
+
+}  // namespace hmy
