@@ -14,7 +14,7 @@ namespace {
 
 // ---- lookup -------------------------------------------------------------------------------------
 
-constexpr int kThreads = 256, kPerThread = 2, kUnits = kThreads * kPerThread;
+constexpr int kThreads = 256, kPerThread = 4, kUnits = kThreads * kPerThread;
 
 struct Lookup {
   const int32_t *ids, *positions;
@@ -24,35 +24,47 @@ struct Lookup {
   float scale;
 };
 
-template <typename E, typename O>
+// Units are numbered row by row, a workgroup takes kUnits of them.  A token's row is found through its id, so that a lane waits twice
+// for memory before it stores: all of its ids are on their way together, and then all of its rows.
+template <typename E, typename O, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *table, const E *pos_table, O *x) {
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
     const int64_t row0 = tile * kUnits / g.per_row;
     const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
+    Unit u[kPerThread];
+    int64_t t[kPerThread];
+    int id[kPerThread], place[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
+      const bool there = tile * kUnits + threadIdx.x + i * kThreads < g.total;
       const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
-      if (tile * kUnits + threadIdx.x + i * kThreads >= g.total) continue;
-      const int64_t t = row0 + down;
-      const int c = int(at - down * g.per_row) * 8, n = g.d - c;
-      const int id = g.ids[t];
-      float v[8] = {}, p[8] = {};
-      if (uint32_t(id) < uint32_t(g.V)) load_columns(v, table + id * g.ldw + c, n);
-      if (g.P) {
-        const int place = g.positions ? g.positions[t] : int(t % g.P);
-        if (uint32_t(place) < uint32_t(g.P)) load_columns(p, pos_table + place * g.ldp + c, n);
-      }
+      u[i] = unit_at<NARROW>(int(at - down * g.per_row) * 8, g.d);
+      if (!there) u[i].skip = 8;
+      t[i] = there ? row0 + down : row0;
+      id[i] = g.ids[t[i]];
+      place[i] = -1;
+      if (g.positions) place[i] = g.positions[t[i]];
+      else if (g.P) place[i] = int(uint32_t(t[i]) % uint32_t(g.P));
+    }
+    Eight<E> v[kPerThread], p[kPerThread];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = fmaf(v[k], g.scale, p[k]);
-      store_columns(x + t * g.ldx + c, v, n);
+    for (int i = 0; i < kPerThread; ++i) {   // what names no row reads the first one and drops it
+      load_unit<NARROW>(v[i], table + (uint32_t(id[i]) < uint32_t(g.V) ? id[i] : 0) * g.ldw, u[i], g.d);
+      if (g.P) load_unit<NARROW>(p[i], pos_table + (uint32_t(place[i]) < uint32_t(g.P) ? place[i] : 0) * g.ldp, u[i], g.d);
+    }
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      const bool named = uint32_t(id[i]) < uint32_t(g.V), placed = uint32_t(place[i]) < uint32_t(g.P);
+      float o[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] = fmaf(named ? v[i].at(k) : 0.f, g.scale, placed ? p[i].at(k) : 0.f);
+      store_unit<NARROW>(x + t[i] * g.ldx, o, u[i], g.d);
     }
   }
 }
 
 // ---- sort -----------------------------------------------------------------------------------------
-// Stable sorting by eight bits of the key at a time, least ones first.  A wave takes 64 tokens at a time: the lanes that share a digit
-// find each other by eight ballots, which gives each its rank among them, and the first of them advances the digit's counter, so that
-// counters are a wave's own and need no atomics.  Tokens that name no row have the key V and end up last.
+// Tokens that name no row have the key V and end up last.
 
 constexpr int kDigits = 256;
 
@@ -98,71 +110,44 @@ __device__ __forceinline__ uint32_t digits_before(uint32_t x, uint32_t *scratch)
   return s;
 }
 
-// All of it in one workgroup's LDS: up to kOneGroup tokens.
-constexpr int kOneGroup = 16384, kSortWaves = 16;
+// Up to kMostRanked tokens: a token's place is the number of tokens before it in the order, counted by comparing it with all of them.  A
+// workgroup places 64 tokens, one a lane, and its waves share the tokens to compare with, 64 at a time; a comparison and an addition with
+// carry for 64 pairs, with the other token's key in a scalar register.
+constexpr int kMostRanked = 8192, kRankWaves = 16;
 
-__global__ __launch_bounds__(kSortWaves *kWave) void k_sort_tokens(const int32_t *ids, int T, int V, int passes, uint32_t *keys, uint32_t *order) {
-  extern __shared__ uint32_t lds[];   // keys[T], and two lists of T tokens in 16 bits
-  __shared__ uint16_t at[kSortWaves][kDigits];
-  __shared__ uint32_t scratch[kDigits / kWave];
-  uint32_t *key = lds;
-  uint16_t *from = reinterpret_cast<uint16_t *>(lds + T), *to = from + T;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  for (int i = tid; i < T; i += kSortWaves * kWave) key[i] = key_of(ids[i], V);
-  const int per = (T + kSortWaves * kWave - 1) / (kSortWaves * kWave) * kWave, begin = wave * per, end = min(T, begin + per);
-  const uint64_t before = (uint64_t(1) << lane) - 1;
+__global__ __launch_bounds__(kRankWaves *kWave) void k_rank_tokens(const int32_t *__restrict__ ids, int T, int V, uint32_t *__restrict__ keys, uint32_t *__restrict__ order) {
+  __shared__ uint32_t part[kRankWaves][kWave];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int t = blockIdx.x * kWave + lane, blocks = (T + kWave - 1) / kWave;
+  const uint32_t key = key_of(ids[min(t, T - 1)], V);
+  uint32_t n = 0;
+  for (int b = wave; b < blocks; b += kRankWaves) {
+    // equal keys keep their order: of a block before this one they count
+    const uint32_t below = key + (b < int(blockIdx.x) ? 1u : 0u);
+    const int32_t *p = ids + b * kWave;
+    if (b != int(blockIdx.x) && (b + 1) * kWave <= T) {
+#pragma unroll
+      for (int i = 0; i < kWave; ++i) n += min(uint32_t(p[i]), uint32_t(V)) < below;
+    } else {
+      const int m = min(kWave, T - b * kWave);
+      for (int i = 0; i < m; ++i) n += min(uint32_t(p[i]), uint32_t(V)) < below + (b == int(blockIdx.x) && i < lane ? 1u : 0u);
+    }
+  }
+  part[wave][lane] = n;
   __syncthreads();
-  for (int pass = 0; pass < passes; ++pass) {
-    const int shift = 8 * pass;
-    for (int b = lane; b < kDigits; b += kWave) at[wave][b] = 0;
-    wave_sees_lds();
-    for (int i0 = begin; i0 < end; i0 += kWave) {
-      const bool active = i0 + lane < end;
-      const int t = active ? (pass ? from[i0 + lane] : i0 + lane) : 0;
-      const uint32_t digit = key[t] >> shift & 255;
-      const uint64_t alike = lanes_alike(digit, active);
-      if (active && !(alike & before)) at[wave][digit] += uint16_t(__popcll(alike));
-      wave_sees_lds();
-    }
-    __syncthreads();
-    uint32_t total = 0;
-    if (tid < kDigits)
-      for (int w = 0; w < kSortWaves; ++w) total += at[w][tid];
-    uint32_t run = digits_before(total, scratch);
-    if (tid < kDigits)
-      for (int w = 0; w < kSortWaves; ++w) {
-        const uint32_t n = at[w][tid];
-        at[w][tid] = uint16_t(run);
-        run += n;
-      }
-    __syncthreads();
-    for (int i0 = begin; i0 < end; i0 += kWave) {
-      const bool active = i0 + lane < end;
-      const int t = active ? (pass ? from[i0 + lane] : i0 + lane) : 0;
-      const uint32_t k = key[t], digit = k >> shift & 255;
-      const uint64_t alike = lanes_alike(digit, active);
-      const uint32_t pos = at[wave][digit] + __popcll(alike & before);
-      wave_sees_lds();
-      if (active && !(alike & before)) at[wave][digit] += uint16_t(__popcll(alike));
-      wave_sees_lds();
-      if (active) {
-        if (pass == passes - 1) {
-          keys[pos] = k;
-          order[pos] = uint32_t(t);
-        } else {
-          to[pos] = uint16_t(t);
-        }
-      }
-    }
-    __syncthreads();
-    uint16_t *s = from;
-    from = to;
-    to = s;
+  if (wave == 0 && t < T) {
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < kRankWaves; ++w) n += part[w][lane];
+    keys[n] = key;
+    order[n] = uint32_t(t);
   }
 }
 
-// The same over workgroups, a pass in two launches: counts[tile][digit] of tiles of kTile tokens, then each tile's tokens to their
-// places, which are those of the digits before, of the tiles before, and of the waves before.
+// More tokens: stable sorting by eight bits of the key at a time, least ones first, a pass in two launches: counts[tile][digit] of tiles of
+// kTile tokens, then each tile's tokens to their places, which are behind those of the digits before, of the tiles before, and of the waves
+// before.  A wave takes 64 tokens at a time: the lanes that share a digit find each other by eight ballots, which gives each its rank among
+// them, and the first of them advances the digit's counter, so that counters are a wave's own and need no atomics.
 constexpr int kTile = 2048, kTileWaves = 4, kTilePerWave = kTile / kTileWaves;
 
 __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_count(const int32_t *ids, const uint32_t *keys, int T, int V, int shift, uint32_t *counts) {
@@ -248,64 +233,180 @@ __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(const int32_t 
 
 struct Runs {
   const uint32_t *keys, *order;   // sorted
+  const int32_t *ids;             // as they are
   int T, d, V;
   int piece, pieces, slabs;       // tokens of a piece; pieces of the list; slabs of columns
   int64_t ldx, ldt;
   float *dtable;
-  float *partial;                 // per piece: the sum of the run that it begins within, of the one that it ends within
+  float *partial;                 // per piece: the sum of a run's tokens in a piece that it goes through, of those in the piece that it starts in
   float scale;
-  int accumulate;
 };
 
-constexpr int kAhead = 16, kFillRows = 16;
+constexpr int kAhead = 16;        // rows on their way at a time
+constexpr int kFillRows = 16;
 
-template <int N> __device__ __forceinline__ void load_some(float (&v)[N], const float *p, int n) {
-  if (n >= N) {
-    typedef u32x4 u32x4_u __attribute__((aligned(4)));
-#pragma unroll
-    for (int k = 0; k < N; k += 4) {
-      const u32x4 a = *reinterpret_cast<const u32x4_u *>(p + k);
-      v[k] = __uint_as_float(a.x); v[k + 1] = __uint_as_float(a.y); v[k + 2] = __uint_as_float(a.z); v[k + 3] = __uint_as_float(a.w);
+// A wave's columns of a row: a slab of kWave * N, N neighbouring ones a lane (WHOLE), or the last columns of a row, which are fewer, every
+// 64th a lane's: those behind the end read the last one, and nothing comes of it.
+template <typename E, bool WHOLE> struct Slab {
+  static constexpr int N = ElemTraits<E>::VEC, WIDTH = kWave * N;
+  int c, d;
+  __device__ __forceinline__ Slab(int slab, int lane, int d_) : c(slab * WIDTH + (WHOLE ? lane * N : lane)), d(d_) {}
+  struct Raw {
+    uint32_t w[WHOLE ? 4 : N];
+    __device__ __forceinline__ float at(int k) const {
+      if constexpr (sizeof(E) == 4) return __uint_as_float(w[k]);
+      else if constexpr (WHOLE) return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+      else return __uint_as_float(w[k] << 16);
     }
-  } else {
+  };
+  __device__ __forceinline__ void load(Raw &v, const E *row) const {
+    if constexpr (WHOLE) {
+      typedef typename Unaligned<E>::type unaligned;
+      const u32x4 a = *reinterpret_cast<const unaligned *>(row + c);
+      v.w[0] = a.x; v.w[1] = a.y; v.w[2] = a.z; v.w[3] = a.w;
+    } else {
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = k < n ? p[k] : 0.f;
-  }
-}
-__device__ __forceinline__ void load_some(float (&v)[8], const bf16_t *p, int n) { load_columns(v, p, n); }
-template <int N> __device__ __forceinline__ void store_some(float *p, const float (&v)[N], int n) {
-  if (n >= N) {
-    typedef u32x4 u32x4_u __attribute__((aligned(4)));
-#pragma unroll
-    for (int k = 0; k < N; k += 4) {
-      u32x4 a;
-      a.x = __float_as_uint(v[k]); a.y = __float_as_uint(v[k + 1]); a.z = __float_as_uint(v[k + 2]); a.w = __float_as_uint(v[k + 3]);
-      *reinterpret_cast<u32x4_u *>(p + k) = a;
+      for (int k = 0; k < N; ++k) {
+        if constexpr (sizeof(E) == 4) v.w[k] = __float_as_uint(row[min(c + kWave * k, d - 1)]);
+        else v.w[k] = reinterpret_cast<const uint16_t *>(row)[min(c + kWave * k, d - 1)];
+      }
     }
-  } else {
-#pragma unroll
-    for (int k = 0; k < N; ++k)
-      if (k < n) p[k] = v[k];
   }
-}
-template <int N> __device__ __forceinline__ void write_row(const Runs &g, uint32_t key, int c, int n, const float (&sum)[N]) {
-  float *out = g.dtable + int64_t(key) * g.ldt + c;
+  __device__ __forceinline__ void load(float (&v)[N], const float *row) const {
+    if constexpr (WHOLE) {
+#pragma unroll
+      for (int k = 0; k < N; k += 4) {
+        const u32x4 a = *reinterpret_cast<const u32x4_by4 *>(row + c + k);
+        v[k] = __uint_as_float(a.x); v[k + 1] = __uint_as_float(a.y); v[k + 2] = __uint_as_float(a.z); v[k + 3] = __uint_as_float(a.w);
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k) v[k] = row[min(c + kWave * k, d - 1)];
+    }
+  }
+  __device__ __forceinline__ void store(float *row, const float (&v)[N]) const {
+    if constexpr (WHOLE) {
+#pragma unroll
+      for (int k = 0; k < N; k += 4) {
+        u32x4 a;
+        a.x = __float_as_uint(v[k]); a.y = __float_as_uint(v[k + 1]); a.z = __float_as_uint(v[k + 2]); a.w = __float_as_uint(v[k + 3]);
+        *reinterpret_cast<u32x4_by4 *>(row + c + k) = a;
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < N; ++k)
+        if (c + kWave * k < d) row[c + kWave * k] = v[k];
+    }
+  }
+};
+
+// sum to row `key`, whose present content is `old` if that is added to
+template <bool ADD, int N, typename S> __device__ __forceinline__ void write_row(const Runs &g, const S &s, uint32_t key, const float (&sum)[N], const float (&old)[N]) {
   float o[N];
-  if (g.accumulate) {
-    load_some(o, out, n);
 #pragma unroll
-    for (int k = 0; k < N; ++k) o[k] = fmaf(sum[k], g.scale, o[k]);
-  } else {
-#pragma unroll
-    for (int k = 0; k < N; ++k) o[k] = sum[k] * g.scale;
-  }
-  store_some(out, o, n);
+  for (int k = 0; k < N; ++k) o[k] = ADD ? fmaf(sum[k], g.scale, old[k]) : sum[k] * g.scale;
+  s.store(g.dtable + int64_t(key) * g.ldt, o);
 }
 
-// A wave sums a piece of the sorted list over a slab of columns; the workgroups behind those write the rows that no token names.
-template <typename E>
+// Zeros to the rows row0 + i for which bit i is set.
+__device__ __forceinline__ void zero_rows(const Runs &g, int64_t row0, uint64_t empty, int lane) {
+  while (empty) {
+    const int i = __builtin_ctzll(empty);
+    empty &= empty - 1;
+    float *out = g.dtable + (row0 + i) * g.ldt;
+    const u32x4 zero = {0, 0, 0, 0};
+    for (int c = 4 * lane; c + 4 <= g.d; c += 4 * kWave) *reinterpret_cast<u32x4_by4 *>(out + c) = zero;
+    if (lane < g.d % 4) out[g.d / 4 * 4 + lane] = 0.f;
+  }
+}
+
+// The first place from lo on, and before hi, that has another key.
+__device__ __forceinline__ int behind_run(const Runs &g, int lo, int hi, uint32_t key) {
+  while (lo < hi) {
+    const int mid = (lo + hi) / 2;
+    if (g.keys[mid] == key) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+// A wave sums a piece of the sorted list over a slab of columns.  A run that ends in the piece behind the one that it starts in, or behind
+// one that it goes through, is taken along to its end; so only runs that go through a whole piece leave parts of their sum to be joined.
+template <typename E, bool WHOLE, bool ADD> __device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
+  constexpr int N = ElemTraits<E>::VEC;
+  const Slab<E, WHOLE> s(slab, lane, g.d);
+  int p = piece * g.piece, end = min(g.T, p + g.piece);
+  uint32_t key = g.keys[p];
+  if (key >= uint32_t(g.V)) return;
+  const uint32_t last = g.keys[end - 1];
+  bool through = false;                               // the run has begun before
+  if (p > 0 && g.keys[p - 1] == key) {
+    if (last != key || end == g.T || g.keys[end] != key) {
+      if (last == key) return;                        // all of the piece was taken along
+      p = behind_run(g, p, end, key);                 // its beginning was
+      key = g.keys[p];
+      if (key >= uint32_t(g.V)) return;
+    } else {
+      through = true;
+    }
+  }
+  bool goes_on = false;                               // the last run goes through all of the next piece
+  if (end < g.T && g.keys[end] == last && last < uint32_t(g.V)) {
+    const int next = min(g.T, end + g.piece);
+    if (next < g.T && g.keys[next] == last) {
+      goes_on = true;
+    } else {
+      int lo = end, hi = next;                        // to the first of another key
+      while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (g.keys[mid] == last) lo = mid + 1;
+        else hi = mid;
+      }
+      end = lo;
+    }
+  }
+  const uint32_t first = g.order[p];
+  float sum[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) sum[k] = 0.f;
+  for (; p < end; p += kAhead) {
+    const int at = min(p + lane % kAhead, g.T - 1);
+    uint32_t keys = g.keys[at], order = g.order[at];
+    if (at != p + lane % kAhead || at >= end || keys >= uint32_t(g.V)) {   // read in place of nothing, and not added
+      keys = 0xffffffffu;
+      order = first;
+    }
+    typename Slab<E, WHOLE>::Raw v[kAhead];
+    float old[ADD ? kAhead : 1][N];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) s.load(v[i], dx + int64_t(__builtin_amdgcn_readlane(order, i)) * g.ldx);
+    if constexpr (ADD) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) s.load(old[i], g.dtable + int64_t(min(uint32_t(__builtin_amdgcn_readlane(keys, i)), uint32_t(g.V - 1))) * g.ldt);
+    }
+    const uint32_t behind = p + kAhead < end ? g.keys[p + kAhead] : 0xfffffffeu;
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const uint32_t k = __builtin_amdgcn_readlane(keys, i), following = i + 1 < kAhead ? __builtin_amdgcn_readlane(keys, (i + 1) % kAhead) : behind;
+      if (k != 0xffffffffu) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) sum[q] += v[i].at(q);
+        if (following != k) {
+          const bool at_end = p + i + 1 >= end;
+          if (through && at_end) s.store(g.partial + int64_t(2 * piece) * g.d, sum);
+          else if (goes_on && at_end) s.store(g.partial + int64_t(2 * piece + 1) * g.d, sum);
+          else write_row<ADD>(g, s, k, sum, old[ADD ? i : 0]);
+#pragma unroll
+          for (int q = 0; q < N; ++q) sum[q] = 0.f;
+        }
+      }
+    }
+  }
+}
+
+// The workgroups behind those of the sums write the rows that no token names.
+template <typename E, bool ADD>
 __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, int run_groups) {
-  constexpr int N = ElemTraits<E>::VEC, kSlab = kWave * N;   // columns of a lane, of a wave
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (int(blockIdx.x) >= run_groups) {
     // kFillRows rows: a lane looks for one of them in the list
@@ -318,92 +419,45 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, in
       else hi = mid;
     }
     const bool named = row >= g.V || (lo < g.T && int64_t(g.keys[lo]) == row);
-    uint64_t empty = __ballot(!named && lane < kFillRows);
-    const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-    while (empty) {
-      const int i = __builtin_ctzll(empty);
-      empty &= empty - 1;
-      float *out = g.dtable + (row0 + i) * g.ldt;
-      for (int c = 4 * lane; c < g.d; c += 4 * kWave) store_some(out + c, zero, g.d - c);
-    }
+    zero_rows(g, row0, __ballot(!named && lane < kFillRows), lane);
     return;
   }
   const int64_t job = int64_t(blockIdx.x) * 4 + wave;
-  const int piece = int(job / g.slabs), c = int(job % g.slabs) * kSlab + lane * N, n = g.d - c;
+  const int piece = int(job / g.slabs), slab = int(job % g.slabs);
   if (piece >= g.pieces) return;
-  const int p0 = piece * g.piece, p1 = min(g.T, p0 + g.piece);
-  uint32_t key = g.keys[p0];
-  const uint32_t after = p1 < g.T ? g.keys[p1] : 0xffffffffu;
-  bool begun = p0 > 0 && g.keys[p0 - 1] == key;   // in a piece before
-  float sum[N];
-#pragma unroll
-  for (int k = 0; k < N; ++k) sum[k] = 0.f;
-  auto end_run = [&](bool goes_on) {
-    if (key >= uint32_t(g.V)) return;
-    if (begun) store_some(g.partial + int64_t(2 * piece) * g.d + c, sum, n);
-    else if (goes_on) store_some(g.partial + int64_t(2 * piece + 1) * g.d + c, sum, n);
-    else write_row(g, key, c, n, sum);
-  };
-  for (int p = p0; p < p1; p += kAhead) {
-    const int at = min(p + lane % kAhead, g.T - 1);
-    const uint32_t keys = g.keys[at], order = g.order[at];
-    float v[kAhead][N];
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const uint32_t t = __builtin_amdgcn_readlane(order, i), k = __builtin_amdgcn_readlane(keys, i);
-      load_some(v[i], dx + int64_t(t) * g.ldx + c, p + i < p1 && k < uint32_t(g.V) ? n : 0);
-    }
-#pragma unroll
-    for (int i = 0; i < kAhead; ++i) {
-      const uint32_t k = __builtin_amdgcn_readlane(keys, i);
-      if (p + i < p1) {
-        if (k != key) {
-          end_run(false);
-          key = k;
-          begun = false;
-#pragma unroll
-          for (int q = 0; q < N; ++q) sum[q] = 0.f;
-        }
-#pragma unroll
-        for (int q = 0; q < N; ++q) sum[q] += v[i][q];
-      }
-    }
-  }
-  end_run(key == after);
+  if ((slab + 1) * Slab<E, true>::WIDTH <= g.d) sum_piece<E, true, ADD>(g, dx, piece, slab, lane);
+  else sum_piece<E, false, ADD>(g, dx, piece, slab, lane);
 }
 
-// The runs that cross pieces: the piece that one starts in joins its end with the beginnings of the pieces that follow.  Four waves take
-// a fourth of them each, joined in one order.
-__global__ __launch_bounds__(256) void k_embed_grad_join(Runs g) {
+// The runs that go through whole pieces: the sum of the piece that one starts in, and of those that follow.  A workgroup looks at
+// kJoinPieces pieces; four waves take a fourth of a run's parts each, joined in one order.
+constexpr int kJoinPieces = 16;
+
+template <bool WHOLE, bool ADD> __device__ __forceinline__ void join_run(const Runs &g, int piece, int slab, int lane, int wave, float (&part)[4][kWave * 4]) {
   constexpr int N = 4;
-  __shared__ float part[4][kWave * N];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const int64_t slabs = (g.d + kWave * N - 1) / (kWave * N);
-  const int piece = int(blockIdx.x / slabs), c = int(blockIdx.x % slabs) * kWave * N + lane * N, n = g.d - c;
-  const int p0 = piece * g.piece, p1 = p0 + g.piece;
-  if (p1 >= g.T) return;
-  const uint32_t key = g.keys[p1];
-  if (key >= uint32_t(g.V) || g.keys[p1 - 1] != key || (p0 > 0 && g.keys[p0 - 1] == key)) return;
-  int last = piece;   // the last piece that begins within the run
+  const Slab<float, WHOLE> s(slab, lane, g.d);
+  const uint32_t key = g.keys[(piece + 1) * g.piece];
+  int parts = 0;                  // pieces that the run goes through, all but the end of the last one
   for (int q = piece + 1;; q += kWave) {
-    const bool in = q + lane < g.pieces && g.keys[min(int64_t(q + lane) * g.piece, int64_t(g.T) - 1)] == key;
-    const int more = __popcll(__ballot(in));
-    last += more;
+    const int64_t next = int64_t(q + lane + 1) * g.piece;
+    const int more = __popcll(__ballot(next < g.T && g.keys[min(next, int64_t(g.T) - 1)] == key));
+    parts += more;
     if (more < kWave) break;
   }
-  const int count = last - piece, per = (count + 3) / 4;   // wave w: pieces piece + 1 + w per ..
-  float sum[N] = {0.f, 0.f, 0.f, 0.f};
-  if (wave == 0) load_some(sum, g.partial + int64_t(2 * piece + 1) * g.d + c, n);
-  const int q1 = min(count, (wave + 1) * per);
+  const int per = (parts + 3) / 4, q1 = min(parts, (wave + 1) * per);
+  float sum[N] = {0.f, 0.f, 0.f, 0.f}, old[N];
+  if (wave == 0) s.load(sum, g.partial + int64_t(2 * piece + 1) * g.d);
+  if (ADD && wave == 0) s.load(old, g.dtable + int64_t(key) * g.ldt);
   for (int q = wave * per; q < q1; q += 8) {
     float v[8][N];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) load_some(v[i], g.partial + int64_t(2 * (piece + 1 + min(q + i, q1 - 1))) * g.d + c, q + i < q1 ? n : 0);
+    for (int i = 0; i < 8; ++i) s.load(v[i], g.partial + int64_t(2 * (piece + 1 + min(q + i, q1 - 1))) * g.d);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int k = 0; k < N; ++k) sum[k] += v[i][k];
+      for (int k = 0; k < N; ++k) sum[k] += q + i < q1 ? v[i][k] : 0.f;
   }
+  __syncthreads();                // of the run before, whose parts wave 0 has read
 #pragma unroll
   for (int k = 0; k < N; ++k) part[wave][lane * N + k] = sum[k];
   __syncthreads();
@@ -412,8 +466,89 @@ __global__ __launch_bounds__(256) void k_embed_grad_join(Runs g) {
     for (int w = 1; w < 4; ++w)
 #pragma unroll
       for (int k = 0; k < N; ++k) sum[k] += part[w][lane * N + k];
-    write_row(g, key, c, n, sum);
+    write_row<ADD>(g, s, key, sum, old);
   }
+}
+
+template <bool ADD>
+__global__ __launch_bounds__(256) void k_embed_grad_join(Runs g, int slabs) {
+  __shared__ float part[4][kWave * 4];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int piece0 = int(blockIdx.x / slabs) * kJoinPieces, slab = int(blockIdx.x % slabs);
+  bool starts = false;
+  const int64_t p0 = int64_t(piece0 + lane) * g.piece, p1 = p0 + g.piece, p2 = p1 + g.piece;
+  if (lane < kJoinPieces && p2 < g.T) {
+    const uint32_t key = g.keys[p1];
+    starts = key < uint32_t(g.V) && g.keys[p1 - 1] == key && g.keys[p2] == key && !(p0 > 0 && g.keys[p0 - 1] == key);
+  }
+  uint64_t todo = __ballot(starts);
+  while (todo) {
+    const int piece = piece0 + __builtin_ctzll(todo);
+    todo &= todo - 1;
+    if ((slab + 1) * Slab<float, true>::WIDTH <= g.d) join_run<true, ADD>(g, piece, slab, lane, wave, part);
+    else join_run<false, ADD>(g, piece, slab, lane, wave, part);
+  }
+}
+
+// Few tokens, in one launch: a wave looks through all ids for those that equal its token's; the first of them adds up their rows.
+constexpr int kFew = 256;
+
+template <typename E, bool WHOLE, bool ADD> __device__ __forceinline__ void sum_alike(const Runs &g, const E *dx, uint32_t key, const uint16_t *list, int n, int slab, int lane) {
+  constexpr int N = ElemTraits<E>::VEC;
+  const Slab<E, WHOLE> s(slab, lane, g.d);
+  float sum[N], old[N];
+#pragma unroll
+  for (int k = 0; k < N; ++k) sum[k] = 0.f;
+  if constexpr (ADD) s.load(old, g.dtable + int64_t(key) * g.ldt);
+  for (int p = 0; p < n; p += kAhead) {
+    const uint32_t order = list[min(p + lane % kAhead, n - 1)];
+    typename Slab<E, WHOLE>::Raw v[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) s.load(v[i], dx + int64_t(__builtin_amdgcn_readlane(order, i)) * g.ldx);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i)
+      if (p + i < n)
+#pragma unroll
+        for (int q = 0; q < N; ++q) sum[q] += v[i].at(q);
+  }
+  write_row<ADD>(g, s, key, sum, old);
+}
+
+template <typename E, bool ADD>
+__global__ __launch_bounds__(256) void k_embed_grad_few(Runs g, const E *dx, int run_groups) {
+  __shared__ uint16_t list[4][kFew];
+  __shared__ uint32_t named[4 * kFillRows];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (int(blockIdx.x) >= run_groups) {
+    const int64_t row0 = int64_t(int(blockIdx.x) - run_groups) * 4 * kFillRows;
+    if (threadIdx.x < 4 * kFillRows) named[threadIdx.x] = row0 + threadIdx.x >= g.V;
+    __syncthreads();
+    const int64_t at = threadIdx.x < unsigned(g.T) ? int64_t(g.ids[threadIdx.x]) - row0 : -1;
+    if (at >= 0 && at < 4 * kFillRows && at + row0 < g.V) named[at] = 1;
+    __syncthreads();
+    zero_rows(g, row0, __ballot(lane < 4 * kFillRows && !named[lane] && lane / kFillRows == wave), lane);
+    return;
+  }
+  const int64_t job = int64_t(blockIdx.x) * 4 + wave;
+  const int t = int(job / g.slabs), slab = int(job % g.slabs);
+  if (t >= g.T) return;   // no barrier below: every wave has a list of its own
+  const int id = g.ids[t];
+  int v[kFew / kWave];
+#pragma unroll
+  for (int i = 0; i < kFew / kWave; ++i) v[i] = g.ids[min(kWave * i + lane, g.T - 1)];
+  if (uint32_t(id) >= uint32_t(g.V)) return;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kFew / kWave; ++i) {
+    const bool hit = kWave * i + lane < g.T && v[i] == id;
+    const uint64_t hits = __ballot(hit);
+    if (hit) list[wave][n + __popcll(hits & ((uint64_t(1) << lane) - 1))] = uint16_t(kWave * i + lane);
+    n += __popcll(hits);
+  }
+  wave_sees_lds();
+  if (__builtin_amdgcn_readfirstlane(list[wave][0]) != t) return;
+  if ((slab + 1) * Slab<E, true>::WIDTH <= g.d) sum_alike<E, true, ADD>(g, dx, uint32_t(id), list[wave], n, slab, lane);
+  else sum_alike<E, false, ADD>(g, dx, uint32_t(id), list[wave], n, slab, lane);
 }
 
 }  // namespace
@@ -445,7 +580,8 @@ int launch_embed_lookup(const hmy_embed_lookup_desc &g, stream_t st) {
   a.tiles = (a.total + kUnits - 1) / kUnits;
   const dim3 grid(uint32_t(std::min<int64_t>(a.tiles, kMaxGrid)));
   DISPATCH_ROWS(g.prec, g.out_prec, {
-    hipLaunchKernelGGL((k_embed_lookup<L, E>), grid, dim3(kThreads), 0, (hipStream_t)st, a, (const L *)g.table, (const L *)g.pos_table, (E *)g.x);
+    auto *kernel = g.d < 8 ? k_embed_lookup<L, E, true> : k_embed_lookup<L, E, false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)st, a, (const L *)g.table, (const L *)g.pos_table, (E *)g.x);
   });
   return check_launch(who);
 }
@@ -475,25 +611,39 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   if (rc) return rc;
   const hipStream_t s = (hipStream_t)st;
   const int T = g.T;
-  Runs a = {nullptr, nullptr, T, g.d, g.V, T <= kOneGroup ? 16 : 64, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale, g.accumulate};
+  const bool few = T <= kFew;
+  Runs a = {nullptr, nullptr, g.ids, T, g.d, g.V, T <= kMostRanked ? 16 : 64, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale};
   a.pieces = (T + a.piece - 1) / a.piece;
   a.partial = (float *)g.workspace + (int64_t(wanted) / 4 - 2 * int64_t(g.d) * a.pieces) / 4 * 4;   // at the workspace's end
-  const int slab = kWave * (g.prec == HMY_PREC_BF16 ? 8 : 4);
+  const int slab = kWave * (g.prec == HMY_PREC_BF16 ? 8 : 4), join_slabs = (g.d + 255) / 256;
   a.slabs = (g.d + slab - 1) / slab;
-  const int64_t run_groups = (int64_t(a.pieces) * a.slabs + 3) / 4, fill_groups = g.accumulate ? 0 : (int64_t(g.V) + 4 * kFillRows - 1) / (4 * kFillRows);
-  const int64_t join_groups = int64_t(a.pieces) * ((g.d + 255) / 256);
+  const int64_t run_groups = (int64_t(few ? T : a.pieces) * a.slabs + 3) / 4;
+  const int64_t fill_groups = g.accumulate ? 0 : (int64_t(g.V) + 4 * kFillRows - 1) / (4 * kFillRows);
+  const int64_t join_groups = (int64_t(a.pieces) + kJoinPieces - 1) / kJoinPieces * join_slabs;
   constexpr int64_t kMostGroups = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
   if (run_groups + fill_groups > kMostGroups || join_groups > kMostGroups) return fail(HMY_E_INVALID, "%s: T, d and V are too large together", who);
+  const dim3 grid{uint32_t(run_groups + fill_groups)}, threads(256);
+#define GRAD(KERNEL)                                                                                                                       \
+  do {                                                                                                                                     \
+    if (g.prec == HMY_PREC_BF16) hipLaunchKernelGGL((g.accumulate ? KERNEL<bf16_t, true> : KERNEL<bf16_t, false>), grid, threads, 0, s, a, \
+                                                    (const bf16_t *)g.dx, int(run_groups));                                                \
+    else hipLaunchKernelGGL((g.accumulate ? KERNEL<float, true> : KERNEL<float, false>), grid, threads, 0, s, a, (const float *)g.dx,      \
+                            int(run_groups));                                                                                              \
+  } while (0)
+  if (few) {
+    GRAD(k_embed_grad_few);
+    return check_launch(who);
+  }
   const int64_t Ta = (int64_t(T) + 3) / 4 * 4;
   uint32_t *base = (uint32_t *)g.workspace;
   uint32_t *keys[2] = {base, base + 2 * Ta}, *order[2] = {base + Ta, base + 3 * Ta}, *counts = base + 4 * Ta;
-  int passes = 1;
-  while (passes < 4 && (uint64_t(g.V) >> (8 * passes))) ++passes;
   int sorted = 0;
-  if (T <= kOneGroup) {
-    hipLaunchKernelGGL(k_sort_tokens, dim3(1), dim3(kSortWaves * kWave), size_t(T) * 8, s, g.ids, T, g.V, passes, keys[0], order[0]);
+  if (T <= kMostRanked) {
+    hipLaunchKernelGGL(k_rank_tokens, dim3((T + kWave - 1) / kWave), dim3(kRankWaves * kWave), 0, s, g.ids, T, g.V, keys[0], order[0]);
   } else {
     const int tiles = (T + kTile - 1) / kTile;
+    int passes = 1;
+    while (passes < 4 && (uint64_t(g.V) >> (8 * passes))) ++passes;
     for (int pass = 0; pass < passes; ++pass) {
       const int32_t *ids = pass ? nullptr : g.ids;
       const int to = pass ? 1 - sorted : 0;
@@ -505,10 +655,9 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   }
   a.keys = keys[sorted];
   a.order = order[sorted];
-  const dim3 grid{uint32_t(run_groups + fill_groups)};
-  if (g.prec == HMY_PREC_BF16) hipLaunchKernelGGL(k_embed_grad_runs<bf16_t>, grid, dim3(256), 0, s, a, (const bf16_t *)g.dx, int(run_groups));
-  else hipLaunchKernelGGL(k_embed_grad_runs<float>, grid, dim3(256), 0, s, a, (const float *)g.dx, int(run_groups));
-  if (a.pieces > 1) hipLaunchKernelGGL(k_embed_grad_join, dim3(uint32_t(join_groups)), dim3(256), 0, s, a);
+  GRAD(k_embed_grad_runs);
+#undef GRAD
+  hipLaunchKernelGGL((g.accumulate ? k_embed_grad_join<true> : k_embed_grad_join<false>), dim3(uint32_t(join_groups)), threads, 0, s, a, join_slabs);
   return check_launch(who);
 }
 

@@ -66,33 +66,34 @@ template <int CODE> __device__ __forceinline__ void decode4(uint32_t w, float s,
   }
 }
 
-// The first n of eight codes from p on.
-__device__ __forceinline__ u32x2 load_codes(const uint8_t *p, int n) {
-  if (n >= 8) return *reinterpret_cast<const u32x2_by1 *>(p);
+// A unit's codes.
+template <bool NARROW> __device__ __forceinline__ u32x2 load_codes(const uint8_t *row, Unit u, int d) {
+  if constexpr (!NARROW) return *reinterpret_cast<const u32x2_by1 *>(row + u.c);
   u32x2 w = {0, 0};
 #pragma unroll
   for (int k = 0; k < 8; ++k)
-    if (k < n) w[k / 4] |= uint32_t(p[k]) << (8 * (k % 4));
+    if (k < d) w[k / 4] |= uint32_t(row[k]) << (8 * (k % 4));
   return w;
 }
-__device__ __forceinline__ void store_codes(uint8_t *p, u32x2 w, int n) {
-  if (n >= 8) {
-    *reinterpret_cast<u32x2_by1 *>(p) = w;
-  } else {
+template <bool NARROW> __device__ __forceinline__ void store_codes(uint8_t *row, u32x2 w, Unit u, int d) {
+  if (!NARROW && u.skip == 0) {
+    *reinterpret_cast<u32x2_by1 *>(row + u.c) = w;
+  } else if (u.skip < 8) {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < n) p[k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
+      if (k >= u.skip && (!NARROW || k < d)) row[u.c + k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
   }
 }
-// Eight columns of a row, from column c on, of which n exist; zeros behind them.
+// Its scale is that of the group that its own columns are in: the last column's, whichever of the eight are its own.
+template <bool NARROW> __device__ __forceinline__ int group_of(Unit u) { return NARROW ? 0 : (u.c + 7) / kGroup; }
 template <int CODE> __device__ __forceinline__ void decode(u32x2 w, uint32_t byte, float (&v)[8]) {
   const float s = scale_of(byte);
   decode4<CODE>(w[0], s, v);
   decode4<CODE>(w[1], s, v + 4);
 }
 
-// Rows are worked through as units of eight columns, rounded up to whole groups, numbered row by row: a workgroup takes kUnits of
-// them, and finds the row of each by one 32-bit division from that of its first.
+// Units are rounded up to whole groups and numbered row by row: a workgroup takes kUnits of them, and finds the row of each by one
+// 32-bit division from that of its first.
 constexpr int kThreads = 256, kPerThread = 2, kUnits = kThreads * kPerThread;
 
 struct Units {
@@ -108,72 +109,79 @@ inline Units units_of(int T, int d) {
   u.tiles = (u.total + kUnits - 1) / kUnits;
   return u;
 }
+struct Places {
+  int64_t row[kPerThread];
+  Unit u[kPerThread];
+};
+// Where the thread's units are; those behind the last row's stand for its last one, and nothing of it is theirs.
+template <bool NARROW> __device__ __forceinline__ Places places_of(const Units &g, int64_t tile) {
+  Places p;
+  const int64_t row0 = tile * kUnits / g.per_row;
+  const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
+#pragma unroll
+  for (int i = 0; i < kPerThread; ++i) {
+    const bool there = tile * kUnits + threadIdx.x + i * kThreads < g.total;
+    const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
+    p.u[i] = unit_at<NARROW>(int(at - down * g.per_row) * 8, g.d);
+    p.row[i] = there ? row0 + down : row0;
+    if (!there) p.u[i].skip = 8;
+  }
+  return p;
+}
 
-template <typename E, int CODE>
+template <typename E, int CODE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, Units g) {
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const int64_t row0 = tile * kUnits / g.per_row;
-    const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
-    float v[kPerThread][8];
-    int64_t row[kPerThread];
-    int c[kPerThread], n[kPerThread];
+    const Places p = places_of<NARROW>(g, tile);
+    Eight<E> raw[kPerThread];
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) load_unit<NARROW>(raw[i], x + p.row[i] * ldx, p.u[i], g.d);
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
-      const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
-      row[i] = row0 + down;
-      c[i] = int(at - down * g.per_row) * 8;
-      n[i] = tile * kUnits + threadIdx.x + i * kThreads < g.total ? g.d - c[i] : -1;
-      load_columns(v[i], x + row[i] * ldx + c[i], n[i]);
-    }
+      float v[8];
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
+      for (int k = 0; k < 8; ++k) v[k] = raw[i].at(k);
+      clear_foreign<NARROW>(v, p.u[i], g.d);
       uint32_t a = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) a = max(a, __float_as_uint(v[i][k]) & 0x7fffffffu);
+      for (int k = 0; k < 8; ++k) a = max(a, __float_as_uint(v[k]) & 0x7fffffffu);
       a = quad_top(a);
       const uint32_t byte = scale_byte<CODE>(a);
       const float inv = __uint_as_float((254u - byte) << 23);
       u32x2 w;
-      w[0] = encode4<CODE>(v[i][0], v[i][1], v[i][2], v[i][3], inv);
-      w[1] = encode4<CODE>(v[i][4], v[i][5], v[i][6], v[i][7], inv);
+      w[0] = encode4<CODE>(v[0], v[1], v[2], v[3], inv);
+      w[1] = encode4<CODE>(v[4], v[5], v[6], v[7], inv);
       if (byte == 255u) w = 0;
-      store_codes(codes + row[i] * ldc + c[i], w, n[i]);
-      if (n[i] > 0 && c[i] % kGroup == 0) scales[row[i] * lds + c[i] / kGroup] = uint8_t(byte);
+      store_codes<NARROW>(codes + p.row[i] * ldc, w, p.u[i], g.d);
+      if (p.u[i].skip < 8 && threadIdx.x % kLanesPerGroup == 0) scales[p.row[i] * lds + group_of<NARROW>(p.u[i])] = uint8_t(byte);
     }
   }
 }
 
-template <typename E, int CODE>
+template <typename E, int CODE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_unpack8(Rows8 r, E *x, int64_t ldx, Units g) {
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const int64_t row0 = tile * kUnits / g.per_row;
-    const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
-    int64_t row[kPerThread];
-    int c[kPerThread], n[kPerThread];
+    const Places p = places_of<NARROW>(g, tile);
     u32x2 w[kPerThread];
     uint32_t byte[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
-      const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
-      row[i] = row0 + down;
-      c[i] = int(at - down * g.per_row) * 8;
-      n[i] = tile * kUnits + threadIdx.x + i * kThreads < g.total ? g.d - c[i] : -1;
-      w[i] = load_codes(r.codes + row[i] * r.ldc + c[i], n[i]);
-      byte[i] = n[i] > 0 ? r.scales[row[i] * r.lds + c[i] / kGroup] : 0;
+      w[i] = load_codes<NARROW>(r.codes + p.row[i] * r.ldc, p.u[i], g.d);
+      byte[i] = r.scales[p.row[i] * r.lds + group_of<NARROW>(p.u[i])];
     }
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
       float v[8];
       decode<CODE>(w[i], byte[i], v);
-      store_columns(x + row[i] * ldx + c[i], v, n[i]);
+      store_unit<NARROW>(x + p.row[i] * ldx, v, p.u[i], g.d);
     }
   }
 }
 
 // ---- layer norm of rows in 8 bits -------------------------------------------------------------
 
-// A row is W waves', NJ units of eight columns a lane: wave w of it has columns 512 NJ w + 8 (lane + 64 j).  Sums over a row: within the
-// wave by lane moves, between waves through LDS, added in the same order by each of them.
+// A row is W waves', NJ units a lane: wave w of it has the units 64 NJ w + lane + 64 j.  Sums over a row: within the wave by lane moves,
+// between waves through LDS, added in the same order by each of them.
 template <int W, int N> __device__ __forceinline__ void row_sums(float (&s)[N], float (*xch)[N], int wave) {
 #pragma unroll
   for (int i = 0; i < N; ++i) s[i] = wave_total(s[i]);
@@ -199,42 +207,49 @@ struct Norm8 {
   float eps;
 };
 
-template <typename E, int CODE, int W, int NJ>
+template <typename E, int CODE, int W, int NJ, bool NARROW>
 __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma, const E *beta, E *y, float *x) {
   constexpr int kSlots = 4 / W;
   __shared__ float xch[2][2][4][1];   // of a round's two sums, and of the round before, which a wave may still read
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, col0 = wave % W * NJ * 512 + 8 * lane;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  Unit u[NJ];
+  Eight<E> ga[NJ], be[NJ];
+#pragma unroll
+  for (int j = 0; j < NJ; ++j) {
+    u[j] = unit_at<NARROW>(8 * (kWave * (NJ * (wave % W) + j) + lane), g.d);
+    load_unit<NARROW>(ga[j], gamma, u[j], g.d);
+    load_unit<NARROW>(be[j], beta, u[j], g.d);
+  }
   int parity = 0;
   for (int64_t base = int64_t(blockIdx.x) * kSlots; base < g.T; base += int64_t(gridDim.x) * kSlots, parity ^= 1) {
-    const int64_t row = base + wave / W;
-    const bool live = row < g.T;
+    const int64_t row = min(base + wave / W, int64_t(g.T) - 1);   // a slot behind the last row does that row again, and stores nothing
+    const bool live = base + wave / W < g.T;
     float v[NJ][8], s[1] = {0.f};
     u32x2 w[NJ];
     uint32_t byte[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = col0 + 512 * j, n = live ? g.d - c : 0;
-      w[j] = load_codes(g.r.codes + row * g.r.ldc + c, n);
-      byte[j] = n > 0 ? g.r.scales[row * g.r.lds + c / kGroup] : 0;
+      w[j] = load_codes<NARROW>(g.r.codes + row * g.r.ldc, u[j], g.d);
+      byte[j] = g.r.scales[row * g.r.lds + group_of<NARROW>(u[j])];
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       decode<CODE>(w[j], byte[j], v[j]);
-      const int n = g.d - (col0 + 512 * j);
+      clear_foreign<NARROW>(v[j], u[j], g.d);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[0] += k < n ? v[j][k] : 0.f;
+      for (int k = 0; k < 8; ++k) s[0] += v[j][k];
     }
     row_sums<W>(s, xch[parity][0], wave);
     const float mu = s[0] / float(g.d);
     s[0] = 0.f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int n = g.d - (col0 + 512 * j);
+      float t[8];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const float t = v[j][k] - mu;
-        s[0] += k < n ? t * t : 0.f;
-      }
+      for (int k = 0; k < 8; ++k) t[k] = v[j][k] - mu;
+      clear_foreign<NARROW>(t, u[j], g.d);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) s[0] = fmaf(t[k], t[k], s[0]);
     }
     row_sums<W>(s, xch[parity][1], wave);
     const float rs = 1.f / sqrtf(s[0] / float(g.d) + g.eps);
@@ -245,16 +260,11 @@ __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma,
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = col0 + 512 * j, n = g.d - c;
-      if (n > 0) {
-        float ga[8], be[8], o[8];
-        load_columns(ga, gamma + c, n);
-        load_columns(be, beta + c, n);
+      float o[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = fmaf(ga[k], (v[j][k] - mu) * rs, be[k]);
-        store_columns(y + row * g.ldy + c, o, n);
-        if (x) store_columns(x + row * g.ldx + c, v[j], n);
-      }
+      for (int k = 0; k < 8; ++k) o[k] = fmaf(ga[j].at(k), (v[j][k] - mu) * rs, be[j].at(k));
+      store_unit<NARROW>(y + row * g.ldy, o, u[j], g.d);
+      if (x) store_unit<NARROW>(x + row * g.ldx, v[j], u[j], g.d);
     }
   }
 }
@@ -271,80 +281,101 @@ struct Norm8Grad {
   int accumulate;
 };
 
+// What a wave reads of a row, on its way while the row before is worked on.
+template <typename E, int NJ> struct Row8 {
+  u32x2 codes[NJ];
+  uint32_t byte[NJ];
+  Eight<E> dy[NJ];
+  Eight<float> res[NJ];
+  float mean, rstd;
+};
+
 // The rows of a workgroup's slots leave their column sums in registers; at the end the slots' meet in LDS and one row of sums per
 // workgroup goes to the workspace.
-template <typename E, int CODE, int W, int NJ>
+template <typename E, int CODE, int W, int NJ, bool NARROW>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_layernorm8_bwd(Norm8Grad g, const E *dy, const E *gamma, E *dx_e) {
   constexpr int kWaves = 8, kSlots = kWaves / W;
   extern __shared__ __align__(16) float lds[];   // kSlots > 1: per slot its sums' ns rows of d floats
   __shared__ float xch[2][kWaves][2];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, slot = wave / W, col0 = wave % W * NJ * 512 + 8 * lane;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, slot = wave / W;
   const int ns = g.sums[2] ? 3 : 2;
-  float ga[NJ][8], dg[NJ][8], db[NJ][8], dr[NJ][8];
+  Unit u[NJ];
+  float dg[NJ][8], db[NJ][8], dr[NJ][8];
+  Eight<E> ga[NJ];
+  Row8<E, NJ> now, next;
+  auto fetch = [&](Row8<E, NJ> &r, int64_t base) {
+    const int64_t row = min(base + slot, int64_t(g.T) - 1);   // a slot behind the last row does that row again, and nothing comes of it
+    r.mean = g.mean[row];
+    r.rstd = g.rstd[row];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      r.codes[j] = load_codes<NARROW>(g.r.codes + row * g.r.ldc, u[j], g.d);
+      r.byte[j] = g.r.scales[row * g.r.lds + group_of<NARROW>(u[j])];
+      load_unit<NARROW>(r.dy[j], dy + row * g.ldy, u[j], g.d);
+      if (g.res) load_unit<NARROW>(r.res[j], g.res + row * g.ldr, u[j], g.d);
+    }
+  };
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    load_columns(ga[j], gamma + col0 + 512 * j, g.d - (col0 + 512 * j));
+    u[j] = unit_at<NARROW>(8 * (kWave * (NJ * (wave % W) + j) + lane), g.d);
+    load_unit<NARROW>(ga[j], gamma, u[j], g.d);
 #pragma unroll
     for (int k = 0; k < 8; ++k) dg[j][k] = db[j][k] = dr[j][k] = 0.f;
   }
+  const int64_t step = int64_t(gridDim.x) * kSlots;
   int parity = 0;
-  for (int64_t base = int64_t(blockIdx.x) * kSlots; base < g.T; base += int64_t(gridDim.x) * kSlots, parity ^= 1) {
+  fetch(now, int64_t(blockIdx.x) * kSlots);
+  for (int64_t base = int64_t(blockIdx.x) * kSlots; base < g.T; base += step, parity ^= 1) {
+    if (base + step < g.T) fetch(next, base + step);
     const int64_t row = base + slot;
     const bool live = row < g.T;
-    const float mu = live ? g.mean[row] : 0.f, rs = live ? g.rstd[row] : 0.f;
     float xh[NJ][8], gy[NJ][8], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const int c = col0 + 512 * j, n = live ? g.d - c : 0;
-      const u32x2 w = load_codes(g.r.codes + row * g.r.ldc + c, n);
-      const uint32_t byte = n > 0 ? g.r.scales[row * g.r.lds + c / kGroup] : 0;
-      load_columns(gy[j], dy + row * g.ldy + c, n);
-      decode<CODE>(w, byte, xh[j]);
+      decode<CODE>(now.codes[j], now.byte[j], xh[j]);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
-        xh[j][k] = (xh[j][k] - mu) * rs;
-        if (k >= n) xh[j][k] = 0.f;
-        const float t = gy[j][k] * ga[j][k];
+        xh[j][k] = (xh[j][k] - now.mean) * now.rstd;
+        gy[j][k] = now.dy[j].at(k);
+      }
+      clear_foreign<NARROW>(xh[j], u[j], g.d);
+      clear_foreign<NARROW>(gy[j], u[j], g.d);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float t = gy[j][k] * ga[j].at(k);
         s[0] += t;
         s[1] = fmaf(t, xh[j][k], s[1]);
-        dg[j][k] = fmaf(gy[j][k], xh[j][k], dg[j][k]);
-        db[j][k] += gy[j][k];
       }
     }
     row_sums<W>(s, xch[parity], wave);
-    if (!live) continue;
     const float m1 = s[0] / float(g.d), m2 = s[1] / float(g.d);
+    if (live) {
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      const int c = col0 + 512 * j, n = g.d - c;
-      if (n > 0) {
+      for (int j = 0; j < NJ; ++j) {
         float o[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) o[k] = (gy[j][k] * ga[j][k] - m1 - xh[j][k] * m2) * rs;
-        if (g.res) {
-          float rv[8];
-          load_columns(rv, g.res + row * g.ldr + c, n);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) {
-            o[k] += rv[k];
-            dr[j][k] += rv[k];
+        for (int k = 0; k < 8; ++k) {
+          o[k] = (gy[j][k] * ga[j].at(k) - m1 - xh[j][k] * m2) * now.rstd;
+          dg[j][k] = fmaf(gy[j][k], xh[j][k], dg[j][k]);
+          db[j][k] += gy[j][k];
+          if (g.res) {
+            o[k] += now.res[j].at(k);
+            dr[j][k] += now.res[j].at(k);
           }
         }
-        store_columns(g.dx + row * g.ldx + c, o, n);
-        if (dx_e) store_columns(dx_e + row * g.lde + c, o, n);
+        store_unit<NARROW>(g.dx + row * g.ldx, o, u[j], g.d);
+        if (dx_e) store_unit<NARROW>(dx_e + row * g.lde, o, u[j], g.d);
       }
     }
+    now = next;
   }
   float *out = g.partial + int64_t(blockIdx.x) * ns * g.d;
   float *mine = kSlots > 1 ? lds + int64_t(slot) * ns * g.d : out;
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    const int c = col0 + 512 * j, n = g.d - c;
-    if (n > 0) {
-      store_columns(mine + c, dg[j], n);
-      store_columns(mine + g.d + c, db[j], n);
-      if (ns == 3) store_columns(mine + 2 * g.d + c, dr[j], n);
-    }
+    store_unit<NARROW>(mine, dg[j], u[j], g.d);
+    store_unit<NARROW>(mine + g.d, db[j], u[j], g.d);
+    if (ns == 3) store_unit<NARROW>(mine + 2 * g.d, dr[j], u[j], g.d);
   }
   if constexpr (kSlots > 1) {
     __syncthreads();
@@ -366,9 +397,9 @@ __global__ __launch_bounds__(1024) void k_layernorm8_sums(Norm8Grad g, int rows)
   if (c < width) {
     float v[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = wave + 16 * i < rows ? g.partial[int64_t(wave + 16 * i) * width + c] : 0.f;
+    for (int i = 0; i < 16; ++i) v[i] = g.partial[int64_t(min(wave + 16 * i, rows - 1)) * width + c];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += v[i];
+    for (int i = 0; i < 16; ++i) t += wave + 16 * i < rows ? v[i] : 0.f;
   }
   part[wave][lane] = t;
   __syncthreads();
@@ -422,7 +453,8 @@ int launch_pack8(const hmy_rows8_desc &g, stream_t st) {
   const Units u = units_of(g.T, g.d);
   const dim3 grid(uint32_t(std::min<int64_t>(u.tiles, kMaxGrid)));
   DISPATCH_ROWS8(g.prec, g.code, {
-    hipLaunchKernelGGL((k_pack8<E, CODE>), grid, dim3(kThreads), 0, (hipStream_t)st, (const E *)g.x, g.ldx, (uint8_t *)g.codes, g.ldc,
+    auto *kernel = g.d < 8 ? k_pack8<E, CODE, true> : k_pack8<E, CODE, false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)st, (const E *)g.x, g.ldx, (uint8_t *)g.codes, g.ldc,
                        (uint8_t *)g.scales, g.lds, u);
   });
   return check_launch("pack8");
@@ -434,7 +466,10 @@ int launch_unpack8(const hmy_rows8_desc &g, stream_t st) {
   const Units u = units_of(g.T, g.d);
   const Rows8 r = {(const uint8_t *)g.codes, (const uint8_t *)g.scales, g.ldc, g.lds};
   const dim3 grid(uint32_t(std::min<int64_t>(u.tiles, kMaxGrid)));
-  DISPATCH_ROWS8(g.prec, g.code, { hipLaunchKernelGGL((k_unpack8<E, CODE>), grid, dim3(kThreads), 0, (hipStream_t)st, r, (E *)g.x, g.ldx, u); });
+  DISPATCH_ROWS8(g.prec, g.code, {
+    auto *kernel = g.d < 8 ? k_unpack8<E, CODE, true> : k_unpack8<E, CODE, false>;
+    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)st, r, (E *)g.x, g.ldx, u);
+  });
   return check_launch("unpack8");
 }
 
@@ -457,13 +492,14 @@ int launch_layernorm8_fwd(const hmy_layernorm8_desc &g, stream_t st) {
   const int slots = g.d <= 2048 ? 4 : 1;
   const dim3 grid(uint32_t(std::min<int64_t>((int64_t(g.T) + slots - 1) / slots, kMaxGrid)));
   const hipStream_t s = (hipStream_t)st;
-#define NORM8_FWD(W, NJ) hipLaunchKernelGGL((k_layernorm8_fwd<E, CODE, W, NJ>), grid, dim3(256), 0, s, a, (const E *)g.gamma, (const E *)g.beta, (E *)g.y, g.x)
+#define NORM8_FWD(W, NJ, NARROW) hipLaunchKernelGGL((k_layernorm8_fwd<E, CODE, W, NJ, NARROW>), grid, dim3(256), 0, s, a, (const E *)g.gamma, (const E *)g.beta, (E *)g.y, g.x)
   DISPATCH_ROWS8(g.prec, g.code, {
-    if (g.d <= 512) NORM8_FWD(1, 1);
-    else if (g.d <= 1024) NORM8_FWD(1, 2);
-    else if (g.d <= 2048) NORM8_FWD(1, 4);
-    else if (g.d <= 4096) NORM8_FWD(4, 2);
-    else NORM8_FWD(4, 4);
+    if (g.d < 8) NORM8_FWD(1, 1, true);
+    else if (g.d <= 512) NORM8_FWD(1, 1, false);
+    else if (g.d <= 1024) NORM8_FWD(1, 2, false);
+    else if (g.d <= 2048) NORM8_FWD(1, 4, false);
+    else if (g.d <= 4096) NORM8_FWD(4, 2, false);
+    else NORM8_FWD(4, 4, false);
   });
 #undef NORM8_FWD
   return check_launch(who);
@@ -501,13 +537,14 @@ int launch_layernorm8_bwd(const hmy_layernorm8_grad_desc &g, stream_t st) {
   const int groups = int(std::min<int64_t>((int64_t(g.T) + slots - 1) / slots, kGradGroups));
   const size_t lds = slots > 1 ? size_t(slots) * ns * g.d * 4 : 0;
   const hipStream_t s = (hipStream_t)st;
-#define NORM8_BWD(W, NJ) hipLaunchKernelGGL((k_layernorm8_bwd<E, CODE, W, NJ>), dim3(groups), dim3(512), lds, s, a, (const E *)g.dy, (const E *)g.gamma, (E *)g.dx_e)
+#define NORM8_BWD(W, NJ, NARROW) hipLaunchKernelGGL((k_layernorm8_bwd<E, CODE, W, NJ, NARROW>), dim3(groups), dim3(512), lds, s, a, (const E *)g.dy, (const E *)g.gamma, (E *)g.dx_e)
   DISPATCH_ROWS8(g.prec, g.code, {
-    if (g.d <= 512) NORM8_BWD(1, 1);
-    else if (g.d <= 1024) NORM8_BWD(1, 2);
-    else if (g.d <= 2048) NORM8_BWD(2, 2);
-    else if (g.d <= 4096) NORM8_BWD(4, 2);
-    else NORM8_BWD(8, 2);
+    if (g.d < 8) NORM8_BWD(1, 1, true);
+    else if (g.d <= 512) NORM8_BWD(1, 1, false);
+    else if (g.d <= 1024) NORM8_BWD(1, 2, false);
+    else if (g.d <= 2048) NORM8_BWD(2, 2, false);
+    else if (g.d <= 4096) NORM8_BWD(4, 2, false);
+    else NORM8_BWD(8, 2, false);
   });
 #undef NORM8_BWD
   hipLaunchKernelGGL(k_layernorm8_sums, dim3((ns * g.d + 63) / 64), dim3(1024), 0, s, a, groups);

@@ -5,25 +5,57 @@
 
 namespace hmy {
 
-// The first n columns from p on, zeros behind them.  Whole groups take wide accesses at any alignment.
-template <typename E> __device__ __forceinline__ void load_columns(float (&v)[8], const E *p, int n) {
-  if (n >= 8) {
-    Eight<E> e;
-    load_whole(e, p);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = e.at(k);
-  } else {
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = k < n ? to_f32(p[k]) : 0.f;
-  }
+// A row of d columns is worked through as units of eight columns.  The last one, where d is no multiple of eight, begins at column
+// d - 8, so that every lane's loads are wide, unconditional and inside of the row (a branch around a load would make the lanes wait for
+// it before the next is sent): its first `skip` columns are the unit's before it.  Units behind the row have skip = 8: nothing is
+// theirs.  Rows of fewer than eight columns (NARROW) are one unit, read element by element.
+struct Unit {
+  int c, skip;
+};
+template <bool NARROW> __device__ __forceinline__ Unit unit_at(int c, int d) {
+  if constexpr (NARROW) return {0, c > 0 ? 8 : 0};
+  const int over = c - (d - 8);
+  return over > 0 ? Unit{d - 8, min(over, 8)} : Unit{c, 0};
 }
-template <typename E> __device__ __forceinline__ void store_columns(E *p, const float (&v)[8], int n) {
-  if (n >= 8) {
-    store_whole(p, v);
+template <bool NARROW, typename E> __device__ __forceinline__ void load_unit(Eight<E> &v, const E *row, Unit u, int d) {
+  if constexpr (!NARROW) {
+    load_whole(v, row + u.c);
   } else {
+#pragma unroll
+    for (int i = 0; i < Eight<E>::WORDS; ++i) v.w[i] = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < n) p[k] = from_f32<E>(v[k]);
+      if (k < d) {
+        if constexpr (sizeof(E) == 4) v.w[k] = __float_as_uint(to_f32(row[k]));
+        else v.w[k / 2] |= (__float_as_uint(to_f32(row[k])) >> 16) << (16 * (k % 2));
+      }
+  }
+}
+template <bool NARROW, typename E> __device__ __forceinline__ void store_unit(E *row, const float (&v)[8], Unit u, int d) {
+  if constexpr (!NARROW) {
+    if (u.skip == 0) {
+      store_whole(row + u.c, v);
+    } else if (u.skip < 8) {
+#pragma unroll
+      for (int k = 1; k < 8; ++k)
+        if (k >= u.skip) row[u.c + k] = from_f32<E>(v[k]);
+    }
+  } else if (u.skip == 0) {
+#pragma unroll
+    for (int k = 0; k < 7; ++k)
+      if (k < d) row[k] = from_f32<E>(v[k]);
+  }
+}
+// zeros in the columns that are not the unit's own
+template <bool NARROW> __device__ __forceinline__ void clear_foreign(float (&v)[8], Unit u, int d) {
+  if constexpr (NARROW) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k >= d || u.skip) v[k] = 0.f;
+  } else if (u.skip) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < u.skip) v[k] = 0.f;
   }
 }
 
