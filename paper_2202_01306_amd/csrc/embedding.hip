@@ -19,7 +19,7 @@ constexpr int kThreads = 256, kPerThread = 4, kUnits = kThreads * kPerThread;
 struct Lookup {
   const int32_t *ids, *positions;
   int T, d, V, P;
-  uint32_t per_row;           // units of eight columns in a row
+  uint32_t per_row;           // units in a row
   int64_t ldw, ldp, ldx, total, tiles;
   float scale;
 };
@@ -28,6 +28,7 @@ struct Lookup {
 // for memory before it stores: all of its ids are on their way together, and then all of its rows.
 template <typename E, typename O, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *table, const E *pos_table, O *x) {
+  constexpr int N = 16 / sizeof(O);
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
     const int64_t row0 = tile * kUnits / g.per_row;
     const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
@@ -38,15 +39,15 @@ __global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *ta
     for (int i = 0; i < kPerThread; ++i) {
       const bool there = tile * kUnits + threadIdx.x + i * kThreads < g.total;
       const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
-      u[i] = unit_at<NARROW>(int(at - down * g.per_row) * 8, g.d);
-      if (!there) u[i].skip = 8;
+      u[i] = unit_at<NARROW, N>(int(at - down * g.per_row) * N, g.d);
+      if (!there) u[i].skip = N;
       t[i] = there ? row0 + down : row0;
       id[i] = g.ids[t[i]];
       place[i] = -1;
       if (g.positions) place[i] = g.positions[t[i]];
       else if (g.P) place[i] = int(uint32_t(t[i]) % uint32_t(g.P));
     }
-    Eight<E> v[kPerThread], p[kPerThread];
+    Cols<E, N> v[kPerThread], p[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {   // what names no row reads the first one and drops it
       load_unit<NARROW>(v[i], table + (uint32_t(id[i]) < uint32_t(g.V) ? id[i] : 0) * g.ldw, u[i], g.d);
@@ -55,9 +56,9 @@ __global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *ta
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
       const bool named = uint32_t(id[i]) < uint32_t(g.V), placed = uint32_t(place[i]) < uint32_t(g.P);
-      float o[8];
+      float o[N];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = fmaf(named ? v[i].at(k) : 0.f, g.scale, placed ? p[i].at(k) : 0.f);
+      for (int k = 0; k < N; ++k) o[k] = fmaf(named ? v[i].at(k) : 0.f, g.scale, placed ? p[i].at(k) : 0.f);
       store_unit<NARROW>(x + t[i] * g.ldx, o, u[i], g.d);
     }
   }
@@ -111,36 +112,36 @@ __device__ __forceinline__ uint32_t digits_before(uint32_t x, uint32_t *scratch)
 }
 
 // Up to kMostRanked tokens: a token's place is the number of tokens before it in the order, counted by comparing it with all of them.  A
-// workgroup places 64 tokens, one a lane, and its waves share the tokens to compare with, 64 at a time; a comparison and an addition with
-// carry for 64 pairs, with the other token's key in a scalar register.
-constexpr int kMostRanked = 8192, kRankWaves = 16;
+// workgroup places kRankTokens tokens against a copy of all keys in LDS; each sixteen lanes of its waves compare them with a 64th of the
+// keys, four at a time.  4096 tokens are a comparison and an addition for each of 64 keys a lane.
+constexpr int kMostRanked = 8192, kRankThreads = 1024, kRankTokens = 16, kRankParts = kRankThreads / kRankTokens;
 
-__global__ __launch_bounds__(kRankWaves *kWave) void k_rank_tokens(const int32_t *__restrict__ ids, int T, int V, uint32_t *__restrict__ keys, uint32_t *__restrict__ order) {
-  __shared__ uint32_t part[kRankWaves][kWave];
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int t = blockIdx.x * kWave + lane, blocks = (T + kWave - 1) / kWave;
-  const uint32_t key = key_of(ids[min(t, T - 1)], V);
-  uint32_t n = 0;
-  for (int b = wave; b < blocks; b += kRankWaves) {
-    // equal keys keep their order: of a block before this one they count
-    const uint32_t below = key + (b < int(blockIdx.x) ? 1u : 0u);
-    const int32_t *p = ids + b * kWave;
-    if (b != int(blockIdx.x) && (b + 1) * kWave <= T) {
-#pragma unroll
-      for (int i = 0; i < kWave; ++i) n += min(uint32_t(p[i]), uint32_t(V)) < below;
-    } else {
-      const int m = min(kWave, T - b * kWave);
-      for (int i = 0; i < m; ++i) n += min(uint32_t(p[i]), uint32_t(V)) < below + (b == int(blockIdx.x) && i < lane ? 1u : 0u);
-    }
-  }
-  part[wave][lane] = n;
+__global__ __launch_bounds__(kRankThreads) void k_rank_tokens(const int32_t *ids, int T, int V, uint32_t *keys, uint32_t *order) {
+  extern __shared__ __align__(16) uint32_t all[];   // keys, up to the next multiple of 4 kRankParts
+  __shared__ uint32_t counts[kRankParts][kRankTokens + 1];
+  const int tid = threadIdx.x, token = tid % kRankTokens, part = tid / kRankTokens;
+  const int t0 = blockIdx.x * kRankTokens, rounds = (T + 4 * kRankParts - 1) / (4 * kRankParts);
+  for (int i = tid; i < rounds * 4 * kRankParts; i += kRankThreads) all[i] = i < T ? key_of(ids[i], V) : 0xffffffffu;
   __syncthreads();
-  if (wave == 0 && t < T) {
+  const uint32_t key = all[min(t0 + token, T - 1)];
+  uint32_t n = 0;
+  for (int i = 0; i < rounds; ++i) {
+    const int at = 4 * (i * kRankParts + part);
+    // equal keys keep their order: those of tokens before these count; among these themselves below
+    const uint32_t below = at < t0 ? key + 1 : at < t0 + kRankTokens ? 0 : key;
+    const uint4 k = *reinterpret_cast<const uint4 *>(all + at);
+    n += (k.x < below) + (k.y < below) + (k.z < below) + (k.w < below);
+  }
+  counts[part][token] = n;
+  __syncthreads();
+  if (tid < kRankTokens && t0 + tid < T) {
     n = 0;
 #pragma unroll
-    for (int w = 0; w < kRankWaves; ++w) n += part[w][lane];
+    for (int p = 0; p < kRankParts; ++p) n += counts[p][tid];
+#pragma unroll
+    for (int i = 0; i < kRankTokens; ++i) n += all[min(t0 + i, rounds * 4 * kRankParts - 1)] < key + (i < tid ? 1u : 0u);
     keys[n] = key;
-    order[n] = uint32_t(t);
+    order[n] = uint32_t(t0 + tid);
   }
 }
 
@@ -148,61 +149,118 @@ __global__ __launch_bounds__(kRankWaves *kWave) void k_rank_tokens(const int32_t
 // kTile tokens, then each tile's tokens to their places, which are behind those of the digits before, of the tiles before, and of the waves
 // before.  A wave takes 64 tokens at a time: the lanes that share a digit find each other by eight ballots, which gives each its rank among
 // them, and the first of them advances the digit's counter, so that counters are a wave's own and need no atomics.
-constexpr int kTile = 2048, kTileWaves = 4, kTilePerWave = kTile / kTileWaves;
+constexpr int kTile = 1024, kTileWaves = 4, kSteps = kTile / kTileWaves / kWave;
+constexpr int kTilesRead = 256;   // tiles whose counts a tile adds up by itself; of more, a launch in between has added them up
 
-__global__ __launch_bounds__(kTileWaves *kWave) void k_sort_count(const int32_t *ids, const uint32_t *keys, int T, int V, int shift, uint32_t *counts) {
-  __shared__ uint32_t at[kTileWaves][kDigits];
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const uint64_t before = (uint64_t(1) << lane) - 1;
-  const int64_t begin = int64_t(blockIdx.x) * kTile + wave * kTilePerWave;
-  for (int b = lane; b < kDigits; b += kWave) at[wave][b] = 0;
+struct Sort {
+  const int32_t *ids;             // the first pass, whose keys are made of them and whose order is their own; later ones: NULL
+  const uint32_t *keys, *order;
+  int T, V, shift, tiles;
+  uint32_t *counts;               // [tiles + 1][kDigits]
+};
+
+__device__ __forceinline__ void load_keys(const Sort &g, uint32_t (&key)[kSteps], int64_t begin) {
+#pragma unroll
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t p = min(begin + kWave * i, int64_t(g.T) - 1);
+    key[i] = g.ids ? key_of(g.ids[p], g.V) : g.keys[p];
+  }
+}
+// counts the digits of a wave's keys
+__device__ __forceinline__ void count_digits(const Sort &g, const uint32_t (&key)[kSteps], int64_t begin, uint32_t *at, uint64_t before, int lane) {
+  for (int b = lane; b < kDigits; b += kWave) at[b] = 0;
   wave_sees_lds();
 #pragma unroll
-  for (int i = 0; i < kTilePerWave; i += kWave) {
-    const int64_t p = begin + i + lane;
-    const bool active = p < T;
-    const uint32_t k = active ? (ids ? key_of(ids[p], V) : keys[p]) : 0, digit = k >> shift & 255;
+  for (int i = 0; i < kSteps; ++i) {
+    const bool active = begin + kWave * i < g.T;
+    const uint32_t digit = key[i] >> g.shift & 255;
     const uint64_t alike = lanes_alike(digit, active);
-    if (active && !(alike & before)) at[wave][digit] += __popcll(alike);
+    if (active && !(alike & before)) at[digit] += __popcll(alike);
     wave_sees_lds();
-  }
-  __syncthreads();
-  if (tid < kDigits) {
-    uint32_t n = 0;
-#pragma unroll
-    for (int w = 0; w < kTileWaves; ++w) n += at[w][tid];
-    counts[int64_t(blockIdx.x) * kDigits + tid] = n;
   }
 }
 
-// `ids`: the first pass, whose keys are made of them and whose order is their own
-__global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(const int32_t *ids, const uint32_t *keys, const uint32_t *order, int T, int V, int shift,
-                                                               const uint32_t *counts, int tiles, uint32_t *to_keys, uint32_t *to_order) {
+__global__ __launch_bounds__(kTileWaves *kWave) void k_sort_count(Sort g) {
+  __shared__ uint32_t at[kTileWaves][kDigits];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int64_t begin = int64_t(blockIdx.x) * kTile + wave * (kSteps * kWave) + lane;
+  uint32_t key[kSteps];
+  load_keys(g, key, begin);
+  count_digits(g, key, begin, at[wave], (uint64_t(1) << lane) - 1, lane);
+  __syncthreads();
+  uint32_t n = 0;
+#pragma unroll
+  for (int w = 0; w < kTileWaves; ++w) n += at[w][tid];
+  g.counts[int64_t(blockIdx.x) * kDigits + tid] = n;
+}
+
+// Many tiles: counts become those of the tiles before, with the totals behind the last.  64 digits a workgroup, whose waves take a
+// sixteenth of the tiles each.
+__global__ __launch_bounds__(1024) void k_sort_scan(uint32_t *counts, int tiles) {
+  __shared__ uint32_t part[16][kWave];
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, per = (tiles + 15) / 16;
+  const int t0 = min(tiles, wave * per), t1 = min(tiles, t0 + per);
+  uint32_t *p = counts + blockIdx.x * kWave + lane;
+  uint32_t n = 0;
+#pragma unroll 8
+  for (int t = t0; t < t1; ++t) n += p[int64_t(t) * kDigits];
+  part[wave][lane] = n;
+  __syncthreads();
+  uint32_t run = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    run += w < wave ? part[w][lane] : 0;
+    total += part[w][lane];
+  }
+#pragma unroll 8
+  for (int t = t0; t < t1; ++t) {
+    const uint32_t m = p[int64_t(t) * kDigits];
+    p[int64_t(t) * kDigits] = run;
+    run += m;
+  }
+  if (wave == 0) p[int64_t(tiles) * kDigits] = total;
+}
+
+__global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(Sort g, uint32_t *to_keys, uint32_t *to_order) {
   static_assert(kTileWaves * kWave == kDigits, "a thread per digit");
   __shared__ uint32_t at[kTileWaves][kDigits];
+  __shared__ uint4 sums[2][kTileWaves][kWave];   // per wave and digit: counts of its tiles, of those before this one
   __shared__ uint32_t scratch[kDigits / kWave];
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave, tile = blockIdx.x;
   const uint64_t before = (uint64_t(1) << lane) - 1;
-  const int64_t begin = int64_t(blockIdx.x) * kTile + wave * kTilePerWave;
-  for (int b = lane; b < kDigits; b += kWave) at[wave][b] = 0;
-  wave_sees_lds();
-  uint32_t key[kTilePerWave / kWave];
+  const int64_t begin = int64_t(tile) * kTile + wave * (kSteps * kWave) + lane;
+  uint32_t key[kSteps], order[kSteps];
+  load_keys(g, key, begin);
 #pragma unroll
-  for (int i = 0; i < kTilePerWave / kWave; ++i) {
-    const int64_t p = begin + kWave * i + lane;
-    const bool active = p < T;
-    key[i] = active ? (ids ? key_of(ids[p], V) : keys[p]) : 0;
-    const uint32_t digit = key[i] >> shift & 255;
-    const uint64_t alike = lanes_alike(digit, active);
-    if (active && !(alike & before)) at[wave][digit] += __popcll(alike);
-    wave_sees_lds();
+  for (int i = 0; i < kSteps; ++i) {
+    const int64_t p = min(begin + kWave * i, int64_t(g.T) - 1);
+    order[i] = g.ids ? uint32_t(p) : g.order[p];
   }
   uint32_t total = 0, mine = 0;   // of this thread's digit: in all tiles, in those before
-#pragma unroll 8
-  for (int i = 0; i < tiles; ++i) {
-    const uint32_t n = counts[int64_t(i) * kDigits + tid];
-    total += n;
-    mine += i < int(blockIdx.x) ? n : 0;
+  if (g.tiles <= kTilesRead) {
+    // each wave takes every fourth tile, four digits a lane
+    uint4 all = make_uint4(0, 0, 0, 0), some = all;
+    const uint4 *p = reinterpret_cast<const uint4 *>(g.counts) + lane;
+#pragma unroll 16
+    for (int t = wave; t < g.tiles; t += kTileWaves) {
+      const uint4 n = p[int64_t(t) * (kDigits / 4)];
+      all.x += n.x; all.y += n.y; all.z += n.z; all.w += n.w;
+      if (t < tile) { some.x += n.x; some.y += n.y; some.z += n.z; some.w += n.w; }
+    }
+    sums[0][wave][lane] = all;
+    sums[1][wave][lane] = some;
+  } else {
+    total = g.counts[int64_t(g.tiles) * kDigits + tid];
+    mine = g.counts[int64_t(tile) * kDigits + tid];
+  }
+  count_digits(g, key, begin, at[wave], before, lane);
+  __syncthreads();
+  if (g.tiles <= kTilesRead) {
+#pragma unroll
+    for (int w = 0; w < kTileWaves; ++w) {
+      total += reinterpret_cast<const uint32_t *>(sums[0][w])[tid];
+      mine += reinterpret_cast<const uint32_t *>(sums[1][w])[tid];
+    }
   }
   uint32_t run = digits_before(total, scratch) + mine;
 #pragma unroll
@@ -213,10 +271,9 @@ __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(const int32_t 
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kTilePerWave / kWave; ++i) {
-    const int64_t p = begin + kWave * i + lane;
-    const bool active = p < T;
-    const uint32_t digit = key[i] >> shift & 255;
+  for (int i = 0; i < kSteps; ++i) {
+    const bool active = begin + kWave * i < g.T;
+    const uint32_t digit = key[i] >> g.shift & 255;
     const uint64_t alike = lanes_alike(digit, active);
     const uint32_t pos = at[wave][digit] + __popcll(alike & before);
     wave_sees_lds();
@@ -224,7 +281,7 @@ __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(const int32_t 
     wave_sees_lds();
     if (active) {
       to_keys[pos] = key[i];
-      to_order[pos] = ids ? uint32_t(p) : order[p];
+      to_order[pos] = order[i];
     }
   }
 }
@@ -243,7 +300,7 @@ struct Runs {
 };
 
 constexpr int kAhead = 16;        // rows on their way at a time
-constexpr int kFillRows = 16;
+constexpr int kFillRows = 4, kFillColumns = 1024;   // rows of a wave, and columns, that it may have to write
 
 // A wave's columns of a row: a slab of kWave * N, N neighbouring ones a lane (WHOLE), or the last columns of a row, which are fewer, every
 // 64th a lane's: those behind the end read the last one, and nothing comes of it.
@@ -308,16 +365,31 @@ template <bool ADD, int N, typename S> __device__ __forceinline__ void write_row
   s.store(g.dtable + int64_t(key) * g.ldt, o);
 }
 
-// Zeros to the rows row0 + i for which bit i is set.
-__device__ __forceinline__ void zero_rows(const Runs &g, int64_t row0, uint64_t empty, int lane) {
+// Zeros to kFillColumns columns from c0 on of the rows row0 + i for which bit i is set.
+__device__ __forceinline__ void zero_rows(const Runs &g, int64_t row0, uint64_t empty, int c0, int lane) {
+  const int c1 = min(g.d, c0 + kFillColumns), whole = c0 + (c1 - c0) / 4 * 4;
   while (empty) {
     const int i = __builtin_ctzll(empty);
     empty &= empty - 1;
     float *out = g.dtable + (row0 + i) * g.ldt;
     const u32x4 zero = {0, 0, 0, 0};
-    for (int c = 4 * lane; c + 4 <= g.d; c += 4 * kWave) *reinterpret_cast<u32x4_by4 *>(out + c) = zero;
-    if (lane < g.d % 4) out[g.d / 4 * 4 + lane] = 0.f;
+    for (int c = c0 + 4 * lane; c < whole; c += 4 * kWave) *reinterpret_cast<u32x4_by4 *>(out + c) = zero;
+    if (whole + lane < c1) out[whole + lane] = 0.f;
   }
+}
+
+// The number of keys below `key`, by the whole wave: 64 places at a time.
+__device__ __forceinline__ int keys_below(const Runs &g, int64_t key, int lane) {
+  int lo = 0, n = g.T;   // it is in lo .. lo + n
+  while (n > 0) {
+    const int step = (n + kWave) / (kWave + 1);   // probes at lo + step - 1, lo + 2 step - 1, ..
+    const int64_t at = int64_t(lo) + int64_t(lane + 1) * step - 1;
+    const int m = __popcll(__ballot(at < int64_t(lo) + n && int64_t(g.keys[min(at, int64_t(g.T) - 1)]) < key));
+    const int end = lo + n;
+    lo += m * step;
+    n = min(m < kWave ? step - 1 : step, end - lo);
+  }
+  return lo;
 }
 
 // The first place from lo on, and before hi, that has another key.
@@ -409,17 +481,18 @@ template <typename E, bool ADD>
 __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, int run_groups) {
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (int(blockIdx.x) >= run_groups) {
-    // kFillRows rows: a lane looks for one of them in the list
-    const int64_t row0 = (int64_t(int(blockIdx.x) - run_groups) * 4 + wave) * kFillRows;
-    const int64_t row = row0 + lane % kFillRows;
-    int lo = 0, hi = g.T;
+    const int job = int(blockIdx.x) - run_groups, slabs = (g.d + kFillColumns - 1) / kFillColumns;
+    const int64_t row0 = (int64_t(job / slabs) * 4 + wave) * kFillRows, row = row0 + lane;
+    int lo = keys_below(g, row0, lane), hi = g.T;
+    // a lane looks for one of the rows behind that
+    if (lane >= kFillRows) hi = lo;
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (int64_t(g.keys[mid]) < row) lo = mid + 1;
       else hi = mid;
     }
     const bool named = row >= g.V || (lo < g.T && int64_t(g.keys[lo]) == row);
-    zero_rows(g, row0, __ballot(!named && lane < kFillRows), lane);
+    zero_rows(g, row0, __ballot(!named && lane < kFillRows), job % slabs * kFillColumns, lane);
     return;
   }
   const int64_t job = int64_t(blockIdx.x) * 4 + wave;
@@ -520,13 +593,14 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(Runs g, const E *dx, int
   __shared__ uint32_t named[4 * kFillRows];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (int(blockIdx.x) >= run_groups) {
-    const int64_t row0 = int64_t(int(blockIdx.x) - run_groups) * 4 * kFillRows;
+    const int job = int(blockIdx.x) - run_groups, slabs = (g.d + kFillColumns - 1) / kFillColumns;
+    const int64_t row0 = int64_t(job / slabs) * 4 * kFillRows;
     if (threadIdx.x < 4 * kFillRows) named[threadIdx.x] = row0 + threadIdx.x >= g.V;
     __syncthreads();
     const int64_t at = threadIdx.x < unsigned(g.T) ? int64_t(g.ids[threadIdx.x]) - row0 : -1;
     if (at >= 0 && at < 4 * kFillRows && at + row0 < g.V) named[at] = 1;
     __syncthreads();
-    zero_rows(g, row0, __ballot(lane < 4 * kFillRows && !named[lane] && lane / kFillRows == wave), lane);
+    zero_rows(g, row0, __ballot(lane < 4 * kFillRows && !named[lane] && lane / kFillRows == wave), job % slabs * kFillColumns, lane);
     return;
   }
   const int64_t job = int64_t(blockIdx.x) * 4 + wave;
@@ -575,7 +649,7 @@ int launch_embed_lookup(const hmy_embed_lookup_desc &g, stream_t st) {
                         {"positions", g.positions, int64_t(g.T) * 4, int64_t(g.T) * 4, 1, false}};
   rc = check_apart(who, spans);
   if (rc) return rc;
-  Lookup a = {g.ids, g.positions, g.T, g.d, g.V, g.P, uint32_t((g.d + 7) / 8), g.ldw, g.ldp, g.ldx, 0, 0, g.scale};
+  Lookup a = {g.ids, g.positions, g.T, g.d, g.V, g.P, uint32_t((g.d + 16 / o - 1) / (16 / o)), g.ldw, g.ldp, g.ldx, 0, 0, g.scale};
   a.total = int64_t(g.T) * a.per_row;
   a.tiles = (a.total + kUnits - 1) / kUnits;
   const dim3 grid(uint32_t(std::min<int64_t>(a.tiles, kMaxGrid)));
@@ -618,7 +692,7 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   const int slab = kWave * (g.prec == HMY_PREC_BF16 ? 8 : 4), join_slabs = (g.d + 255) / 256;
   a.slabs = (g.d + slab - 1) / slab;
   const int64_t run_groups = (int64_t(few ? T : a.pieces) * a.slabs + 3) / 4;
-  const int64_t fill_groups = g.accumulate ? 0 : (int64_t(g.V) + 4 * kFillRows - 1) / (4 * kFillRows);
+  const int64_t fill_groups = g.accumulate ? 0 : (int64_t(g.V) + 4 * kFillRows - 1) / (4 * kFillRows) * ((g.d + kFillColumns - 1) / kFillColumns);
   const int64_t join_groups = (int64_t(a.pieces) + kJoinPieces - 1) / kJoinPieces * join_slabs;
   constexpr int64_t kMostGroups = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
   if (run_groups + fill_groups > kMostGroups || join_groups > kMostGroups) return fail(HMY_E_INVALID, "%s: T, d and V are too large together", who);
@@ -639,17 +713,18 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   uint32_t *keys[2] = {base, base + 2 * Ta}, *order[2] = {base + Ta, base + 3 * Ta}, *counts = base + 4 * Ta;
   int sorted = 0;
   if (T <= kMostRanked) {
-    hipLaunchKernelGGL(k_rank_tokens, dim3((T + kWave - 1) / kWave), dim3(kRankWaves * kWave), 0, s, g.ids, T, g.V, keys[0], order[0]);
+    hipLaunchKernelGGL(k_rank_tokens, dim3((T + kRankTokens - 1) / kRankTokens), dim3(kRankThreads),
+                       size_t(T + 4 * kRankParts - 1) / (4 * kRankParts) * (4 * kRankParts) * 4, s, g.ids, T, g.V, keys[0], order[0]);
   } else {
     const int tiles = (T + kTile - 1) / kTile;
     int passes = 1;
     while (passes < 4 && (uint64_t(g.V) >> (8 * passes))) ++passes;
     for (int pass = 0; pass < passes; ++pass) {
-      const int32_t *ids = pass ? nullptr : g.ids;
       const int to = pass ? 1 - sorted : 0;
-      hipLaunchKernelGGL(k_sort_count, dim3(tiles), dim3(kTileWaves * kWave), 0, s, ids, keys[sorted], T, g.V, 8 * pass, counts);
-      hipLaunchKernelGGL(k_sort_place, dim3(tiles), dim3(kTileWaves * kWave), 0, s, ids, keys[sorted], order[sorted], T, g.V, 8 * pass, counts, tiles,
-                         keys[to], order[to]);
+      const Sort q = {pass ? nullptr : g.ids, keys[sorted], order[sorted], T, g.V, 8 * pass, tiles, counts};
+      hipLaunchKernelGGL(k_sort_count, dim3(tiles), dim3(kTileWaves * kWave), 0, s, q);
+      if (tiles > kTilesRead) hipLaunchKernelGGL(k_sort_scan, dim3(kDigits / kWave), dim3(1024), 0, s, counts, tiles);
+      hipLaunchKernelGGL(k_sort_place, dim3(tiles), dim3(kTileWaves * kWave), 0, s, q, keys[to], order[to]);
       sorted = to;
     }
   }

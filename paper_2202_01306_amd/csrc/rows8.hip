@@ -13,19 +13,17 @@ namespace hmy {
 namespace {
 
 constexpr int kGroup = HMY_ROWS8_GROUP;
-constexpr int kLanesPerGroup = kGroup / 8;
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-typedef u32x2 u32x2_by1 __attribute__((aligned(1)));
 
 struct Rows8 {
   const uint8_t *codes, *scales;
   int64_t ldc, lds;
 };
 
-// The largest of four neighbouring lanes' values.
-__device__ __forceinline__ uint32_t quad_top(uint32_t x) {
+// The largest value of a group's lanes, of which each has N of its columns.
+template <int N> __device__ __forceinline__ uint32_t group_top(uint32_t x) {
   x = max(x, uint32_t(__builtin_amdgcn_update_dpp(0, x, 0xb1, 0xf, 0xf, false)));   // from lane ^ 1
   x = max(x, uint32_t(__builtin_amdgcn_update_dpp(0, x, 0x4e, 0xf, 0xf, false)));   // from lane ^ 2
+  if constexpr (N == 4) x = max(x, uint32_t(__builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false)));   // from the other four of eight
   return x;
 }
 
@@ -67,44 +65,56 @@ template <int CODE> __device__ __forceinline__ void decode4(uint32_t w, float s,
 }
 
 // A unit's codes.
-template <bool NARROW> __device__ __forceinline__ u32x2 load_codes(const uint8_t *row, Unit u, int d) {
-  if constexpr (!NARROW) return *reinterpret_cast<const u32x2_by1 *>(row + u.c);
-  u32x2 w = {0, 0};
+template <bool NARROW, int N> __device__ __forceinline__ void load_codes(uint32_t (&w)[N / 4], const uint8_t *row, Unit u, int d) {
+  if constexpr (NARROW) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k)
-    if (k < d) w[k / 4] |= uint32_t(row[k]) << (8 * (k % 4));
-  return w;
-}
-template <bool NARROW> __device__ __forceinline__ void store_codes(uint8_t *row, u32x2 w, Unit u, int d) {
-  if (!NARROW && u.skip == 0) {
-    *reinterpret_cast<u32x2_by1 *>(row + u.c) = w;
-  } else if (u.skip < 8) {
+    for (int i = 0; i < N / 4; ++i) w[i] = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k >= u.skip && (!NARROW || k < d)) row[u.c + k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
+    for (int k = 0; k < N; ++k)
+      if (u.c + k < d) w[k / 4] |= uint32_t(row[u.c + k]) << (8 * (k % 4));
+  } else if constexpr (N == 8) {
+    const u32x2 a = *reinterpret_cast<const u32x2_by1 *>(row + u.c);
+    w[0] = a.x; w[1] = a.y;
+  } else {
+    w[0] = *reinterpret_cast<const u32_by1 *>(row + u.c);
   }
 }
-// Its scale is that of the group that its own columns are in: the last column's, whichever of the eight are its own.
-template <bool NARROW> __device__ __forceinline__ int group_of(Unit u) { return NARROW ? 0 : (u.c + 7) / kGroup; }
-template <int CODE> __device__ __forceinline__ void decode(u32x2 w, uint32_t byte, float (&v)[8]) {
+template <bool NARROW, int N> __device__ __forceinline__ void store_codes(uint8_t *row, const uint32_t (&w)[N / 4], Unit u, int d) {
+  if (!NARROW && u.skip == 0) {
+    if constexpr (N == 8) {
+      u32x2 a;
+      a.x = w[0]; a.y = w[1];
+      *reinterpret_cast<u32x2_by1 *>(row + u.c) = a;
+    } else {
+      *reinterpret_cast<u32_by1 *>(row + u.c) = w[0];
+    }
+  } else if (u.skip < N) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (owns<NARROW, N>(u, k, d)) row[u.c + k] = uint8_t(w[k / 4] >> (8 * (k % 4)));
+  }
+}
+// Its scale is that of the group that its own columns are in: the last column's, whichever of them are its own.
+template <bool NARROW, int N> __device__ __forceinline__ int group_of(Unit u) { return NARROW ? 0 : (u.c + N - 1) / kGroup; }
+template <int CODE, int N> __device__ __forceinline__ void decode(const uint32_t (&w)[N / 4], uint32_t byte, float (&v)[N]) {
   const float s = scale_of(byte);
-  decode4<CODE>(w[0], s, v);
-  decode4<CODE>(w[1], s, v + 4);
+#pragma unroll
+  for (int i = 0; i < N / 4; ++i) decode4<CODE>(w[i], s, v + 4 * i);
 }
 
 // Units are rounded up to whole groups and numbered row by row: a workgroup takes kUnits of them, and finds the row of each by one
 // 32-bit division from that of its first.
-constexpr int kThreads = 256, kPerThread = 2, kUnits = kThreads * kPerThread;
+constexpr int kThreads = 256, kPerThread = 4, kUnits = kThreads * kPerThread;
 
 struct Units {
   int d;
   uint32_t per_row;
   int64_t total, tiles;
 };
-inline Units units_of(int T, int d) {
+template <int N> inline Units units_of(int T, int d) {
   Units u;
   u.d = d;
-  u.per_row = uint32_t((d + kGroup - 1) / kGroup * kLanesPerGroup);
+  u.per_row = uint32_t((d + kGroup - 1) / kGroup * (kGroup / N));
   u.total = int64_t(T) * u.per_row;
   u.tiles = (u.total + kUnits - 1) / kUnits;
   return u;
@@ -113,8 +123,8 @@ struct Places {
   int64_t row[kPerThread];
   Unit u[kPerThread];
 };
-// Where the thread's units are; those behind the last row's stand for its last one, and nothing of it is theirs.
-template <bool NARROW> __device__ __forceinline__ Places places_of(const Units &g, int64_t tile) {
+// Where the thread's units are; for those behind the last row's the tile's first row is read, and nothing of it is theirs.
+template <bool NARROW, int N> __device__ __forceinline__ Places places_of(const Units &g, int64_t tile) {
   Places p;
   const int64_t row0 = tile * kUnits / g.per_row;
   const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
@@ -122,56 +132,56 @@ template <bool NARROW> __device__ __forceinline__ Places places_of(const Units &
   for (int i = 0; i < kPerThread; ++i) {
     const bool there = tile * kUnits + threadIdx.x + i * kThreads < g.total;
     const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
-    p.u[i] = unit_at<NARROW>(int(at - down * g.per_row) * 8, g.d);
+    p.u[i] = unit_at<NARROW, N>(int(at - down * g.per_row) * N, g.d);
     p.row[i] = there ? row0 + down : row0;
-    if (!there) p.u[i].skip = 8;
+    if (!there) p.u[i].skip = N;
   }
   return p;
 }
 
 template <typename E, int CODE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, Units g) {
+  constexpr int N = 16 / sizeof(E);
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const Places p = places_of<NARROW>(g, tile);
-    Eight<E> raw[kPerThread];
+    const Places p = places_of<NARROW, N>(g, tile);
+    Cols<E, N> raw[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) load_unit<NARROW>(raw[i], x + p.row[i] * ldx, p.u[i], g.d);
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
-      float v[8];
+      float v[N];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] = raw[i].at(k);
+      for (int k = 0; k < N; ++k) v[k] = raw[i].at(k);
       clear_foreign<NARROW>(v, p.u[i], g.d);
       uint32_t a = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) a = max(a, __float_as_uint(v[k]) & 0x7fffffffu);
-      a = quad_top(a);
+      for (int k = 0; k < N; ++k) a = max(a, __float_as_uint(v[k]) & 0x7fffffffu);
+      a = group_top<N>(a);
       const uint32_t byte = scale_byte<CODE>(a);
       const float inv = __uint_as_float((254u - byte) << 23);
-      u32x2 w;
-      w[0] = encode4<CODE>(v[0], v[1], v[2], v[3], inv);
-      w[1] = encode4<CODE>(v[4], v[5], v[6], v[7], inv);
-      if (byte == 255u) w = 0;
-      store_codes<NARROW>(codes + p.row[i] * ldc, w, p.u[i], g.d);
-      if (p.u[i].skip < 8 && threadIdx.x % kLanesPerGroup == 0) scales[p.row[i] * lds + group_of<NARROW>(p.u[i])] = uint8_t(byte);
+      uint32_t w[N / 4];
+#pragma unroll
+      for (int k = 0; k < N; k += 4) w[k / 4] = byte == 255u ? 0u : encode4<CODE>(v[k], v[k + 1], v[k + 2], v[k + 3], inv);
+      store_codes<NARROW, N>(codes + p.row[i] * ldc, w, p.u[i], g.d);
+      if (p.u[i].skip < N && threadIdx.x % (kGroup / N) == 0) scales[p.row[i] * lds + group_of<NARROW, N>(p.u[i])] = uint8_t(byte);
     }
   }
 }
 
 template <typename E, int CODE, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_unpack8(Rows8 r, E *x, int64_t ldx, Units g) {
+  constexpr int N = 16 / sizeof(E);
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const Places p = places_of<NARROW>(g, tile);
-    u32x2 w[kPerThread];
-    uint32_t byte[kPerThread];
+    const Places p = places_of<NARROW, N>(g, tile);
+    uint32_t w[kPerThread][N / 4], byte[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
-      w[i] = load_codes<NARROW>(r.codes + p.row[i] * r.ldc, p.u[i], g.d);
-      byte[i] = r.scales[p.row[i] * r.lds + group_of<NARROW>(p.u[i])];
+      load_codes<NARROW, N>(w[i], r.codes + p.row[i] * r.ldc, p.u[i], g.d);
+      byte[i] = r.scales[p.row[i] * r.lds + group_of<NARROW, N>(p.u[i])];
     }
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
-      float v[8];
+      float v[N];
       decode<CODE>(w[i], byte[i], v);
       store_unit<NARROW>(x + p.row[i] * ldx, v, p.u[i], g.d);
     }
@@ -180,18 +190,20 @@ __global__ __launch_bounds__(kThreads) void k_unpack8(Rows8 r, E *x, int64_t ldx
 
 // ---- layer norm of rows in 8 bits -------------------------------------------------------------
 
-// A row is W waves', NJ units a lane: wave w of it has the units 64 NJ w + lane + 64 j.  Sums over a row: within the wave by lane moves,
+// A row is W waves', NJ units of kN columns a lane: wave w of it has the units 64 NJ w + lane + 64 j.  Sums over a row: within the wave by lane moves,
 // between waves through LDS, added in the same order by each of them.
-template <int W, int N> __device__ __forceinline__ void row_sums(float (&s)[N], float (*xch)[N], int wave) {
+constexpr int kN = 4;
+
+template <int W, int M> __device__ __forceinline__ void row_sums(float (&s)[M], float (*xch)[M], int wave) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) s[i] = wave_total(s[i]);
+  for (int i = 0; i < M; ++i) s[i] = wave_total(s[i]);
   if constexpr (W > 1) {
     if (threadIdx.x % kWave == 0)
 #pragma unroll
-      for (int i = 0; i < N; ++i) xch[wave][i] = s[i];
+      for (int i = 0; i < M; ++i) xch[wave][i] = s[i];
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
+    for (int i = 0; i < M; ++i) {
       s[i] = 0.f;
 #pragma unroll
       for (int w = 0; w < W; ++w) s[i] += xch[wave / W * W + w][i];
@@ -213,10 +225,10 @@ __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma,
   __shared__ float xch[2][2][4][1];   // of a round's two sums, and of the round before, which a wave may still read
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   Unit u[NJ];
-  Eight<E> ga[NJ], be[NJ];
+  Cols<E, kN> ga[NJ], be[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    u[j] = unit_at<NARROW>(8 * (kWave * (NJ * (wave % W) + j) + lane), g.d);
+    u[j] = unit_at<NARROW, kN>(kN * (kWave * (NJ * (wave % W) + j) + lane), g.d);
     load_unit<NARROW>(ga[j], gamma, u[j], g.d);
     load_unit<NARROW>(be[j], beta, u[j], g.d);
   }
@@ -224,32 +236,31 @@ __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma,
   for (int64_t base = int64_t(blockIdx.x) * kSlots; base < g.T; base += int64_t(gridDim.x) * kSlots, parity ^= 1) {
     const int64_t row = min(base + wave / W, int64_t(g.T) - 1);   // a slot behind the last row does that row again, and stores nothing
     const bool live = base + wave / W < g.T;
-    float v[NJ][8], s[1] = {0.f};
-    u32x2 w[NJ];
-    uint32_t byte[NJ];
+    float v[NJ][kN], s[1] = {0.f};
+    uint32_t w[NJ][kN / 4], byte[NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      w[j] = load_codes<NARROW>(g.r.codes + row * g.r.ldc, u[j], g.d);
-      byte[j] = g.r.scales[row * g.r.lds + group_of<NARROW>(u[j])];
+      load_codes<NARROW, kN>(w[j], g.r.codes + row * g.r.ldc, u[j], g.d);
+      byte[j] = g.r.scales[row * g.r.lds + group_of<NARROW, kN>(u[j])];
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       decode<CODE>(w[j], byte[j], v[j]);
       clear_foreign<NARROW>(v[j], u[j], g.d);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[0] += v[j][k];
+      for (int k = 0; k < kN; ++k) s[0] += v[j][k];
     }
     row_sums<W>(s, xch[parity][0], wave);
     const float mu = s[0] / float(g.d);
     s[0] = 0.f;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      float t[8];
+      float t[kN];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) t[k] = v[j][k] - mu;
+      for (int k = 0; k < kN; ++k) t[k] = v[j][k] - mu;
       clear_foreign<NARROW>(t, u[j], g.d);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) s[0] = fmaf(t[k], t[k], s[0]);
+      for (int k = 0; k < kN; ++k) s[0] = fmaf(t[k], t[k], s[0]);
     }
     row_sums<W>(s, xch[parity][1], wave);
     const float rs = 1.f / sqrtf(s[0] / float(g.d) + g.eps);
@@ -260,9 +271,9 @@ __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma,
     }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      float o[8];
+      float o[kN];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] = fmaf(ga[j].at(k), (v[j][k] - mu) * rs, be[j].at(k));
+      for (int k = 0; k < kN; ++k) o[k] = fmaf(ga[j].at(k), (v[j][k] - mu) * rs, be[j].at(k));
       store_unit<NARROW>(y + row * g.ldy, o, u[j], g.d);
       if (x) store_unit<NARROW>(x + row * g.ldx, v[j], u[j], g.d);
     }
@@ -283,10 +294,10 @@ struct Norm8Grad {
 
 // What a wave reads of a row, on its way while the row before is worked on.
 template <typename E, int NJ> struct Row8 {
-  u32x2 codes[NJ];
+  uint32_t codes[NJ][kN / 4];
   uint32_t byte[NJ];
-  Eight<E> dy[NJ];
-  Eight<float> res[NJ];
+  Cols<E, kN> dy[NJ];
+  Cols<float, kN> res[NJ];
   float mean, rstd;
 };
 
@@ -300,8 +311,8 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, slot = wave / W;
   const int ns = g.sums[2] ? 3 : 2;
   Unit u[NJ];
-  float dg[NJ][8], db[NJ][8], dr[NJ][8];
-  Eight<E> ga[NJ];
+  float dg[NJ][kN], db[NJ][kN], dr[NJ][kN];
+  Cols<E, kN> ga[NJ];
   Row8<E, NJ> now, next;
   auto fetch = [&](Row8<E, NJ> &r, int64_t base) {
     const int64_t row = min(base + slot, int64_t(g.T) - 1);   // a slot behind the last row does that row again, and nothing comes of it
@@ -309,18 +320,18 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     r.rstd = g.rstd[row];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      r.codes[j] = load_codes<NARROW>(g.r.codes + row * g.r.ldc, u[j], g.d);
-      r.byte[j] = g.r.scales[row * g.r.lds + group_of<NARROW>(u[j])];
+      load_codes<NARROW, kN>(r.codes[j], g.r.codes + row * g.r.ldc, u[j], g.d);
+      r.byte[j] = g.r.scales[row * g.r.lds + group_of<NARROW, kN>(u[j])];
       load_unit<NARROW>(r.dy[j], dy + row * g.ldy, u[j], g.d);
       if (g.res) load_unit<NARROW>(r.res[j], g.res + row * g.ldr, u[j], g.d);
     }
   };
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    u[j] = unit_at<NARROW>(8 * (kWave * (NJ * (wave % W) + j) + lane), g.d);
+    u[j] = unit_at<NARROW, kN>(kN * (kWave * (NJ * (wave % W) + j) + lane), g.d);
     load_unit<NARROW>(ga[j], gamma, u[j], g.d);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) dg[j][k] = db[j][k] = dr[j][k] = 0.f;
+    for (int k = 0; k < kN; ++k) dg[j][k] = db[j][k] = dr[j][k] = 0.f;
   }
   const int64_t step = int64_t(gridDim.x) * kSlots;
   int parity = 0;
@@ -329,19 +340,19 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     if (base + step < g.T) fetch(next, base + step);
     const int64_t row = base + slot;
     const bool live = row < g.T;
-    float xh[NJ][8], gy[NJ][8], s[2] = {0.f, 0.f};
+    float xh[NJ][kN], gy[NJ][kN], s[2] = {0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       decode<CODE>(now.codes[j], now.byte[j], xh[j]);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < kN; ++k) {
         xh[j][k] = (xh[j][k] - now.mean) * now.rstd;
         gy[j][k] = now.dy[j].at(k);
       }
       clear_foreign<NARROW>(xh[j], u[j], g.d);
       clear_foreign<NARROW>(gy[j], u[j], g.d);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < kN; ++k) {
         const float t = gy[j][k] * ga[j].at(k);
         s[0] += t;
         s[1] = fmaf(t, xh[j][k], s[1]);
@@ -352,9 +363,9 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
     if (live) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
-        float o[8];
+        float o[kN];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
+        for (int k = 0; k < kN; ++k) {
           o[k] = (gy[j][k] * ga[j].at(k) - m1 - xh[j][k] * m2) * now.rstd;
           dg[j][k] = fmaf(gy[j][k], xh[j][k], dg[j][k]);
           db[j][k] += gy[j][k];
@@ -450,7 +461,7 @@ static int check_move8(const char *who, const hmy_rows8_desc &g, bool pack) {
 int launch_pack8(const hmy_rows8_desc &g, stream_t st) {
   const int rc = check_move8("pack8", g, true);
   if (rc) return rc;
-  const Units u = units_of(g.T, g.d);
+  const Units u = g.prec == HMY_PREC_BF16 ? units_of<8>(g.T, g.d) : units_of<4>(g.T, g.d);
   const dim3 grid(uint32_t(std::min<int64_t>(u.tiles, kMaxGrid)));
   DISPATCH_ROWS8(g.prec, g.code, {
     auto *kernel = g.d < 8 ? k_pack8<E, CODE, true> : k_pack8<E, CODE, false>;
@@ -463,7 +474,7 @@ int launch_pack8(const hmy_rows8_desc &g, stream_t st) {
 int launch_unpack8(const hmy_rows8_desc &g, stream_t st) {
   const int rc = check_move8("unpack8", g, false);
   if (rc) return rc;
-  const Units u = units_of(g.T, g.d);
+  const Units u = g.prec == HMY_PREC_BF16 ? units_of<8>(g.T, g.d) : units_of<4>(g.T, g.d);
   const Rows8 r = {(const uint8_t *)g.codes, (const uint8_t *)g.scales, g.ldc, g.lds};
   const dim3 grid(uint32_t(std::min<int64_t>(u.tiles, kMaxGrid)));
   DISPATCH_ROWS8(g.prec, g.code, {
@@ -495,11 +506,12 @@ int launch_layernorm8_fwd(const hmy_layernorm8_desc &g, stream_t st) {
 #define NORM8_FWD(W, NJ, NARROW) hipLaunchKernelGGL((k_layernorm8_fwd<E, CODE, W, NJ, NARROW>), grid, dim3(256), 0, s, a, (const E *)g.gamma, (const E *)g.beta, (E *)g.y, g.x)
   DISPATCH_ROWS8(g.prec, g.code, {
     if (g.d < 8) NORM8_FWD(1, 1, true);
-    else if (g.d <= 512) NORM8_FWD(1, 1, false);
-    else if (g.d <= 1024) NORM8_FWD(1, 2, false);
-    else if (g.d <= 2048) NORM8_FWD(1, 4, false);
-    else if (g.d <= 4096) NORM8_FWD(4, 2, false);
-    else NORM8_FWD(4, 4, false);
+    else if (g.d <= 256) NORM8_FWD(1, 1, false);
+    else if (g.d <= 512) NORM8_FWD(1, 2, false);
+    else if (g.d <= 1024) NORM8_FWD(1, 4, false);
+    else if (g.d <= 2048) NORM8_FWD(1, 8, false);
+    else if (g.d <= 4096) NORM8_FWD(4, 4, false);
+    else NORM8_FWD(4, 8, false);
   });
 #undef NORM8_FWD
   return check_launch(who);
@@ -540,11 +552,12 @@ int launch_layernorm8_bwd(const hmy_layernorm8_grad_desc &g, stream_t st) {
 #define NORM8_BWD(W, NJ, NARROW) hipLaunchKernelGGL((k_layernorm8_bwd<E, CODE, W, NJ, NARROW>), dim3(groups), dim3(512), lds, s, a, (const E *)g.dy, (const E *)g.gamma, (E *)g.dx_e)
   DISPATCH_ROWS8(g.prec, g.code, {
     if (g.d < 8) NORM8_BWD(1, 1, true);
-    else if (g.d <= 512) NORM8_BWD(1, 1, false);
-    else if (g.d <= 1024) NORM8_BWD(1, 2, false);
-    else if (g.d <= 2048) NORM8_BWD(2, 2, false);
-    else if (g.d <= 4096) NORM8_BWD(4, 2, false);
-    else NORM8_BWD(8, 2, false);
+    else if (g.d <= 256) NORM8_BWD(1, 1, false);
+    else if (g.d <= 512) NORM8_BWD(1, 2, false);
+    else if (g.d <= 1024) NORM8_BWD(1, 4, false);
+    else if (g.d <= 2048) NORM8_BWD(2, 4, false);
+    else if (g.d <= 4096) NORM8_BWD(4, 4, false);
+    else NORM8_BWD(8, 4, false);
   });
 #undef NORM8_BWD
   hipLaunchKernelGGL(k_layernorm8_sums, dim3((ns * g.d + 63) / 64), dim3(1024), 0, s, a, groups);

@@ -5,57 +5,100 @@
 
 namespace hmy {
 
-// A row of d columns is worked through as units of eight columns.  The last one, where d is no multiple of eight, begins at column
-// d - 8, so that every lane's loads are wide, unconditional and inside of the row (a branch around a load would make the lanes wait for
-// it before the next is sent): its first `skip` columns are the unit's before it.  Units behind the row have skip = 8: nothing is
-// theirs.  Rows of fewer than eight columns (NARROW) are one unit, read element by element.
+// A row of d columns is worked through as units of N = 4 or 8 neighbouring columns a lane, so many that a lane's widest access takes 16
+// bytes: then an instruction of a wave covers a kilobyte without holes (fp32 rows of 134 MB written in units of 8 columns: see k_unpack8).
+// The last unit, where d is no multiple of N, begins at column d - N, so that every lane's loads are wide, unconditional and inside of the
+// row (a branch around a load would make the lanes wait for it before the next is sent): its first `skip` columns are the unit's before
+// it.  Units behind the row have skip = N: nothing is theirs.  Rows of fewer than eight columns (NARROW) are read element by element.
 struct Unit {
   int c, skip;
 };
-template <bool NARROW> __device__ __forceinline__ Unit unit_at(int c, int d) {
-  if constexpr (NARROW) return {0, c > 0 ? 8 : 0};
-  const int over = c - (d - 8);
-  return over > 0 ? Unit{d - 8, min(over, 8)} : Unit{c, 0};
+template <bool NARROW, int N> __device__ __forceinline__ Unit unit_at(int c, int d) {
+  if constexpr (NARROW) return {c, c < d ? 0 : N};
+  const int over = c - (d - N);
+  return over > 0 ? Unit{d - N, min(over, N)} : Unit{c, 0};
 }
-template <bool NARROW, typename E> __device__ __forceinline__ void load_unit(Eight<E> &v, const E *row, Unit u, int d) {
-  if constexpr (!NARROW) {
-    load_whole(v, row + u.c);
-  } else {
+template <bool NARROW, int N> __device__ __forceinline__ bool owns(Unit u, int k, int d) { return k >= u.skip && (!NARROW || u.c + k < d); }
+
+// N columns as they are stored.
+template <typename E, int N> struct Cols {
+  static constexpr int WORDS = N * sizeof(E) / 4;
+  uint32_t w[WORDS];
+  __device__ __forceinline__ float at(int k) const {
+    if constexpr (sizeof(E) == 4) return __uint_as_float(w[k]);
+    else return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+  }
+};
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_by1 __attribute__((aligned(1)));
+typedef u32x2 u32x2_by2 __attribute__((aligned(2)));
+typedef uint32_t u32_by1 __attribute__((aligned(1)));
+template <bool NARROW, typename E, int N> __device__ __forceinline__ void load_unit(Cols<E, N> &v, const E *row, Unit u, int d) {
+  const char *p = reinterpret_cast<const char *>(row + u.c);
+  if constexpr (NARROW) {
 #pragma unroll
-    for (int i = 0; i < Eight<E>::WORDS; ++i) v.w[i] = 0;
+    for (int i = 0; i < Cols<E, N>::WORDS; ++i) v.w[i] = 0;
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k < d) {
-        if constexpr (sizeof(E) == 4) v.w[k] = __float_as_uint(to_f32(row[k]));
-        else v.w[k / 2] |= (__float_as_uint(to_f32(row[k])) >> 16) << (16 * (k % 2));
+    for (int k = 0; k < N; ++k)
+      if (u.c + k < d) {
+        if constexpr (sizeof(E) == 4) v.w[k] = __float_as_uint(to_f32(row[u.c + k]));
+        else v.w[k / 2] |= (__float_as_uint(to_f32(row[u.c + k])) >> 16) << (16 * (k % 2));
       }
+  } else if constexpr (Cols<E, N>::WORDS == 2) {
+    const u32x2 a = *reinterpret_cast<const u32x2_by2 *>(p);
+    v.w[0] = a.x; v.w[1] = a.y;
+  } else {
+    typedef typename Unaligned<E>::type unaligned;
+#pragma unroll
+    for (int i = 0; i < Cols<E, N>::WORDS; i += 4) {
+      const u32x4 a = *reinterpret_cast<const unaligned *>(p + 4 * i);
+      v.w[i] = a.x; v.w[i + 1] = a.y; v.w[i + 2] = a.z; v.w[i + 3] = a.w;
+    }
   }
 }
-template <bool NARROW, typename E> __device__ __forceinline__ void store_unit(E *row, const float (&v)[8], Unit u, int d) {
-  if constexpr (!NARROW) {
-    if (u.skip == 0) {
-      store_whole(row + u.c, v);
-    } else if (u.skip < 8) {
+template <bool NARROW, typename E, int N> __device__ __forceinline__ void store_unit(E *row, const float (&v)[N], Unit u, int d) {
+  if (!NARROW && u.skip == 0) {
+    Cols<E, N> o;
+    if constexpr (sizeof(E) == 4) {
 #pragma unroll
-      for (int k = 1; k < 8; ++k)
-        if (k >= u.skip) row[u.c + k] = from_f32<E>(v[k]);
+      for (int k = 0; k < N; ++k) o.w[k] = __float_as_uint(v[k]);
+    } else {
+      typedef E pair __attribute__((ext_vector_type(2)));
+      typedef float floats __attribute__((ext_vector_type(2)));
+#pragma unroll
+      for (int k = 0; k < N; k += 2) {   // both halves of a word by one instruction
+        floats f;
+        f.x = v[k];
+        f.y = v[k + 1];
+        o.w[k / 2] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f, pair));
+      }
     }
-  } else if (u.skip == 0) {
+    char *p = reinterpret_cast<char *>(row + u.c);
+    if constexpr (Cols<E, N>::WORDS == 2) {
+      u32x2 a;
+      a.x = o.w[0]; a.y = o.w[1];
+      *reinterpret_cast<u32x2_by2 *>(p) = a;
+    } else {
+      typedef typename Unaligned<E>::type unaligned;
 #pragma unroll
-    for (int k = 0; k < 7; ++k)
-      if (k < d) row[k] = from_f32<E>(v[k]);
+      for (int i = 0; i < Cols<E, N>::WORDS; i += 4) {
+        u32x4 a;
+        a.x = o.w[i]; a.y = o.w[i + 1]; a.z = o.w[i + 2]; a.w = o.w[i + 3];
+        *reinterpret_cast<unaligned *>(p + 4 * i) = a;
+      }
+    }
+  } else if (u.skip < N) {
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (owns<NARROW, N>(u, k, d)) row[u.c + k] = from_f32<E>(v[k]);
   }
 }
 // zeros in the columns that are not the unit's own
-template <bool NARROW> __device__ __forceinline__ void clear_foreign(float (&v)[8], Unit u, int d) {
-  if constexpr (NARROW) {
+template <bool NARROW, int N> __device__ __forceinline__ void clear_foreign(float (&v)[N], Unit u, int d) {
+  if (NARROW || u.skip) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k >= d || u.skip) v[k] = 0.f;
-  } else if (u.skip) {
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (k < u.skip) v[k] = 0.f;
+    for (int k = 0; k < N; ++k)
+      if (!owns<NARROW, N>(u, k, d)) v[k] = 0.f;
   }
 }
 
