@@ -14,44 +14,45 @@ namespace {
 
 // ---- lookup -------------------------------------------------------------------------------------
 
-constexpr int kThreads = 256, kPerThread = 4, kUnits = kThreads * kPerThread;
-
 struct Lookup {
   const int32_t *ids, *positions;
-  int T, d, V, P;
-  uint32_t per_row;           // units in a row
-  int64_t ldw, ldp, ldx, total, tiles;
+  int V, P;
+  int64_t ldw, ldp, ldx;
   float scale;
 };
 
-// Units are numbered row by row, a workgroup takes kUnits of them.  A token's row is found through its id, so that a lane waits twice
-// for memory before it stores: all of its ids are on their way together, and then all of its rows.
-template <typename E, typename O, bool NARROW>
-__global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *table, const E *pos_table, O *x) {
+// A token's row is found through its id, so that a lane waits twice for memory before it stores: all of its ids are on their way together,
+// and then all of its rows.
+template <typename E, typename O, int K, bool NARROW>
+__global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *table, const E *pos_table, O *x, Units units) {
   constexpr int N = 16 / sizeof(O);
-  for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const int64_t row0 = tile * kUnits / g.per_row;
-    const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
-    Unit u[kPerThread];
-    int64_t t[kPerThread];
+  for (int64_t tile = blockIdx.x; tile < units.tiles; tile += gridDim.x) {
+    const Places at = places_of<K, NARROW, N>(units, tile);
     int id[kPerThread], place[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
-      const bool there = tile * kUnits + threadIdx.x + i * kThreads < g.total;
-      const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
-      u[i] = unit_at<NARROW, N>(int(at - down * g.per_row) * N, g.d);
-      if (!there) u[i].skip = N;
-      t[i] = there ? row0 + down : row0;
-      id[i] = g.ids[t[i]];
+      if (K && i % (K ? K : 1)) {   // the same row
+        id[i] = id[i - 1];
+        place[i] = place[i - 1];
+        continue;
+      }
+      id[i] = g.ids[at.row[i]];
       place[i] = -1;
-      if (g.positions) place[i] = g.positions[t[i]];
-      else if (g.P) place[i] = int(uint32_t(t[i]) % uint32_t(g.P));
+      if (g.positions) place[i] = g.positions[at.row[i]];
+      else if (g.P) place[i] = int(uint32_t(at.row[i]) % uint32_t(g.P));
+    }
+    if constexpr (K > 0) {
+#pragma unroll
+      for (int i = 0; i < kPerThread; ++i) {
+        id[i] = __builtin_amdgcn_readfirstlane(id[i]);
+        place[i] = __builtin_amdgcn_readfirstlane(place[i]);
+      }
     }
     Cols<E, N> v[kPerThread], p[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {   // what names no row reads the first one and drops it
-      load_unit<NARROW>(v[i], table + (uint32_t(id[i]) < uint32_t(g.V) ? id[i] : 0) * g.ldw, u[i], g.d);
-      if (g.P) load_unit<NARROW>(p[i], pos_table + (uint32_t(place[i]) < uint32_t(g.P) ? place[i] : 0) * g.ldp, u[i], g.d);
+      load_unit<NARROW>(v[i], table + (uint32_t(id[i]) < uint32_t(g.V) ? id[i] : 0) * g.ldw, at.u[i], units.d);
+      if (g.P) load_unit<NARROW>(p[i], pos_table + (uint32_t(place[i]) < uint32_t(g.P) ? place[i] : 0) * g.ldp, at.u[i], units.d);
     }
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
@@ -59,7 +60,7 @@ __global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *ta
       float o[N];
 #pragma unroll
       for (int k = 0; k < N; ++k) o[k] = fmaf(named ? v[i].at(k) : 0.f, g.scale, placed ? p[i].at(k) : 0.f);
-      store_unit<NARROW>(x + t[i] * g.ldx, o, u[i], g.d);
+      store_unit<NARROW>(x + at.row[i] * g.ldx, o, at.u[i], units.d);
     }
   }
 }
@@ -649,13 +650,13 @@ int launch_embed_lookup(const hmy_embed_lookup_desc &g, stream_t st) {
                         {"positions", g.positions, int64_t(g.T) * 4, int64_t(g.T) * 4, 1, false}};
   rc = check_apart(who, spans);
   if (rc) return rc;
-  Lookup a = {g.ids, g.positions, g.T, g.d, g.V, g.P, uint32_t((g.d + 16 / o - 1) / (16 / o)), g.ldw, g.ldp, g.ldx, 0, 0, g.scale};
-  a.total = int64_t(g.T) * a.per_row;
-  a.tiles = (a.total + kUnits - 1) / kUnits;
-  const dim3 grid(uint32_t(std::min<int64_t>(a.tiles, kMaxGrid)));
+  const Lookup a = {g.ids, g.positions, g.V, g.P, g.ldw, g.ldp, g.ldx, g.scale};
+  const Shares h = shares_of(g.T, g.d, 16 / o, 16 / o);
   DISPATCH_ROWS(g.prec, g.out_prec, {
-    auto *kernel = g.d < 8 ? k_embed_lookup<L, E, true> : k_embed_lookup<L, E, false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)st, a, (const L *)g.table, (const L *)g.pos_table, (E *)g.x);
+    DISPATCH_SHARES(h.K, g.d, {
+      hipLaunchKernelGGL((k_embed_lookup<L, E, K, NARROW>), h.grid, dim3(kThreads), 0, (hipStream_t)st, a, (const L *)g.table, (const L *)g.pos_table, (E *)g.x,
+                         h.units);
+    });
   });
   return check_launch(who);
 }

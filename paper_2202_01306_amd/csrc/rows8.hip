@@ -102,48 +102,11 @@ template <int CODE, int N> __device__ __forceinline__ void decode(const uint32_t
   for (int i = 0; i < N / 4; ++i) decode4<CODE>(w[i], s, v + 4 * i);
 }
 
-// Units are rounded up to whole groups and numbered row by row: a workgroup takes kUnits of them, and finds the row of each by one
-// 32-bit division from that of its first.
-constexpr int kThreads = 256, kPerThread = 4, kUnits = kThreads * kPerThread;
-
-struct Units {
-  int d;
-  uint32_t per_row;
-  int64_t total, tiles;
-};
-template <int N> inline Units units_of(int T, int d) {
-  Units u;
-  u.d = d;
-  u.per_row = uint32_t((d + kGroup - 1) / kGroup * (kGroup / N));
-  u.total = int64_t(T) * u.per_row;
-  u.tiles = (u.total + kUnits - 1) / kUnits;
-  return u;
-}
-struct Places {
-  int64_t row[kPerThread];
-  Unit u[kPerThread];
-};
-// Where the thread's units are; for those behind the last row's the tile's first row is read, and nothing of it is theirs.
-template <bool NARROW, int N> __device__ __forceinline__ Places places_of(const Units &g, int64_t tile) {
-  Places p;
-  const int64_t row0 = tile * kUnits / g.per_row;
-  const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
-#pragma unroll
-  for (int i = 0; i < kPerThread; ++i) {
-    const bool there = tile * kUnits + threadIdx.x + i * kThreads < g.total;
-    const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
-    p.u[i] = unit_at<NARROW, N>(int(at - down * g.per_row) * N, g.d);
-    p.row[i] = there ? row0 + down : row0;
-    if (!there) p.u[i].skip = N;
-  }
-  return p;
-}
-
-template <typename E, int CODE, bool NARROW>
+template <typename E, int CODE, int K, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, Units g) {
   constexpr int N = 16 / sizeof(E);
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const Places p = places_of<NARROW, N>(g, tile);
+    const Places p = places_of<K, NARROW, N>(g, tile);
     Cols<E, N> raw[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) load_unit<NARROW>(raw[i], x + p.row[i] * ldx, p.u[i], g.d);
@@ -168,11 +131,11 @@ __global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uin
   }
 }
 
-template <typename E, int CODE, bool NARROW>
+template <typename E, int CODE, int K, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_unpack8(Rows8 r, E *x, int64_t ldx, Units g) {
   constexpr int N = 16 / sizeof(E);
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const Places p = places_of<NARROW, N>(g, tile);
+    const Places p = places_of<K, NARROW, N>(g, tile);
     uint32_t w[kPerThread][N / 4], byte[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
@@ -461,12 +424,12 @@ static int check_move8(const char *who, const hmy_rows8_desc &g, bool pack) {
 int launch_pack8(const hmy_rows8_desc &g, stream_t st) {
   const int rc = check_move8("pack8", g, true);
   if (rc) return rc;
-  const Units u = g.prec == HMY_PREC_BF16 ? units_of<8>(g.T, g.d) : units_of<4>(g.T, g.d);
-  const dim3 grid(uint32_t(std::min<int64_t>(u.tiles, kMaxGrid)));
+  const Shares h = shares_of(g.T, g.d, 16 / bytes_of(g.prec), kGroup);
   DISPATCH_ROWS8(g.prec, g.code, {
-    auto *kernel = g.d < 8 ? k_pack8<E, CODE, true> : k_pack8<E, CODE, false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)st, (const E *)g.x, g.ldx, (uint8_t *)g.codes, g.ldc,
-                       (uint8_t *)g.scales, g.lds, u);
+    DISPATCH_SHARES(h.K, g.d, {
+      hipLaunchKernelGGL((k_pack8<E, CODE, K, NARROW>), h.grid, dim3(kThreads), 0, (hipStream_t)st, (const E *)g.x, g.ldx, (uint8_t *)g.codes, g.ldc,
+                         (uint8_t *)g.scales, g.lds, h.units);
+    });
   });
   return check_launch("pack8");
 }
@@ -474,12 +437,12 @@ int launch_pack8(const hmy_rows8_desc &g, stream_t st) {
 int launch_unpack8(const hmy_rows8_desc &g, stream_t st) {
   const int rc = check_move8("unpack8", g, false);
   if (rc) return rc;
-  const Units u = g.prec == HMY_PREC_BF16 ? units_of<8>(g.T, g.d) : units_of<4>(g.T, g.d);
+  const Shares h = shares_of(g.T, g.d, 16 / bytes_of(g.prec), kGroup);
   const Rows8 r = {(const uint8_t *)g.codes, (const uint8_t *)g.scales, g.ldc, g.lds};
-  const dim3 grid(uint32_t(std::min<int64_t>(u.tiles, kMaxGrid)));
   DISPATCH_ROWS8(g.prec, g.code, {
-    auto *kernel = g.d < 8 ? k_unpack8<E, CODE, true> : k_unpack8<E, CODE, false>;
-    hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, (hipStream_t)st, r, (E *)g.x, g.ldx, u);
+    DISPATCH_SHARES(h.K, g.d, {
+      hipLaunchKernelGGL((k_unpack8<E, CODE, K, NARROW>), h.grid, dim3(kThreads), 0, (hipStream_t)st, r, (E *)g.x, g.ldx, h.units);
+    });
   });
   return check_launch("unpack8");
 }

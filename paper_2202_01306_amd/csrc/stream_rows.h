@@ -102,6 +102,55 @@ template <bool NARROW, int N> __device__ __forceinline__ void clear_foreign(floa
   }
 }
 
+// ---- the units of rows, shared out over a launch ----
+// Wide rows: a wave takes kPerThread / K rows, K units of each a lane, with everything but the column in scalar registers; tiles of
+// kWaves waves, one chunk of their rows after the other.  K = 0: rows of less than half a wave's units are numbered through instead,
+// unit by unit, and a lane finds its row by one 32-bit division from that of its workgroup's first (some 150 instructions a unit, against
+// some 40: a lookup of 32768 x 1024 fp32 took 46 us that way, most of it in these).
+constexpr int kThreads = 256, kWaves = kThreads / kWave, kPerThread = 4;
+
+struct Units {
+  int T, d;
+  uint32_t per_row;           // K = 0: units in a row
+  uint32_t chunks;            // of 64 K N columns in a row
+  int64_t tiles;              // times chunks
+};
+struct Places {
+  int64_t row[kPerThread];
+  Unit u[kPerThread];
+};
+// Where the thread's units are; for those behind the last row's another row is read, and nothing of it is theirs.
+template <int K, bool NARROW, int N> __device__ __forceinline__ Places places_of(const Units &g, int64_t tile) {
+  Places p;
+  const int lane = threadIdx.x % kWave;
+  if constexpr (K > 0) {
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int64_t rows = tile / g.chunks;
+    const int chunk = int(tile - rows * g.chunks);
+    const int64_t row0 = (rows * kWaves + wave) * (kPerThread / K);
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      const int64_t row = row0 + i / K;
+      p.row[i] = min(row, int64_t(g.T) - 1);
+      p.u[i] = unit_at<NARROW, N>(((chunk * K + i % K) * kWave + lane) * N, g.d);
+      if (row >= g.T) p.u[i].skip = N;
+    }
+  } else {
+    constexpr int kUnits = kThreads * kPerThread;
+    const int64_t row0 = tile * kUnits / g.per_row;
+    const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
+#pragma unroll
+    for (int i = 0; i < kPerThread; ++i) {
+      const uint32_t at = first + threadIdx.x + i * kThreads, down = at / g.per_row;
+      const bool there = row0 + down < g.T;
+      p.u[i] = unit_at<NARROW, N>(int(at - down * g.per_row) * N, g.d);
+      p.row[i] = there ? row0 + down : row0;
+      if (!there) p.u[i].skip = N;
+    }
+  }
+  return p;
+}
+
 // ---- on the host ----
 inline bool known_prec(int prec) { return prec == HMY_PREC_FP32 || prec == HMY_PREC_BF16; }
 
@@ -116,6 +165,32 @@ inline int check_extent(const char *who, int T, int d, int most) {
   if (T < 1 || d < 1 || d > most) return fail(HMY_E_INVALID, "%s: T >= 1 and 1 <= d <= %d wanted, got T = %d, d = %d", who, most, T, d);
   return HMY_OK;
 }
+
+// How rows of d columns in units of N, rounded up to `whole` columns, are shared out: K, and the launch's extent.
+struct Shares {
+  Units units;
+  int K;
+  dim3 grid;
+};
+inline Shares shares_of(int T, int d, int N, int whole) {
+  Shares s;
+  const int per_row = (d + whole - 1) / whole * (whole / N), waves = (per_row + kWave - 1) / kWave;
+  s.K = per_row < kWave / 2 ? 0 : waves >= 3 ? 4 : waves;
+  s.units = {T, d, uint32_t(per_row), s.K ? uint32_t((waves + s.K - 1) / s.K) : 1u, 0};
+  const int64_t parts = s.K ? (int64_t(T) + kPerThread / s.K - 1) / (kPerThread / s.K) : (int64_t(T) * per_row + kWave * kPerThread - 1) / (kWave * kPerThread);
+  s.units.tiles = (parts + kWaves - 1) / kWaves * s.units.chunks;
+  s.grid = dim3(uint32_t(s.units.tiles < kMaxGrid ? s.units.tiles : kMaxGrid));
+  return s;
+}
+#define DISPATCH_SHARES(k, d, ...)                                                   \
+  do {                                                                               \
+    constexpr bool NARROW = false;                                                   \
+    if ((d) < 8) { constexpr int K = 0; constexpr bool NARROW = true; __VA_ARGS__ }  \
+    else if ((k) == 0) { constexpr int K = 0; __VA_ARGS__ }                          \
+    else if ((k) == 1) { constexpr int K = 1; __VA_ARGS__ }                          \
+    else if ((k) == 2) { constexpr int K = 2; __VA_ARGS__ }                          \
+    else { constexpr int K = 4; __VA_ARGS__ }                                        \
+  } while (0)
 
 // T rows of `cols` bytes at a pitch of `ld` bytes
 struct Span {
