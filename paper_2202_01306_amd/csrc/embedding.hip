@@ -126,13 +126,18 @@ __global__ __launch_bounds__(kRankThreads) void k_rank_tokens(const int32_t *ids
   __syncthreads();
   const uint32_t key = all[min(t0 + token, T - 1)];
   uint32_t n = 0;
-  for (int i = 0; i < rounds; ++i) {
-    const int at = 4 * (i * kRankParts + part);
-    // equal keys keep their order: those of tokens before these count; among these themselves below
-    const uint32_t below = at < t0 ? key + 1 : at < t0 + kRankTokens ? 0 : key;
-    const uint4 k = *reinterpret_cast<const uint4 *>(all + at);
+  const uint4 *p = reinterpret_cast<const uint4 *>(all) + part;
+  auto compare = [&](int round, uint32_t below) {
+    const uint4 k = p[round * kRankParts];
     n += (k.x < below) + (k.y < below) + (k.z < below) + (k.w < below);
-  }
+  };
+  // equal keys keep their order: those of tokens before these count; among these themselves below
+  const int own = t0 / (4 * kRankParts), at = 4 * (own * kRankParts + part);
+#pragma unroll 4
+  for (int i = 0; i < own; ++i) compare(i, key + 1);
+  compare(own, at < t0 ? key + 1 : at < t0 + kRankTokens ? 0 : key);
+#pragma unroll 4
+  for (int i = own + 1; i < rounds; ++i) compare(i, key);
   counts[part][token] = n;
   __syncthreads();
   if (tid < kRankTokens && t0 + tid < T) {
@@ -687,7 +692,7 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   const hipStream_t s = (hipStream_t)st;
   const int T = g.T;
   const bool few = T <= kFew;
-  Runs a = {nullptr, nullptr, g.ids, T, g.d, g.V, T <= kMostRanked ? 16 : 64, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale};
+  Runs a = {nullptr, nullptr, g.ids, T, g.d, g.V, T <= kMostRanked ? 16 : 32, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale};
   a.pieces = (T + a.piece - 1) / a.piece;
   a.partial = (float *)g.workspace + (int64_t(wanted) / 4 - 2 * int64_t(g.d) * a.pieces) / 4 * 4;   // at the workspace's end
   const int slab = kWave * (g.prec == HMY_PREC_BF16 ? 8 : 4), join_slabs = (g.d + 255) / 256;
