@@ -303,10 +303,12 @@ struct Runs {
   float *dtable;
   float *partial;                 // per piece: the sum of a run's tokens in a piece that it goes through, of those in the piece that it starts in
   float scale;
+  int fill_rows;                  // rows that a wave looks after
 };
 
 constexpr int kAhead = 16;        // rows on their way at a time
-constexpr int kFillRows = 4, kFillColumns = 1024;   // rows of a wave, and columns, that it may have to write
+// A wave that may have to write rows with zeros looks after up to kMostFilled rows and kFillColumns columns of them, some 16 KB.
+constexpr int kMostFilled = 64, kFillColumns = 1024;
 
 // A wave's columns of a row: a slab of kWave * N, N neighbouring ones a lane (WHOLE), or the last columns of a row, which are fewer, every
 // 64th a lane's: those behind the end read the last one, and nothing comes of it.
@@ -488,17 +490,17 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, in
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (int(blockIdx.x) >= run_groups) {
     const int job = int(blockIdx.x) - run_groups, slabs = (g.d + kFillColumns - 1) / kFillColumns;
-    const int64_t row0 = (int64_t(job / slabs) * 4 + wave) * kFillRows, row = row0 + lane;
+    const int64_t row0 = (int64_t(job / slabs) * 4 + wave) * g.fill_rows, row = row0 + lane;
     int lo = keys_below(g, row0, lane), hi = g.T;
     // a lane looks for one of the rows behind that
-    if (lane >= kFillRows) hi = lo;
+    if (lane >= g.fill_rows) hi = lo;
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
       if (int64_t(g.keys[mid]) < row) lo = mid + 1;
       else hi = mid;
     }
     const bool named = row >= g.V || (lo < g.T && int64_t(g.keys[lo]) == row);
-    zero_rows(g, row0, __ballot(!named && lane < kFillRows), job % slabs * kFillColumns, lane);
+    zero_rows(g, row0, __ballot(!named && lane < g.fill_rows), job % slabs * kFillColumns, lane);
     return;
   }
   const int64_t job = int64_t(blockIdx.x) * 4 + wave;
@@ -509,43 +511,64 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, in
 }
 
 // The runs that go through whole pieces: the sum of the piece that one starts in, and of those that follow.  A workgroup looks at
-// kJoinPieces pieces; four waves take a fourth of a run's parts each, joined in one order.
-constexpr int kJoinPieces = 16;
+// kJoinPieces pieces.  Runs of up to kShortRun parts are a wave's each; of a longer one each of the four waves takes a fourth of the
+// parts, joined in one order.
+constexpr int kJoinPieces = 16, kShortRun = 8;
 
-template <bool WHOLE, bool ADD> __device__ __forceinline__ void join_run(const Runs &g, int piece, int slab, int lane, int wave, float (&part)[4][kWave * 4]) {
-  constexpr int N = 4;
-  const Slab<float, WHOLE> s(slab, lane, g.d);
-  const uint32_t key = g.keys[(piece + 1) * g.piece];
-  int parts = 0;                  // pieces that the run goes through, all but the end of the last one
+// parts q0 .. q1 - 1 of the run that starts in `piece`, added to sum
+template <bool WHOLE, int DEEP> __device__ __forceinline__ void add_parts(const Runs &g, const Slab<float, WHOLE> &s, int piece, int q0, int q1, float (&sum)[4]) {
+  for (int q = q0; q < q1; q += DEEP) {
+    float v[DEEP][4];
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i) s.load(v[i], g.partial + int64_t(2 * (piece + 1 + min(q + i, q1 - 1))) * g.d);
+#pragma unroll
+    for (int i = 0; i < DEEP; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sum[k] += q + i < q1 ? v[i][k] : 0.f;
+  }
+}
+// pieces that the run of `key` goes through behind the one that it starts in: all but the end of the last one
+__device__ __forceinline__ int parts_of(const Runs &g, int piece, uint32_t key, int lane) {
+  int parts = 0;
   for (int q = piece + 1;; q += kWave) {
     const int64_t next = int64_t(q + lane + 1) * g.piece;
     const int more = __popcll(__ballot(next < g.T && g.keys[min(next, int64_t(g.T) - 1)] == key));
     parts += more;
-    if (more < kWave) break;
+    if (more < kWave) return parts;
   }
-  const int per = (parts + 3) / 4, q1 = min(parts, (wave + 1) * per);
-  float sum[N] = {0.f, 0.f, 0.f, 0.f}, old[N];
-  if (wave == 0) s.load(sum, g.partial + int64_t(2 * piece + 1) * g.d);
-  if (ADD && wave == 0) s.load(old, g.dtable + int64_t(key) * g.ldt);
-  for (int q = wave * per; q < q1; q += 8) {
-    float v[8][N];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) s.load(v[i], g.partial + int64_t(2 * (piece + 1 + min(q + i, q1 - 1))) * g.d);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int k = 0; k < N; ++k) sum[k] += q + i < q1 ? v[i][k] : 0.f;
-  }
-  __syncthreads();                // of the run before, whose parts wave 0 has read
-#pragma unroll
-  for (int k = 0; k < N; ++k) part[wave][lane * N + k] = sum[k];
-  __syncthreads();
-  if (wave == 0) {
-#pragma unroll
-    for (int w = 1; w < 4; ++w)
-#pragma unroll
-      for (int k = 0; k < N; ++k) sum[k] += part[w][lane * N + k];
+}
+template <bool WHOLE, bool ADD> __device__ __forceinline__ void join_runs(const Runs &g, uint64_t shorts, uint64_t longs, int piece0, int slab, int lane, int wave, float (&part)[4][kWave * 4]) {
+  const Slab<float, WHOLE> s(slab, lane, g.d);
+  float sum[4], old[4];
+  for (int turn = 0; shorts; ++turn, shorts &= shorts - 1) {
+    if (turn % 4 != wave) continue;
+    const int piece = piece0 + __builtin_ctzll(shorts);
+    const uint32_t key = g.keys[(piece + 1) * g.piece];
+    s.load(sum, g.partial + int64_t(2 * piece + 1) * g.d);
+    if (ADD) s.load(old, g.dtable + int64_t(key) * g.ldt);
+    add_parts<WHOLE, kShortRun>(g, s, piece, 0, parts_of(g, piece, key, lane), sum);
     write_row<ADD>(g, s, key, sum, old);
+  }
+  for (; longs; longs &= longs - 1) {
+    const int piece = piece0 + __builtin_ctzll(longs);
+    const uint32_t key = g.keys[(piece + 1) * g.piece];
+    const int parts = parts_of(g, piece, key, lane), per = (parts + 3) / 4;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[k] = 0.f;
+    if (wave == 0) s.load(sum, g.partial + int64_t(2 * piece + 1) * g.d);
+    if (ADD && wave == 0) s.load(old, g.dtable + int64_t(key) * g.ldt);
+    add_parts<WHOLE, 16>(g, s, piece, wave * per, min(parts, (wave + 1) * per), sum);
+    __syncthreads();              // of the run before, whose parts wave 0 has read
+#pragma unroll
+    for (int k = 0; k < 4; ++k) part[wave][lane * 4 + k] = sum[k];
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int w = 1; w < 4; ++w)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sum[k] += part[w][lane * 4 + k];
+      write_row<ADD>(g, s, key, sum, old);
+    }
   }
 }
 
@@ -554,19 +577,17 @@ __global__ __launch_bounds__(256) void k_embed_grad_join(Runs g, int slabs) {
   __shared__ float part[4][kWave * 4];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int piece0 = int(blockIdx.x / slabs) * kJoinPieces, slab = int(blockIdx.x % slabs);
-  bool starts = false;
-  const int64_t p0 = int64_t(piece0 + lane) * g.piece, p1 = p0 + g.piece, p2 = p1 + g.piece;
+  bool starts = false, is_long = false;
+  const int64_t p0 = int64_t(piece0 + lane) * g.piece, p1 = p0 + g.piece, p2 = p1 + g.piece, far = p1 + int64_t(kShortRun + 1) * g.piece;
   if (lane < kJoinPieces && p2 < g.T) {
-    const uint32_t key = g.keys[p1];
-    starts = key < uint32_t(g.V) && g.keys[p1 - 1] == key && g.keys[p2] == key && !(p0 > 0 && g.keys[p0 - 1] == key);
+    const uint32_t key = g.keys[p1], next = g.keys[p2], last = g.keys[p1 - 1], before = g.keys[max(p0 - 1, int64_t(0))], beyond = g.keys[min(far, int64_t(g.T) - 1)];
+    starts = key < uint32_t(g.V) && last == key && next == key && !(p0 > 0 && before == key);
+    is_long = far < g.T && beyond == key;
   }
-  uint64_t todo = __ballot(starts);
-  while (todo) {
-    const int piece = piece0 + __builtin_ctzll(todo);
-    todo &= todo - 1;
-    if ((slab + 1) * Slab<float, true>::WIDTH <= g.d) join_run<true, ADD>(g, piece, slab, lane, wave, part);
-    else join_run<false, ADD>(g, piece, slab, lane, wave, part);
-  }
+  const uint64_t shorts = __ballot(starts && !is_long), longs = __ballot(starts && is_long);
+  if (!(shorts | longs)) return;
+  if ((slab + 1) * Slab<float, true>::WIDTH <= g.d) join_runs<true, ADD>(g, shorts, longs, piece0, slab, lane, wave, part);
+  else join_runs<false, ADD>(g, shorts, longs, piece0, slab, lane, wave, part);
 }
 
 // Few tokens, in one launch: a wave looks through all ids for those that equal its token's; the first of them adds up their rows.
@@ -596,17 +617,18 @@ template <typename E, bool WHOLE, bool ADD> __device__ __forceinline__ void sum_
 template <typename E, bool ADD>
 __global__ __launch_bounds__(256) void k_embed_grad_few(Runs g, const E *dx, int run_groups) {
   __shared__ uint16_t list[4][kFew];
-  __shared__ uint32_t named[4 * kFillRows];
+  __shared__ uint32_t named[4 * kMostFilled];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (int(blockIdx.x) >= run_groups) {
     const int job = int(blockIdx.x) - run_groups, slabs = (g.d + kFillColumns - 1) / kFillColumns;
-    const int64_t row0 = int64_t(job / slabs) * 4 * kFillRows;
-    if (threadIdx.x < 4 * kFillRows) named[threadIdx.x] = row0 + threadIdx.x >= g.V;
+    const int n = 4 * g.fill_rows;
+    const int64_t row0 = int64_t(job / slabs) * n;
+    named[threadIdx.x] = row0 + threadIdx.x >= g.V;
     __syncthreads();
     const int64_t at = threadIdx.x < unsigned(g.T) ? int64_t(g.ids[threadIdx.x]) - row0 : -1;
-    if (at >= 0 && at < 4 * kFillRows && at + row0 < g.V) named[at] = 1;
+    if (at >= 0 && at < n) named[at] = 1;
     __syncthreads();
-    zero_rows(g, row0, __ballot(lane < 4 * kFillRows && !named[lane] && lane / kFillRows == wave), job % slabs * kFillColumns, lane);
+    zero_rows(g, row0 + wave * g.fill_rows, __ballot(lane < g.fill_rows && !named[wave * g.fill_rows + lane]), job % slabs * kFillColumns, lane);
     return;
   }
   const int64_t job = int64_t(blockIdx.x) * 4 + wave;
@@ -692,13 +714,13 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   const hipStream_t s = (hipStream_t)st;
   const int T = g.T;
   const bool few = T <= kFew;
-  Runs a = {nullptr, nullptr, g.ids, T, g.d, g.V, T <= kMostRanked ? 16 : 32, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale};
+  Runs a = {nullptr, nullptr, g.ids, T, g.d, g.V, T <= kMostRanked ? 16 : 32, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale, std::max(4, std::min(kMostFilled, 4096 / std::min(g.d, kFillColumns)))};
   a.pieces = (T + a.piece - 1) / a.piece;
   a.partial = (float *)g.workspace + (int64_t(wanted) / 4 - 2 * int64_t(g.d) * a.pieces) / 4 * 4;   // at the workspace's end
   const int slab = kWave * (g.prec == HMY_PREC_BF16 ? 8 : 4), join_slabs = (g.d + 255) / 256;
   a.slabs = (g.d + slab - 1) / slab;
   const int64_t run_groups = (int64_t(few ? T : a.pieces) * a.slabs + 3) / 4;
-  const int64_t fill_groups = g.accumulate ? 0 : (int64_t(g.V) + 4 * kFillRows - 1) / (4 * kFillRows) * ((g.d + kFillColumns - 1) / kFillColumns);
+  const int64_t fill_groups = g.accumulate ? 0 : (int64_t(g.V) + 4 * a.fill_rows - 1) / (4 * a.fill_rows) * ((g.d + kFillColumns - 1) / kFillColumns);
   const int64_t join_groups = (int64_t(a.pieces) + kJoinPieces - 1) / kJoinPieces * join_slabs;
   constexpr int64_t kMostGroups = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
   if (run_groups + fill_groups > kMostGroups || join_groups > kMostGroups) return fail(HMY_E_INVALID, "%s: T, d and V are too large together", who);
