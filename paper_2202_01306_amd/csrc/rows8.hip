@@ -153,13 +153,23 @@ __global__ __launch_bounds__(kThreads) void k_unpack8(Rows8 r, E *x, int64_t ldx
 
 // ---- layer norm of rows in 8 bits -------------------------------------------------------------
 
-// A row is W waves', NJ units of kN columns a lane: wave w of it has the units 64 NJ w + lane + 64 j.  Sums over a row: within the wave by lane moves,
-// between waves through LDS, added in the same order by each of them.
+// A row is LPR lanes' of a wave (8, 16, 32 or 64: narrow rows lie side by side in one), or W waves', NJ units of kN columns a lane: wave w of
+// a row has the units 64 NJ w + lane + 64 j.  Sums over a row: between lanes by moves, between waves through LDS, added in the same order
+// by each of them.
 constexpr int kN = 4;
 
-template <int W, int M> __device__ __forceinline__ void row_sums(float (&s)[M], float (*xch)[M], int wave) {
+template <int LPR> __device__ __forceinline__ float lanes_total(float x) {
+  if constexpr (LPR == 64) return wave_total(x);
+  x += lane_move<0xb1, 0xf>(x, 0.f);                            // from lane ^ 1
+  x += lane_move<0x4e, 0xf>(x, 0.f);                            // from lane ^ 2
+  x += lane_move<0x141, 0xf>(x, 0.f);                           // from the other four of eight
+  if constexpr (LPR >= 16) x += lane_move<0x140, 0xf>(x, 0.f);  // from the other eight of sixteen
+  if constexpr (LPR >= 32) x += __shfl_xor(x, 16, kWave);
+  return x;
+}
+template <int LPR, int W, int M> __device__ __forceinline__ void row_sums(float (&s)[M], float (*xch)[M], int wave) {
 #pragma unroll
-  for (int i = 0; i < M; ++i) s[i] = wave_total(s[i]);
+  for (int i = 0; i < M; ++i) s[i] = lanes_total<LPR>(s[i]);
   if constexpr (W > 1) {
     if (threadIdx.x % kWave == 0)
 #pragma unroll
@@ -182,63 +192,79 @@ struct Norm8 {
   float eps;
 };
 
-template <typename E, int CODE, int W, int NJ, bool NARROW>
+// A wave has ROWS rows (times 64 / LPR) on their way at a time.
+template <typename E, int CODE, int LPR, int W, int NJ, int ROWS, bool NARROW>
 __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma, const E *beta, E *y, float *x) {
-  constexpr int kSlots = 4 / W;
-  __shared__ float xch[2][2][4][1];   // of a round's two sums, and of the round before, which a wave may still read
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  static_assert((LPR == 64 && W * ROWS >= 1) || (W == 1 && NJ == 1), "narrow rows are one unit a lane");
+  constexpr int kAbreast = kWave / LPR, kSlot = ROWS * kAbreast, kSlots = 4 / W * kSlot;
+  __shared__ float xch[2][2][4][ROWS];   // of a round's two sums, and of the round before, which a wave may still read
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   Unit u[NJ];
   Cols<E, kN> ga[NJ], be[NJ];
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    u[j] = unit_at<NARROW, kN>(kN * (kWave * (NJ * (wave % W) + j) + lane), g.d);
+    u[j] = unit_at<NARROW, kN>(kN * (kWave * (NJ * (wave % W) + j) + lane % LPR), g.d);
     load_unit<NARROW>(ga[j], gamma, u[j], g.d);
     load_unit<NARROW>(be[j], beta, u[j], g.d);
   }
   int parity = 0;
   for (int64_t base = int64_t(blockIdx.x) * kSlots; base < g.T; base += int64_t(gridDim.x) * kSlots, parity ^= 1) {
-    const int64_t row = min(base + wave / W, int64_t(g.T) - 1);   // a slot behind the last row does that row again, and stores nothing
-    const bool live = base + wave / W < g.T;
-    float v[NJ][kN], s[1] = {0.f};
-    uint32_t w[NJ][kN / 4], byte[NJ];
+    const int64_t first = base + wave / W * kSlot + (LPR < kWave ? lane / LPR : 0);
+    float v[ROWS][NJ][kN], s[ROWS], mu[ROWS];
+    uint32_t w[ROWS][NJ][kN / 4], byte[ROWS][NJ];
+    int64_t row[ROWS];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      load_codes<NARROW, kN>(w[j], g.r.codes + row * g.r.ldc, u[j], g.d);
-      byte[j] = g.r.scales[row * g.r.lds + group_of<NARROW, kN>(u[j])];
+    for (int r = 0; r < ROWS; ++r) {
+      row[r] = min(first + r * kAbreast, int64_t(g.T) - 1);   // one behind the last row does that row again, and stores nothing
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        load_codes<NARROW, kN>(w[r][j], g.r.codes + row[r] * g.r.ldc, u[j], g.d);
+        byte[r][j] = g.r.scales[row[r] * g.r.lds + group_of<NARROW, kN>(u[j])];
+      }
     }
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      decode<CODE>(w[j], byte[j], v[j]);
-      clear_foreign<NARROW>(v[j], u[j], g.d);
+    for (int r = 0; r < ROWS; ++r) {
+      s[r] = 0.f;
 #pragma unroll
-      for (int k = 0; k < kN; ++k) s[0] += v[j][k];
+      for (int j = 0; j < NJ; ++j) {
+        decode<CODE>(w[r][j], byte[r][j], v[r][j]);
+        clear_foreign<NARROW>(v[r][j], u[j], g.d);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) s[r] += v[r][j][k];
+      }
     }
-    row_sums<W>(s, xch[parity][0], wave);
-    const float mu = s[0] / float(g.d);
-    s[0] = 0.f;
+    row_sums<LPR, W>(s, xch[parity][0], wave);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      float t[kN];
+    for (int r = 0; r < ROWS; ++r) {
+      mu[r] = s[r] / float(g.d);
+      s[r] = 0.f;
 #pragma unroll
-      for (int k = 0; k < kN; ++k) t[k] = v[j][k] - mu;
-      clear_foreign<NARROW>(t, u[j], g.d);
+      for (int j = 0; j < NJ; ++j) {
+        float t[kN];
 #pragma unroll
-      for (int k = 0; k < kN; ++k) s[0] = fmaf(t[k], t[k], s[0]);
+        for (int k = 0; k < kN; ++k) t[k] = v[r][j][k] - mu[r];
+        clear_foreign<NARROW>(t, u[j], g.d);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) s[r] = fmaf(t[k], t[k], s[r]);
+      }
     }
-    row_sums<W>(s, xch[parity][1], wave);
-    const float rs = 1.f / sqrtf(s[0] / float(g.d) + g.eps);
-    if (!live) continue;
-    if (lane == 0 && wave % W == 0) {
-      if (g.mean) g.mean[row] = mu;
-      if (g.rstd) g.rstd[row] = rs;
-    }
+    row_sums<LPR, W>(s, xch[parity][1], wave);
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      float o[kN];
+    for (int r = 0; r < ROWS; ++r) {
+      if (first + r * kAbreast >= g.T) continue;
+      const float rs = 1.f / sqrtf(s[r] / float(g.d) + g.eps);
+      if (lane % LPR == 0 && wave % W == 0) {
+        if (g.mean) g.mean[row[r]] = mu[r];
+        if (g.rstd) g.rstd[row[r]] = rs;
+      }
 #pragma unroll
-      for (int k = 0; k < kN; ++k) o[k] = fmaf(ga[j].at(k), (v[j][k] - mu) * rs, be[j].at(k));
-      store_unit<NARROW>(y + row * g.ldy, o, u[j], g.d);
-      if (x) store_unit<NARROW>(x + row * g.ldx, v[j], u[j], g.d);
+      for (int j = 0; j < NJ; ++j) {
+        float o[kN];
+#pragma unroll
+        for (int k = 0; k < kN; ++k) o[k] = fmaf(ga[j].at(k), (v[r][j][k] - mu[r]) * rs, be[j].at(k));
+        store_unit<NARROW>(y + row[r] * g.ldy, o, u[j], g.d);
+        if (x) store_unit<NARROW>(x + row[r] * g.ldx, v[r][j], u[j], g.d);
+      }
     }
   }
 }
@@ -266,19 +292,21 @@ template <typename E, int NJ> struct Row8 {
 
 // The rows of a workgroup's slots leave their column sums in registers; at the end the slots' meet in LDS and one row of sums per
 // workgroup goes to the workspace.
-template <typename E, int CODE, int W, int NJ, bool NARROW>
+template <typename E, int CODE, int LPR, int W, int NJ, bool NARROW>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_layernorm8_bwd(Norm8Grad g, const E *dy, const E *gamma, E *dx_e) {
-  constexpr int kWaves = 8, kSlots = kWaves / W;
+  static_assert(LPR == 64 || (W == 1 && NJ == 1), "narrow rows are one unit a lane");
+  constexpr int kWaves = 8, kSlots = kWaves / W, kAbreast = kWave / LPR;
   extern __shared__ __align__(16) float lds[];   // kSlots > 1: per slot its sums' ns rows of d floats
   __shared__ float xch[2][kWaves][2];
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, slot = wave / W;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), slot = wave / W;
   const int ns = g.sums[2] ? 3 : 2;
   Unit u[NJ];
   float dg[NJ][kN], db[NJ][kN], dr[NJ][kN];
   Cols<E, kN> ga[NJ];
   Row8<E, NJ> now, next;
   auto fetch = [&](Row8<E, NJ> &r, int64_t base) {
-    const int64_t row = min(base + slot, int64_t(g.T) - 1);   // a slot behind the last row does that row again, and nothing comes of it
+    // a slot behind the last row does that row again, and nothing comes of it
+    const int64_t row = min(base + slot * kAbreast + (LPR < kWave ? lane / LPR : 0), int64_t(g.T) - 1);
     r.mean = g.mean[row];
     r.rstd = g.rstd[row];
 #pragma unroll
@@ -291,17 +319,17 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
   };
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
-    u[j] = unit_at<NARROW, kN>(kN * (kWave * (NJ * (wave % W) + j) + lane), g.d);
+    u[j] = unit_at<NARROW, kN>(kN * (kWave * (NJ * (wave % W) + j) + lane % LPR), g.d);
     load_unit<NARROW>(ga[j], gamma, u[j], g.d);
 #pragma unroll
     for (int k = 0; k < kN; ++k) dg[j][k] = db[j][k] = dr[j][k] = 0.f;
   }
-  const int64_t step = int64_t(gridDim.x) * kSlots;
+  const int64_t step = int64_t(gridDim.x) * kSlots * kAbreast;
   int parity = 0;
-  fetch(now, int64_t(blockIdx.x) * kSlots);
-  for (int64_t base = int64_t(blockIdx.x) * kSlots; base < g.T; base += step, parity ^= 1) {
+  fetch(now, int64_t(blockIdx.x) * kSlots * kAbreast);
+  for (int64_t base = int64_t(blockIdx.x) * kSlots * kAbreast; base < g.T; base += step, parity ^= 1) {
     if (base + step < g.T) fetch(next, base + step);
-    const int64_t row = base + slot;
+    const int64_t row = base + slot * kAbreast + (LPR < kWave ? lane / LPR : 0);
     const bool live = row < g.T;
     float xh[NJ][kN], gy[NJ][kN], s[2] = {0.f, 0.f};
 #pragma unroll
@@ -321,7 +349,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
         s[1] = fmaf(t, xh[j][k], s[1]);
       }
     }
-    row_sums<W>(s, xch[parity], wave);
+    row_sums<LPR, W>(s, xch[parity], wave);
     const float m1 = s[0] / float(g.d), m2 = s[1] / float(g.d);
     if (live) {
 #pragma unroll
@@ -342,6 +370,16 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       }
     }
     now = next;
+  }
+  if constexpr (LPR < kWave) {   // rows side by side in the wave: their sums, left in each of them
+#pragma unroll
+    for (int k = 0; k < kN; ++k)
+#pragma unroll
+      for (int o = LPR; o < kWave; o *= 2) {
+        dg[0][k] += __shfl_xor(dg[0][k], o, kWave);
+        db[0][k] += __shfl_xor(db[0][k], o, kWave);
+        dr[0][k] += __shfl_xor(dr[0][k], o, kWave);
+      }
   }
   float *out = g.partial + int64_t(blockIdx.x) * ns * g.d;
   float *mine = kSlots > 1 ? lds + int64_t(slot) * ns * g.d : out;
@@ -463,18 +501,26 @@ int launch_layernorm8_fwd(const hmy_layernorm8_desc &g, stream_t st) {
   rc = check_apart(who, spans);
   if (rc) return rc;
   const Norm8 a = {{(const uint8_t *)g.codes, (const uint8_t *)g.scales, g.ldc, g.lds}, g.T, g.d, g.ldy, g.ldx, g.mean, g.rstd, g.eps};
-  const int slots = g.d <= 2048 ? 4 : 1;
-  const dim3 grid(uint32_t(std::min<int64_t>((int64_t(g.T) + slots - 1) / slots, kMaxGrid)));
   const hipStream_t s = (hipStream_t)st;
-#define NORM8_FWD(W, NJ, NARROW) hipLaunchKernelGGL((k_layernorm8_fwd<E, CODE, W, NJ, NARROW>), grid, dim3(256), 0, s, a, (const E *)g.gamma, (const E *)g.beta, (E *)g.y, g.x)
+#define NORM8_FWD(LPR, W, NJ, ROWS, NARROW)                                                                                             \
+  do {                                                                                                                                  \
+    constexpr int kRows = 4 / W * ROWS * (kWave / LPR);                                                                                 \
+    const dim3 grid(uint32_t(std::min<int64_t>((int64_t(g.T) + kRows - 1) / kRows, kMaxGrid)));                                          \
+    hipLaunchKernelGGL((k_layernorm8_fwd<E, CODE, LPR, W, NJ, ROWS, NARROW>), grid, dim3(256), 0, s, a, (const E *)g.gamma, (const E *)g.beta, \
+                       (E *)g.y, g.x);                                                                                                  \
+  } while (0)
   DISPATCH_ROWS8(g.prec, g.code, {
-    if (g.d < 8) NORM8_FWD(1, 1, true);
-    else if (g.d <= 256) NORM8_FWD(1, 1, false);
-    else if (g.d <= 512) NORM8_FWD(1, 2, false);
-    else if (g.d <= 1024) NORM8_FWD(1, 4, false);
-    else if (g.d <= 2048) NORM8_FWD(1, 8, false);
-    else if (g.d <= 4096) NORM8_FWD(4, 4, false);
-    else NORM8_FWD(4, 8, false);
+    if (g.d < 8) NORM8_FWD(8, 1, 1, 2, true);
+    else if (g.d <= 32) NORM8_FWD(8, 1, 1, 2, false);
+    else if (g.d <= 64) NORM8_FWD(16, 1, 1, 2, false);
+    else if (g.d <= 128) NORM8_FWD(32, 1, 1, 2, false);
+    else if (g.d <= 256) NORM8_FWD(64, 1, 1, 2, false);
+    else if (g.d <= 512) NORM8_FWD(64, 1, 2, 1, false);
+    else if (g.d <= 1024 && g.T >= 8192) NORM8_FWD(64, 1, 4, 2, false);
+    else if (g.d <= 1024) NORM8_FWD(64, 1, 4, 1, false);
+    else if (g.d <= 2048) NORM8_FWD(64, 1, 8, 1, false);
+    else if (g.d <= 4096) NORM8_FWD(64, 4, 4, 1, false);
+    else NORM8_FWD(64, 4, 8, 1, false);
   });
 #undef NORM8_FWD
   return check_launch(who);
@@ -509,18 +555,23 @@ int launch_layernorm8_bwd(const hmy_layernorm8_grad_desc &g, stream_t st) {
   const Norm8Grad a = {{(const uint8_t *)g.codes, (const uint8_t *)g.scales, g.ldc, g.lds}, g.T, g.d, g.ldy, g.ldr, g.ldx, g.lde, g.mean, g.rstd, g.res, g.dx,
                        {g.dgamma, g.dbeta, g.dres_sum}, (float *)g.workspace, g.accumulate};
   const int W = g.d <= 1024 ? 1 : g.d <= 2048 ? 2 : g.d <= 4096 ? 4 : 8, slots = 8 / W, ns = g.dres_sum ? 3 : 2;
-  const int groups = int(std::min<int64_t>((int64_t(g.T) + slots - 1) / slots, kGradGroups));
+  const int abreast = g.d <= 32 ? 8 : g.d <= 64 ? 4 : g.d <= 128 ? 2 : 1, rows = slots * abreast;
+  const int groups = int(std::min<int64_t>((int64_t(g.T) + rows - 1) / rows, kGradGroups));
   const size_t lds = slots > 1 ? size_t(slots) * ns * g.d * 4 : 0;
   const hipStream_t s = (hipStream_t)st;
-#define NORM8_BWD(W, NJ, NARROW) hipLaunchKernelGGL((k_layernorm8_bwd<E, CODE, W, NJ, NARROW>), dim3(groups), dim3(512), lds, s, a, (const E *)g.dy, (const E *)g.gamma, (E *)g.dx_e)
+#define NORM8_BWD(LPR, W, NJ, NARROW) \
+  hipLaunchKernelGGL((k_layernorm8_bwd<E, CODE, LPR, W, NJ, NARROW>), dim3(groups), dim3(512), lds, s, a, (const E *)g.dy, (const E *)g.gamma, (E *)g.dx_e)
   DISPATCH_ROWS8(g.prec, g.code, {
-    if (g.d < 8) NORM8_BWD(1, 1, true);
-    else if (g.d <= 256) NORM8_BWD(1, 1, false);
-    else if (g.d <= 512) NORM8_BWD(1, 2, false);
-    else if (g.d <= 1024) NORM8_BWD(1, 4, false);
-    else if (g.d <= 2048) NORM8_BWD(2, 4, false);
-    else if (g.d <= 4096) NORM8_BWD(4, 4, false);
-    else NORM8_BWD(8, 4, false);
+    if (g.d < 8) NORM8_BWD(8, 1, 1, true);
+    else if (g.d <= 32) NORM8_BWD(8, 1, 1, false);
+    else if (g.d <= 64) NORM8_BWD(16, 1, 1, false);
+    else if (g.d <= 128) NORM8_BWD(32, 1, 1, false);
+    else if (g.d <= 256) NORM8_BWD(64, 1, 1, false);
+    else if (g.d <= 512) NORM8_BWD(64, 1, 2, false);
+    else if (g.d <= 1024) NORM8_BWD(64, 1, 4, false);
+    else if (g.d <= 2048) NORM8_BWD(64, 2, 4, false);
+    else if (g.d <= 4096) NORM8_BWD(64, 4, 4, false);
+    else NORM8_BWD(64, 8, 4, false);
   });
 #undef NORM8_BWD
   hipLaunchKernelGGL(k_layernorm8_sums, dim3((ns * g.d + 63) / 64), dim3(1024), 0, s, a, groups);
