@@ -310,59 +310,21 @@ constexpr int kAhead = 16;        // rows on their way at a time
 // A wave that may have to write rows with zeros looks after up to kMostFilled rows and kFillColumns columns of them, some 16 KB.
 constexpr int kMostFilled = 64, kFillColumns = 1024;
 
-// A wave's columns of a row: a slab of kWave * N, N neighbouring ones a lane (WHOLE), or the last columns of a row, which are fewer, every
-// 64th a lane's: those behind the end read the last one, and nothing comes of it.
-template <typename E, bool WHOLE> struct Slab {
-  static constexpr int N = ElemTraits<E>::VEC, WIDTH = kWave * N;
-  int c, d;
-  __device__ __forceinline__ Slab(int slab, int lane, int d_) : c(slab * WIDTH + (WHOLE ? lane * N : lane)), d(d_) {}
-  struct Raw {
-    uint32_t w[WHOLE ? 4 : N];
-    __device__ __forceinline__ float at(int k) const {
-      if constexpr (sizeof(E) == 4) return __uint_as_float(w[k]);
-      else if constexpr (WHOLE) return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
-      else return __uint_as_float(w[k] << 16);
-    }
-  };
-  __device__ __forceinline__ void load(Raw &v, const E *row) const {
-    if constexpr (WHOLE) {
-      typedef typename Unaligned<E>::type unaligned;
-      const u32x4 a = *reinterpret_cast<const unaligned *>(row + c);
-      v.w[0] = a.x; v.w[1] = a.y; v.w[2] = a.z; v.w[3] = a.w;
-    } else {
-#pragma unroll
-      for (int k = 0; k < N; ++k) {
-        if constexpr (sizeof(E) == 4) v.w[k] = __float_as_uint(row[min(c + kWave * k, d - 1)]);
-        else v.w[k] = reinterpret_cast<const uint16_t *>(row)[min(c + kWave * k, d - 1)];
-      }
-    }
-  }
+// A wave's columns of a row: a slab of kWave * N of them, a unit a lane.
+template <typename E, bool NARROW> struct Slab {
+  static constexpr int N = ElemTraits<E>::VEC;
+  typedef Cols<E, N> Raw;
+  Unit u;
+  int d;
+  __device__ __forceinline__ Slab(int slab, int lane, int d_) : u(unit_at<NARROW, N>((slab * kWave + lane) * N, d_)), d(d_) {}
+  __device__ __forceinline__ void load(Raw &v, const E *row) const { load_unit<NARROW>(v, row, u, d); }
   __device__ __forceinline__ void load(float (&v)[N], const float *row) const {
-    if constexpr (WHOLE) {
+    Cols<float, N> c;
+    load_unit<NARROW>(c, row, u, d);
 #pragma unroll
-      for (int k = 0; k < N; k += 4) {
-        const u32x4 a = *reinterpret_cast<const u32x4_by4 *>(row + c + k);
-        v[k] = __uint_as_float(a.x); v[k + 1] = __uint_as_float(a.y); v[k + 2] = __uint_as_float(a.z); v[k + 3] = __uint_as_float(a.w);
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < N; ++k) v[k] = row[min(c + kWave * k, d - 1)];
-    }
+    for (int k = 0; k < N; ++k) v[k] = c.at(k);
   }
-  __device__ __forceinline__ void store(float *row, const float (&v)[N]) const {
-    if constexpr (WHOLE) {
-#pragma unroll
-      for (int k = 0; k < N; k += 4) {
-        u32x4 a;
-        a.x = __float_as_uint(v[k]); a.y = __float_as_uint(v[k + 1]); a.z = __float_as_uint(v[k + 2]); a.w = __float_as_uint(v[k + 3]);
-        *reinterpret_cast<u32x4_by4 *>(row + c + k) = a;
-      }
-    } else {
-#pragma unroll
-      for (int k = 0; k < N; ++k)
-        if (c + kWave * k < d) row[c + kWave * k] = v[k];
-    }
-  }
+  __device__ __forceinline__ void store(float *row, const float (&v)[N]) const { store_unit<NARROW>(row, v, u, d); }
 };
 
 // sum to row `key`, whose present content is `old` if that is added to
@@ -412,9 +374,9 @@ __device__ __forceinline__ int behind_run(const Runs &g, int lo, int hi, uint32_
 
 // A wave sums a piece of the sorted list over a slab of columns.  A run that ends in the piece behind the one that it starts in, or behind
 // one that it goes through, is taken along to its end; so only runs that go through a whole piece leave parts of their sum to be joined.
-template <typename E, bool WHOLE, bool ADD> __device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
+template <typename E, bool NARROW, bool ADD> __device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
   constexpr int N = ElemTraits<E>::VEC;
-  const Slab<E, WHOLE> s(slab, lane, g.d);
+  const Slab<E, NARROW> s(slab, lane, g.d);
   int p = piece * g.piece, end = min(g.T, p + g.piece);
   uint32_t key = g.keys[p];
   if (key >= uint32_t(g.V)) return;
@@ -456,7 +418,7 @@ template <typename E, bool WHOLE, bool ADD> __device__ __forceinline__ void sum_
       keys = 0xffffffffu;
       order = first;
     }
-    typename Slab<E, WHOLE>::Raw v[kAhead];
+    typename Slab<E, NARROW>::Raw v[kAhead];
     float old[ADD ? kAhead : 1][N];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) s.load(v[i], dx + int64_t(__builtin_amdgcn_readlane(order, i)) * g.ldx);
@@ -485,7 +447,7 @@ template <typename E, bool WHOLE, bool ADD> __device__ __forceinline__ void sum_
 }
 
 // The workgroups behind those of the sums write the rows that no token names.
-template <typename E, bool ADD>
+template <typename E, bool NARROW, bool ADD>
 __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, int run_groups) {
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (int(blockIdx.x) >= run_groups) {
@@ -506,8 +468,7 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, in
   const int64_t job = int64_t(blockIdx.x) * 4 + wave;
   const int piece = int(job / g.slabs), slab = int(job % g.slabs);
   if (piece >= g.pieces) return;
-  if ((slab + 1) * Slab<E, true>::WIDTH <= g.d) sum_piece<E, true, ADD>(g, dx, piece, slab, lane);
-  else sum_piece<E, false, ADD>(g, dx, piece, slab, lane);
+  sum_piece<E, NARROW, ADD>(g, dx, piece, slab, lane);
 }
 
 // The runs that go through whole pieces: the sum of the piece that one starts in, and of those that follow.  A workgroup looks at
@@ -516,7 +477,7 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, in
 constexpr int kJoinPieces = 16, kShortRun = 8;
 
 // parts q0 .. q1 - 1 of the run that starts in `piece`, added to sum
-template <bool WHOLE, int DEEP> __device__ __forceinline__ void add_parts(const Runs &g, const Slab<float, WHOLE> &s, int piece, int q0, int q1, float (&sum)[4]) {
+template <bool NARROW, int DEEP> __device__ __forceinline__ void add_parts(const Runs &g, const Slab<float, NARROW> &s, int piece, int q0, int q1, float (&sum)[4]) {
   for (int q = q0; q < q1; q += DEEP) {
     float v[DEEP][4];
 #pragma unroll
@@ -537,8 +498,8 @@ __device__ __forceinline__ int parts_of(const Runs &g, int piece, uint32_t key, 
     if (more < kWave) return parts;
   }
 }
-template <bool WHOLE, bool ADD> __device__ __forceinline__ void join_runs(const Runs &g, uint64_t shorts, uint64_t longs, int piece0, int slab, int lane, int wave, float (&part)[4][kWave * 4]) {
-  const Slab<float, WHOLE> s(slab, lane, g.d);
+template <bool NARROW, bool ADD> __device__ __forceinline__ void join_runs(const Runs &g, uint64_t shorts, uint64_t longs, int piece0, int slab, int lane, int wave, float (&part)[4][kWave * 4]) {
+  const Slab<float, NARROW> s(slab, lane, g.d);
   float sum[4], old[4];
   for (int turn = 0; shorts; ++turn, shorts &= shorts - 1) {
     if (turn % 4 != wave) continue;
@@ -546,7 +507,7 @@ template <bool WHOLE, bool ADD> __device__ __forceinline__ void join_runs(const 
     const uint32_t key = g.keys[(piece + 1) * g.piece];
     s.load(sum, g.partial + int64_t(2 * piece + 1) * g.d);
     if (ADD) s.load(old, g.dtable + int64_t(key) * g.ldt);
-    add_parts<WHOLE, kShortRun>(g, s, piece, 0, parts_of(g, piece, key, lane), sum);
+    add_parts<NARROW, kShortRun>(g, s, piece, 0, parts_of(g, piece, key, lane), sum);
     write_row<ADD>(g, s, key, sum, old);
   }
   for (; longs; longs &= longs - 1) {
@@ -557,7 +518,7 @@ template <bool WHOLE, bool ADD> __device__ __forceinline__ void join_runs(const 
     for (int k = 0; k < 4; ++k) sum[k] = 0.f;
     if (wave == 0) s.load(sum, g.partial + int64_t(2 * piece + 1) * g.d);
     if (ADD && wave == 0) s.load(old, g.dtable + int64_t(key) * g.ldt);
-    add_parts<WHOLE, 16>(g, s, piece, wave * per, min(parts, (wave + 1) * per), sum);
+    add_parts<NARROW, 16>(g, s, piece, wave * per, min(parts, (wave + 1) * per), sum);
     __syncthreads();              // of the run before, whose parts wave 0 has read
 #pragma unroll
     for (int k = 0; k < 4; ++k) part[wave][lane * 4 + k] = sum[k];
@@ -572,7 +533,7 @@ template <bool WHOLE, bool ADD> __device__ __forceinline__ void join_runs(const 
   }
 }
 
-template <bool ADD>
+template <bool NARROW, bool ADD>
 __global__ __launch_bounds__(256) void k_embed_grad_join(Runs g, int slabs) {
   __shared__ float part[4][kWave * 4];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -586,23 +547,22 @@ __global__ __launch_bounds__(256) void k_embed_grad_join(Runs g, int slabs) {
   }
   const uint64_t shorts = __ballot(starts && !is_long), longs = __ballot(starts && is_long);
   if (!(shorts | longs)) return;
-  if ((slab + 1) * Slab<float, true>::WIDTH <= g.d) join_runs<true, ADD>(g, shorts, longs, piece0, slab, lane, wave, part);
-  else join_runs<false, ADD>(g, shorts, longs, piece0, slab, lane, wave, part);
+  join_runs<NARROW, ADD>(g, shorts, longs, piece0, slab, lane, wave, part);
 }
 
 // Few tokens, in one launch: a wave looks through all ids for those that equal its token's; the first of them adds up their rows.
 constexpr int kFew = 256;
 
-template <typename E, bool WHOLE, bool ADD> __device__ __forceinline__ void sum_alike(const Runs &g, const E *dx, uint32_t key, const uint16_t *list, int n, int slab, int lane) {
+template <typename E, bool NARROW, bool ADD> __device__ __forceinline__ void sum_alike(const Runs &g, const E *dx, uint32_t key, const uint16_t *list, int n, int slab, int lane) {
   constexpr int N = ElemTraits<E>::VEC;
-  const Slab<E, WHOLE> s(slab, lane, g.d);
+  const Slab<E, NARROW> s(slab, lane, g.d);
   float sum[N], old[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) sum[k] = 0.f;
   if constexpr (ADD) s.load(old, g.dtable + int64_t(key) * g.ldt);
   for (int p = 0; p < n; p += kAhead) {
     const uint32_t order = list[min(p + lane % kAhead, n - 1)];
-    typename Slab<E, WHOLE>::Raw v[kAhead];
+    typename Slab<E, NARROW>::Raw v[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) s.load(v[i], dx + int64_t(__builtin_amdgcn_readlane(order, i)) * g.ldx);
 #pragma unroll
@@ -614,7 +574,7 @@ template <typename E, bool WHOLE, bool ADD> __device__ __forceinline__ void sum_
   write_row<ADD>(g, s, key, sum, old);
 }
 
-template <typename E, bool ADD>
+template <typename E, bool NARROW, bool ADD>
 __global__ __launch_bounds__(256) void k_embed_grad_few(Runs g, const E *dx, int run_groups) {
   __shared__ uint16_t list[4][kFew];
   __shared__ uint32_t named[4 * kMostFilled];
@@ -649,8 +609,7 @@ __global__ __launch_bounds__(256) void k_embed_grad_few(Runs g, const E *dx, int
   }
   wave_sees_lds();
   if (__builtin_amdgcn_readfirstlane(list[wave][0]) != t) return;
-  if ((slab + 1) * Slab<E, true>::WIDTH <= g.d) sum_alike<E, true, ADD>(g, dx, uint32_t(id), list[wave], n, slab, lane);
-  else sum_alike<E, false, ADD>(g, dx, uint32_t(id), list[wave], n, slab, lane);
+  sum_alike<E, NARROW, ADD>(g, dx, uint32_t(id), list[wave], n, slab, lane);
 }
 
 }  // namespace
@@ -725,12 +684,17 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   constexpr int64_t kMostGroups = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
   if (run_groups + fill_groups > kMostGroups || join_groups > kMostGroups) return fail(HMY_E_INVALID, "%s: T, d and V are too large together", who);
   const dim3 grid{uint32_t(run_groups + fill_groups)}, threads(256);
-#define GRAD(KERNEL)                                                                                                                       \
-  do {                                                                                                                                     \
-    if (g.prec == HMY_PREC_BF16) hipLaunchKernelGGL((g.accumulate ? KERNEL<bf16_t, true> : KERNEL<bf16_t, false>), grid, threads, 0, s, a, \
-                                                    (const bf16_t *)g.dx, int(run_groups));                                                \
-    else hipLaunchKernelGGL((g.accumulate ? KERNEL<float, true> : KERNEL<float, false>), grid, threads, 0, s, a, (const float *)g.dx,      \
-                            int(run_groups));                                                                                              \
+#define GRAD_AS(KERNEL, E, NARROW) \
+  hipLaunchKernelGGL((g.accumulate ? KERNEL<E, NARROW, true> : KERNEL<E, NARROW, false>), grid, threads, 0, s, a, (const E *)g.dx, int(run_groups))
+#define GRAD(KERNEL)                                             \
+  do {                                                           \
+    if (g.prec == HMY_PREC_BF16) {                               \
+      if (g.d < 8) GRAD_AS(KERNEL, bf16_t, true);                \
+      else GRAD_AS(KERNEL, bf16_t, false);                       \
+    } else {                                                     \
+      if (g.d < 8) GRAD_AS(KERNEL, float, true);                 \
+      else GRAD_AS(KERNEL, float, false);                        \
+    }                                                            \
   } while (0)
   if (few) {
     GRAD(k_embed_grad_few);
@@ -760,7 +724,10 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   a.order = order[sorted];
   GRAD(k_embed_grad_runs);
 #undef GRAD
-  hipLaunchKernelGGL((g.accumulate ? k_embed_grad_join<true> : k_embed_grad_join<false>), dim3(uint32_t(join_groups)), threads, 0, s, a, join_slabs);
+#undef GRAD_AS
+  auto *join = g.d < 8 ? (g.accumulate ? k_embed_grad_join<true, true> : k_embed_grad_join<true, false>)
+                       : (g.accumulate ? k_embed_grad_join<false, true> : k_embed_grad_join<false, false>);
+  hipLaunchKernelGGL(join, dim3(uint32_t(join_groups)), threads, 0, s, a, join_slabs);
   return check_launch(who);
 }
 
