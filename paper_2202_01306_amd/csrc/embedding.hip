@@ -2,8 +2,10 @@
 //
 // The gradient of a lookup adds up rows that share a token.  Sorted by token (and, for one token, in their own order) those rows are
 // neighbours, a sum is a run of the sorted list, and no row of the table is written by two workgroups: no atomics, one order.
-// Three steps: the sort (keys only: 8 bytes per token), the sums of runs inside pieces of the list, and the joining of those runs that
-// cross from one piece into the next.  Bound by HBM: every row of dx is read once, every row of the table written once.
+// Three steps: the order (keys only: 8 bytes per token), the sums of runs inside pieces of the list, and the joining of those runs that
+// go through whole pieces.  Bound by HBM where there are many tokens: every row of dx is read once, every row of the table written once.
+// 131072 tokens of 1024 fp32 columns, 30522 rows, 662 MB: 180 us, of which 23 for the order (two passes, four launches), 146 for the sums
+// (4.5 TB/s) and 9 for the joining; 4096 tokens, 50257 rows of which most are empty, 222 MB: 6, 40 (5.5 TB/s) and 4.5.
 #include <algorithm>
 
 #include "stream_rows.h"
@@ -22,7 +24,9 @@ struct Lookup {
 };
 
 // A token's row is found through its id, so that a lane waits twice for memory before it stores: all of its ids are on their way together,
-// and then all of its rows.
+// and then all of its rows.  Bound by HBM, with what the eight L2s each fetch of popular rows: 32768 tokens of 1024 columns, bf16 to fp32
+// with positions, 134 MB written and 41 read (20 of them what the call cannot do without): 43 us (4.1 TB/s; from a table of 512 rows,
+// which the L2s hold, 29).  Workgroups that stay and fetch their next rows ahead take 47 to 49.
 template <typename E, typename O, int K, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *table, const E *pos_table, O *x, Units units) {
   constexpr int N = 16 / sizeof(O);
@@ -114,7 +118,8 @@ __device__ __forceinline__ uint32_t digits_before(uint32_t x, uint32_t *scratch)
 
 // Up to kMostRanked tokens: a token's place is the number of tokens before it in the order, counted by comparing it with all of them.  A
 // workgroup places kRankTokens tokens against a copy of all keys in LDS; each sixteen lanes of its waves compare them with a 64th of the
-// keys, four at a time.  4096 tokens are a comparison and an addition for each of 64 keys a lane.
+// keys, four at a time: for 4096 tokens a comparison and an addition for each of 64 keys a lane.  4096 tokens: 5.8 us in one launch; 16384
+// take 34, the radix sort's four launches 21.
 constexpr int kMostRanked = 8192, kRankThreads = 1024, kRankTokens = 16, kRankParts = kRankThreads / kRankTokens;
 
 __global__ __launch_bounds__(kRankThreads) void k_rank_tokens(const int32_t *ids, int T, int V, uint32_t *keys, uint32_t *order) {
@@ -154,8 +159,9 @@ __global__ __launch_bounds__(kRankThreads) void k_rank_tokens(const int32_t *ids
 // More tokens: stable sorting by eight bits of the key at a time, least ones first, a pass in two launches: counts[tile][digit] of tiles of
 // kTile tokens, then each tile's tokens to their places, which are behind those of the digits before, of the tiles before, and of the waves
 // before.  A wave takes 64 tokens at a time: the lanes that share a digit find each other by eight ballots, which gives each its rank among
-// them, and the first of them advances the digit's counter, so that counters are a wave's own and need no atomics.
-constexpr int kTile = 1024, kTileWaves = 4, kSteps = kTile / kTileWaves / kWave;
+// them, and the first of them advances the digit's counter, so that counters are a wave's own and need no atomics.  Bound by latency: a
+// pass of 131072 tokens takes 4 and 8 us with eight waves a tile (4 and 10 with four).
+constexpr int kTile = 1024, kTileWaves = 8, kSteps = kTile / kTileWaves / kWave;
 constexpr int kTilesRead = 256;   // tiles whose counts a tile adds up by itself; of more, a launch in between has added them up
 
 struct Sort {
@@ -194,10 +200,12 @@ __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_count(Sort g) {
   load_keys(g, key, begin);
   count_digits(g, key, begin, at[wave], (uint64_t(1) << lane) - 1, lane);
   __syncthreads();
-  uint32_t n = 0;
+  if (tid < kDigits) {
+    uint32_t n = 0;
 #pragma unroll
-  for (int w = 0; w < kTileWaves; ++w) n += at[w][tid];
-  g.counts[int64_t(blockIdx.x) * kDigits + tid] = n;
+    for (int w = 0; w < kTileWaves; ++w) n += at[w][tid];
+    g.counts[int64_t(blockIdx.x) * kDigits + tid] = n;
+  }
 }
 
 // Many tiles: counts become those of the tiles before, with the totals behind the last.  64 digits a workgroup, whose waves take a
@@ -228,7 +236,7 @@ __global__ __launch_bounds__(1024) void k_sort_scan(uint32_t *counts, int tiles)
 }
 
 __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(Sort g, uint32_t *to_keys, uint32_t *to_order) {
-  static_assert(kTileWaves * kWave == kDigits, "a thread per digit");
+  static_assert(kTileWaves * kWave >= kDigits, "a thread per digit");
   __shared__ uint32_t at[kTileWaves][kDigits];
   __shared__ uint4 sums[2][kTileWaves][kWave];   // per wave and digit: counts of its tiles, of those before this one
   __shared__ uint32_t scratch[kDigits / kWave];
@@ -244,7 +252,7 @@ __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(Sort g, uint32
   }
   uint32_t total = 0, mine = 0;   // of this thread's digit: in all tiles, in those before
   if (g.tiles <= kTilesRead) {
-    // each wave takes every fourth tile, four digits a lane
+    // the waves take turns at the tiles, four digits a lane
     uint4 all = make_uint4(0, 0, 0, 0), some = all;
     const uint4 *p = reinterpret_cast<const uint4 *>(g.counts) + lane;
 #pragma unroll 16
@@ -255,13 +263,13 @@ __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(Sort g, uint32
     }
     sums[0][wave][lane] = all;
     sums[1][wave][lane] = some;
-  } else {
+  } else if (tid < kDigits) {
     total = g.counts[int64_t(g.tiles) * kDigits + tid];
     mine = g.counts[int64_t(tile) * kDigits + tid];
   }
   count_digits(g, key, begin, at[wave], before, lane);
   __syncthreads();
-  if (g.tiles <= kTilesRead) {
+  if (g.tiles <= kTilesRead && tid < kDigits) {
 #pragma unroll
     for (int w = 0; w < kTileWaves; ++w) {
       total += reinterpret_cast<const uint32_t *>(sums[0][w])[tid];
@@ -269,12 +277,13 @@ __global__ __launch_bounds__(kTileWaves *kWave) void k_sort_place(Sort g, uint32
     }
   }
   uint32_t run = digits_before(total, scratch) + mine;
+  if (tid < kDigits)
 #pragma unroll
-  for (int w = 0; w < kTileWaves; ++w) {
-    const uint32_t n = at[w][tid];
-    at[w][tid] = run;
-    run += n;
-  }
+    for (int w = 0; w < kTileWaves; ++w) {
+      const uint32_t n = at[w][tid];
+      at[w][tid] = run;
+      run += n;
+    }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < kSteps; ++i) {
@@ -374,6 +383,8 @@ __device__ __forceinline__ int behind_run(const Runs &g, int lo, int hi, uint32_
 
 // A wave sums a piece of the sorted list over a slab of columns.  A run that ends in the piece behind the one that it starts in, or behind
 // one that it goes through, is taken along to its end; so only runs that go through a whole piece leave parts of their sum to be joined.
+// Pieces of 16 tokens up to kMostRanked, for the waves' number, of 32 beyond (16384 x 1024 fp32: 78 us with 16, 79 with 32, 81 with 64; 131072
+// x 1024: 190, 184, 184).  kAhead rows are on their way before the first is added (8 instead of 16: 90 instead of 81 us at 16384 x 1024).
 template <typename E, bool NARROW, bool ADD> __device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
   constexpr int N = ElemTraits<E>::VEC;
   const Slab<E, NARROW> s(slab, lane, g.d);
@@ -398,13 +409,7 @@ template <typename E, bool NARROW, bool ADD> __device__ __forceinline__ void sum
     if (next < g.T && g.keys[next] == last) {
       goes_on = true;
     } else {
-      int lo = end, hi = next;                        // to the first of another key
-      while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (g.keys[mid] == last) lo = mid + 1;
-        else hi = mid;
-      }
-      end = lo;
+      end = behind_run(g, end, next, last);
     }
   }
   const uint32_t first = g.order[p];
@@ -550,7 +555,9 @@ __global__ __launch_bounds__(256) void k_embed_grad_join(Runs g, int slabs) {
   join_runs<NARROW, ADD>(g, shorts, longs, piece0, slab, lane, wave, part);
 }
 
-// Few tokens, in one launch: a wave looks through all ids for those that equal its token's; the first of them adds up their rows.
+// Few tokens, in one launch: a wave looks through all ids for those that equal its token's; the first of them adds up their rows.  Bound
+// by the launch: 20 tokens of 64 columns 5 us, 12 by the three steps.  The rows of one token are one wave's: 16 rows at a time, so that up
+// to kFew of them take no longer than those steps.
 constexpr int kFew = 256;
 
 template <typename E, bool NARROW, bool ADD> __device__ __forceinline__ void sum_alike(const Runs &g, const E *dx, uint32_t key, const uint16_t *list, int n, int slab, int lane) {

@@ -195,7 +195,7 @@ struct Norm8 {
 // A wave has ROWS rows (times 64 / LPR) on their way at a time.
 template <typename E, int CODE, int LPR, int W, int NJ, int ROWS, bool NARROW>
 __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma, const E *beta, E *y, float *x) {
-  static_assert((LPR == 64 && W * ROWS >= 1) || (W == 1 && NJ == 1), "narrow rows are one unit a lane");
+  static_assert(LPR == 64 || (W == 1 && NJ == 1), "narrow rows are one unit a lane");
   constexpr int kAbreast = kWave / LPR, kSlot = ROWS * kAbreast, kSlots = 4 / W * kSlot;
   __shared__ float xch[2][2][4][ROWS];   // of a round's two sums, and of the round before, which a wave may still read
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);

@@ -3,15 +3,18 @@ oracle, element by element.
 
 Bounds, in units of u = 2^-24, half a step of fp32 relative to the value.
   lookup       one multiply-add: u |x|; a bf16 output is rounded once more, by 2^-8 of its value
-  gradient     a sum of n rows: a term passes through at most 64 additions in its piece of the list, a quarter of the pieces of the run
-               and 5 more where those join, D(n) = min(n, 64 + n / 64 + 8); with the scaling (D + 1) u of the sum of magnitudes, and u of
-               the result where it is added to what is there
+  gradient     a sum of n rows: one after the other in calls of up to 256 tokens, D = n; in longer ones a term passes through at most 63
+               additions in its piece of the list and the one behind (32 tokens each), a quarter of the run's pieces or 8 of them, and 5
+               more where those join, D = min(n, 64 + n / 64 + 8); with the scaling (D + 1) u of the sum of magnitudes, and u of the
+               result where it is added to what is there
   8 bits       codes, scales and what is read are exact
-  layer norm   a sum over a row: a term passes through 8 NJ <= 32 additions in a lane, 6 in the wave, 4 between waves: D = 44.
+  layer norm   a sum over a row: a term passes through up to 32 additions in a lane, 6 in the wave, 4 between waves (16, 6 and 8 in the
+               backward pass): D = 44 at most.
                mean: (D + 1) u mean|v| =: m.  v - mean is off by m + u |v - mean|; the terms that are linear in m cancel in the variance, which is
                off by (D + 4) u relative and m^2; rstd by half that and 4 u for its sum, root and quotient
   its gradient xh carries 2 u, g = dy gamma one more; the two means are off by (D + 4) u of the mean magnitudes of their terms; dx is
-               formed of three terms by five operations.  Sums over T rows: ceil(T / 256) additions in a slot, 8 slots, 32 partial sums"""
+               formed of three terms by five operations.  Sums over T rows: ceil(T / 256) additions at most in a lane, 3 between rows side by
+               side in a wave, 8 waves, 16 and 16 of the 256 partial sums: ceil(T / 256) + 8 + 32 has room for them"""
 import ctypes
 import math
 
@@ -124,8 +127,8 @@ def text_like(rng, T, V):
     return rng.permutation(V)[rank]
 
 
-def depth(n):
-    return np.minimum(n, 64 + n / 64 + 8)
+def depth(n, T):
+    return n if T <= 256 else np.minimum(n, 64 + n / 64 + 8)
 
 
 def grad(prec, ids, dx, V, d, ldx, ldt, scale=1.0, accumulate=False, into=None, ws=None, stream=None):
@@ -161,7 +164,7 @@ def test_gradient_of_a_table_against_64_bits(prec, T, d, V, ldx, ldt, shift):
     if V > 1 << 20:
         bad = (ids < 0) | (ids >= V)
         ref, size, n = os_.embed_grad(np.where(bad, -1, np.searchsorted(named, ids)), dx, len(named), s)
-    bound = (depth(n)[:, None] + 1) * U * size
+    bound = (depth(n, len(ids))[:, None] + 1) * U * size
     t = grad(prec, i32(ids), dd, V, d, ldx, ldt, scale)
     again = grad(prec, i32(ids), dd, V, d, ldx, ldt, scale)
     assert torch.equal(t, again)                         # one order, whatever order workgroups run in
@@ -185,7 +188,7 @@ def test_gradient_of_a_table_against_64_bits(prec, T, d, V, ldx, ldt, shift):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 15, 16, 17, 100, 1000, 16384, 17000])
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 100, 256, 257, 1000, 8192, 8193, 16384, 17000])
 @pytest.mark.parametrize("kind", ["one", "none", "ascending", "descending", "last", "blocks"])
 def test_gradient_of_lists_where_it_can_go_wrong(T, kind):
     say(f"grad {kind} T={T}")
@@ -196,7 +199,48 @@ def test_gradient_of_lists_where_it_can_go_wrong(T, kind):
     dx = np.random.default_rng(T).standard_normal((T, d)).astype(np.float32)
     ref, size, n = os_.embed_grad(ids, dx, V)
     t = grad("fp32", i32(ids), rows_of(dx, d, torch.float32), V, d, d, d)
-    near(host(t), ref, (depth(n)[:, None] + 1) * U * size)
+    near(host(t), ref, (depth(n, T)[:, None] + 1) * U * size)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [3, 20, 300])
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("least,seed", [(257, 1), (257, 2), (257, 3), (1500, 4), (3000, 5), (8300, 6), (8300, 7), (12000, 8)])
+def test_gradient_of_runs_of_every_length(prec, d, least, seed):
+    """Runs that begin and end around the ends of pieces of 16 and 32 tokens, up to some that go through eight, nine and many of them."""
+    say(f"grad runs {prec} d={d} least={least} seed={seed}")
+    rng = np.random.default_rng(seed)
+    piece = 16 if least < 8192 else 32
+    lengths = [1, 1, 1, 2, 3, piece - 1, piece, piece + 1, 2 * piece - 1, 2 * piece, 2 * piece + 1, 3 * piece, 3 * piece + 5, 8 * piece, 9 * piece - 1, 9 * piece,
+               10 * piece + 3, 11 * piece + 1, 40 * piece + 7, 70 * piece]
+    runs = []
+    while sum(runs) < least:
+        runs.append(int(rng.choice(lengths)))
+    names = np.sort(rng.choice(3000, len(runs), replace=False))
+    ids = rng.permutation(np.repeat(names, runs))
+    ids = np.concatenate([ids, np.full(int(rng.integers(0, 40)), -1)])
+    assert (len(ids) <= 8192) == (piece == 16) and len(ids) > 256
+    dx = rounded(rng.standard_normal((len(ids), d)), prec)
+    ref, size, n = os_.embed_grad(ids, dx, 3000)
+    dd = rows_of(dx, d, DT[prec])
+    t = grad(prec, i32(ids), dd, 3000, d, d, d)
+    bound = (depth(n, len(ids))[:, None] + 1) * U * size
+    near(host(t), ref, bound)
+    old = torch.randn(3000, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(6))
+    t = grad(prec, i32(ids), dd, 3000, d, d, d, accumulate=True, into=old.clone())
+    near(host(t), ref + host(old), bound + U * np.abs(ref + host(old)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [200, 70000])
+def test_gradient_of_so_many_tokens_that_the_sort_scans_its_counts(V):
+    T, d = 300001, 2
+    rng = np.random.default_rng(V)
+    ids = text_like(rng, T, V)
+    ids[::50] = -1
+    dx = rng.standard_normal((T, d)).astype(np.float32)
+    ref, size, n = os_.embed_grad(ids, dx, V)
+    near(host(grad("fp32", i32(ids), rows_of(dx, d, torch.float32), V, d, d, d)), ref, (depth(n, len(ids))[:, None] + 1) * U * size)
 
 
 @pytest.mark.gpu
@@ -207,7 +251,7 @@ def test_gradient_of_the_positions_is_the_same_call():
     places[::9] = -1
     dx = rng.standard_normal((T, d)).astype(np.float32)
     ref, size, n = os_.embed_grad(places, dx, P)
-    near(host(grad("fp32", i32(places), rows_of(dx, d, torch.float32), P, d, d, d)), ref, (depth(n)[:, None] + 1) * U * size)
+    near(host(grad("fp32", i32(places), rows_of(dx, d, torch.float32), P, d, d, d)), ref, (depth(n, T)[:, None] + 1) * U * size)
 
 
 @pytest.mark.gpu
@@ -334,7 +378,7 @@ def test_every_code_and_every_scale_is_read_as_it_is_defined(code):
 D = 44
 NORMS = [(1, 1, 1, 0), (3, 7, 9, 1), (5, 33, 40, 0), (64, 128, 128, 0), (9, 512, 512, 0), (10, 513, 515, 3), (70, 1024, 1024, 0), (13, 1025, 1025, 0),
          (11, 1600, 1601, 1), (9, 2048, 2048, 0), (7, 2049, 2056, 0), (6, 4096, 4096, 0), (5, 4099, 4103, 2), (4, 8192, 8192, 0), (3, 8185, 8191, 5),
-         (2500, 65, 65, 0), (5000, 1024, 1024, 0), (1100, 4096, 4096, 0)]
+         (2500, 65, 65, 0), (3001, 8, 8, 0), (2777, 31, 33, 1), (2049, 32, 32, 0), (2600, 64, 64, 0), (3000, 100, 101, 0), (2500, 129, 129, 2), (2200, 260, 260, 0), (8200, 700, 700, 0), (5000, 1024, 1024, 0), (1100, 4096, 4096, 0)]
 
 
 def dx_bound(dy, v, mean, rstd, gamma, dx, res=None):
@@ -538,7 +582,7 @@ def test_a_step_from_tokens_to_the_gradient_of_their_table(code):
     near(host(s.dx), dx, dx_bound(s.dy.astype(np.float64), v, host(s.mean), host(s.rstd), s.gamma.astype(np.float64), dx, s.res.astype(np.float64)))
     for out, at, V, scale in ((s.dtable, s.ids, s.V, 16.0), (s.dpos, s.places, s.P, 1.0)):
         ref, size, n = os_.embed_grad(at, host(s.dx), V, scale)
-        near(host(out), ref, (depth(n)[:, None] + 1) * U * size)
+        near(host(out), ref, (depth(n, s.T)[:, None] + 1) * U * size)
 
 
 @pytest.mark.gpu
