@@ -316,6 +316,7 @@ struct Runs {
 };
 
 constexpr int kAhead = 16;        // rows on their way at a time
+constexpr int kPieceRanked = 16, kPieceSorted = 32;
 // A wave that may have to write rows with zeros looks after up to kMostFilled rows and kFillColumns columns of them, some 16 KB.
 constexpr int kMostFilled = 64, kFillColumns = 1024;
 
@@ -371,71 +372,63 @@ __device__ __forceinline__ int keys_below(const Runs &g, int64_t key, int lane) 
   return lo;
 }
 
-// The first place from lo on, and before hi, that has another key.
-__device__ __forceinline__ int behind_run(const Runs &g, int lo, int hi, uint32_t key) {
-  while (lo < hi) {
-    const int mid = (lo + hi) / 2;
-    if (g.keys[mid] == key) lo = mid + 1;
-    else hi = mid;
-  }
-  return lo;
-}
-
 // A wave sums a piece of the sorted list over a slab of columns.  A run that ends in the piece behind the one that it starts in, or behind
 // one that it goes through, is taken along to its end; so only runs that go through a whole piece leave parts of their sum to be joined.
 // Pieces of 16 tokens up to kMostRanked, for the waves' number, of 32 beyond (16384 x 1024 fp32: 78 us with 16, 79 with 32, 81 with 64; 131072
 // x 1024: 190, 184, 184).  kAhead rows are on their way before the first is added (8 instead of 16: 90 instead of 81 us at 16384 x 1024).
-template <typename E, bool NARROW, bool ADD> __device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
+// What the wave has to know of the list it reads in one go, a place a lane: the piece, the one behind, and a key at either end.
+template <typename E, int PIECE, bool NARROW, bool ADD> __device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
+  static_assert(2 * PIECE <= kWave, "a place a lane");
   constexpr int N = ElemTraits<E>::VEC;
+  constexpr uint32_t kNone = 0xffffffffu, kBefore = 0xfffffffeu;   // no token's key: behind the list, before it
   const Slab<E, NARROW> s(slab, lane, g.d);
-  int p = piece * g.piece, end = min(g.T, p + g.piece);
-  uint32_t key = g.keys[p];
+  const int p0 = piece * PIECE, at = p0 + lane, len = min(PIECE, g.T - p0);
+  uint32_t keys = g.keys[min(at, g.T - 1)], next = g.keys[min(p0 + 2 * PIECE, g.T - 1)], before = g.keys[max(p0 - 1, 0)];
+  const uint32_t order = g.order[min(at, g.T - 1)];
+  if (at >= g.T) keys = kNone;
+  if (p0 + 2 * PIECE >= g.T) next = kNone;
+  if (p0 == 0) before = kBefore;
+  const uint32_t key = __builtin_amdgcn_readlane(keys, 0), last = __builtin_amdgcn_readlane(keys, len - 1), after = __builtin_amdgcn_readlane(keys, PIECE);
   if (key >= uint32_t(g.V)) return;
-  const uint32_t last = g.keys[end - 1];
-  bool through = false;                               // the run has begun before
-  if (p > 0 && g.keys[p - 1] == key) {
-    if (last != key || end == g.T || g.keys[end] != key) {
-      if (last == key) return;                        // all of the piece was taken along
-      p = behind_run(g, p, end, key);                 // its beginning was
-      key = g.keys[p];
-      if (key >= uint32_t(g.V)) return;
-    } else {
-      through = true;
+  int begin = 0, end = len;
+  bool through = false;                               // all of the piece, and what is behind, is a run that has begun before
+  if (before == key) {
+    through = after == key;
+    if (!through) {                                   // the run ends here: its end was taken along
+      if (last == key) return;
+      begin = __popcll(__ballot(keys == key && lane < PIECE));
+      if (uint32_t(__builtin_amdgcn_readlane(keys, begin)) >= uint32_t(g.V)) return;
     }
   }
   bool goes_on = false;                               // the last run goes through all of the next piece
-  if (end < g.T && g.keys[end] == last && last < uint32_t(g.V)) {
-    const int next = min(g.T, end + g.piece);
-    if (next < g.T && g.keys[next] == last) {
-      goes_on = true;
-    } else {
-      end = behind_run(g, end, next, last);
-    }
+  if (after == last && last < uint32_t(g.V)) {
+    if (next == last) goes_on = true;
+    else end = PIECE + __popcll(__ballot(keys == last && lane >= PIECE && lane < 2 * PIECE));
   }
-  const uint32_t first = g.order[p];
+  const uint32_t first = __builtin_amdgcn_readlane(order, begin);
   float sum[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) sum[k] = 0.f;
-  for (; p < end; p += kAhead) {
-    const int at = min(p + lane % kAhead, g.T - 1);
-    uint32_t keys = g.keys[at], order = g.order[at];
-    if (at != p + lane % kAhead || at >= end || keys >= uint32_t(g.V)) {   // read in place of nothing, and not added
-      keys = 0xffffffffu;
-      order = first;
+  for (int p = begin; p < end; p += kAhead) {
+    const int from = p + lane % kAhead;
+    uint32_t k16 = __shfl(keys, from, kWave), o16 = __shfl(order, from, kWave);
+    if (from >= end || k16 >= uint32_t(g.V)) {        // read in place of nothing, and not added
+      k16 = kNone;
+      o16 = first;
     }
     typename Slab<E, NARROW>::Raw v[kAhead];
     float old[ADD ? kAhead : 1][N];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) s.load(v[i], dx + int64_t(__builtin_amdgcn_readlane(order, i)) * g.ldx);
+    for (int i = 0; i < kAhead; ++i) s.load(v[i], dx + int64_t(__builtin_amdgcn_readlane(o16, i)) * g.ldx);
     if constexpr (ADD) {
 #pragma unroll
-      for (int i = 0; i < kAhead; ++i) s.load(old[i], g.dtable + int64_t(min(uint32_t(__builtin_amdgcn_readlane(keys, i)), uint32_t(g.V - 1))) * g.ldt);
+      for (int i = 0; i < kAhead; ++i) s.load(old[i], g.dtable + int64_t(min(uint32_t(__builtin_amdgcn_readlane(k16, i)), uint32_t(g.V - 1))) * g.ldt);
     }
-    const uint32_t behind = p + kAhead < end ? g.keys[p + kAhead] : 0xfffffffeu;
+    const uint32_t behind = p + kAhead < end ? __builtin_amdgcn_readlane(keys, p + kAhead) : kBefore;
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const uint32_t k = __builtin_amdgcn_readlane(keys, i), following = i + 1 < kAhead ? __builtin_amdgcn_readlane(keys, (i + 1) % kAhead) : behind;
-      if (k != 0xffffffffu) {
+      const uint32_t k = __builtin_amdgcn_readlane(k16, i), following = i + 1 < kAhead ? __builtin_amdgcn_readlane(k16, (i + 1) % kAhead) : behind;
+      if (k != kNone) {
 #pragma unroll
         for (int q = 0; q < N; ++q) sum[q] += v[i].at(q);
         if (following != k) {
@@ -473,13 +466,15 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, in
   const int64_t job = int64_t(blockIdx.x) * 4 + wave;
   const int piece = int(job / g.slabs), slab = int(job % g.slabs);
   if (piece >= g.pieces) return;
-  sum_piece<E, NARROW, ADD>(g, dx, piece, slab, lane);
+  if (g.piece == kPieceRanked) sum_piece<E, kPieceRanked, NARROW, ADD>(g, dx, piece, slab, lane);
+  else sum_piece<E, kPieceSorted, NARROW, ADD>(g, dx, piece, slab, lane);
 }
 
 // The runs that go through whole pieces: the sum of the piece that one starts in, and of those that follow.  A workgroup looks at
-// kJoinPieces pieces.  Runs of up to kShortRun parts are a wave's each; of a longer one each of the four waves takes a fourth of the
-// parts, joined in one order.
-constexpr int kJoinPieces = 16, kShortRun = 8;
+// kJoinPieces pieces (1841 tokens of 203 rows, twice: 28 us with 4 pieces, 30 with 16; 131072 tokens of 30522: 179 and 178).  Runs of up to
+// kShortRun parts are a wave's each; of a longer one each of the four waves takes a fourth of the parts, joined in one order (eight or
+// sixteen waves are slower: most runs are short).  Bound by latency: keys, their count, the parts, the row.
+constexpr int kJoinPieces = 4, kShortRun = 8;
 
 // parts q0 .. q1 - 1 of the run that starts in `piece`, added to sum
 template <bool NARROW, int DEEP> __device__ __forceinline__ void add_parts(const Runs &g, const Slab<float, NARROW> &s, int piece, int q0, int q1, float (&sum)[4]) {
@@ -503,13 +498,13 @@ __device__ __forceinline__ int parts_of(const Runs &g, int piece, uint32_t key, 
     if (more < kWave) return parts;
   }
 }
-template <bool NARROW, bool ADD> __device__ __forceinline__ void join_runs(const Runs &g, uint64_t shorts, uint64_t longs, int piece0, int slab, int lane, int wave, float (&part)[4][kWave * 4]) {
+template <bool NARROW, bool ADD> __device__ __forceinline__ void join_runs(const Runs &g, uint64_t shorts, uint64_t longs, uint32_t keys, int piece0, int slab, int lane, int wave, float (&part)[4][kWave * 4]) {
   const Slab<float, NARROW> s(slab, lane, g.d);
   float sum[4], old[4];
   for (int turn = 0; shorts; ++turn, shorts &= shorts - 1) {
     if (turn % 4 != wave) continue;
     const int piece = piece0 + __builtin_ctzll(shorts);
-    const uint32_t key = g.keys[(piece + 1) * g.piece];
+    const uint32_t key = __builtin_amdgcn_readlane(keys, __builtin_ctzll(shorts));
     s.load(sum, g.partial + int64_t(2 * piece + 1) * g.d);
     if (ADD) s.load(old, g.dtable + int64_t(key) * g.ldt);
     add_parts<NARROW, kShortRun>(g, s, piece, 0, parts_of(g, piece, key, lane), sum);
@@ -517,7 +512,7 @@ template <bool NARROW, bool ADD> __device__ __forceinline__ void join_runs(const
   }
   for (; longs; longs &= longs - 1) {
     const int piece = piece0 + __builtin_ctzll(longs);
-    const uint32_t key = g.keys[(piece + 1) * g.piece];
+    const uint32_t key = __builtin_amdgcn_readlane(keys, __builtin_ctzll(longs));
     const int parts = parts_of(g, piece, key, lane), per = (parts + 3) / 4;
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum[k] = 0.f;
@@ -544,15 +539,17 @@ __global__ __launch_bounds__(256) void k_embed_grad_join(Runs g, int slabs) {
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int piece0 = int(blockIdx.x / slabs) * kJoinPieces, slab = int(blockIdx.x % slabs);
   bool starts = false, is_long = false;
+  uint32_t key = 0;
   const int64_t p0 = int64_t(piece0 + lane) * g.piece, p1 = p0 + g.piece, p2 = p1 + g.piece, far = p1 + int64_t(kShortRun + 1) * g.piece;
   if (lane < kJoinPieces && p2 < g.T) {
-    const uint32_t key = g.keys[p1], next = g.keys[p2], last = g.keys[p1 - 1], before = g.keys[max(p0 - 1, int64_t(0))], beyond = g.keys[min(far, int64_t(g.T) - 1)];
+    key = g.keys[p1];
+    const uint32_t next = g.keys[p2], last = g.keys[p1 - 1], before = g.keys[max(p0 - 1, int64_t(0))], beyond = g.keys[min(far, int64_t(g.T) - 1)];
     starts = key < uint32_t(g.V) && last == key && next == key && !(p0 > 0 && before == key);
     is_long = far < g.T && beyond == key;
   }
   const uint64_t shorts = __ballot(starts && !is_long), longs = __ballot(starts && is_long);
   if (!(shorts | longs)) return;
-  join_runs<NARROW, ADD>(g, shorts, longs, piece0, slab, lane, wave, part);
+  join_runs<NARROW, ADD>(g, shorts, longs, key, piece0, slab, lane, wave, part);
 }
 
 // Few tokens, in one launch: a wave looks through all ids for those that equal its token's; the first of them adds up their rows.  Bound
@@ -680,7 +677,7 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   const hipStream_t s = (hipStream_t)st;
   const int T = g.T;
   const bool few = T <= kFew;
-  Runs a = {nullptr, nullptr, g.ids, T, g.d, g.V, T <= kMostRanked ? 16 : 32, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale, std::max(4, std::min(kMostFilled, 4096 / std::min(g.d, kFillColumns)))};
+  Runs a = {nullptr, nullptr, g.ids, T, g.d, g.V, T <= kMostRanked ? kPieceRanked : kPieceSorted, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale, std::max(4, std::min(kMostFilled, 4096 / std::min(g.d, kFillColumns)))};
   a.pieces = (T + a.piece - 1) / a.piece;
   a.partial = (float *)g.workspace + (int64_t(wanted) / 4 - 2 * int64_t(g.d) * a.pieces) / 4 * 4;   // at the workspace's end
   const int slab = kWave * (g.prec == HMY_PREC_BF16 ? 8 : 4), join_slabs = (g.d + 255) / 256;

@@ -119,13 +119,16 @@ struct Places {
   int64_t row[kPerThread];
   Unit u[kPerThread];
 };
+// a / b, of which the 64-bit division's hundred instructions are left out where a has 32 bits, as it has nearly always
+__device__ __forceinline__ int64_t quotient(int64_t a, uint32_t b) { return a >> 32 ? a / b : int64_t(uint32_t(a) / b); }
+
 // Where the thread's units are; for those behind the last row's another row is read, and nothing of it is theirs.
 template <int K, bool NARROW, int N> __device__ __forceinline__ Places places_of(const Units &g, int64_t tile) {
   Places p;
   const int lane = threadIdx.x % kWave;
   if constexpr (K > 0) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int64_t rows = tile / g.chunks;
+    const int64_t rows = g.chunks == 1 ? tile : quotient(tile, g.chunks);
     const int chunk = int(tile - rows * g.chunks);
     const int64_t row0 = (rows * kWaves + wave) * (kPerThread / K);
 #pragma unroll
@@ -137,7 +140,7 @@ template <int K, bool NARROW, int N> __device__ __forceinline__ Places places_of
     }
   } else {
     constexpr int kUnits = kThreads * kPerThread;
-    const int64_t row0 = tile * kUnits / g.per_row;
+    const int64_t row0 = quotient(tile * kUnits, g.per_row);
     const uint32_t first = uint32_t(tile * kUnits - row0 * g.per_row);
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {
