@@ -4,8 +4,8 @@
 // neighbours, a sum is a run of the sorted list, and no row of the table is written by two workgroups: no atomics, one order.
 // Three steps: the order (keys only: 8 bytes per token), the sums of runs inside pieces of the list, and the joining of those runs that
 // go through whole pieces.  Bound by HBM where there are many tokens: every row of dx is read once, every row of the table written once.
-// 131072 tokens of 1024 fp32 columns, 30522 rows, 662 MB: 180 us, of which 23 for the order (two passes, four launches), 146 for the sums
-// (4.5 TB/s) and 9 for the joining; 4096 tokens, 50257 rows of which most are empty, 222 MB: 6, 40 (5.5 TB/s) and 4.5.
+// 131072 tokens of 1024 fp32 columns, 30522 rows, 662 MB: 179 us, of which 25 for the order (two passes, four launches), 145 for the sums
+// (4.6 TB/s) and 11 for the joining; 4096 tokens, 50257 rows of which most are empty, 222 MB: 6, 41 (5.4 TB/s) and 4.7.
 #include <algorithm>
 
 #include "stream_rows.h"

@@ -105,8 +105,8 @@ template <bool NARROW, int N> __device__ __forceinline__ void clear_foreign(floa
 // ---- the units of rows, shared out over a launch ----
 // Wide rows: a wave takes kPerThread / K rows, K units of each a lane, with everything but the column in scalar registers; tiles of
 // kWaves waves, one chunk of their rows after the other.  K = 0: rows of less than half a wave's units are numbered through instead,
-// unit by unit, and a lane finds its row by one 32-bit division from that of its workgroup's first (some 150 instructions a unit, against
-// some 40: a lookup of 32768 x 1024 fp32 took 46 us that way, most of it in these).
+// unit by unit, and a lane finds its row by one 32-bit division from that of its workgroup's first (a lookup of 32768 x 1024 fp32 took 46 us
+// that way, 43 by waves).
 constexpr int kThreads = 256, kWaves = kThreads / kWave, kPerThread = 4;
 
 struct Units {
