@@ -29,9 +29,9 @@ struct Lookup {
 // which the L2s hold, 29).  Workgroups that stay and fetch their next rows ahead take 47 to 49.
 template <typename E, typename O, int K, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *table, const E *pos_table, O *x, Units units) {
-  constexpr int N = 16 / sizeof(O);
+  constexpr int N = 16 / sizeof(O), kPerThread = per_thread(K);
   for (int64_t tile = blockIdx.x; tile < units.tiles; tile += gridDim.x) {
-    const Places at = places_of<K, NARROW, N>(units, tile);
+    const Places<kPerThread> at = places_of<K, NARROW, N>(units, tile);
     int id[kPerThread], place[kPerThread];
 #pragma unroll
     for (int i = 0; i < kPerThread; ++i) {

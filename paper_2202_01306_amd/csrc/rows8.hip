@@ -107,12 +107,13 @@ template <typename E, int CODE, int K, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, Units g) {
   constexpr int N = 16 / sizeof(E);
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const Places p = places_of<K, NARROW, N>(g, tile);
-    Cols<E, N> raw[kPerThread];
+    constexpr int kPer = per_thread(K);
+    const Places<kPer> p = places_of<K, NARROW, N>(g, tile);
+    Cols<E, N> raw[kPer];
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) load_unit<NARROW>(raw[i], x + p.row[i] * ldx, p.u[i], g.d);
+    for (int i = 0; i < kPer; ++i) load_unit<NARROW>(raw[i], x + p.row[i] * ldx, p.u[i], g.d);
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
+    for (int i = 0; i < kPer; ++i) {
       float v[N];
 #pragma unroll
       for (int k = 0; k < N; ++k) v[k] = raw[i].at(k);
@@ -138,15 +139,16 @@ template <typename E, int CODE, int K, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_unpack8(Rows8 r, E *x, int64_t ldx, Units g) {
   constexpr int N = 16 / sizeof(E);
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
-    const Places p = places_of<K, NARROW, N>(g, tile);
-    uint32_t w[kPerThread][N / 4], byte[kPerThread];
+    constexpr int kPer = per_thread(K);
+    const Places<kPer> p = places_of<K, NARROW, N>(g, tile);
+    uint32_t w[kPer][N / 4], byte[kPer];
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
+    for (int i = 0; i < kPer; ++i) {
       load_codes<NARROW, N>(w[i], r.codes + p.row[i] * r.ldc, p.u[i], g.d);
       byte[i] = r.scales[p.row[i] * r.lds + group_of<NARROW, N>(p.u[i])];
     }
 #pragma unroll
-    for (int i = 0; i < kPerThread; ++i) {
+    for (int i = 0; i < kPer; ++i) {
       float v[N];
       decode<CODE>(w[i], byte[i], v);
       store_unit<NARROW>(x + p.row[i] * ldx, v, p.u[i], g.d);
@@ -198,7 +200,7 @@ struct Norm8 {
 // A wave has ROWS rows (times 64 / LPR) on their way at a time; gamma and beta stay in registers.  One pass over the codes: the row is held
 // in registers through mean, variance and output.  4096 x 1024 to bf16 with the rows themselves, 29.5 MB: 7.5 us, of which 3 are a launch
 // that does next to nothing; 16384 rows 25.6 (4.6 TB/s; 27.7 with one row on its way, which is 2 % faster at 4096).  Narrow rows: 131072 x
-// 128 take 27 us side by side, 50 with a wave each.
+// 128 take 27 us side by side, 50 with a wave each.  As many units a lane as the row needs: 20000 x 1096 take 41 us with five, 52 with eight.
 template <typename E, int CODE, int LPR, int W, int NJ, int ROWS, bool NARROW>
 __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma, const E *beta, E *y, float *x) {
   static_assert(LPR == 64 || (W == 1 && NJ == 1), "narrow rows are one unit a lane");
@@ -527,8 +529,15 @@ int launch_layernorm8_fwd(const hmy_layernorm8_desc &g, stream_t st) {
     else if (g.d <= 512) NORM8_FWD(64, 1, 2, 1, false);
     else if (g.d <= 1024 && g.T >= 8192) NORM8_FWD(64, 1, 4, 2, false);
     else if (g.d <= 1024) NORM8_FWD(64, 1, 4, 1, false);
+    else if (g.d <= 1280) NORM8_FWD(64, 1, 5, 1, false);
+    else if (g.d <= 1536) NORM8_FWD(64, 1, 6, 1, false);
+    else if (g.d <= 1792) NORM8_FWD(64, 1, 7, 1, false);
     else if (g.d <= 2048) NORM8_FWD(64, 1, 8, 1, false);
+    else if (g.d <= 3 * 1024) NORM8_FWD(64, 4, 3, 1, false);
     else if (g.d <= 4096) NORM8_FWD(64, 4, 4, 1, false);
+    else if (g.d <= 5120) NORM8_FWD(64, 4, 5, 1, false);
+    else if (g.d <= 6144) NORM8_FWD(64, 4, 6, 1, false);
+    else if (g.d <= 7168) NORM8_FWD(64, 4, 7, 1, false);
     else NORM8_FWD(64, 4, 8, 1, false);
   });
 #undef NORM8_FWD
@@ -577,9 +586,13 @@ int launch_layernorm8_bwd(const hmy_layernorm8_grad_desc &g, stream_t st) {
     else if (g.d <= 128) NORM8_BWD(32, 1, 1, false);
     else if (g.d <= 256) NORM8_BWD(64, 1, 1, false);
     else if (g.d <= 512) NORM8_BWD(64, 1, 2, false);
+    else if (g.d <= 768) NORM8_BWD(64, 1, 3, false);
     else if (g.d <= 1024) NORM8_BWD(64, 1, 4, false);
+    else if (g.d <= 1536) NORM8_BWD(64, 2, 3, false);
     else if (g.d <= 2048) NORM8_BWD(64, 2, 4, false);
+    else if (g.d <= 3 * 1024) NORM8_BWD(64, 4, 3, false);
     else if (g.d <= 4096) NORM8_BWD(64, 4, 4, false);
+    else if (g.d <= 6144) NORM8_BWD(64, 8, 3, false);
     else NORM8_BWD(64, 8, 4, false);
   });
 #undef NORM8_BWD

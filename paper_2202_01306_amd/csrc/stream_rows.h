@@ -103,11 +103,12 @@ template <bool NARROW, int N> __device__ __forceinline__ void clear_foreign(floa
 }
 
 // ---- the units of rows, shared out over a launch ----
-// Wide rows: a wave takes kPerThread / K rows, K units of each a lane, with everything but the column in scalar registers; tiles of
-// kWaves waves, one chunk of their rows after the other.  K = 0: rows of less than half a wave's units are numbered through instead,
+// Wide rows: a wave takes K units a lane of a row, or of two or four rows where it has few, with everything but the column in scalar
+// registers; tiles of kWaves waves, one chunk of their rows after the other.  K = 0: rows of less than half a wave's units are numbered through instead,
 // unit by unit, and a lane finds its row by one 32-bit division from that of its workgroup's first (a lookup of 32768 x 1024 fp32 took 46 us
 // that way, 43 by waves).
-constexpr int kThreads = 256, kWaves = kThreads / kWave, kPerThread = 4;
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int per_thread(int K) { return K == 3 ? 3 : 4; }   // units
 
 struct Units {
   int T, d;
@@ -115,16 +116,17 @@ struct Units {
   uint32_t chunks;            // of 64 K N columns in a row
   int64_t tiles;              // times chunks
 };
-struct Places {
-  int64_t row[kPerThread];
-  Unit u[kPerThread];
+template <int PER> struct Places {
+  int64_t row[PER];
+  Unit u[PER];
 };
 // a / b, of which the 64-bit division's hundred instructions are left out where a has 32 bits, as it has nearly always
 __device__ __forceinline__ int64_t quotient(int64_t a, uint32_t b) { return a >> 32 ? a / b : int64_t(uint32_t(a) / b); }
 
 // Where the thread's units are; for those behind the last row's another row is read, and nothing of it is theirs.
-template <int K, bool NARROW, int N> __device__ __forceinline__ Places places_of(const Units &g, int64_t tile) {
-  Places p;
+template <int K, bool NARROW, int N> __device__ __forceinline__ Places<per_thread(K)> places_of(const Units &g, int64_t tile) {
+  constexpr int kPerThread = per_thread(K);
+  Places<kPerThread> p;
   const int lane = threadIdx.x % kWave;
   if constexpr (K > 0) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -178,9 +180,13 @@ struct Shares {
 inline Shares shares_of(int T, int d, int N, int whole) {
   Shares s;
   const int per_row = (d + whole - 1) / whole * (whole / N), waves = (per_row + kWave - 1) / kWave;
-  s.K = per_row < kWave / 2 ? 0 : waves >= 3 ? 4 : waves;
-  s.units = {T, d, uint32_t(per_row), s.K ? uint32_t((waves + s.K - 1) / s.K) : 1u, 0};
-  const int64_t parts = s.K ? (int64_t(T) + kPerThread / s.K - 1) / (kPerThread / s.K) : (int64_t(T) * per_row + kWave * kPerThread - 1) / (kWave * kPerThread);
+  // chunks of up to four waves' units, as even as they go (a lookup of 20000 rows of 1096 fp32 columns, in
+  // chunks of 3 and 2 instead of 4 and 1: 37 us instead of 42); a branch around units that are no one's costs more than they do
+  const int chunks = (waves + 3) / 4;
+  s.K = per_row < kWave / 2 ? 0 : (waves + chunks - 1) / chunks;
+  s.units = {T, d, uint32_t(per_row), s.K ? uint32_t(chunks) : 1u, 0};
+  const int per = per_thread(s.K);
+  const int64_t parts = s.K ? (int64_t(T) + per / s.K - 1) / (per / s.K) : (int64_t(T) * per_row + kWave * per - 1) / (kWave * per);
   s.units.tiles = (parts + kWaves - 1) / kWaves * s.units.chunks;
   s.grid = dim3(uint32_t(s.units.tiles < kMaxGrid ? s.units.tiles : kMaxGrid));
   return s;
@@ -192,6 +198,7 @@ inline Shares shares_of(int T, int d, int N, int whole) {
     else if ((k) == 0) { constexpr int K = 0; __VA_ARGS__ }                          \
     else if ((k) == 1) { constexpr int K = 1; __VA_ARGS__ }                          \
     else if ((k) == 2) { constexpr int K = 2; __VA_ARGS__ }                          \
+    else if ((k) == 3) { constexpr int K = 3; __VA_ARGS__ }                          \
     else { constexpr int K = 4; __VA_ARGS__ }                                        \
   } while (0)
 
