@@ -552,68 +552,101 @@ __global__ __launch_bounds__(256) void k_embed_grad_join(Runs g, int slabs) {
   join_runs<NARROW, ADD>(g, shorts, longs, key, piece0, slab, lane, wave, part);
 }
 
-// Few tokens, in one launch: a wave looks through all ids for those that equal its token's; the first of them adds up their rows.  Bound
-// by the launch: 20 tokens of 64 columns 5 us, 12 by the three steps.  The rows of one token are one wave's: 16 rows at a time, so that up
-// to kFew of them take no longer than those steps.
-constexpr int kFew = 256;
+// Few tokens, in one launch: a workgroup for each token and slab looks through all ids, kFewEach a lane, for those that equal its token's; the
+// workgroup of the first of them adds up their rows, by one wave up to kAhead rows, by all of its waves beyond.  One wave for up to 256
+// tokens, four for up to 1024, while there are no more than kFewGroups workgroups.  Bound by the launch: 512 x 1024 take 5.3 us, 12 by the
+// three steps; 1024 x 2048 (8192 workgroups) 11.2 and 13, 1024 x 4096 18.7 and 14.7; 256 x 4096 6.4 with one wave and 8.4 with four.
+constexpr int kFewEach = 4, kFewGroups = 8192;
 
-template <typename E, bool NARROW, bool ADD> __device__ __forceinline__ void sum_alike(const Runs &g, const E *dx, uint32_t key, const uint16_t *list, int n, int slab, int lane) {
-  constexpr int N = ElemTraits<E>::VEC;
+template <typename E, bool NARROW, bool ADD, int WAVES>
+__global__ __launch_bounds__(WAVES *kWave) void k_embed_grad_few(Runs g, const E *dx, int run_groups) {
+  constexpr int N = ElemTraits<E>::VEC, kFew = WAVES * kWave * kFewEach;
+  __shared__ uint16_t list[kFew];
+  __shared__ uint32_t named[WAVES * kMostFilled];
+  __shared__ int found[WAVES], earlier[WAVES];
+  __shared__ float part[WAVES][kWave * N];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (int(blockIdx.x) >= run_groups) {
+    const int job = int(blockIdx.x) - run_groups, slabs = (g.d + kFillColumns - 1) / kFillColumns;
+    const int n = WAVES * g.fill_rows;
+    const int64_t row0 = int64_t(job / slabs) * n;
+    named[threadIdx.x] = row0 + threadIdx.x >= g.V;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFewEach; ++i) {
+      const int t = i * (WAVES * kWave) + threadIdx.x;
+      const int64_t at = t < g.T ? int64_t(g.ids[min(t, g.T - 1)]) - row0 : -1;
+      if (at >= 0 && at < n) named[at] = 1;
+    }
+    __syncthreads();
+    zero_rows(g, row0 + wave * g.fill_rows, __ballot(lane < g.fill_rows && !named[wave * g.fill_rows + lane]), job % slabs * kFillColumns, lane);
+    return;
+  }
+  const int t = int(blockIdx.x) / g.slabs, slab = int(blockIdx.x) % g.slabs;
+  const int id = g.ids[t];
+  int v[kFewEach];
+#pragma unroll
+  for (int i = 0; i < kFewEach; ++i) v[i] = g.ids[min((wave * kFewEach + i) * kWave + lane, g.T - 1)];
+  if (uint32_t(id) >= uint32_t(g.V)) return;
+  uint64_t hits[kFewEach];
+  int n = 0, before = 0;
+#pragma unroll
+  for (int i = 0; i < kFewEach; ++i) {
+    const int at = (wave * kFewEach + i) * kWave + lane;
+    hits[i] = __ballot(at < g.T && v[i] == id);
+    before += __popcll(__ballot(at < t && v[i] == id));
+    n += __popcll(hits[i]);
+  }
+  if (lane == 0) {
+    found[wave] = n;
+    earlier[wave] = before;
+  }
+  __syncthreads();
+  int total = 0, mine = 0, first = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    mine += w < wave ? found[w] : 0;
+    total += found[w];
+    first += earlier[w];
+  }
+  if (__builtin_amdgcn_readfirstlane(first)) return;   // another workgroup's
+  n = __builtin_amdgcn_readfirstlane(total);
+#pragma unroll
+  for (int i = 0; i < kFewEach; ++i) {
+    if (hits[i] >> lane & 1) list[mine + __popcll(hits[i] & ((uint64_t(1) << lane) - 1))] = uint16_t((wave * kFewEach + i) * kWave + lane);
+    mine += __popcll(hits[i]);
+  }
+  __syncthreads();
   const Slab<E, NARROW> s(slab, lane, g.d);
+  const bool shared = n > kAhead;
+  if (!shared && wave) return;
+  const int per = shared ? (n + WAVES - 1) / WAVES : n, p1 = min(n, (wave + 1) * per);
   float sum[N], old[N];
 #pragma unroll
   for (int k = 0; k < N; ++k) sum[k] = 0.f;
-  if constexpr (ADD) s.load(old, g.dtable + int64_t(key) * g.ldt);
-  for (int p = 0; p < n; p += kAhead) {
-    const uint32_t order = list[min(p + lane % kAhead, n - 1)];
+  if (ADD && wave == 0) s.load(old, g.dtable + int64_t(id) * g.ldt);
+  for (int p = wave * per; p < p1; p += kAhead) {
+    const uint32_t order = list[min(p + lane % kAhead, p1 - 1)];
     typename Slab<E, NARROW>::Raw v[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) s.load(v[i], dx + int64_t(__builtin_amdgcn_readlane(order, i)) * g.ldx);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i)
-      if (p + i < n)
+      if (p + i < p1)
 #pragma unroll
         for (int q = 0; q < N; ++q) sum[q] += v[i].at(q);
   }
-  write_row<ADD>(g, s, key, sum, old);
-}
-
-template <typename E, bool NARROW, bool ADD>
-__global__ __launch_bounds__(256) void k_embed_grad_few(Runs g, const E *dx, int run_groups) {
-  __shared__ uint16_t list[4][kFew];
-  __shared__ uint32_t named[4 * kMostFilled];
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  if (int(blockIdx.x) >= run_groups) {
-    const int job = int(blockIdx.x) - run_groups, slabs = (g.d + kFillColumns - 1) / kFillColumns;
-    const int n = 4 * g.fill_rows;
-    const int64_t row0 = int64_t(job / slabs) * n;
-    named[threadIdx.x] = row0 + threadIdx.x >= g.V;
-    __syncthreads();
-    const int64_t at = threadIdx.x < unsigned(g.T) ? int64_t(g.ids[threadIdx.x]) - row0 : -1;
-    if (at >= 0 && at < n) named[at] = 1;
-    __syncthreads();
-    zero_rows(g, row0 + wave * g.fill_rows, __ballot(lane < g.fill_rows && !named[wave * g.fill_rows + lane]), job % slabs * kFillColumns, lane);
-    return;
-  }
-  const int64_t job = int64_t(blockIdx.x) * 4 + wave;
-  const int t = int(job / g.slabs), slab = int(job % g.slabs);
-  if (t >= g.T) return;   // no barrier below: every wave has a list of its own
-  const int id = g.ids[t];
-  int v[kFew / kWave];
+  if (shared) {
 #pragma unroll
-  for (int i = 0; i < kFew / kWave; ++i) v[i] = g.ids[min(kWave * i + lane, g.T - 1)];
-  if (uint32_t(id) >= uint32_t(g.V)) return;
-  int n = 0;
+    for (int k = 0; k < N; ++k) part[wave][lane * N + k] = sum[k];
+    __syncthreads();
+    if (wave) return;
 #pragma unroll
-  for (int i = 0; i < kFew / kWave; ++i) {
-    const bool hit = kWave * i + lane < g.T && v[i] == id;
-    const uint64_t hits = __ballot(hit);
-    if (hit) list[wave][n + __popcll(hits & ((uint64_t(1) << lane) - 1))] = uint16_t(kWave * i + lane);
-    n += __popcll(hits);
+    for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+      for (int k = 0; k < N; ++k) sum[k] += part[w][lane * N + k];
   }
-  wave_sees_lds();
-  if (__builtin_amdgcn_readfirstlane(list[wave][0]) != t) return;
-  sum_alike<E, NARROW, ADD>(g, dx, uint32_t(id), list[wave], n, slab, lane);
+  write_row<ADD>(g, s, uint32_t(id), sum, old);
 }
 
 }  // namespace
@@ -676,32 +709,35 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   if (rc) return rc;
   const hipStream_t s = (hipStream_t)st;
   const int T = g.T;
-  const bool few = T <= kFew;
+  const int slab = kWave * (g.prec == HMY_PREC_BF16 ? 8 : 4), slabs = (g.d + slab - 1) / slab, join_slabs = (g.d + 255) / 256;
+  const int few = int64_t(T) * slabs > kFewGroups ? 0 : T <= kWave * kFewEach ? 1 : T <= 4 * kWave * kFewEach ? 4 : 0;   // waves of a workgroup
   Runs a = {nullptr, nullptr, g.ids, T, g.d, g.V, T <= kMostRanked ? kPieceRanked : kPieceSorted, 0, 0, g.ldx, g.ldt, g.dtable, nullptr, g.scale, std::max(4, std::min(kMostFilled, 4096 / std::min(g.d, kFillColumns)))};
   a.pieces = (T + a.piece - 1) / a.piece;
   a.partial = (float *)g.workspace + (int64_t(wanted) / 4 - 2 * int64_t(g.d) * a.pieces) / 4 * 4;   // at the workspace's end
-  const int slab = kWave * (g.prec == HMY_PREC_BF16 ? 8 : 4), join_slabs = (g.d + 255) / 256;
-  a.slabs = (g.d + slab - 1) / slab;
-  const int64_t run_groups = (int64_t(few ? T : a.pieces) * a.slabs + 3) / 4;
-  const int64_t fill_groups = g.accumulate ? 0 : (int64_t(g.V) + 4 * a.fill_rows - 1) / (4 * a.fill_rows) * ((g.d + kFillColumns - 1) / kFillColumns);
+  a.slabs = slabs;
+  const int64_t run_groups = few ? int64_t(T) * slabs : (int64_t(a.pieces) * slabs + 3) / 4;
+  const int filled = (few ? few : 4) * a.fill_rows;   // rows of a workgroup
+  const int64_t fill_groups = g.accumulate ? 0 : (int64_t(g.V) + filled - 1) / filled * ((g.d + kFillColumns - 1) / kFillColumns);
   const int64_t join_groups = (int64_t(a.pieces) + kJoinPieces - 1) / kJoinPieces * join_slabs;
   constexpr int64_t kMostGroups = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
   if (run_groups + fill_groups > kMostGroups || join_groups > kMostGroups) return fail(HMY_E_INVALID, "%s: T, d and V are too large together", who);
-  const dim3 grid{uint32_t(run_groups + fill_groups)}, threads(256);
-#define GRAD_AS(KERNEL, E, NARROW) \
-  hipLaunchKernelGGL((g.accumulate ? KERNEL<E, NARROW, true> : KERNEL<E, NARROW, false>), grid, threads, 0, s, a, (const E *)g.dx, int(run_groups))
-#define GRAD(KERNEL)                                             \
-  do {                                                           \
-    if (g.prec == HMY_PREC_BF16) {                               \
-      if (g.d < 8) GRAD_AS(KERNEL, bf16_t, true);                \
-      else GRAD_AS(KERNEL, bf16_t, false);                       \
-    } else {                                                     \
-      if (g.d < 8) GRAD_AS(KERNEL, float, true);                 \
-      else GRAD_AS(KERNEL, float, false);                        \
-    }                                                            \
+  const dim3 grid{uint32_t(run_groups + fill_groups)};
+#define GRAD_AS(N, KERNEL, E, NARROW, ...)                                                                                                       \
+  hipLaunchKernelGGL((g.accumulate ? KERNEL<E, NARROW, true, ##__VA_ARGS__> : KERNEL<E, NARROW, false, ##__VA_ARGS__>), grid, dim3(N), 0, s, a, \
+                     (const E *)g.dx, int(run_groups))
+#define GRAD(N, KERNEL, ...)                                             \
+  do {                                                                   \
+    if (g.prec == HMY_PREC_BF16) {                                       \
+      if (g.d < 8) GRAD_AS(N, KERNEL, bf16_t, true, ##__VA_ARGS__);      \
+      else GRAD_AS(N, KERNEL, bf16_t, false, ##__VA_ARGS__);             \
+    } else {                                                             \
+      if (g.d < 8) GRAD_AS(N, KERNEL, float, true, ##__VA_ARGS__);       \
+      else GRAD_AS(N, KERNEL, float, false, ##__VA_ARGS__);              \
+    }                                                                    \
   } while (0)
   if (few) {
-    GRAD(k_embed_grad_few);
+    if (few == 1) GRAD(64, k_embed_grad_few, 1);
+    else GRAD(256, k_embed_grad_few, 4);
     return check_launch(who);
   }
   const int64_t Ta = (int64_t(T) + 3) / 4 * 4;
@@ -726,12 +762,12 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   }
   a.keys = keys[sorted];
   a.order = order[sorted];
-  GRAD(k_embed_grad_runs);
+  GRAD(256, k_embed_grad_runs);
 #undef GRAD
 #undef GRAD_AS
   auto *join = g.d < 8 ? (g.accumulate ? k_embed_grad_join<true, true> : k_embed_grad_join<true, false>)
                        : (g.accumulate ? k_embed_grad_join<false, true> : k_embed_grad_join<false, false>);
-  hipLaunchKernelGGL(join, dim3(uint32_t(join_groups)), threads, 0, s, a, join_slabs);
+  hipLaunchKernelGGL(join, dim3(uint32_t(join_groups)), dim3(256), 0, s, a, join_slabs);
   return check_launch(who);
 }
 

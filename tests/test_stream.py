@@ -3,7 +3,7 @@ oracle, element by element.
 
 Bounds, in units of u = 2^-24, half a step of fp32 relative to the value.
   lookup       one multiply-add: u |x|; a bf16 output is rounded once more, by 2^-8 of its value
-  gradient     a sum of n rows: one after the other in calls of up to 256 tokens, D = n; in longer ones a term passes through at most 63
+  gradient     a sum of n rows: D = n in calls of up to 1024 tokens, where one wave, or four, add them up; in longer ones a term passes through at most 63
                additions in its piece of the list and the one behind (32 tokens each), a quarter of the run's pieces or 8 of them, and 5
                more where those join, D = min(n, 64 + n / 64 + 8); with the scaling (D + 1) u of the sum of magnitudes, and u of the
                result where it is added to what is there
@@ -128,7 +128,7 @@ def text_like(rng, T, V):
 
 
 def depth(n, T):
-    return n if T <= 256 else np.minimum(n, 64 + n / 64 + 8)
+    return n if T <= 1024 else np.minimum(n, 64 + n / 64 + 8)
 
 
 def grad(prec, ids, dx, V, d, ldx, ldt, scale=1.0, accumulate=False, into=None, ws=None, stream=None):
@@ -139,7 +139,7 @@ def grad(prec, ids, dx, V, d, ldx, ldt, scale=1.0, accumulate=False, into=None, 
     return t
 
 
-GRADS = [(1, 1, 1, 1, 1, 0), (2, 5, 3, 5, 5, 0), (16, 8, 2, 8, 8, 0), (17, 31, 4, 33, 32, 1), (64, 128, 512, 128, 128, 0), (1000, 130, 3, 131, 133, 3),
+GRADS = [(1, 1, 1, 1, 1, 0), (2, 5, 3, 5, 5, 0), (16, 8, 2, 8, 8, 0), (17, 31, 4, 33, 32, 1), (64, 128, 512, 128, 128, 0), (1000, 130, 3, 131, 133, 3), (700, 3000, 90, 3000, 3000, 0), (256, 9000, 40, 9000, 9001, 0), (1024, 2040, 300, 2048, 2040, 0),
          (4096, 64, 50257, 64, 64, 0), (3001, 260, 255, 260, 260, 0), (3001, 20, 256, 20, 20, 0), (1024, 520, 257, 528, 520, 0), (5000, 12, 65535, 12, 12, 0),
          (5000, 12, 65536, 13, 12, 1), (16384, 16, 1000, 16, 16, 0), (16385, 16, 1000, 16, 16, 0), (20000, 9, 70000, 9, 9, 0), (40001, 33, 300, 33, 33, 0),
          (33000, 8, 1, 8, 8, 0), (18000, 4, 16777300, 4, 4, 0)]
@@ -188,7 +188,7 @@ def test_gradient_of_a_table_against_64_bits(prec, T, d, V, ldx, ldt, shift):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T", [1, 15, 16, 17, 100, 256, 257, 1000, 8192, 8193, 16384, 17000])
+@pytest.mark.parametrize("T", [1, 15, 16, 17, 100, 256, 257, 1000, 1024, 1025, 8192, 8193, 16384, 17000])
 @pytest.mark.parametrize("kind", ["one", "none", "ascending", "descending", "last", "blocks"])
 def test_gradient_of_lists_where_it_can_go_wrong(T, kind):
     say(f"grad {kind} T={T}")
