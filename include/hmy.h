@@ -660,7 +660,7 @@ typedef struct hmy_embed_lookup_desc {
 int hmy_k_embed_lookup(const hmy_embed_lookup_desc *g, void *stream);
 
 /* dtable[v] = scale * sum over the t with ids[t] = v of dx[t] (dx of type prec, dtable fp32), with the tokens sorted by id: a row's
- * sum runs over its tokens in ascending order, in pieces that the ids and the sizes alone determine, without atomics.  accumulate = 0: all V rows
+ * sum runs over its tokens in ascending order, in pieces that ids, sizes and type alone determine, without atomics.  accumulate = 0: all V rows
  * are written, those that no token names with zeros; 1: the sums are added to the rows that tokens name, the others are not touched.
  * Ids outside of [0, V) name no token.  The gradient of pos_table is the same call with the positions as ids and scale 1.
  * workspace: HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d) of device memory, aligned to 16 bytes; calls that may overlap need one each, and
