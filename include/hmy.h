@@ -682,7 +682,7 @@ int hmy_k_embed_grad(const hmy_embed_grad_desc *g, void *stream);
 /* Rows held in 8 bits (a checkpoint of the stream at about a byte per element): each HMY_ROWS8_GROUP columns share a power of two.
  * With a = the group's largest magnitude and e the least integer >= -126 for which a <= top 2^e, x_j is held as q_j = x_j / 2^e, rounded to
  * the nearest of its format's numbers, to the even one of two:
- *   HMY_CODE_INT8  whole numbers, top = 127: off by at most 2^(e-1), which is at most a / 127 (half that at best);
+ *   HMY_CODE_INT8  whole numbers, top = 127: off by at most 2^(e-1), which is less than a / 127 (half that at best) where e > -126;
  *   HMY_CODE_E4M3  floats of four bits of exponent and three of mantissa (1-4-3, bias 7, no infinities), top = 448: off by at most
  *                  2^-4 of the value, from 2^(e-6) on.
  * codes[T, ldc] holds q, scales[T, lds] one byte e + 127 per group (ceil(d / HMY_ROWS8_GROUP) of them in a row, the last one of the

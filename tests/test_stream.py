@@ -93,7 +93,7 @@ def scratch(nbytes):
 # ---- lookup ----------------------------------------------------------------------------------------
 
 LOOKUPS = [(1, 1, 1, 1, 1, 0, 0), (3, 7, 5, 7, 9, 4, 0), (64, 128, 512, 128, 128, 64, 0), (65, 33, 40, 35, 41, 7, 1), (300, 1600, 77, 1600, 1600, 128, 0),
-           (5, 4099, 300, 4100, 4103, 3, 3), (2050, 8, 20, 8, 8, 1, 0), (17, 1024, 50257, 1024, 1025, 1024, 0), (1030, 24, 65537, 27, 24, 0, 2)]
+           (5, 4099, 300, 4100, 4103, 3, 3), (2050, 8, 20, 8, 8, 1, 0), (17, 1024, 50257, 1024, 1025, 1024, 0), (37, 400, 60, 401, 400, 9, 0), (38, 601, 60, 601, 602, 9, 1), (39, 1096, 60, 1096, 1096, 9, 0), (21, 2500, 60, 2500, 2500, 9, 0), (1030, 24, 65537, 27, 24, 0, 2)]
 
 
 @pytest.mark.gpu
@@ -324,7 +324,8 @@ def check_packed(x, prec, code, codes, scales):
 
 
 MOVES = [(1, 1, 1, 1, 1, 0), (1, 8, 8, 8, 1, 0), (3, 31, 33, 31, 2, 1), (4, 32, 32, 32, 1, 0), (5, 33, 35, 40, 3, 3), (64, 128, 128, 128, 4, 0),
-         (7, 1601, 1603, 1607, 51, 5), (300, 1024, 1024, 1024, 32, 0), (2, 8193, 8193, 8193, 257, 0), (1000, 40, 40, 41, 2, 0), (33, 4096, 4100, 4096, 130, 2)]
+         (7, 1601, 1603, 1607, 51, 5), (300, 1024, 1024, 1024, 32, 0), (2, 8193, 8193, 8193, 257, 0), (1000, 40, 40, 41, 2, 0), (33, 4096, 4100, 4096, 130, 2),
+         (37, 400, 401, 400, 13, 0), (38, 601, 601, 603, 19, 1), (39, 1096, 1096, 1096, 35, 0), (21, 2500, 2500, 2500, 79, 0), (130, 4400, 4400, 4400, 138, 0)]
 
 
 @pytest.mark.gpu
@@ -377,7 +378,7 @@ def test_every_code_and_every_scale_is_read_as_it_is_defined(code):
 
 D = 44
 NORMS = [(1, 1, 1, 0), (3, 7, 9, 1), (5, 33, 40, 0), (64, 128, 128, 0), (9, 512, 512, 0), (10, 513, 515, 3), (70, 1024, 1024, 0), (13, 1025, 1025, 0),
-         (11, 1600, 1601, 1), (9, 2048, 2048, 0), (7, 2049, 2056, 0), (6, 4096, 4096, 0), (5, 4099, 4103, 2), (4, 8192, 8192, 0), (3, 8185, 8191, 5),
+         (11, 1600, 1601, 1), (10, 1280, 1280, 0), (9, 1500, 1500, 0), (8, 1300, 1301, 0), (7, 5130, 5130, 0), (6, 7000, 7001, 1), (9, 2048, 2048, 0), (7, 2049, 2056, 0), (6, 4096, 4096, 0), (5, 4099, 4103, 2), (4, 8192, 8192, 0), (3, 8185, 8191, 5),
          (2500, 65, 65, 0), (3001, 8, 8, 0), (2777, 31, 33, 1), (2049, 32, 32, 0), (2600, 64, 64, 0), (3000, 100, 101, 0), (2500, 129, 129, 2), (2200, 260, 260, 0), (8200, 700, 700, 0), (5000, 1024, 1024, 0), (1100, 4096, 4096, 0)]
 
 
