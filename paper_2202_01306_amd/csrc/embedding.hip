@@ -4,8 +4,8 @@
 // neighbours, a sum is a run of the sorted list, and no row of the table is written by two workgroups: no atomics, one order.
 // Three steps: the order (keys only: 8 bytes per token), the sums of runs inside pieces of the list, and the joining of those runs that
 // go through whole pieces.  Bound by HBM where there are many tokens: every row of dx is read once, every row of the table written once.
-// 131072 tokens of 1024 fp32 columns, 30522 rows, 662 MB: 175 us, of which 25 for the order (two passes, four launches), 141 for the sums
-// (4.7 TB/s) and 11 for the joining; 4096 tokens, 50257 rows of which most are empty, 222 MB: 6, 37 (6.0 TB/s) and 4.7.
+// 131072 tokens of 1024 fp32 columns, 30522 rows, 662 MB: 163 us, of which 24 for the order (two passes, four launches), 134 for the sums
+// (4.9 TB/s) and 10 for the joining; 4096 tokens, 50257 rows of which most are empty, 222 MB: 5, 42 (5.3 TB/s) and 4.7.
 #include <algorithm>
 
 #include "stream_rows.h"
@@ -327,7 +327,7 @@ template <typename E, bool NARROW> struct Slab {
   Unit u;
   int d;
   __device__ __forceinline__ Slab(int slab, int lane, int d_) : u(unit_at<NARROW, N>((slab * kWave + lane) * N, d_)), d(d_) {}
-  __device__ __forceinline__ void load(Raw &v, const E *row) const { load_unit<NARROW>(v, row, u, d); }
+  template <bool ONCE = false> __device__ __forceinline__ void load(Raw &v, const E *row) const { load_unit<NARROW, ONCE>(v, row, u, d); }
   __device__ __forceinline__ void load(float (&v)[N], const float *row) const {
     Cols<float, N> c;
     load_unit<NARROW>(c, row, u, d);
@@ -376,9 +376,14 @@ __device__ __forceinline__ int keys_below(const Runs &g, int64_t key, int lane) 
 // A wave sums a piece of the sorted list over a slab of columns.  A run that ends in the piece behind the one that it starts in, or behind
 // one that it goes through, is taken along to its end; so only runs that go through a whole piece leave parts of their sum to be joined.
 // Pieces of 16 tokens up to kMostRanked, for the waves' number, of 32 beyond (16384 x 1024 fp32: 78 us with 16, 79 with 32, 81 with 64; 131072
-// x 1024: 190, 184, 184).  kAhead rows are on their way before the first is added (8 instead of 16: 90 instead of 81 us at 16384 x 1024).
+// x 1024: 190, 184, 184; all before any loads were streaming ones).  kAhead rows are on their way before the first is added (8 instead of 16: 90
+// instead of 81 us at 16384 x 1024).
 // What the wave has to know of the list it reads in one go, a place a lane: the piece, the one behind, and a key at either end.
-template <typename E, int PIECE, bool NARROW, bool ADD> __device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
+// ONCE, from kStreamed bytes on: the caches are left to the table and to sums of parts of runs (fp32 rows of 1024 columns, 131072 tokens 163 us
+// instead of 176, 65536 102 and 112, 20480 60.0 and 61.6, but 16384 54 and 52; bf16 x 2048, 20480 tokens 80 and 85; fp32 x 5000, 16384 tokens
+// 223 and 221).
+template <typename E, int PIECE, bool NARROW, bool ADD, bool ONCE>
+__device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
   static_assert(2 * PIECE <= kWave, "a place a lane");
   constexpr int N = ElemTraits<E>::VEC;
   constexpr uint32_t kNone = 0xffffffffu, kBefore = 0xfffffffeu;   // no token's key: behind the list, before it
@@ -420,7 +425,7 @@ template <typename E, int PIECE, bool NARROW, bool ADD> __device__ __forceinline
     typename Slab<E, NARROW>::Raw v[kAhead];
     float old[ADD ? kAhead : 1][N];
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) s.load(v[i], dx + int64_t(__builtin_amdgcn_readlane(o16, i)) * g.ldx);
+    for (int i = 0; i < kAhead; ++i) s.template load<ONCE>(v[i], dx + int64_t(__builtin_amdgcn_readlane(o16, i)) * g.ldx);
     if constexpr (ADD) {
 #pragma unroll
       for (int i = 0; i < kAhead; ++i) s.load(old[i], g.dtable + int64_t(min(uint32_t(__builtin_amdgcn_readlane(k16, i)), uint32_t(g.V - 1))) * g.ldt);
@@ -446,7 +451,7 @@ template <typename E, int PIECE, bool NARROW, bool ADD> __device__ __forceinline
 }
 
 // The workgroups behind those of the sums write the rows that no token names.
-template <typename E, bool NARROW, bool ADD>
+template <typename E, bool NARROW, bool ADD, bool ONCE>
 __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, int run_groups) {
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   if (int(blockIdx.x) >= run_groups) {
@@ -467,14 +472,14 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, in
   const int64_t job = int64_t(blockIdx.x) * 4 + wave;
   const int piece = int(job / g.slabs), slab = int(job % g.slabs);
   if (piece >= g.pieces) return;
-  if (g.piece == kPieceRanked) sum_piece<E, kPieceRanked, NARROW, ADD>(g, dx, piece, slab, lane);
-  else sum_piece<E, kPieceSorted, NARROW, ADD>(g, dx, piece, slab, lane);
+  if (g.piece == kPieceRanked) sum_piece<E, kPieceRanked, NARROW, ADD, ONCE>(g, dx, piece, slab, lane);
+  else sum_piece<E, kPieceSorted, NARROW, ADD, ONCE>(g, dx, piece, slab, lane);
 }
 
 // The runs that go through whole pieces: the sum of the piece that one starts in, and of those that follow.  A workgroup looks at
-// kJoinPieces pieces (1841 tokens of 203 rows, twice: 28 us with 4 pieces, 30 with 16; 131072 tokens of 30522: 179 and 178).  Runs of up to
-// kShortRun parts are a wave's each; of a longer one each of the four waves takes a fourth of the parts, joined in one order (eight or
-// sixteen waves are slower: most runs are short).  Bound by latency: keys, their count, the parts, the row.
+// kJoinPieces pieces (1841 tokens of 203 rows, twice: 28 us with 4 pieces, 30 with 16; 131072 tokens of 30522, without streaming loads:
+// 179 and 178).  Runs of up to kShortRun parts are a wave's each; of a longer one each of the four waves takes a fourth of the parts, joined
+// in one order (eight or sixteen waves are slower: most runs are short).  Bound by latency: keys, their count, the parts, the row.
 constexpr int kJoinPieces = 4, kShortRun = 8;
 
 // parts q0 .. q1 - 1 of the run that starts in `piece`, added to sum
@@ -763,7 +768,8 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   }
   a.keys = keys[sorted];
   a.order = order[sorted];
-  GRAD(256, k_embed_grad_runs);
+  if (int64_t(T) * g.d * e >= kStreamed) GRAD(256, k_embed_grad_runs, true);
+  else GRAD(256, k_embed_grad_runs, false);
 #undef GRAD
 #undef GRAD_AS
   auto *join = g.d < 8 ? (g.accumulate ? k_embed_grad_join<true, true> : k_embed_grad_join<true, false>)

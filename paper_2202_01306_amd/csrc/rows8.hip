@@ -102,8 +102,10 @@ template <int CODE, int N> __device__ __forceinline__ void decode(const uint32_t
   for (int i = 0; i < N / 4; ++i) decode4<CODE>(w[i], s, v + 4 * i);
 }
 
-// 32768 x 4096 fp32, 537 MB read and 138 written: 118 us (5.7 TB/s); with a row's four chunks in four sweeps over all rows 132.
-template <typename E, int CODE, int K, bool NARROW>
+// 32768 x 4096 fp32, 537 MB read and 138 written: 111 us (6.1 TB/s); with a row's four chunks in four sweeps over all rows 14 more.
+// ONCE, from kStreamed bytes on: 111 us instead of 118, 65536 x 1024 57 and 61, 20480 x 1024 20.3 and 20.9, but 16384 x 1024 16 and 15; bf16
+// 20480 x 2048 23.6 and 24.9, 65536 x 1601 61 and 60.
+template <typename E, int CODE, int K, bool NARROW, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, Units g) {
   constexpr int N = 16 / sizeof(E);
   for (int64_t tile = blockIdx.x; tile < g.tiles; tile += gridDim.x) {
@@ -111,7 +113,7 @@ __global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uin
     const Places<kPer> p = places_of<K, NARROW, N>(g, tile);
     Cols<E, N> raw[kPer];
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) load_unit<NARROW>(raw[i], x + p.row[i] * ldx, p.u[i], g.d);
+    for (int i = 0; i < kPer; ++i) load_unit<NARROW, ONCE>(raw[i], x + p.row[i] * ldx, p.u[i], g.d);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       float v[N];
@@ -474,10 +476,11 @@ int launch_pack8(const hmy_rows8_desc &g, stream_t st) {
   const int rc = check_move8("pack8", g, true);
   if (rc) return rc;
   const Shares h = shares_of(g.T, g.d, 16 / bytes_of(g.prec), kGroup);
+  const bool once = int64_t(g.T) * g.d * bytes_of(g.prec) >= kStreamed;
   DISPATCH_ROWS8(g.prec, g.code, {
     DISPATCH_SHARES(h.K, g.d, {
-      hipLaunchKernelGGL((k_pack8<E, CODE, K, NARROW>), h.grid, dim3(kThreads), 0, (hipStream_t)st, (const E *)g.x, g.ldx, (uint8_t *)g.codes, g.ldc,
-                         (uint8_t *)g.scales, g.lds, h.units);
+      hipLaunchKernelGGL((once ? k_pack8<E, CODE, K, NARROW, true> : k_pack8<E, CODE, K, NARROW, false>), h.grid, dim3(kThreads), 0,
+                         (hipStream_t)st, (const E *)g.x, g.ldx, (uint8_t *)g.codes, g.ldc, (uint8_t *)g.scales, g.lds, h.units);
     });
   });
   return check_launch("pack8");

@@ -33,7 +33,11 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x2 u32x2_by1 __attribute__((aligned(1)));
 typedef u32x2 u32x2_by2 __attribute__((aligned(2)));
 typedef uint32_t u32_by1 __attribute__((aligned(1)));
-template <bool NARROW, typename E, int N> __device__ __forceinline__ void load_unit(Cols<E, N> &v, const E *row, Unit u, int d) {
+// ONCE: a streaming load, whose data the caches do not keep.  For rows that are read once and are kStreamed bytes or more: a third of the
+// memory-side cache of 256 MB, where fewer are found if the last two or three kernels have had them (both sides are measured at the kernels, with
+// three sets of rows in turn: it gains from 84 MB on and loses at 67).
+constexpr int64_t kStreamed = int64_t(80) << 20;
+template <bool NARROW, bool ONCE = false, typename E, int N> __device__ __forceinline__ void load_unit(Cols<E, N> &v, const E *row, Unit u, int d) {
   const char *p = reinterpret_cast<const char *>(row + u.c);
   if constexpr (NARROW) {
 #pragma unroll
@@ -45,13 +49,15 @@ template <bool NARROW, typename E, int N> __device__ __forceinline__ void load_u
         else v.w[k / 2] |= (__float_as_uint(to_f32(row[u.c + k])) >> 16) << (16 * (k % 2));
       }
   } else if constexpr (Cols<E, N>::WORDS == 2) {
-    const u32x2 a = *reinterpret_cast<const u32x2_by2 *>(p);
+    const u32x2_by2 *from = reinterpret_cast<const u32x2_by2 *>(p);
+    const u32x2 a = ONCE ? __builtin_nontemporal_load(from) : *from;
     v.w[0] = a.x; v.w[1] = a.y;
   } else {
     typedef typename Unaligned<E>::type unaligned;
 #pragma unroll
     for (int i = 0; i < Cols<E, N>::WORDS; i += 4) {
-      const u32x4 a = *reinterpret_cast<const unaligned *>(p + 4 * i);
+      const unaligned *from = reinterpret_cast<const unaligned *>(p + 4 * i);
+      const u32x4 a = ONCE ? __builtin_nontemporal_load(from) : *from;
       v.w[i] = a.x; v.w[i + 1] = a.y; v.w[i + 2] = a.z; v.w[i + 3] = a.w;
     }
   }

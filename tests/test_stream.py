@@ -244,6 +244,24 @@ def test_gradient_of_so_many_tokens_that_the_sort_scans_its_counts(V):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("prec,T,d,ldx,shift", [("fp32", 2100, 16001, 16003, 1), ("bf16", 2100, 32001, 32001, 0), ("fp32", 9001, 3730, 3731, 0), ("bf16", 9001, 7463, 7463, 1)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_gradient_of_more_rows_than_the_caches_hold(prec, T, d, ldx, shift, accumulate):
+    """128 MiB of dx and more: whole numbers, whose sums fp32 holds."""
+    say(f"grad large {prec} T={T} d={d} accumulate={accumulate}")
+    V = 300
+    rng = np.random.default_rng(T + d)
+    ids = text_like(rng, T, V)
+    ids[5::40] = -1
+    dx = rng.integers(-9, 10, (T, d), dtype=np.int8)     # up to 9 * 9001 in a sum, below 2^24
+    ref = np.stack([dx[ids == v].sum(0, dtype=np.int64) for v in range(V)])
+    dd = rows_of(dx.astype(np.float32), ldx, DT[prec], shift=shift)
+    old = torch.full((V, d), 3.0, device="cuda") if accumulate else None
+    t = grad(prec, i32(ids), dd, V, d, ldx, d, scale=2.0, accumulate=accumulate, into=old)
+    assert torch.equal(t, torch.from_numpy(2 * ref + 3 * accumulate).float().cuda())
+
+
+@pytest.mark.gpu
 def test_gradient_of_the_positions_is_the_same_call():
     T, d, P = 700, 40, 128
     rng = np.random.default_rng(1)
@@ -343,6 +361,26 @@ def test_rows_to_8_bits_and_back(prec, code, T, d, ldx, ldc, lds, shift):
         B.hmy_k_unpack8(PC[out], CODE[code], codes, scales, y, T, d, ldc, lds, ldx)
         np.testing.assert_array_equal(host(y[:, :d]), ref)
         assert torch.all(y[:, d:] == 7.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec,T,d,ld,shift", [("fp32", 8200, 4099, 4099, 1), ("bf16", 42000, 1601, 1603, 0), ("fp32", 1400000, 24, 24, 0), ("bf16", 10000000, 7, 7, 1), ("fp32", 131072, 256, 260, 0)])
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+def test_more_rows_to_8_bits_than_the_caches_hold(prec, code, T, d, ld, shift):
+    """128 MiB of rows and more in one call give what calls of few rows each give."""
+    say(f"pack8 large {prec} {code} T={T} d={d}")
+    x = torch.randn(T * ld + shift, device="cuda", generator=torch.Generator(device="cuda").manual_seed(d)).to(DT[prec])[shift:].view(T, ld)
+    x[:, ::5] *= 30.0
+    g, step = groups(d), T // 3 + 1
+
+    def pack(lo, hi, codes, scales):
+        B.hmy_k_pack8(PC[prec], CODE[code], x[lo:hi], codes[lo:hi], scales[lo:hi], hi - lo, d, ld, d, g)
+
+    whole, parts = [[torch.full((T, n), 0x5a, device="cuda", dtype=torch.uint8) for n in (d, g)] for _ in range(2)]
+    pack(0, T, *whole)
+    for lo in range(0, T, step):
+        pack(lo, min(T, lo + step), *parts)
+    assert torch.equal(whole[0], parts[0]) and torch.equal(whole[1], parts[1])
 
 
 @pytest.mark.gpu
