@@ -664,8 +664,9 @@ int hmy_k_embed_lookup(const hmy_embed_lookup_desc *g, void *stream);
  * are written, those that no token names with zeros; 1: the sums are added to the rows that tokens name, the others are not touched.
  * Ids outside of [0, V) name no token.  The gradient of pos_table is the same call with the positions as ids and scale 1.
  * workspace: HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d) of device memory, aligned to 16 bytes; calls that may overlap need one each, and
- * a captured call's is written at each replay.  Nothing in it has to be cleared.  T <= HMY_MAX_SORTED; sizes that make more than 2^24
- * workgroups (V d / 2^14 and T d / 2^14 each below that, roughly) are HMY_E_INVALID. */
+ * a captured call's is written at each replay.  Nothing in it has to be cleared.  T <= HMY_MAX_SORTED; sizes that make 2^26 waves
+ * are HMY_E_INVALID: one for each 16 (T <= 8192) or 32 tokens and 256 columns, and, unless accumulate is set, one for each f rows and 1024
+ * columns of dtable, f = 4096 / min(d, 1024) but no more than 64 (so that tables of up to 64 columns are never too large). */
 #define HMY_MAX_SORTED (1 << 24)
 #define HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d) (65536 + 32 * (uint64_t)(T) + 8 * (uint64_t)(d) * (((uint64_t)(T) + 15) / 16))
 typedef struct hmy_embed_grad_desc {

@@ -725,8 +725,10 @@ int launch_embed_grad(const hmy_embed_grad_desc &g, stream_t st) {
   const int filled = (few ? few : 4) * a.fill_rows;   // rows of a workgroup
   const int64_t fill_groups = g.accumulate ? 0 : (int64_t(g.V) + filled - 1) / filled * ((g.d + kFillColumns - 1) / kFillColumns);
   const int64_t join_groups = (int64_t(a.pieces) + kJoinPieces - 1) / kJoinPieces * join_slabs;
-  constexpr int64_t kMostGroups = (1 << 24) - 1;   // of 256 threads: a launch has fewer than 2^32
-  if (run_groups + fill_groups > kMostGroups || join_groups > kMostGroups) return fail(HMY_E_INVALID, "%s: T, d and V are too large together", who);
+  // a launch has fewer than 2^32 threads, of which a workgroup has one wave's or four waves'
+  const auto most_groups = [](int64_t threads) { return (int64_t(1) << 32) / threads - 1; };
+  if (run_groups + fill_groups > most_groups(kWave * (few ? few : 4)) || join_groups > most_groups(4 * kWave))
+    return fail(HMY_E_INVALID, "%s: T, d and V are too large together", who);
   const dim3 grid{uint32_t(run_groups + fill_groups)};
 #define GRAD_AS(N, KERNEL, E, NARROW, ...)                                                                                                       \
   hipLaunchKernelGGL((g.accumulate ? KERNEL<E, NARROW, true, ##__VA_ARGS__> : KERNEL<E, NARROW, false, ##__VA_ARGS__>), grid, dim3(N), 0, s, a, \

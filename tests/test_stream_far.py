@@ -1,0 +1,46 @@
+"""Operators around the residual stream at the ends of what they accept: many rows, long runs, many rounds, rows side by side.
+
+Bounds as in test_stream.py, but where a sum's depth is given here."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2202_01306_amd import binding as B
+from tests.test_stream import PC, at, grad, gradient, i32, rows_of, say
+
+
+# ---- a table's gradient: tables of very many rows ----------------------------------------------------------
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the addresses are no memory: accepted calls would be launched")
+@pytest.mark.parametrize("T", [1, 10, 256, 257, 300, 1024, 1025, 9000])
+@pytest.mark.parametrize("V", [(1 << 30) + 100, 2 ** 31 - 2])
+def test_tables_of_many_rows_are_accepted_whatever_the_number_of_tokens(T, V):
+    """A call that passes all checks ends at the launch, for want of a device."""
+    with pytest.raises(B.HmyError) as e:
+        gradient(T=T, d=1, V=V, ldx=1, ldt=1, dtable=1 << 40)
+    assert e.value.code != B.HMY_E_INVALID, str(e.value)
+
+
+@pytest.mark.parametrize("T", [1, 256, 257, 1024, 9000])
+def test_more_workgroups_than_a_launch_has_are_refused_whatever_the_number_of_tokens(T):
+    """2^22 rows of 2^17 columns: four rows of 1024 columns a wave are 2^27 waves."""
+    d, V = 1 << 17, 1 << 22
+    with pytest.raises(B.HmyError, match="too large together") as e:
+        gradient(T=T, d=d, V=V, ldx=d, ldt=d, dx=1 << 50, dtable=1 << 52, workspace=1 << 54, workspace_bytes=1 << 40)
+    assert e.value.code == B.HMY_E_INVALID
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,V", [(256, (1 << 30) + 100), (10, 2 ** 31 - 2), (257, 2 ** 31 - 2)])
+def test_tables_of_many_rows(T, V):
+    """Every row written once: those that tokens name with their sums of whole numbers, all others with zeros."""
+    say(f"grad T={T} V={V}")
+    rng = np.random.default_rng(T)
+    ids = rng.integers(0, V, T)
+    ids[-7:] = V - 1, 0, -1, V - 1, V - 2, 1 << 30, 63
+    dx = rng.integers(1, 9, (T, 1)).astype(np.float32)
+    t = grad("fp32", i32(ids), rows_of(dx, 1, torch.float32), V, 1, 1, 1)
+    named = np.unique(ids[ids >= 0])
+    want = np.array([dx[ids == v].sum() for v in named], np.float32)
+    assert torch.equal(t[torch.from_numpy(named).cuda(), 0].cpu(), torch.from_numpy(want))
+    assert sum(int(p.count_nonzero()) for p in t.view(-1).split(1 << 28)) == len(named)
