@@ -480,7 +480,9 @@ __global__ __launch_bounds__(256) void k_embed_grad_runs(Runs g, const E *dx, in
 // kJoinPieces pieces (1841 tokens of 203 rows, twice: 28 us with 4 pieces, 30 with 16; 131072 tokens of 30522, without streaming loads:
 // 179 and 178).  Runs of up to kShortRun parts are a wave's each; of a longer one each of the four waves takes a fourth of the parts, joined
 // in one order (eight or sixteen waves are slower: most runs are short).  Bound by latency: keys, their count, the parts, the row.
-constexpr int kJoinPieces = 4, kShortRun = 8;
+// A wave adds up kStretch parts one after the other, then as many of these sums, then those: a term goes through 63 additions in its piece and
+// 165 here at most, where one chain over a run of 2^24 tokens has 131072 (equal terms of 0.1: off by 1.0e-3 of the sum, 9e-7 this way).
+constexpr int kJoinPieces = 4, kShortRun = 8, kStretch = 64;
 
 // parts q0 .. q1 - 1 of the run that starts in `piece`, added to sum
 template <bool NARROW, int DEEP> __device__ __forceinline__ void add_parts(const Runs &g, const Slab<float, NARROW> &s, int piece, int q0, int q1, float (&sum)[4]) {
@@ -524,7 +526,24 @@ template <bool NARROW, bool ADD> __device__ __forceinline__ void join_runs(const
     for (int k = 0; k < 4; ++k) sum[k] = 0.f;
     if (wave == 0) s.load(sum, g.partial + int64_t(2 * piece + 1) * g.d);
     if (ADD && wave == 0) s.load(old, g.dtable + int64_t(key) * g.ldt);
-    add_parts<NARROW, 16>(g, s, piece, wave * per, min(parts, (wave + 1) * per), sum);
+    float some[4] = {0.f, 0.f, 0.f, 0.f}, all[4] = {0.f, 0.f, 0.f, 0.f};
+    const int q1 = min(parts, (wave + 1) * per);
+    for (int q = wave * per, turn = 1; q < q1; q += kStretch, ++turn) {
+      add_parts<NARROW, 16>(g, s, piece, q, min(q1, q + kStretch), sum);
+      if (q + kStretch >= q1) break;
+      const bool far = turn % kStretch == 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        some[k] += sum[k];
+        sum[k] = 0.f;
+        if (far) {
+          all[k] += some[k];
+          some[k] = 0.f;
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[k] = all[k] + (some[k] + sum[k]);
     __syncthreads();              // of the run before, whose parts wave 0 has read
 #pragma unroll
     for (int k = 0; k < 4; ++k) part[wave][lane * 4 + k] = sum[k];

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2202_01306_amd import binding as B
-from tests.test_stream import PC, at, grad, gradient, i32, rows_of, say
+from tests.test_stream import PC, U, grad, gradient, i32, rows_of, say
 
 
 # ---- a table's gradient: tables of very many rows ----------------------------------------------------------
@@ -44,3 +44,33 @@ def test_tables_of_many_rows(T, V):
     want = np.array([dx[ids == v].sum() for v in named], np.float32)
     assert torch.equal(t[torch.from_numpy(named).cuda(), 0].cpu(), torch.from_numpy(want))
     assert sum(int(p.count_nonzero()) for p in t.view(-1).split(1 << 28)) == len(named)
+
+
+# ---- a table's gradient: long runs ----------------------------------------------------------------------------
+
+# A term goes through at most 63 additions in its piece of the list and the one behind, 64 among the parts of its run, 64 among sums of 64
+# parts, 32 among sums of 64 of those (2^24 tokens are 2^19 parts, a quarter of them a wave's), 2 and 3 more where these and the waves meet,
+# and the scaling: 229 roundings, however long the run is.
+LONG = 229
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("T,V,d", [(1 << 20, 1, 8), ((1 << 20) + 77, 2, 5), (1 << 22, 2, 8), (1 << 24, 1, 4), (1 << 24, 2, 8), ((1 << 24) - 1, 5, 3)])
+def test_long_runs_of_terms_that_round_the_same_way(prec, accumulate, T, V, d):
+    """Equal terms in a column, as of a bias: a rounding repeats itself instead of cancelling."""
+    say(f"grad long {prec} T={T} V={V} d={d} accumulate={accumulate}")
+    gen = torch.Generator(device="cuda").manual_seed(T + V)
+    ids = torch.randint(0, V, (T,), device="cuda", generator=gen, dtype=torch.int32)
+    terms = torch.tensor([0.1, 0.9, 3.3, 0.7, 1 / 7, 1.1, 1 / 3, 0.013][:d], device="cuda").to(torch.float32 if prec == "fp32" else torch.bfloat16)
+    dx = terms.expand(T, d).contiguous()
+    into = torch.full((V, d), 2.5, device="cuda") if accumulate else torch.full((V, d), 7.0, device="cuda")
+    ws = torch.full((B.HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d),), 0xff, device="cuda", dtype=torch.uint8)
+    B.hmy_k_embed_grad(PC[prec], ids, dx, into, T, d, V, d, d, scale=1.5, accumulate=accumulate, workspace=ws)
+    n = torch.bincount(ids.long(), minlength=V).double().cpu().numpy()
+    size = 1.5 * n[:, None] * terms.double().cpu().numpy()[None]
+    want = size + 2.5 * accumulate
+    off = np.abs(into.double().cpu().numpy() - want)
+    bound = LONG * U * size + U * want
+    assert np.all(off <= bound), float((off / bound).max())
