@@ -291,6 +291,8 @@ struct Norm8Grad {
   int accumulate;
 };
 
+constexpr int kStretch = 256;   // rows that a lane adds up one after the other
+
 // What a wave reads of a row, on its way while the row before is worked on.
 template <typename E, int NJ> struct Row8 {
   uint32_t codes[NJ][kN / 4];
@@ -304,6 +306,8 @@ template <typename E, int NJ> struct Row8 {
 // workgroup goes to the workspace: 256 workgroups, one per compute unit, of eight waves with up to 256 registers, seven bytes per column
 // of the row at hand and of the next one among them.  4096 x 1024 bf16 with res, dx_e and all sums, 54.7 MB: 13.4 us (the rows beyond the first
 // 2048 at 7 TB/s; the rest is launch, the first loads and the slots' joining) and 3.7 for the sums; 32768 rows 81 (5.4 TB/s); 4095 x 4096 40.
+// Registers take kStretch rows' sums, which then go to those that the slot has in LDS (a workgroup of one slot: in the workspace), so that a term
+// goes through 256 additions and one for each 256 of its rows: in one chain 2^28 rows of 8 equal columns were off by up to 2e-4 of their sum.
 // Sixteen waves of half the registers are 1 to 5 % faster there, 3 % slower at 16384 x 1024 and 19 % at 2000 x 8000.
 template <typename E, int CODE, int LPR, int W, int NJ, bool NARROW>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_layernorm8_bwd(Norm8Grad g, const E *dy, const E *gamma, E *dx_e) {
@@ -330,77 +334,94 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) voi
       if (g.res) load_unit<NARROW>(r.res[j], g.res + row * g.ldr, u[j], g.d);
     }
   };
+  // a unit's sums to the slot's, where only this lane has its columns; of lanes whose rows lie side by side the first ones
+  auto leave = [&](float *to, float (&t)[kN], Unit at, bool more) {
+    if (LPR < kWave && lane >= LPR) return;
+    if (more) {
+      Cols<float, kN> before;
+      load_unit<NARROW>(before, to, at, g.d);
+#pragma unroll
+      for (int k = 0; k < kN; ++k) t[k] += before.at(k);
+    }
+    store_unit<NARROW>(to, t, at, g.d);
+  };
 #pragma unroll
   for (int j = 0; j < NJ; ++j) {
     u[j] = unit_at<NARROW, kN>(kN * (kWave * (NJ * (wave % W) + j) + lane % LPR), g.d);
     load_unit<NARROW>(ga[j], gamma, u[j], g.d);
-#pragma unroll
-    for (int k = 0; k < kN; ++k) dg[j][k] = db[j][k] = dr[j][k] = 0.f;
-  }
-  const int64_t step = int64_t(gridDim.x) * kSlots * kAbreast;
-  int parity = 0;
-  fetch(now, int64_t(blockIdx.x) * kSlots * kAbreast);
-  for (int64_t base = int64_t(blockIdx.x) * kSlots * kAbreast; base < g.T; base += step, parity ^= 1) {
-    if (base + step < g.T) fetch(next, base + step);
-    const int64_t row = base + slot * kAbreast + (LPR < kWave ? lane / LPR : 0);
-    const bool live = row < g.T;
-    float xh[NJ][kN], gy[NJ][kN], s[2] = {0.f, 0.f};
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-      decode<CODE>(now.codes[j], now.byte[j], xh[j]);
-#pragma unroll
-      for (int k = 0; k < kN; ++k) {
-        xh[j][k] = (xh[j][k] - now.mean) * now.rstd;
-        gy[j][k] = now.dy[j].at(k);
-      }
-      clear_foreign<NARROW>(xh[j], u[j], g.d);
-      clear_foreign<NARROW>(gy[j], u[j], g.d);
-#pragma unroll
-      for (int k = 0; k < kN; ++k) {
-        const float t = gy[j][k] * ga[j].at(k);
-        s[0] += t;
-        s[1] = fmaf(t, xh[j][k], s[1]);
-      }
-    }
-    row_sums<LPR, W>(s, xch[parity], wave);
-    const float m1 = s[0] / float(g.d), m2 = s[1] / float(g.d);
-    if (live) {
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        float o[kN];
-#pragma unroll
-        for (int k = 0; k < kN; ++k) {
-          o[k] = (gy[j][k] * ga[j].at(k) - m1 - xh[j][k] * m2) * now.rstd;
-          dg[j][k] = fmaf(gy[j][k], xh[j][k], dg[j][k]);
-          db[j][k] += gy[j][k];
-          if (g.res) {
-            o[k] += now.res[j].at(k);
-            dr[j][k] += now.res[j].at(k);
-          }
-        }
-        store_unit<NARROW>(g.dx + row * g.ldx, o, u[j], g.d);
-        if (dx_e) store_unit<NARROW>(dx_e + row * g.lde, o, u[j], g.d);
-      }
-    }
-    now = next;
-  }
-  if constexpr (LPR < kWave) {   // rows side by side in the wave: their sums, left in each of them
-#pragma unroll
-    for (int k = 0; k < kN; ++k)
-#pragma unroll
-      for (int o = LPR; o < kWave; o *= 2) {
-        dg[0][k] += __shfl_xor(dg[0][k], o, kWave);
-        db[0][k] += __shfl_xor(db[0][k], o, kWave);
-        dr[0][k] += __shfl_xor(dr[0][k], o, kWave);
-      }
   }
   float *out = g.partial + int64_t(blockIdx.x) * ns * g.d;
   float *mine = kSlots > 1 ? lds + int64_t(slot) * ns * g.d : out;
+  const int64_t begin = int64_t(blockIdx.x) * kSlots * kAbreast, step = int64_t(gridDim.x) * kSlots * kAbreast;
+  int parity = 0;
+  fetch(now, begin);
+  for (int64_t base = begin; base < g.T;) {
+    const int64_t until = min(int64_t(g.T), base + kStretch * step);
+    const bool more = base != begin;   // sums of rows before are in place already
 #pragma unroll
-  for (int j = 0; j < NJ; ++j) {
-    store_unit<NARROW>(mine, dg[j], u[j], g.d);
-    store_unit<NARROW>(mine + g.d, db[j], u[j], g.d);
-    if (ns == 3) store_unit<NARROW>(mine + 2 * g.d, dr[j], u[j], g.d);
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int k = 0; k < kN; ++k) dg[j][k] = db[j][k] = dr[j][k] = 0.f;
+    for (; base < until; base += step, parity ^= 1) {
+      if (base + step < g.T) fetch(next, base + step);
+      const int64_t row = base + slot * kAbreast + (LPR < kWave ? lane / LPR : 0);
+      const bool live = row < g.T;
+      float xh[NJ][kN], gy[NJ][kN], s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        decode<CODE>(now.codes[j], now.byte[j], xh[j]);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+          xh[j][k] = (xh[j][k] - now.mean) * now.rstd;
+          gy[j][k] = now.dy[j].at(k);
+        }
+        clear_foreign<NARROW>(xh[j], u[j], g.d);
+        clear_foreign<NARROW>(gy[j], u[j], g.d);
+#pragma unroll
+        for (int k = 0; k < kN; ++k) {
+          const float t = gy[j][k] * ga[j].at(k);
+          s[0] += t;
+          s[1] = fmaf(t, xh[j][k], s[1]);
+        }
+      }
+      row_sums<LPR, W>(s, xch[parity], wave);
+      const float m1 = s[0] / float(g.d), m2 = s[1] / float(g.d);
+      if (live) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          float o[kN];
+#pragma unroll
+          for (int k = 0; k < kN; ++k) {
+            o[k] = (gy[j][k] * ga[j].at(k) - m1 - xh[j][k] * m2) * now.rstd;
+            dg[j][k] = fmaf(gy[j][k], xh[j][k], dg[j][k]);
+            db[j][k] += gy[j][k];
+            if (g.res) {
+              o[k] += now.res[j].at(k);
+              dr[j][k] += now.res[j].at(k);
+            }
+          }
+          store_unit<NARROW>(g.dx + row * g.ldx, o, u[j], g.d);
+          if (dx_e) store_unit<NARROW>(dx_e + row * g.lde, o, u[j], g.d);
+        }
+      }
+      now = next;
+    }
+    if constexpr (LPR < kWave) {   // rows side by side in the wave: their sums, left in each of them
+#pragma unroll
+      for (int k = 0; k < kN; ++k)
+#pragma unroll
+        for (int o = LPR; o < kWave; o *= 2) {
+          dg[0][k] += __shfl_xor(dg[0][k], o, kWave);
+          db[0][k] += __shfl_xor(db[0][k], o, kWave);
+          dr[0][k] += __shfl_xor(dr[0][k], o, kWave);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      leave(mine, dg[j], u[j], more);
+      leave(mine + g.d, db[j], u[j], more);
+      if (ns == 3) leave(mine + 2 * g.d, dr[j], u[j], more);
+    }
   }
   if constexpr (kSlots > 1) {
     __syncthreads();

@@ -74,3 +74,42 @@ def test_long_runs_of_terms_that_round_the_same_way(prec, accumulate, T, V, d):
     off = np.abs(into.double().cpu().numpy() - want)
     bound = LONG * U * size + U * want
     assert np.all(off <= bound), float((off / bound).max())
+
+
+# ---- layer norm of rows in 8 bits: column sums over many rows --------------------------------------------------
+
+def slots_of(d):
+    """Rows that a workgroup of the backward pass has at a time."""
+    return 8 // (1 if d <= 1024 else 2 if d <= 2048 else 4 if d <= 4096 else 8) * (8 if d <= 32 else 4 if d <= 64 else 2 if d <= 128 else 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec,T,d,accumulate", [("fp32", 1 << 28, 8, False), ("bf16", (1 << 24) + 9, 24, True), ("bf16", 1 << 25, 100, False), ("bf16", (1 << 22) + 1, 300, True),
+                                                 ("bf16", (1 << 20) + 3, 1100, False), ("fp32", (1 << 20) + 5, 2100, False), ("bf16", (1 << 20) + 3, 4100, True)])
+def test_column_sums_over_rows_that_round_the_same_way(prec, T, d, accumulate):
+    """Equal rows.  A term goes through at most 256 additions in a lane, one for each 256 of its rows, 3 between rows side by side, 8 between a
+    workgroup's, 16 and 16 of the 256 partial sums; products with what the codes stand for are exact."""
+    say(f"norm8 sums {prec} T={T} d={d} accumulate={accumulate}")
+    dt = torch.float32 if prec == "fp32" else torch.bfloat16
+    at = torch.arange(d, device="cuda")
+    v = (at * 37 % 251 - 125).to(torch.int8)
+    row = (0.1 + 0.8 * (at * 13 % 101) / 101).to(dt)
+    with_res = d <= 24
+    codes, dy = v.expand(T, d).contiguous(), row.expand(T, d).contiguous()
+    scales = torch.full((T, (d + 31) // 32), 127, device="cuda", dtype=torch.uint8)
+    mean, rstd = torch.zeros(T, device="cuda"), torch.ones(T, device="cuda")
+    res = (row.float() + 0.3).expand(T, d).contiguous() if with_res else None
+    dx = res if with_res else torch.empty(T, d, device="cuda")
+    sums = [torch.full((d,), 2.5 if accumulate else 7.0, device="cuda") for _ in range(3)]
+    r = (row.float() + 0.3).double().cpu().numpy()
+    ws = torch.full((B.HMY_NORM8_WORKSPACE_BYTES(d),), 0xff, device="cuda", dtype=torch.uint8)
+    B.hmy_k_layernorm8_bwd(PC[prec], B.HMY_CODE_INT8, dy, codes, scales, mean, rstd, torch.ones(d, device="cuda", dtype=dt), dx, sums[0], sums[1], T, d, d,
+                           (d + 31) // 32, d, d, res=res, ldr=d, dres_sum=sums[2] if with_res else None, accumulate=accumulate, workspace=ws)
+    y, x = row.double().cpu().numpy(), v.double().cpu().numpy()
+    rounds = -(-T // (256 * slots_of(d)))
+    n = 256 + -(-rounds // 256) + 3 + 8 + 32
+    for t, terms in zip(sums, [y * x, y] + ([r] if with_res else [])):
+        want = T * terms + 2.5 * accumulate
+        off = np.abs(t.double().cpu().numpy() - want)
+        bound = n * U * T * np.abs(terms) + U * np.abs(want)
+        assert np.all(off <= bound), float((off[bound > 0] / bound[bound > 0]).max())
