@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from paper_2202_01306_amd import binding as B
-from tests.test_stream import PC, U, grad, gradient, i32, rows_of, say
+from tests.test_stream import DT, PC, Norm, U, dx_bound, grad, gradient, host, i32, near, os_, rows_of, say
 
 
 # ---- a table's gradient: tables of very many rows ----------------------------------------------------------
@@ -76,12 +76,36 @@ def test_long_runs_of_terms_that_round_the_same_way(prec, accumulate, T, V, d):
     assert np.all(off <= bound), float((off / bound).max())
 
 
-# ---- layer norm of rows in 8 bits: column sums over many rows --------------------------------------------------
+# ---- layer norm of rows in 8 bits: several rounds of rows --------------------------------------------------------
 
 def slots_of(d):
     """Rows that a workgroup of the backward pass has at a time."""
     return 8 // (1 if d <= 1024 else 2 if d <= 2048 else 4 if d <= 4096 else 8) * (8 if d <= 32 else 4 if d <= 64 else 2 if d <= 128 else 1)
 
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec,code", [("fp32", "int8"), ("bf16", "e4m3")])
+@pytest.mark.parametrize("T,d,ld,shift", [(3001, 1100, 1100, 0), (2500, 2048, 2051, 1), (1300, 2500, 2500, 0), (700, 4099, 4100, 3), (600, 8192, 8192, 0), (5001, 1023, 1023, 0),
+                                          (40001, 24, 24, 0), (33000, 5, 6, 1), (20003, 50, 53, 2), (10001, 100, 100, 0)])
+def test_layer_norm_backward_in_three_rounds_and_a_ragged_one(prec, code, T, d, ld, shift):
+    """Rows fetched ahead, waves of a row that exchange sums round after round, sums carried from one round to the next."""
+    say(f"norm8 rounds {prec} {code} T={T} d={d}")
+    assert 2 * 256 * slots_of(d) < T and T % (256 * slots_of(d))
+    n = Norm(prec, code, T, d, ld, shift)
+    n.forward()
+    n.check_forward()
+    first = [t.clone() for t in n.backward()]
+    n.check_backward()
+    for a, b in zip(first, n.backward()):
+        assert torch.equal(a, b)
+    n.backward(in_place=True, accumulate=True, into=[torch.full((d,), 3.0, device="cuda") for _ in range(3)])
+    n.check_backward(base=3.0)
+    assert torch.equal(n.dx[:, :d], first[0][:, :d])
+    n.backward(res=False, rounded_too=False)
+    n.check_backward(res=False)
+
+
+# ---- layer norm of rows in 8 bits: column sums over many rows --------------------------------------------------
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("prec,T,d,accumulate", [("fp32", 1 << 28, 8, False), ("bf16", (1 << 24) + 9, 24, True), ("bf16", 1 << 25, 100, False), ("bf16", (1 << 22) + 1, 300, True),
