@@ -137,3 +137,75 @@ def test_column_sums_over_rows_that_round_the_same_way(prec, T, d, accumulate):
         off = np.abs(t.double().cpu().numpy() - want)
         bound = n * U * T * np.abs(terms) + U * np.abs(want)
         assert np.all(off <= bound), float((off[bound > 0] / bound[bound > 0]).max())
+
+
+# ---- rows side by side in one array ----------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,d", [(50, 97), (300, 33), (70, 5), (40, 1025), (20, 2501), (30, 4099)])
+def test_a_gradient_beside_the_gradient_that_it_reads(prec, T, d):
+    """Layer norm backward with res and dx, and dy of fp32, as ranges of columns of one array; odd widths, whose last unit begins in the one before."""
+    say(f"norm8 beside {prec} T={T} d={d}")
+    n = Norm(prec, "int8", T, d, d)
+    n.forward()
+    ld = 3 * d + 11
+    store = torch.full((T, ld), 7.0, device="cuda")
+    res, dx = store[:, 3:], store[:, d + 3:]             # no column between them
+    store[:, 3:d + 3] = torch.from_numpy(n.res).cuda()
+    dy, ldy = (store[:, 2 * d + 6:], ld) if prec == "fp32" else (rows_of(n.dy, d, DT[prec]), d)
+    dy[:, :d] = torch.from_numpy(n.dy).cuda()
+    before = store.clone()
+    sums = [torch.full((d,), 7.0, device="cuda") for _ in range(3)]
+    ws = torch.full((B.HMY_NORM8_WORKSPACE_BYTES(d),), 0xff, device="cuda", dtype=torch.uint8)
+    B.hmy_k_layernorm8_bwd(PC[prec], B.HMY_CODE_INT8, dy, n.codes, n.scales, n.mean, n.rstd, n.g, dx, sums[0], sums[1], T, d, d, n.G, ldy, ld, res=res, ldr=ld,
+                           dres_sum=sums[2], workspace=ws)
+    args = (n.dy.astype(np.float64), n.v, host(n.mean), host(n.rstd), n.gamma.astype(np.float64))
+    ref = os_.layernorm_grad(*args, n.res.astype(np.float64))[0]
+    near(host(dx[:, :d]), ref, dx_bound(*args, ref, n.res.astype(np.float64)))
+    alone = n.backward()
+    assert torch.equal(dx[:, :d], alone[0][:, :d]) and all(torch.equal(a, b) for a, b in zip(sums, n.sums))
+    dx[:, :d] = 7.0
+    assert torch.equal(store, before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [60, 700, 1500, 9001])
+@pytest.mark.parametrize("d", [3, 37, 261])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_a_tables_gradient_beside_the_rows_that_it_adds_up(T, d, accumulate):
+    """dtable and dx as ranges of columns of one array."""
+    say(f"grad beside T={T} d={d} accumulate={accumulate}")
+    rng = np.random.default_rng(T + d)
+    V = T // 3
+    ids = rng.integers(-1, V + 1, T)
+    ids[ids == 5] = 6                                    # a row that no token names
+    dx = rng.integers(-9, 10, (T, d)).astype(np.float32)
+    ld = 2 * d + 5
+    store = torch.full((T, ld), 7.0, device="cuda")
+    rows, table = store[:, 2:], store[:, d + 2:]
+    rows[:, :d] = torch.from_numpy(dx).cuda()
+    before = store.clone()
+    grad("fp32", i32(ids), rows, V, d, ld, ld, scale=0.5, accumulate=accumulate, into=table)
+    want, _, named = os_.embed_grad(ids, dx, V, 0.5)
+    np.testing.assert_array_equal(host(table[:V, :d]), want + 7.0 * accumulate)   # whole numbers and halves: exact
+    table[:V, :d] = 7.0
+    assert torch.equal(store, before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [3, 37, 400, 1601])
+def test_rows_of_a_lookup_beside_the_rows_of_its_table(d):
+    T, V = 90, 70
+    rng = np.random.default_rng(d)
+    values = rng.standard_normal((V, d)).astype(np.float32)
+    ids = rng.integers(-1, V + 1, T)
+    ld = 2 * d + 1
+    store = torch.full((T, ld), 7.0, device="cuda")
+    store[:V, :d] = torch.from_numpy(values).cuda()
+    before = store.clone()
+    x = store[:, d:]
+    B.hmy_k_embed_lookup(0, 0, i32(ids), store, x, T, d, V, ld, ld, scale=2.0)
+    np.testing.assert_array_equal(host(x[:, :d]), os_.embed_lookup(ids, values, 2.0))
+    x[:, :d] = 7.0
+    assert torch.equal(store, before)
