@@ -209,3 +209,66 @@ def test_rows_of_a_lookup_beside_the_rows_of_its_table(d):
     np.testing.assert_array_equal(host(x[:, :d]), os_.embed_lookup(ids, values, 2.0))
     x[:, :d] = 7.0
     assert torch.equal(store, before)
+
+
+# ---- offsets beyond 32 bits, the longest lists -------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("prec,out,T,d,ldx", [("bf16", "bf16", (1 << 20) + 3, 4096, 4096), ("fp32", "fp32", (1 << 20) + 1, 1025, 4100), ("bf16", "fp32", (1 << 30) + 5, 16, 16)])
+def test_rows_of_a_lookup_beyond_32_bits(prec, out, T, d, ldx):
+    """2^32 elements and more, with as many units of a lane in the last one."""
+    say(f"lookup far {prec} {out} T={T} d={d}")
+    V = 251
+    table = torch.randn(V, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(d)).to(DT[prec])
+    ids = torch.arange(T, device="cuda", dtype=torch.int32) % (V + 2) - 1   # none, 0 .. V - 1, none
+    x = torch.full((T, ldx), 7.0, device="cuda", dtype=DT[out])
+    B.hmy_k_embed_lookup(PC[prec], PC[out], ids, table, x, T, d, V, d, ldx, scale=0.25)
+    zero = torch.zeros(1, d, device="cuda", dtype=DT[prec])
+    want = (torch.cat([zero, table, zero]).float() * 0.25).to(DT[out])      # a power of two: exact
+    step = (V + 2) * max(1, (1 << 26) // ((V + 2) * d))
+    for r in range(0, T, step):
+        part = x[r:r + step]
+        assert torch.equal(part[:, :d], want.repeat(step // (V + 2), 1)[:len(part)])
+        assert ldx == d or torch.all(part[:, d:] == 7.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,d,ldx", [(600, 64, 1 << 23), (8000, 64, (1 << 20) + 1), (70001, 64, 65600), (70001, 640, 65600)])
+@pytest.mark.parametrize("accumulate", [False, True])
+def test_rows_that_a_gradient_adds_up_beyond_32_bits(T, d, ldx, accumulate):
+    """Rows far apart: in one launch, ranked, sorted, and by streaming loads."""
+    say(f"grad far T={T} d={d} accumulate={accumulate}")
+    V = 90
+    gen = torch.Generator(device="cuda").manual_seed(T + d)
+    dx = torch.full((T, ldx), 99.0, device="cuda", dtype=torch.bfloat16)
+    dx[:, :d] = torch.randint(-9, 10, (T, d), device="cuda", generator=gen).bfloat16()
+    ids = torch.randint(-1, V, (T,), device="cuda", generator=gen, dtype=torch.int32)
+    into = torch.full((V, d), 3.0, device="cuda")
+    ws = torch.full((B.HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d),), 0xff, device="cuda", dtype=torch.uint8)
+    B.hmy_k_embed_grad(1, ids, dx, into, T, d, V, ldx, d, accumulate=accumulate, workspace=ws)
+    x, at = host(dx[:, :d]), ids.cpu().numpy()
+    want = np.stack([x[at == v].sum(0) for v in range(V)]) + 3.0 * accumulate   # whole numbers below 2^24
+    np.testing.assert_array_equal(host(into), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T,V,d", [(B.HMY_MAX_SORTED, 100000, 2), (B.HMY_MAX_SORTED - 3, 200, 3), (1 << 22, 2 ** 31 - 2, 1), ((1 << 23) + 1023, 1 << 24, 1)])
+def test_gradient_of_the_longest_lists(T, V, d):
+    """Up to 2^24 tokens, one to four passes of the sort: whole numbers, whose sums fp32 holds."""
+    say(f"grad T={T} V={V} d={d}")
+    gen = torch.Generator(device="cuda").manual_seed(V % 1000)
+    rank = torch.exp(torch.rand(T, device="cuda", generator=gen, dtype=torch.float64) * np.log(V + 1.0)).long().sub_(1).clamp_(0, V - 1)
+    ids = ((rank * 7919 + 17) % V).to(torch.int32)                          # spread over the table
+    ids[5::50] = -1
+    ids[-1] = V - 1
+    dx = torch.randint(-4, 5, (T, d), device="cuda", generator=gen).float()
+    t = torch.full((V, d), 7.0, device="cuda")
+    ws = torch.full((B.HMY_EMBED_GRAD_WORKSPACE_BYTES(T, d),), 0xff, device="cuda", dtype=torch.uint8)
+    B.hmy_k_embed_grad(0, ids, dx, t, T, d, V, d, d, workspace=ws)
+    at, x = ids.cpu().numpy(), host(dx)
+    named, inverse = np.unique(at[at >= 0], return_inverse=True)
+    rows = torch.from_numpy(named).cuda()
+    for c in range(d):
+        np.testing.assert_array_equal(host(t[rows, c]), np.bincount(inverse, weights=x[at >= 0, c], minlength=len(named)))
+    t[rows] = 0.0
+    assert all(int(p.count_nonzero()) == 0 for p in t.view(-1).split(1 << 28))
