@@ -642,7 +642,8 @@ int hmy_k_distill(const hmy_distill_desc *g, void *stream);
  * Rows of T tokens and d columns in fp32 or bf16 (HMY_PREC_*), each array with a row stride of its own (in elements, >= d) and aligned
  * to its elements only; columns behind the d-th are left as they are.  T >= 1, 1 <= d <= 2^24.  Nothing is allocated, results do not
  * depend on the order in which workgroups run, and every call can be captured into a graph.  Outputs overlap neither each other nor
- * an input (HMY_E_INVALID where a call's rows do), but where it is said. */
+ * an input, but where it is said: HMY_E_INVALID where a call's rows do, and where arrays of different pitch lie in each other's gaps (those of
+ * one pitch may lie side by side). */
 
 /* x[t] (type out_prec) = scale * table[ids[t]] + pos_table[positions[t]], in fp32, rounded once.  An id outside of [0, V) names no
  * token and a position outside of [0, P) no place: their term is left out, so that a token of padding with both at -1 has a row of

@@ -4,8 +4,11 @@
 // neighbours, a sum is a run of the sorted list, and no row of the table is written by two workgroups: no atomics, one order.
 // Three steps: the order (keys only: 8 bytes per token), the sums of runs inside pieces of the list, and the joining of those runs that
 // go through whole pieces.  Bound by HBM where there are many tokens: every row of dx is read once, every row of the table written once.
-// 131072 tokens of 1024 fp32 columns, 30522 rows, 662 MB: 163 us, of which 24 for the order (two passes, four launches), 134 for the sums
-// (4.9 TB/s) and 10 for the joining; 4096 tokens, 50257 rows of which most are empty, 222 MB: 5, 42 (5.3 TB/s) and 4.7.
+// 131072 tokens of 1024 fp32 columns, 30522 rows, 662 MB: 164 us a call; one by one, in a trace, which adds some 0.6 us to a kernel, 24 for the
+// order (two passes, four launches), 134 for the sums (4.9 TB/s) and 10 for the joining; 4096 tokens, 50257 rows of which most are empty, 222 MB:
+// 5, 42 (5.3 TB/s) and 4.7.  Far from HBM, by the order's launches and by lanes without columns: 131072 x 24 41 us (3 at a copy's rate), x 128
+// 45 (17), x 256 63 (35); and by the joining of a few very long runs on a workgroup each: 131072 x 1024 in 2 rows 142 (112), 2^24 x 4 in one row
+// 18.9 ms (0.07).
 #include <algorithm>
 
 #include "stream_rows.h"
@@ -25,7 +28,7 @@ struct Lookup {
 
 // A token's row is found through its id, so that a lane waits twice for memory before it stores: all of its ids are on their way together,
 // and then all of its rows.  Bound by HBM, with what the eight L2s each fetch of popular rows: 32768 tokens of 1024 columns, bf16 to fp32
-// with positions, 134 MB written and 41 read (20 of them what the call cannot do without): 43 us (4.1 TB/s; from a table of 512 rows,
+// with positions, 134 MB written and 42 read (23 of them what the call cannot do without): 43 us (4.1 TB/s; from a table of 512 rows,
 // which the L2s hold, 29).  Workgroups that stay and fetch their next rows ahead take 47 to 49.
 template <typename E, typename O, int K, bool NARROW>
 __global__ __launch_bounds__(kThreads) void k_embed_lookup(Lookup g, const E *table, const E *pos_table, O *x, Units units) {
@@ -379,9 +382,12 @@ __device__ __forceinline__ int keys_below(const Runs &g, int64_t key, int lane) 
 // x 1024: 190, 184, 184; all before any loads were streaming ones).  kAhead rows are on their way before the first is added (8 instead of 16: 90
 // instead of 81 us at 16384 x 1024).
 // What the wave has to know of the list it reads in one go, a place a lane: the piece, the one behind, and a key at either end.
-// ONCE, from kStreamed bytes on: the caches are left to the table and to sums of parts of runs (fp32 rows of 1024 columns, 131072 tokens 163 us
-// instead of 176, 65536 102 and 112, 20480 60.0 and 61.6, but 16384 54 and 52; bf16 x 2048, 20480 tokens 80 and 85; fp32 x 5000, 16384 tokens
-// 223 and 221).
+// ONCE, from kStreamed bytes on: the caches are left to the table and to sums of parts of runs.  Calls with three sets of inputs in turn: fp32 rows of
+// 1024 columns, 131072 tokens 167 us instead of 178, 65536 105 and 115, 32768 74 and 79, 20480 63 and 65, but 16384 57 and 55; bf16 x 2048, 20480
+// tokens 84 and 90; it does not pay at fp32 x 5000, 16384 tokens: 226 and 224.  With dx written by the kernel just before: 131072 tokens 158 us
+// instead of 198, 65536 96 and 102, 16384 x 5000 210 and 227, but 32768 69 and 65, 20480 58 and 56 (16384 54 and 54).
+// ADD: what is in the table is on its way for every token, though only the last one of a run needs it; bf16 rows, eight columns a lane, take 218 to
+// 223 registers for it, two waves per SIMD, fp32 rows 150 to 155: 4096 x 1024 18 us for either, 20480 x 2048 75 (fp32) and 66 (bf16).
 template <typename E, int PIECE, bool NARROW, bool ADD, bool ONCE>
 __device__ __forceinline__ void sum_piece(const Runs &g, const E *dx, int piece, int slab, int lane) {
   static_assert(2 * PIECE <= kWave, "a place a lane");

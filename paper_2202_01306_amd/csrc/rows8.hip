@@ -103,8 +103,9 @@ template <int CODE, int N> __device__ __forceinline__ void decode(const uint32_t
 }
 
 // 32768 x 4096 fp32, 537 MB read and 138 written: 111 us (6.1 TB/s); with a row's four chunks in four sweeps over all rows 14 more.
-// ONCE, from kStreamed bytes on: 111 us instead of 118, 65536 x 1024 57 and 61, 20480 x 1024 20.3 and 20.9, but 16384 x 1024 16 and 15; bf16
-// 20480 x 2048 23.6 and 24.9, 65536 x 1601 61 and 60.
+// ONCE, from kStreamed bytes on, calls with three sets of rows in turn: 114 us instead of 120, 65536 x 1024 59 and 62, 32768 x 1024 32 and 34, 20480 x
+// 1024 22 and 24, but 16384 x 1024 18 and 16; bf16 20480 x 2048 25 and 27; it does not pay at bf16 65536 x 1601: 61 and 61.  With x written by the
+// kernel just before: 109 us instead of 156, 65536 x 1024 53 and 68, but 32768 x 1024 29 and 28, 20480 x 1024 20.3 and 20.0, bf16 23.8 and 23.3.
 template <typename E, int CODE, int K, bool NARROW, bool ONCE>
 __global__ __launch_bounds__(kThreads) void k_pack8(const E *x, int64_t ldx, uint8_t *codes, int64_t ldc, uint8_t *scales, int64_t lds, Units g) {
   constexpr int N = 16 / sizeof(E);
@@ -200,9 +201,11 @@ struct Norm8 {
 };
 
 // A wave has ROWS rows (times 64 / LPR) on their way at a time; gamma and beta stay in registers.  One pass over the codes: the row is held
-// in registers through mean, variance and output.  4096 x 1024 to bf16 with the rows themselves, 29.5 MB: 7.5 us, of which 3 are a launch
+// in registers through mean, variance and output.  4096 x 1024 to bf16 with the rows themselves, 29.5 MB: 7.4 us (8 in a trace), of which 3 are a launch
 // that does next to nothing; 16384 rows 25.6 (4.6 TB/s; 27.7 with one row on its way, which is 2 % faster at 4096).  Narrow rows: 131072 x
 // 128 take 27 us side by side, 50 with a wave each.  As many units a lane as the row needs: 20000 x 1096 take 41 us with five, 52 with eight.
+// Seven and eight units take 184 to 209 registers, two waves per SIMD, and one row is on its way: 4000 x 2048 to bf16 with the rows 12.5 us (4.6
+// TB/s), to fp32 without them 10.8 (3.8), 4000 x 8192 51 (4.5) and 44 (3.7); 4000 x 4096 with four units 27.6 (4.2) and 16.8 (4.9).
 template <typename E, int CODE, int LPR, int W, int NJ, int ROWS, bool NARROW>
 __global__ __launch_bounds__(256) void k_layernorm8_fwd(Norm8 g, const E *gamma, const E *beta, E *y, float *x) {
   static_assert(LPR == 64 || (W == 1 && NJ == 1), "narrow rows are one unit a lane");
@@ -305,7 +308,7 @@ template <typename E, int NJ> struct Row8 {
 // The rows of a workgroup's slots leave their column sums in registers; at the end the slots' meet in LDS and one row of sums per
 // workgroup goes to the workspace: 256 workgroups, one per compute unit, of eight waves with up to 256 registers, seven bytes per column
 // of the row at hand and of the next one among them.  4096 x 1024 bf16 with res, dx_e and all sums, 54.7 MB: 13.4 us (the rows beyond the first
-// 2048 at 7 TB/s; the rest is launch, the first loads and the slots' joining) and 3.7 for the sums; 32768 rows 81 (5.4 TB/s); 4095 x 4096 40.
+// 2048 at 7 TB/s; the rest is launch, the first loads and the slots' joining) and 3.9 for the sums; 32768 rows 81 (5.4 TB/s); 4095 x 4096 40.
 // Registers take kStretch rows' sums, which then go to those that the slot has in LDS (a workgroup of one slot: in the workspace), so that a term
 // goes through 256 additions and one for each 256 of its rows: in one chain 2^28 rows of 8 equal columns were off by up to 2e-4 of their sum.
 // Sixteen waves of half the registers are 1 to 5 % faster there, 3 % slower at 16384 x 1024 and 19 % at 2000 x 8000.

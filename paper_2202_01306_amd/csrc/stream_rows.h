@@ -34,8 +34,10 @@ typedef u32x2 u32x2_by1 __attribute__((aligned(1)));
 typedef u32x2 u32x2_by2 __attribute__((aligned(2)));
 typedef uint32_t u32_by1 __attribute__((aligned(1)));
 // ONCE: a streaming load, whose data the caches do not keep.  For rows that are read once and are kStreamed bytes or more: a third of the
-// memory-side cache of 256 MB, where fewer are found if the last two or three kernels have had them (both sides are measured at the kernels, with
-// three sets of rows in turn: it gains from 84 MB on and loses at 67).
+// memory-side cache of 256 MB, where fewer are found if the last two or three kernels have had them.  What it gives depends on what came before and
+// on the width (both sides stand at the kernels): with three sets of rows in turn 3 to 9 % from 84 MB on, -1 % at 328 MB of rows of 5000 columns, 0 at
+// 210 MB of 1601 in bf16, -3 to -11 % at 67 MB; with rows that the kernel just before has written, and which the cache still holds, 6 to 43 % from 268
+// MB on (0 at the 210 MB of 1601), 0 to -5 % at 84 and 134 MB.
 constexpr int64_t kStreamed = int64_t(80) << 20;
 template <bool NARROW, bool ONCE = false, typename E, int N> __device__ __forceinline__ void load_unit(Cols<E, N> &v, const E *row, Unit u, int d) {
   const char *p = reinterpret_cast<const char *>(row + u.c);
