@@ -309,9 +309,9 @@ template <typename E, int NJ> struct Row8 {
 // workgroup goes to the workspace: 256 workgroups, one per compute unit, of eight waves with up to 256 registers, seven bytes per column
 // of the row at hand and of the next one among them.  4096 x 1024 bf16 with res, dx_e and all sums, 54.7 MB: 13.4 us (the rows beyond the first
 // 2048 at 7 TB/s; the rest is launch, the first loads and the slots' joining) and 3.9 for the sums; 32768 rows 81 (5.4 TB/s); 4095 x 4096 40.
+// Sixteen waves of half the registers are 1 to 5 % faster there, 3 % slower at 16384 x 1024 and 19 % at 2000 x 8000.
 // Registers take kStretch rows' sums, which then go to those that the slot has in LDS (a workgroup of one slot: in the workspace), so that a term
 // goes through 256 additions and one for each 256 of its rows: in one chain 2^28 rows of 8 equal columns were off by up to 2e-4 of their sum.
-// Sixteen waves of half the registers are 1 to 5 % faster there, 3 % slower at 16384 x 1024 and 19 % at 2000 x 8000.
 template <typename E, int CODE, int LPR, int W, int NJ, bool NARROW>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(1, 2))) void k_layernorm8_bwd(Norm8Grad g, const E *dy, const E *gamma, E *dx_e) {
   static_assert(LPR == 64 || (W == 1 && NJ == 1), "narrow rows are one unit a lane");
